@@ -384,6 +384,100 @@ int h2o_debug_set_prefill_events(h2o_cache_t* cache, void* const* events);
 int h2o_debug_bounds_checked(void);
 const char* h2o_strerror(int code);
 
+/*
+ * K/V store: rows that many queries read and nothing evicts - an encoder's states, a prompt that a whole batch
+ * shares, a sequence's own tokens - next to the caches above, whose rows belong to one unit and are evicted (the
+ * paper covers self attention with eviction only; no counterpart there).  The handle describes caller-owned memory;
+ * it must stay valid until h2o_store_destroy.  Calls on one store may run on several streams at once as far as
+ * their memory allows: every call has its own scratch, and the caller orders writes against reads of the same rows.
+ *
+ *   format H2O_F32, H2O_BF16: k, v dev [rows, n_heads, head_dim], `row_stride` elements from row to row (0: dense;
+ *     a multiple of 8 otherwise).  The caller writes these rows itself.
+ *   format H2O_KV8: k, v dev uint8 [n_heads, rows, head_dim] e4m3 codes and k_scale, v_scale dev uint8
+ *     [n_heads, rows], dense: value = code * 2^(scale - 127).  Written by h2o_store_write.
+ *
+ * H2O_KV8 quantisation, per row of a head (this library's own): a = the largest finite magnitude; e = the smallest
+ * integer in [-15, 7] with a <= 448 * 2^e; code = x * 2^-e rounded to e4m3 (nearest, ties to even), magnitudes beyond
+ * 448 * 2^e (and infinities) become it, NaN stays NaN; scale = e + 127.  So values up to 57344 keep 4 significant
+ * bits, and every stored value is exactly a bf16, f16 and f32 number.
+ */
+#define H2O_KV8 3
+typedef struct h2o_store h2o_store_t; /* opaque, host-side */
+typedef struct {
+  int32_t n_heads;    /* K/V heads, >= 1                                              */
+  int32_t head_dim;   /* 64 or 128                                                    */
+  int32_t format;     /* H2O_F32, H2O_BF16 or H2O_KV8                                 */
+  int32_t device;     /* CUDA device ordinal                                          */
+  int64_t rows;       /* rows the memory holds, >= 1; for H2O_KV8 rows * n_heads < 2^31 */
+  int64_t row_stride; /* elements between rows, 0: n_heads * head_dim (H2O_KV8: 0)    */
+  void *k, *v;        /* dev, 16-byte aligned                                         */
+  uint8_t *k_scale, *v_scale; /* dev, H2O_KV8 only                                    */
+  int32_t* status;    /* dev, one int32 the caller has set to 0, or NULL: where a kernel's bounded wait that gives
+                         up leaves H2O_ERR_TIMEOUT                                    */
+} h2o_store_config_t;
+int h2o_store_create(h2o_store_t** out, const h2o_store_config_t* cfg);
+int h2o_store_destroy(h2o_store_t* store); /* the handle only; NULL is accepted */
+
+/*
+ * Quantise n_tokens rows as they are written into an H2O_KV8 store / read rows of one back (H2O_ERR_UNSUPPORTED for
+ * other formats).  k, v: dev [n_tokens, n_heads, head_dim] of `dtype` (H2O_F32 or H2O_BF16), `stride` elements from
+ * token to token (0: dense; a multiple of 8 otherwise), 16-byte aligned.  Token i goes to (comes from) store row
+ * rows[i] (dev int64), or first_row + i where rows is NULL.  A rows[i] outside the store is skipped: nothing is
+ * written for that token.  Rows that one h2o_store_write names must differ from each other; a row named twice holds
+ * bytes of both tokens afterwards.
+ */
+int h2o_store_write(h2o_store_t* store, const void* k, const void* v, int32_t dtype, int64_t n_tokens, int64_t stride,
+                    const int64_t* rows, int64_t first_row, void* stream);
+int h2o_store_read(h2o_store_t* store, void* k, void* v, int32_t dtype, int64_t n_tokens, int64_t stride,
+                   const int64_t* rows, int64_t first_row, void* stream);
+
+/* The queries of an attention call and where its results go. */
+typedef struct {
+  const void* q;       /* dev [q_rows, n_heads * query_group, head_dim], query head = head * query_group + g  */
+  void* out;           /* dev, the same shape; not q                                                         */
+  float* lse;          /* dev [q_rows, n_heads * query_group] or NULL: log of the sum of exp(c q.k)           */
+  const int32_t* cu_q; /* dev [batch + 1]: sequence b has tokens cu_q[b] .. cu_q[b + 1] - 1; NULL: token b alone */
+  int64_t q_rows;      /* tokens in q and out                                                                */
+  int64_t q_stride, out_stride; /* elements between tokens, 0: dense; multiples of 8                          */
+  float softmax_scale; /* c; <= 0 selects 1/sqrt(head_dim)                                                   */
+  int32_t dtype;       /* of q and out: the store's format; H2O_F32 or H2O_BF16 for an H2O_KV8 store          */
+  int32_t query_group; /* query heads per K/V head, 1 .. 32                                                  */
+  int32_t batch;       /* sequences, 0 .. 65535                                                              */
+  int32_t max_q;       /* upper bound of a sequence's tokens (1 without cu_q)                                */
+} h2o_queries_t;
+/* Ranges of store rows: range i is rows begin[i] .. begin[i] + length[i] - 1.  Device arrays, read by the kernels. */
+typedef struct {
+  const int64_t* begin;
+  const int32_t* length;
+  int32_t max_length; /* upper bound of the lengths */
+} h2o_ranges_t;
+
+/*
+ * Cross attention: every query token of sequence b attends all rows of range b (an encoder's states, say, of
+ * another length than the queries):
+ *   out = sum_x p_x v_x,  p = softmax over the range of c q.k_x,  lse = log sum_x exp(c q.k_x)
+ * Attention over a shared prefix: groups of consecutive sequences (cu_group dev [n_groups + 1]: group g is sequences
+ * cu_group[g] .. cu_group[g + 1] - 1; NULL: one group of all) share range g of `prefix`, and sequence b has rows of
+ * its own, range b of `own`, whose last n_b rows belong to its n_b query tokens: query i of n_b attends the prefix
+ * and the own rows but the last n_b - 1 - i.  The prefix is read once for all the queries of a group.
+ *
+ * A query without a single key (empty ranges), or whose every logit is -infinity, gets out 0 and lse -infinity.
+ * What lies outside a range is not read into any result (it may hold NaN).  Rows of q behind the last sequence leave
+ * out and lse as they were.  max_q, max_length and max_group (sequences in a group) size the launch: they must be
+ * upper bounds; tokens, rows and sequences beyond them are left out, and ranges are cut to the store's rows.
+ * cu_q, cu_group, begin and length are read on the device when the kernels run, so a captured graph follows them.
+ * scratch: dev, 256-byte aligned, at least the size the matching function returns for the same arguments (possibly 0:
+ * then NULL will do); used by the work this call enqueues only, with any contents.  0 also for invalid arguments.
+ */
+size_t h2o_cross_scratch_bytes(const h2o_store_t* store, const h2o_queries_t* queries, const h2o_ranges_t* ranges);
+int h2o_cross_attend(h2o_store_t* store, const h2o_queries_t* queries, const h2o_ranges_t* ranges, void* scratch,
+                     size_t scratch_bytes, void* stream);
+size_t h2o_prefix_scratch_bytes(const h2o_store_t* store, const h2o_queries_t* queries, const h2o_ranges_t* prefix,
+                                int32_t n_groups, const int32_t* cu_group, int32_t max_group, const h2o_ranges_t* own);
+int h2o_prefix_attend(h2o_store_t* store, const h2o_queries_t* queries, const h2o_ranges_t* prefix, int32_t n_groups,
+                      const int32_t* cu_group, int32_t max_group, const h2o_ranges_t* own, void* scratch,
+                      size_t scratch_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

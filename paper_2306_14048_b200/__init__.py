@@ -14,9 +14,11 @@ from .binding import (  # noqa: F401
     H2O_ERR_UNSUPPORTED,
     H2O_ERR_WORKSPACE,
     H2O_F32,
+    H2O_KV8,
     H2O_OK,
     H2OCache,
     H2OError,
+    H2OStore,
     h2o_cache_workspace_bytes,
     h2o_config_t,
     h2o_prefill_scratch_bytes,

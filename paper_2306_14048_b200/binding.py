@@ -27,6 +27,7 @@ H2O_ERR_TIMEOUT = -6
 H2O_F32 = 0
 H2O_BF16 = 1
 H2O_BF16_KV4 = 2  # bf16 inputs, 4-bit group-quantised K/V slots
+H2O_KV8 = 3  # rows of an H2OStore as e4m3 codes and one power of two per row and head
 
 EXPORTED = (
     "h2o_cache_workspace_bytes",
@@ -49,6 +50,14 @@ EXPORTED = (
     "h2o_cache_get_decode_path",
     "h2o_debug_set_early_prefetch",
     "h2o_prefill_scratch_layout",
+    "h2o_store_create",
+    "h2o_store_destroy",
+    "h2o_store_write",
+    "h2o_store_read",
+    "h2o_cross_scratch_bytes",
+    "h2o_cross_attend",
+    "h2o_prefix_scratch_bytes",
+    "h2o_prefix_attend",
     "h2o_strerror",
 )
 
@@ -65,6 +74,43 @@ class h2o_config_t(ctypes.Structure):
         ("device", ctypes.c_int32),
         ("query_group", ctypes.c_int32),
     ]
+
+
+class h2o_store_config_t(ctypes.Structure):
+    _fields_ = [
+        ("n_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("format", ctypes.c_int32),
+        ("device", ctypes.c_int32),
+        ("rows", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("status", ctypes.c_void_p),
+    ]
+
+
+class h2o_queries_t(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("lse", ctypes.c_void_p),
+        ("cu_q", ctypes.c_void_p),
+        ("q_rows", ctypes.c_int64),
+        ("q_stride", ctypes.c_int64),
+        ("out_stride", ctypes.c_int64),
+        ("softmax_scale", ctypes.c_float),
+        ("dtype", ctypes.c_int32),
+        ("query_group", ctypes.c_int32),
+        ("batch", ctypes.c_int32),
+        ("max_q", ctypes.c_int32),
+    ]
+
+
+class h2o_ranges_t(ctypes.Structure):
+    _fields_ = [("begin", ctypes.c_void_p), ("length", ctypes.c_void_p), ("max_length", ctypes.c_int32)]
 
 
 def _load() -> ctypes.CDLL:
@@ -135,6 +181,22 @@ def _load() -> ctypes.CDLL:
     lib.h2o_debug_set_prefill_events.argtypes = [vp, c.POINTER(vp)]
     lib.h2o_debug_bounds_checked.restype = c.c_int
     lib.h2o_debug_bounds_checked.argtypes = []
+    qp, rp = c.POINTER(h2o_queries_t), c.POINTER(h2o_ranges_t)
+    lib.h2o_store_create.restype = c.c_int
+    lib.h2o_store_create.argtypes = [c.POINTER(vp), c.POINTER(h2o_store_config_t)]
+    lib.h2o_store_destroy.restype = c.c_int
+    lib.h2o_store_destroy.argtypes = [vp]
+    for f in (lib.h2o_store_write, lib.h2o_store_read):
+        f.restype = c.c_int
+        f.argtypes = [vp, vp, vp, c.c_int32, c.c_int64, c.c_int64, vp, c.c_int64, vp]
+    lib.h2o_cross_scratch_bytes.restype = c.c_size_t
+    lib.h2o_cross_scratch_bytes.argtypes = [vp, qp, rp]
+    lib.h2o_cross_attend.restype = c.c_int
+    lib.h2o_cross_attend.argtypes = [vp, qp, rp, vp, c.c_size_t, vp]
+    lib.h2o_prefix_scratch_bytes.restype = c.c_size_t
+    lib.h2o_prefix_scratch_bytes.argtypes = [vp, qp, rp, c.c_int32, vp, c.c_int32, rp]
+    lib.h2o_prefix_attend.restype = c.c_int
+    lib.h2o_prefix_attend.argtypes = [vp, qp, rp, c.c_int32, vp, c.c_int32, rp, vp, c.c_size_t, vp]
     lib.h2o_strerror.restype = c.c_char_p
     lib.h2o_strerror.argtypes = [c.c_int]
     return lib
@@ -349,6 +411,178 @@ class H2OCache:
     def close(self):
         if getattr(self, "_h", None) is not None:
             lib.h2o_cache_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+_DTYPES = {torch.float32: H2O_F32, torch.bfloat16: H2O_BF16}
+
+
+def _bad(why: str):
+    raise ValueError("H2OStore: " + why)
+
+
+class H2OStore:
+    """K/V rows that many queries read and nothing evicts (h2o_store_*): an encoder's states, a prompt that a batch
+    shares, a sequence's own tokens.
+
+    ``k``, ``v``: float32 or bfloat16 [rows, heads, head_dim] (rows may be strided), or uint8 e4m3 codes
+    [heads, rows, head_dim] with ``k_scale``, ``v_scale`` uint8 [heads, rows].  The tensors stay the caller's (this
+    object keeps a reference) and are read where they lie.  Methods mirror the C calls: ``write`` ->
+    h2o_store_write, ``read`` -> h2o_store_read, ``cross_attend`` -> h2o_cross_attend, ``prefix_attend`` ->
+    h2o_prefix_attend, ``close`` -> h2o_store_destroy.  Results go to tensors that the caller passes; scratch comes
+    from torch's allocator on the call's stream, one piece per call.
+    """
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        if not k.is_cuda or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.dim() != 3:
+            _bad("k and v must be CUDA tensors of one 3-d shape, dtype and device")
+        eight = k.dtype == torch.uint8
+        if eight:
+            self.n_heads, self.rows, self.head_dim = k.shape
+            if not k.is_contiguous() or not v.is_contiguous():
+                _bad("8-bit k and v must be contiguous")
+            for s in (k_scale, v_scale):
+                if s is None or s.dtype != torch.uint8 or s.shape != k.shape[:2] or not s.is_contiguous() or s.device != k.device:
+                    _bad("8-bit rows need contiguous uint8 scales [heads, rows] on the same device")
+        else:
+            if k.dtype not in _DTYPES:
+                _bad("k and v must be float32, bfloat16 or uint8")
+            if k_scale is not None or v_scale is not None:
+                _bad("scales belong to 8-bit rows")
+            self.rows, self.n_heads, self.head_dim = k.shape
+            if k.stride() != v.stride() or k.stride(2) != 1 or k.stride(1) != self.head_dim:
+                _bad("rows of k and v must have one stride and dense heads")
+        self.format = H2O_KV8 if eight else _DTYPES[k.dtype]
+        self.device = k.device
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        torch.cuda.current_stream(self.device).synchronize()  # the zero is there, whatever stream comes next
+        cfg = h2o_store_config_t(self.n_heads, self.head_dim, self.format, self.device.index, self.rows,
+                                 0 if eight or self.rows <= 1 else k.stride(0), k.data_ptr(), v.data_ptr(),
+                                 k_scale.data_ptr() if eight else None, v_scale.data_ptr() if eight else None,
+                                 self._status.data_ptr())
+        self._h = None
+        handle = ctypes.c_void_p()
+        _check(lib.h2o_store_create(ctypes.byref(handle), ctypes.byref(cfg)), "h2o_store_create")
+        self._h = handle
+
+    @classmethod
+    def empty_kv8(cls, rows: int, n_heads: int, head_dim: int, device=0):
+        """A store of 8-bit rows, all zero."""
+        dev = torch.device("cuda", device) if isinstance(device, int) else device
+        k = torch.zeros((n_heads, rows, head_dim), dtype=torch.uint8, device=dev)
+        scale = torch.full((n_heads, rows), 127, dtype=torch.uint8, device=dev)
+        return cls(k, torch.zeros_like(k), scale, scale.clone())
+
+    # ---- argument checks ----
+    def _stream(self, stream) -> int:
+        return int((torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream)
+
+    def _rows(self, k, v, rows, first_row):
+        if k.shape != v.shape or k.dtype != v.dtype or k.dim() != 3 or k.shape[1:] != (self.n_heads, self.head_dim):
+            _bad("k and v must be [tokens, %d, %d] of one dtype" % (self.n_heads, self.head_dim))
+        if k.dtype not in _DTYPES or k.device != self.device or v.device != self.device:
+            _bad("k and v must be float32 or bfloat16 on %s" % self.device)
+        n = k.shape[0]
+        if k.stride() != v.stride() or (n and (k.stride(2) != 1 or k.stride(1) != self.head_dim)):
+            _bad("k and v must have one token stride and dense heads")
+        if rows is not None and (rows.dtype != torch.int64 or rows.shape != (n,) or rows.device != self.device or not rows.is_contiguous()):
+            _bad("rows must be a contiguous int64 [tokens] on %s" % self.device)
+        return (k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], n, k.stride(0) if n > 1 else 0,
+                None if rows is None else rows.data_ptr(), int(first_row))
+
+    def _queries(self, q, out, cu_q, max_q, lse, softmax_scale, batch):
+        heads = q.shape[1] if q.dim() == 3 else 0
+        if q.dim() != 3 or q.shape[2] != self.head_dim or heads < self.n_heads or heads % self.n_heads:
+            _bad("q must be [tokens, multiple of %d, %d]" % (self.n_heads, self.head_dim))
+        if out.shape != q.shape or out.dtype != q.dtype or q.dtype not in _DTYPES:
+            _bad("q and out must be float32 or bfloat16 of one shape and dtype")
+        if q.device != self.device or out.device != self.device:
+            _bad("q and out must be on %s" % self.device)
+        if q.numel() and (q.stride(2) != 1 or q.stride(1) != self.head_dim or out.stride(2) != 1 or out.stride(1) != self.head_dim):
+            _bad("q and out must have dense heads")
+        tokens = q.shape[0]
+        if cu_q is None:
+            if max_q != 1 or tokens < batch:
+                _bad("without cu_q there is one token per sequence")
+        elif cu_q.dtype != torch.int32 or cu_q.shape != (batch + 1,) or cu_q.device != self.device or not cu_q.is_contiguous():
+            _bad("cu_q must be a contiguous int32 [batch + 1] on %s" % self.device)
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != (tokens, heads) or lse.device != self.device or not lse.is_contiguous()):
+            _bad("lse must be a contiguous float32 [tokens, heads] on %s" % self.device)
+        return h2o_queries_t(q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
+                             None if cu_q is None else cu_q.data_ptr(), tokens, q.stride(0) if tokens > 1 else 0,
+                             out.stride(0) if tokens > 1 else 0, softmax_scale, _DTYPES[q.dtype], heads // self.n_heads,
+                             batch, max_q)
+
+    def _ranges(self, begin, length, most, count):
+        if begin.dtype != torch.int64 or length.dtype != torch.int32 or begin.shape != (count,) or length.shape != (count,):
+            _bad("begin must be int64 and length int32, one entry per range")
+        if begin.device != self.device or length.device != self.device or not begin.is_contiguous() or not length.is_contiguous():
+            _bad("begin and length must be contiguous on %s" % self.device)
+        return h2o_ranges_t(begin.data_ptr(), length.data_ptr(), most)
+
+    def _scratch(self, nbytes, stream):
+        """A piece of scratch of this call's own, on its stream; torch's blocks are 512-byte aligned."""
+        if stream is None:
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        with torch.cuda.stream(stream):
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+
+    # ---- calls ----
+    def write(self, k, v, rows=None, first_row=0, stream=None):
+        """Quantise k, v [tokens, heads, head_dim] into store rows ``rows`` (int64, device) or first_row, first_row + 1, ..."""
+        _check(lib.h2o_store_write(self._h, *self._rows(k, v, rows, first_row), self._stream(stream)), "h2o_store_write")
+
+    def read(self, k, v, rows=None, first_row=0, stream=None):
+        """Read store rows back into k, v [tokens, heads, head_dim]."""
+        _check(lib.h2o_store_read(self._h, *self._rows(k, v, rows, first_row), self._stream(stream)), "h2o_store_read")
+
+    def cross_attend(self, q, begin, length, out, max_len, cu_q=None, max_q=1, lse=None, softmax_scale=0.0, stream=None):
+        """Sequence b's query tokens attend store rows begin[b] .. begin[b] + length[b] - 1.  q, out: [tokens, query
+        heads, head_dim]; cu_q: int32 [batch + 1] first token of each sequence (None: token b is sequence b); max_q,
+        max_len: upper bounds; lse: float32 [tokens, query heads] or None."""
+        batch = begin.shape[0]
+        qs = ctypes.byref(self._queries(q, out, cu_q, max_q, lse, softmax_scale, batch))
+        rs = ctypes.byref(self._ranges(begin, length, max_len, batch))
+        need = lib.h2o_cross_scratch_bytes(self._h, qs, rs)
+        scratch = self._scratch(need, stream) if need else None
+        _check(lib.h2o_cross_attend(self._h, qs, rs, scratch.data_ptr() if need else None, need, self._stream(stream)),
+               "h2o_cross_attend")
+
+    def prefix_attend(self, q, prefix_begin, prefix_len, own_begin, own_len, out, max_prefix, max_own, cu_group=None,
+                      max_group=0, cu_q=None, max_q=1, lse=None, softmax_scale=0.0, stream=None):
+        """Groups of consecutive sequences (cu_group: int32 [groups + 1], None: one group) share the store rows
+        prefix_begin[g] .. + prefix_len[g] - 1; sequence b's own rows are own_begin[b] .. + own_len[b] - 1, the last
+        of them those of its query tokens.  max_group: upper bound of a group's sequences (0: the batch)."""
+        batch, groups = own_begin.shape[0], prefix_begin.shape[0]
+        if cu_group is None:
+            if groups != 1:
+                _bad("several groups need cu_group")
+        elif cu_group.dtype != torch.int32 or cu_group.shape != (groups + 1,) or cu_group.device != self.device or not cu_group.is_contiguous():
+            _bad("cu_group must be a contiguous int32 [groups + 1] on %s" % self.device)
+        qs = ctypes.byref(self._queries(q, out, cu_q, max_q, lse, softmax_scale, batch))
+        ps = ctypes.byref(self._ranges(prefix_begin, prefix_len, max_prefix, groups))
+        os_ = ctypes.byref(self._ranges(own_begin, own_len, max_own, batch))
+        cg = None if cu_group is None else cu_group.data_ptr()
+        most = max_group or max(1, batch)
+        need = lib.h2o_prefix_scratch_bytes(self._h, qs, ps, groups, cg, most, os_)
+        scratch = self._scratch(need, stream) if need else None
+        _check(lib.h2o_prefix_attend(self._h, qs, ps, groups, cg, most, os_, scratch.data_ptr() if need else None, need,
+                                     self._stream(stream)), "h2o_prefix_attend")
+
+    def status(self) -> int:
+        """H2O_OK, or the H2O_ERR_* a kernel recorded (synchronises)."""
+        return int(self._status.item())
+
+    def close(self):
+        if getattr(self, "_h", None) is not None:
+            lib.h2o_store_destroy(self._h)
             self._h = None
 
     def __del__(self):

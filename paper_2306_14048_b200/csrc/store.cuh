@@ -1,0 +1,117 @@
+// Internal declarations of the K/V store operators (h2o_store_*, h2o_cross_attend, h2o_prefix_attend).
+//
+// A store is caller-owned K and V rows that many queries read and nothing evicts.  An attention call is one or two
+// PARTS: a part is a list of problems, each a range of query tokens against a range of store rows; the keys of a
+// problem can be split into chunks whose results are joined afterwards (each chunk leaves its normalised output and
+// the logarithm of its sum of exponentials).
+//   cross attention    one part: a problem per sequence
+//   shared prefix      part 0: a problem per group of sequences (all their query tokens against the group's prefix),
+//                      part 1: a problem per sequence against its own rows, causal
+#pragma once
+#include "h2o_internal.cuh"
+
+// The handle: host memory only.
+struct h2o_store {
+  h2o_store_config_t cfg;  // strides filled in
+  alignas(64) unsigned char map_k[128], map_v[128];  // tensor maps of the rows (opaque here)
+  bool maps;               // they are there
+};
+
+namespace h2o {
+
+constexpr int kKv8 = H2O_KV8;
+
+struct AttendPart {
+  const int64_t* begin;    // dev [problems]: first store row
+  const int32_t* length;   // dev [problems]: rows
+  int max_length;          // upper bound of the lengths (longer ones are cut)
+  int problems;            // sequences, or groups of sequences
+  int grouped;             // 1: a problem is a group (its token range comes from cu_group)
+  int causal;              // 1: query i of n sees all rows but the last n - 1 - i
+  int chunk, splits;       // keys per split, splits per problem (of the longest)
+  int row_tiles;           // tiles of query rows per problem (of the longest)
+  int slot0;               // first partial slot of this part
+};
+
+struct AttendView {
+  const void* q;
+  void* out;
+  float* lse;              // nullable
+  int64_t q_stride, out_stride, q_rows;  // elements between tokens; tokens
+  const int32_t* cu_q;     // dev [batch + 1], or null: token b belongs to sequence b
+  const int32_t* cu_group; // dev [n_groups + 1], or null: one group of all sequences
+  int batch, n_groups, max_q, max_group;
+  int heads, group, dim;   // K/V heads, query heads per K/V head
+  float scale2;            // softmax scale times log2(e)
+  const void *k, *v;
+  const uint8_t *k_scale, *v_scale;  // 8-bit rows only
+  int64_t rows, row_stride;
+  float *part_out, *part_lse;  // [slots][q_rows][heads * group](dim), null when the kernel writes the result itself
+  int32_t* status;
+  int n_parts;
+  AttendPart part[2];
+};
+
+// A problem's query tokens and store rows, cut to what the caller allowed for, so that no index leaves its array
+// whatever the device arrays hold.
+struct Problem {
+  int64_t t0, row0;  // first query token, first store row
+  int nt, len;       // tokens, rows
+};
+__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : (x > hi ? hi : x); }
+__device__ __forceinline__ int64_t first_token(const AttendView& a, int seq) {
+  return clamp64(a.cu_q ? (int64_t)a.cu_q[seq] : (int64_t)seq, 0, a.q_rows);
+}
+__device__ __forceinline__ Problem locate(const AttendView& a, const AttendPart& p, int i) {
+  int s0 = i, s1 = i + 1;
+  int64_t most = a.max_q;
+  if (p.grouped) {
+    s0 = a.cu_group ? max(0, min(a.cu_group[i], a.batch)) : 0;
+    s1 = a.cu_group ? max(s0, min(a.cu_group[i + 1], a.batch)) : a.batch;
+    s1 = min(s1, s0 + a.max_group);
+    most *= a.max_group;
+  }
+  Problem r;
+  r.t0 = first_token(a, s0);
+  r.nt = (int)clamp64(first_token(a, s1) - r.t0, 0, most);
+  r.row0 = clamp64(p.begin[i], 0, a.rows);
+  r.len = (int)clamp64(p.length[i], 0, min((int64_t)p.max_length, a.rows - r.row0));
+  return r;
+}
+// Rows of a problem that its query token `i` sees.
+__device__ __forceinline__ int seen_rows(const AttendPart& p, const Problem& r, int i) {
+  return p.causal ? max(0, r.len - (r.nt - 1 - i)) : r.len;
+}
+
+// What one thread block works on: row tile fastest, then head, split, problem.
+struct BlockWork {
+  int problem, head, split, row_tile;
+};
+__device__ __forceinline__ BlockWork block_work(const AttendView& a, const AttendPart& p, unsigned idx) {
+  BlockWork w;
+  w.row_tile = idx % p.row_tiles;
+  idx /= p.row_tiles;
+  w.head = idx % a.heads;
+  idx /= a.heads;
+  w.split = idx % p.splits;
+  w.problem = idx / p.splits;
+  return w;
+}
+inline int64_t part_blocks(const AttendView& a, const AttendPart& p) {
+  return (int64_t)p.row_tiles * a.heads * p.splits * p.problems;
+}
+
+// The value of a scale byte (a biased exponent).  Only bytes 112 .. 134 are ever written; others, in rows nobody
+// has written, are cut to that range.
+__device__ __forceinline__ float kv8_scale(uint32_t byte) { return __uint_as_float(min(max(byte, 112u), 134u) << 23); }
+
+// Launchers.
+cudaError_t launch_store_write(const h2o_store_config_t& c, const void* k, const void* v, int dtype, int64_t stride,
+                               int64_t n, const int64_t* rows, int64_t first_row, cudaStream_t stream);
+cudaError_t launch_store_read(const h2o_store_config_t& c, void* k, void* v, int dtype, int64_t stride, int64_t n,
+                              const int64_t* rows, int64_t first_row, cudaStream_t stream);
+int attend_fma_row_tile(int64_t rows);  // rows of a tile for problems of up to `rows` rows
+cudaError_t launch_attend_fma(const AttendView& a, int part, int tile, int q_dtype, int format, cudaStream_t stream);
+cudaError_t launch_attend_join(const AttendView& a, int q_dtype, cudaStream_t stream);
+
+}  // namespace h2o
