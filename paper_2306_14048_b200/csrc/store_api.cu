@@ -98,6 +98,7 @@ int check_ranges(const h2o_ranges_t* r) {
 struct Plan {
   h2o::AttendView a;
   int tile[2];        // query rows of a block, per part
+  bool fma;           // float32 queries: the FMA kernels
   size_t scratch;     // bytes of scratch
   size_t lse_offset;  // of the partial log-sums in it
   int rc;
@@ -111,7 +112,7 @@ void split_part(h2o::AttendPart& p, int64_t units, int64_t blocks_wanted) {
   const int64_t most = std::max<int64_t>(1, (p.max_length + kMinChunk - 1) / kMinChunk);
   const int64_t splits = std::min(want, most);
   const int64_t len = std::max(1, p.max_length);
-  p.chunk = (int)(((len + splits - 1) / splits + 63) / 64 * 64);
+  p.chunk = (int)(((len + splits - 1) / splits + 127) / 128 * 128);
   p.splits = (int)((len + p.chunk - 1) / p.chunk);
 }
 
@@ -146,6 +147,7 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
   a.rows = c.rows;
   a.row_stride = c.row_stride;
   a.status = c.status;
+  pl.fma = q->dtype == H2O_F32;
   int n = 0;
   for (int k = 0; k < 2; ++k) {
     const h2o_ranges_t* r = k == 0 ? prefix : own;
@@ -158,7 +160,7 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
     p.causal = prefix && k == 1;
     p.problems = p.grouped ? n_groups : a.batch;
     const int64_t rows = std::min<int64_t>((p.grouped ? (int64_t)a.max_group * a.max_q : a.max_q), a.q_rows) * a.group;
-    pl.tile[n] = h2o::attend_fma_row_tile(rows);
+    pl.tile[n] = pl.fma ? h2o::attend_fma_row_tile(rows) : h2o::attend_mma_row_tile(rows);
     p.row_tiles = (int)((rows + pl.tile[n] - 1) / pl.tile[n]);
     const int64_t units = (int64_t)p.row_tiles * a.heads * p.problems;
     split_part(p, units, 2 * h2o::sm_count());
@@ -187,8 +189,10 @@ int run_plan(const h2o_store_t* store, const h2o_queries_t* q, Plan& pl, void* s
   if (!guard.ok) return H2O_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
-  for (int k = 0; k < pl.a.n_parts && e == cudaSuccess; ++k)
-    e = h2o::launch_attend_fma(pl.a, k, pl.tile[k], q->dtype, store->cfg.format, st);
+  if (pl.fma)
+    for (int k = 0; k < pl.a.n_parts && e == cudaSuccess; ++k) e = h2o::launch_attend_fma(pl.a, k, pl.tile[k], store->cfg.format, st);
+  else
+    e = h2o::launch_attend_mma(pl.a, pl.tile, store->cfg.format, store->map_k, store->map_v, st);
   if (e == cudaSuccess && pl.scratch > 0) e = h2o::launch_attend_join(pl.a, q->dtype, st);
   if (e != cudaSuccess) {
     cudaGetLastError();
@@ -235,7 +239,12 @@ int h2o_store_create(h2o_store_t** out, const h2o_store_config_t* cfg) {
   if (!s) return H2O_ERR_INVALID_ARG;
   s->cfg = *cfg;
   if (s->cfg.row_stride == 0) s->cfg.row_stride = (int64_t)cfg->n_heads * cfg->head_dim;
-  s->maps = false;
+  // the kernels for bfloat16 queries read the rows by TMA
+  if (cfg->format != H2O_F32 && (!h2o::make_store_map(reinterpret_cast<CUtensorMap_st*>(s->map_k), s->cfg, cfg->k, h2o::kStoreBoxRows) ||
+                                 !h2o::make_store_map(reinterpret_cast<CUtensorMap_st*>(s->map_v), s->cfg, cfg->v, h2o::kStoreBoxRows))) {
+    delete s;
+    return H2O_ERR_CUDA;
+  }
   *out = s;
   return H2O_OK;
 }

@@ -1,5 +1,5 @@
-// Attention over a K/V store on the fp32 FMA pipe: every format, head_dim 64 and 128, and the kernel that joins the
-// parts of a split.
+// Attention over a K/V store for float32 queries, on the fp32 FMA pipe (float32 or 8-bit rows, head_dim 64 and 128), and
+// the kernel that joins the parts of a split, for every type.
 //
 // A block takes BM query rows (query tokens times the query heads of one K/V head) and walks over its keys 64 at a
 // time: S = Q K^T by register tiles, softmax with the running maximum and sum of each row, O += P V.
@@ -22,15 +22,7 @@ __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_grou
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
-  uint2 w;
-  w.x = Vec16<__nv_bfloat16>::pack2(v.x, v.y);
-  w.y = Vec16<__nv_bfloat16>::pack2(v.z, v.w);
-  *reinterpret_cast<uint2*>(p) = w;
-}
 
 // e4m3 -> float, by its bits: exponent and mantissa moved into place, times 2^120 (exact, subnormals included)
 __device__ __forceinline__ float e4m3(uint32_t b) {
@@ -59,15 +51,6 @@ __device__ __forceinline__ void load_tile(float* dst, const void* base, const ui
       if (r < n) cp_async16(to, static_cast<const float*>(base) + (row0 + r) * a.row_stride + (int64_t)head * D + c);
       else *reinterpret_cast<float4*>(to) = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-  } else if constexpr (FMT == H2O_BF16) {
-    constexpr int kV = D / 8;
-    for (int i = threadIdx.x; i < kBN * kV; i += kThreads) {
-      const int r = i / kV, c = (i % kV) * 8;
-      float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (r < n) Vec16<__nv_bfloat16>::load(static_cast<const __nv_bfloat16*>(base) + (row0 + r) * a.row_stride + (int64_t)head * D + c, f);
-      *reinterpret_cast<float4*>(dst + r * PITCH + c) = make_float4(f[0], f[1], f[2], f[3]);
-      *reinterpret_cast<float4*>(dst + r * PITCH + c + 4) = make_float4(f[4], f[5], f[6], f[7]);
-    }
   } else {
     constexpr int kV = D / 16;
     for (int i = threadIdx.x; i < kBN * kV; i += kThreads) {
@@ -89,7 +72,7 @@ __device__ __forceinline__ void load_tile(float* dst, const void* base, const ui
   cp_commit();
 }
 
-template <typename T, int FMT, int D, int BM>
+template <int FMT, int D, int BM>
 __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_constant__ AttendView a, int part_index) {
   constexpr int RM = BM / 16, NC = D / 64;
   extern __shared__ __align__(16) unsigned char dyn[];
@@ -115,8 +98,7 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
     float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r < n_rows) {
       const int tok = (r0 + r) / a.group, g = (r0 + r) - tok * a.group;
-      const T* src = static_cast<const T*>(a.q) + (pr.t0 + tok) * a.q_stride + ((int64_t)w.head * a.group + g) * D + c;
-      f = make_float4(to_float(src[0]), to_float(src[1]), to_float(src[2]), to_float(src[3]));
+      f = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (pr.t0 + tok) * a.q_stride + ((int64_t)w.head * a.group + g) * D + c);
     }
     *reinterpret_cast<float4*>(&sh.q[r][c]) = f;
   }
@@ -238,7 +220,7 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
     const float inv = none ? 0.f : 1.f / sum;
     const float lse2 = none ? -INFINITY : m[i] + log2f(sum);
     if (direct) {
-      T* to = static_cast<T*>(a.out) + token * a.out_stride + (int64_t)hq * D;
+      float* to = static_cast<float*>(a.out) + token * a.out_stride + (int64_t)hq * D;
 #pragma unroll
       for (int j = 0; j < NC; ++j)
         store4(to + 4 * x + 64 * j, make_float4(o[i][j].x * inv, o[i][j].y * inv, o[i][j].z * inv, o[i][j].w * inv));
@@ -315,30 +297,27 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
   if (a.lse && lane == 0) a.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
 }
 
-template <typename T, int FMT, int D, int BM>
+template <int FMT, int D, int BM>
 cudaError_t launch(const AttendView& a, int part, cudaStream_t stream) {
   constexpr int smem = (int)sizeof(Smem<D, BM>);
   static unsigned long long flags = 0;
-  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(attend_fma_kernel<T, FMT, D, BM>), smem, &flags);
+  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(attend_fma_kernel<FMT, D, BM>), smem, &flags);
   if (e != cudaSuccess) return e;
-  attend_fma_kernel<T, FMT, D, BM><<<(unsigned)part_blocks(a, a.part[part]), kThreads, smem, stream>>>(a, part);
+  attend_fma_kernel<FMT, D, BM><<<(unsigned)part_blocks(a, a.part[part]), kThreads, smem, stream>>>(a, part);
   return cudaGetLastError();
 }
-template <typename T, int FMT>
+template <int FMT>
 cudaError_t launch_shape(const AttendView& a, int part, int tile, cudaStream_t stream) {
-  if (a.dim == 128) return tile == 16 ? launch<T, FMT, 128, 16>(a, part, stream) : launch<T, FMT, 128, 64>(a, part, stream);
-  return tile == 16 ? launch<T, FMT, 64, 16>(a, part, stream) : launch<T, FMT, 64, 64>(a, part, stream);
+  if (a.dim == 128) return tile == 16 ? launch<FMT, 128, 16>(a, part, stream) : launch<FMT, 128, 64>(a, part, stream);
+  return tile == 16 ? launch<FMT, 64, 16>(a, part, stream) : launch<FMT, 64, 64>(a, part, stream);
 }
 
 }  // namespace
 
 int attend_fma_row_tile(int64_t rows) { return rows <= 16 ? 16 : 64; }
 
-cudaError_t launch_attend_fma(const AttendView& a, int part, int tile, int q_dtype, int format, cudaStream_t stream) {
-  if (q_dtype == H2O_F32)
-    return format == H2O_F32 ? launch_shape<float, H2O_F32>(a, part, tile, stream) : launch_shape<float, H2O_KV8>(a, part, tile, stream);
-  return format == H2O_BF16 ? launch_shape<__nv_bfloat16, H2O_BF16>(a, part, tile, stream)
-                            : launch_shape<__nv_bfloat16, H2O_KV8>(a, part, tile, stream);
+cudaError_t launch_attend_fma(const AttendView& a, int part, int tile, int format, cudaStream_t stream) {
+  return format == H2O_F32 ? launch_shape<H2O_F32>(a, part, tile, stream) : launch_shape<H2O_KV8>(a, part, tile, stream);
 }
 
 cudaError_t launch_attend_join(const AttendView& a, int q_dtype, cudaStream_t stream) {
