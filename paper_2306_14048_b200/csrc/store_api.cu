@@ -94,26 +94,41 @@ int check_ranges(const h2o_ranges_t* r) {
   return H2O_OK;
 }
 
+enum class Kernel { Fma, Mma, Tc };
+
 // What a call launches and how much scratch it needs.
 struct Plan {
   h2o::AttendView a;
+  Kernel kernel[2];   // per part
   int tile[2];        // query rows of a block, per part
-  bool fma;           // float32 queries: the FMA kernels
   size_t scratch;     // bytes of scratch
   size_t lse_offset;  // of the partial log-sums in it
   int rc;
 };
 
-// Keys per split: as many splits as fill the SMs `waves` times over, but none of fewer than kMinChunk keys (a
-// split costs its result's trip through memory and the joining kernel).
-constexpr int kMinChunk = 256;
-void split_part(h2o::AttendPart& p, int64_t units, int64_t blocks_wanted) {
-  const int64_t want = std::max<int64_t>(1, blocks_wanted / std::max<int64_t>(1, units));
-  const int64_t most = std::max<int64_t>(1, (p.max_length + kMinChunk - 1) / kMinChunk);
-  const int64_t splits = std::min(want, most);
+// More query rows than this (of one K/V head) run on the tcgen05 kernel, 256 to a block; up to it the mma.sync kernel
+// reads each key once.
+constexpr int kFewRows = 32;
+
+// Splits the keys of a part: `units` blocks per split, `room` blocks that run at once.  A block costs its keys plus
+// about `fixed` keys' time (start, merge, its result's trip through memory); blocks run in waves while there are few of
+// them.
+void split_part(h2o::AttendPart& p, int64_t units, int64_t room, int64_t fixed) {
   const int64_t len = std::max(1, p.max_length);
-  p.chunk = (int)(((len + splits - 1) / splits + 127) / 128 * 128);
-  p.splits = (int)((len + p.chunk - 1) / p.chunk);
+  int64_t best = -1;
+  for (int64_t n = 1; n <= 64; ++n) {
+    const int64_t chunk = ((len + n - 1) / n + 127) / 128 * 128;
+    const int64_t splits = (len + chunk - 1) / chunk;
+    const int64_t blocks = units * splits, waves = (blocks + room - 1) / room;
+    int64_t cost = waves <= 4 ? waves * (std::min(chunk, len) + fixed) : blocks * (std::min(chunk, len) + fixed) / room;
+    if (splits > 1) cost += fixed;
+    if (best < 0 || cost < best) {
+      best = cost;
+      p.chunk = (int)chunk;
+      p.splits = (int)splits;
+    }
+    if (chunk == 128) break;
+  }
 }
 
 Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_ranges_t* prefix, int n_groups,
@@ -147,7 +162,6 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
   a.rows = c.rows;
   a.row_stride = c.row_stride;
   a.status = c.status;
-  pl.fma = q->dtype == H2O_F32;
   int n = 0;
   for (int k = 0; k < 2; ++k) {
     const h2o_ranges_t* r = k == 0 ? prefix : own;
@@ -160,10 +174,13 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
     p.causal = prefix && k == 1;
     p.problems = p.grouped ? n_groups : a.batch;
     const int64_t rows = std::min<int64_t>((p.grouped ? (int64_t)a.max_group * a.max_q : a.max_q), a.q_rows) * a.group;
-    pl.tile[n] = pl.fma ? h2o::attend_fma_row_tile(rows) : h2o::attend_mma_row_tile(rows);
+    pl.kernel[n] = q->dtype == H2O_F32 ? Kernel::Fma : rows > kFewRows ? Kernel::Tc : Kernel::Mma;
+    pl.tile[n] = pl.kernel[n] == Kernel::Fma  ? h2o::attend_fma_row_tile(rows)
+                 : pl.kernel[n] == Kernel::Tc ? h2o::kManyRowTile
+                                              : h2o::attend_mma_row_tile(rows);
     p.row_tiles = (int)((rows + pl.tile[n] - 1) / pl.tile[n]);
     const int64_t units = (int64_t)p.row_tiles * a.heads * p.problems;
-    split_part(p, units, 2 * h2o::sm_count());
+    split_part(p, units, h2o::sm_count() * (pl.kernel[n] == Kernel::Tc ? 1 : 2), pl.kernel[n] == Kernel::Tc ? 512 : 256);
     if (units * p.splits > INT32_MAX) pl.rc = H2O_ERR_UNSUPPORTED;
     p.slot0 = n == 0 ? 0 : a.part[0].splits;
     ++n;
@@ -189,10 +206,13 @@ int run_plan(const h2o_store_t* store, const h2o_queries_t* q, Plan& pl, void* s
   if (!guard.ok) return H2O_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
-  if (pl.fma)
-    for (int k = 0; k < pl.a.n_parts && e == cudaSuccess; ++k) e = h2o::launch_attend_fma(pl.a, k, pl.tile[k], store->cfg.format, st);
-  else
-    e = h2o::launch_attend_mma(pl.a, pl.tile, store->cfg.format, store->map_k, store->map_v, st);
+  const int format = store->cfg.format;
+  const bool both = pl.a.n_parts == 2 && pl.kernel[0] == Kernel::Mma && pl.kernel[1] == Kernel::Mma;
+  for (int k = 0; k < (both ? 1 : pl.a.n_parts) && e == cudaSuccess; ++k) {
+    if (pl.kernel[k] == Kernel::Fma) e = h2o::launch_attend_fma(pl.a, k, pl.tile[k], format, st);
+    else if (pl.kernel[k] == Kernel::Tc) e = h2o::launch_attend_tc(pl.a, k, format, store->many_k, store->many_v, st);
+    else e = h2o::launch_attend_mma(pl.a, k, both, pl.tile, format, store->few_k, store->few_v, st);
+  }
   if (e == cudaSuccess && pl.scratch > 0) e = h2o::launch_attend_join(pl.a, q->dtype, st);
   if (e != cudaSuccess) {
     cudaGetLastError();
@@ -240,10 +260,18 @@ int h2o_store_create(h2o_store_t** out, const h2o_store_config_t* cfg) {
   s->cfg = *cfg;
   if (s->cfg.row_stride == 0) s->cfg.row_stride = (int64_t)cfg->n_heads * cfg->head_dim;
   // the kernels for bfloat16 queries read the rows by TMA
-  if (cfg->format != H2O_F32 && (!h2o::make_store_map(reinterpret_cast<CUtensorMap_st*>(s->map_k), s->cfg, cfg->k, h2o::kStoreBoxRows) ||
-                                 !h2o::make_store_map(reinterpret_cast<CUtensorMap_st*>(s->map_v), s->cfg, cfg->v, h2o::kStoreBoxRows))) {
-    delete s;
-    return H2O_ERR_CUDA;
+  if (cfg->format != H2O_F32) {
+    struct {
+      unsigned char* map;
+      const void* base;
+      int box;
+    } const maps[4] = {{s->few_k, cfg->k, h2o::kFewBoxRows}, {s->few_v, cfg->v, h2o::kFewBoxRows},
+                       {s->many_k, cfg->k, h2o::kManyBoxRows}, {s->many_v, cfg->v, h2o::kManyBoxRows}};
+    for (const auto& m : maps)
+      if (!h2o::make_store_map(reinterpret_cast<CUtensorMap_st*>(m.map), s->cfg, m.base, m.box)) {
+        delete s;
+        return H2O_ERR_CUDA;
+      }
   }
   *out = s;
   return H2O_OK;

@@ -34,7 +34,7 @@ namespace {
 using namespace ptx;
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
-constexpr int kKeys = kStoreBoxRows;                  // keys of a tile
+constexpr int kKeys = kFewBoxRows;                  // keys of a tile
 constexpr uint32_t kSpin = 1u << 22;
 constexpr float kRescale = 8.f;
 constexpr int kRingBytes = 96 * 1024;                 // per block: two blocks on an SM
@@ -508,41 +508,43 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   }
 }
 
-// Rows of a block for part 0 and part 1 (a shared prefix: many and few); one launch for both parts.
+// One launch for part `first` alone, with 8 NT0 rows to a block, or for parts 0 and 1 (a shared prefix: many rows and
+// few), with 8 NT0 and 8 NT1.
 template <int FMT, int D, int NT0, int NT1>
 __global__ void __launch_bounds__(kThreads, 2)
 attend_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                  const __grid_constant__ AttendView a, unsigned blocks0) {
+                  const __grid_constant__ AttendView a, int first, unsigned blocks0) {
   extern __shared__ unsigned char dyn[];
   __shared__ Shared sh;
   unsigned char* ring = dyn + ((1024u - (smem_u32(dyn) & 1023u)) & 1023u);
   if (NT0 == NT1 || blockIdx.x < blocks0) {
     const bool second = blockIdx.x >= blocks0;
-    attend<FMT, D, NT0>(a, &map_k, &map_v, a.part[second], blockIdx.x - (second ? blocks0 : 0), ring, sh);
+    attend<FMT, D, NT0>(a, &map_k, &map_v, a.part[second ? 1 : first], blockIdx.x - (second ? blocks0 : 0), ring, sh);
   } else {
     attend<FMT, D, NT1>(a, &map_k, &map_v, a.part[1], blockIdx.x - blocks0, ring, sh);
   }
 }
 
 template <int FMT, int D, int NT0, int NT1>
-cudaError_t launch(const AttendView& a, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t stream) {
+cudaError_t launch(const AttendView& a, int first, bool both, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t stream) {
   constexpr int smem = kWarps * ring_slots(FMT, D) * tile_bytes(FMT, D) + 1024;
   static unsigned long long flags = 0;
   const void* f = reinterpret_cast<const void*>(attend_mma_kernel<FMT, D, NT0, NT1>);
   const cudaError_t e = ensure_dynamic_smem(f, smem, &flags);
   if (e != cudaSuccess) return e;
-  const int64_t b0 = part_blocks(a, a.part[0]), b1 = a.n_parts == 2 ? part_blocks(a, a.part[1]) : 0;
-  attend_mma_kernel<FMT, D, NT0, NT1><<<(unsigned)(b0 + b1), kThreads, smem, stream>>>(map_k, map_v, a, (unsigned)b0);
+  const int64_t b0 = part_blocks(a, a.part[first]), b1 = both ? part_blocks(a, a.part[1]) : 0;
+  attend_mma_kernel<FMT, D, NT0, NT1><<<(unsigned)(b0 + b1), kThreads, smem, stream>>>(map_k, map_v, a, first, (unsigned)b0);
   return cudaGetLastError();
 }
 
 template <int FMT, int D>
-cudaError_t launch_rows(const AttendView& a, const int* tile, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t st) {
-  const int t0 = tile[0], t1 = a.n_parts == 2 ? tile[1] : t0;
-  if (t0 == 8) return launch<FMT, D, 1, 1>(a, map_k, map_v, st);
-  if (t0 == 16) return t1 == 8 ? launch<FMT, D, 2, 1>(a, map_k, map_v, st) : launch<FMT, D, 2, 2>(a, map_k, map_v, st);
-  if (t1 == 8) return launch<FMT, D, 4, 1>(a, map_k, map_v, st);
-  return t1 == 16 ? launch<FMT, D, 4, 2>(a, map_k, map_v, st) : launch<FMT, D, 4, 4>(a, map_k, map_v, st);
+cudaError_t launch_rows(const AttendView& a, int first, bool both, const int* tile, const CUtensorMap& map_k, const CUtensorMap& map_v,
+                        cudaStream_t st) {
+  const int t0 = tile[first], t1 = both ? tile[1] : t0;
+  if (t0 == 8) return launch<FMT, D, 1, 1>(a, first, both, map_k, map_v, st);
+  if (t0 == 16) return t1 == 8 ? launch<FMT, D, 2, 1>(a, first, both, map_k, map_v, st) : launch<FMT, D, 2, 2>(a, first, both, map_k, map_v, st);
+  if (t1 == 8) return launch<FMT, D, 4, 1>(a, first, both, map_k, map_v, st);
+  return t1 == 16 ? launch<FMT, D, 4, 2>(a, first, both, map_k, map_v, st) : launch<FMT, D, 4, 4>(a, first, both, map_k, map_v, st);
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
@@ -578,11 +580,12 @@ bool make_store_map(CUtensorMap_st* map, const h2o_store_config_t& c, const void
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-cudaError_t launch_attend_mma(const AttendView& a, const int* tile, int format, const void* map_k, const void* map_v, cudaStream_t st) {
+cudaError_t launch_attend_mma(const AttendView& a, int first, bool both, const int* tile, int format, const void* map_k,
+                              const void* map_v, cudaStream_t st) {
   const CUtensorMap& k = *static_cast<const CUtensorMap*>(map_k);
   const CUtensorMap& v = *static_cast<const CUtensorMap*>(map_v);
-  if (format == H2O_KV8) return a.dim == 128 ? launch_rows<H2O_KV8, 128>(a, tile, k, v, st) : launch_rows<H2O_KV8, 64>(a, tile, k, v, st);
-  return a.dim == 128 ? launch_rows<H2O_BF16, 128>(a, tile, k, v, st) : launch_rows<H2O_BF16, 64>(a, tile, k, v, st);
+  if (format == H2O_KV8) return a.dim == 128 ? launch_rows<H2O_KV8, 128>(a, first, both, tile, k, v, st) : launch_rows<H2O_KV8, 64>(a, first, both, tile, k, v, st);
+  return a.dim == 128 ? launch_rows<H2O_BF16, 128>(a, first, both, tile, k, v, st) : launch_rows<H2O_BF16, 64>(a, first, both, tile, k, v, st);
 }
 
 }  // namespace h2o
