@@ -112,7 +112,8 @@ cudaError_t launch_store_read(const h2o_store_config_t& c, void* k, void* v, int
                               const int64_t* rows, int64_t first_row, cudaStream_t stream);
 int attend_fma_row_tile(int64_t rows);  // rows of a tile for problems of up to `rows` rows
 cudaError_t launch_attend_fma(const AttendView& a, int part, int tile, int format, cudaStream_t stream);
-constexpr int kFewBoxRows = 32, kManyBoxRows = 128;  // rows of a box of the store's tensor maps
+constexpr int kFewBoxRows = 32;  // rows of a box of the store's tensor maps
+inline int many_box_rows(int dim) { return dim == 128 ? 80 : 96; }
 bool make_store_map(CUtensorMap_st* map, const h2o_store_config_t& c, const void* base, int box_rows);
 int attend_mma_row_tile(int64_t rows);
 // part `first`, or (both) parts 0 and 1 in one launch

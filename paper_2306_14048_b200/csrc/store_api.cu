@@ -266,7 +266,7 @@ int h2o_store_create(h2o_store_t** out, const h2o_store_config_t* cfg) {
       const void* base;
       int box;
     } const maps[4] = {{s->few_k, cfg->k, h2o::kFewBoxRows}, {s->few_v, cfg->v, h2o::kFewBoxRows},
-                       {s->many_k, cfg->k, h2o::kManyBoxRows}, {s->many_v, cfg->v, h2o::kManyBoxRows}};
+                       {s->many_k, cfg->k, h2o::many_box_rows(cfg->head_dim)}, {s->many_v, cfg->v, h2o::many_box_rows(cfg->head_dim)}};
     for (const auto& m : maps)
       if (!h2o::make_store_map(reinterpret_cast<CUtensorMap_st*>(m.map), s->cfg, m.base, m.box)) {
         delete s;

@@ -2,25 +2,33 @@
 // accumulators in tensor memory; bfloat16 queries, bfloat16 or 8-bit rows, head_dim 64 or 128.
 //
 // A block takes up to 256 query rows (query tokens times the query heads of one K/V head) as two groups of 128, A and
-// B, which share every tile of 128 keys.  Per group g and key tile j:
-//   S_g(j) = Q_g K_j^T     M 128, N 128: with fewer keys per instruction the operands' shared-memory reads bind
-//   P_g(j) = exp2(S - m)   written over S_g as 16-bit values (tensor memory holds O and S of both groups: all 512
-//                          columns, so S is not double-buffered: while one group computes exponentials the tensor
-//                          cores work for the other)
+// B, which share every key tile (80 keys for head_dim 128, 96 for 64); up to 128 rows are given to both groups, which
+// then take the tiles in turn and join their results at the end.  Per group g and key tile j:
+//   S_g(j) = Q_g K_j^T     into tensor memory, from there into the softmax threads' registers, which frees S_g at once:
+//                          S_g(j + 1) runs while the exponentials of tile j are computed
+//   P_g(j) = exp2(S - m)   16-bit, into tensor memory of its own
 //   O_g   += P_g(j) V_j    P is the tensor-memory operand, V the MN-major shared-memory operand
-// Roles: warp 0 TMA, warps 1 and 2 issue the matrix instructions of A and B (A's also clears what lies behind the range
-// in its last V tile: 0 * NaN must not reach the sums), warp 3 tensor memory, warps 4..7 and 8..11 the softmax of A
-// and B, one thread per row; with 8-bit rows warps 12..15 turn code tiles into f16 tiles.
-// The reference maximum follows lazily (O is rescaled when a logit exceeds it by 8, base 2).  The commit behind
-// S_g(j) covers P V(j - 1) too, so a softmax thread that sees S_g(j) may rescale O without another wait.
+// The tile size is what tensor memory holds of O (2 x 128 columns), S (2 x 80) and P (2 x 40).  With S and P in one place
+// and tiles of 128 keys the chain S - exponentials - P V of a group is serial: 3700 cycles per tile of both groups for
+// 2048 of tensor work.  Measured (4 x 2048 queries against 4096 keys, 32 heads): 593 us that way, 505 us this way (1090
+// TFLOP/s); tiles of 64 keys with S prefetched into registers and P in two buffers 650 us; two threads to a row 725 us.
+// Roles: warp 0 TMA and tensor memory, warps 1 and 2 issue S of A and B (they also clear what lies behind the range in
+// its last V tile: 0 * NaN must not reach the sums), warp 3 issues P V of both, warps 4..7 and 8..11 the softmax of A and
+// B, one thread per row; with 8-bit rows warps 12..15 turn code tiles into f16 tiles.  A wait on a barrier costs 300 to
+// 400 cycles here even when it is complete (it queues behind the exponentials), so the issuers have few: K and V of a tile
+// arrive on one barrier, and P V waits for P alone, which comes after S and so after the tile.  Their loops run on
+// values the compiler knows to be uniform (constant tensor-memory addresses, counts from a shuffle): 575 -> 550 us.
+// The reference m of a row is the maximum of its first tile.  Later tiles compute their exponentials against it without
+// looking for a maximum: only when a tile's sum comes out large (kLargeSum) the tile is done again with the new
+// maximum and O is rescaled.  A value far above the reference costs no precision in floating point, only range.
 //
 // Rounding: P is one bf16 (8-bit rows: one f16).  Its error, 2^-9 relative per key and of either sign, averages over
 // the keys to about that of the output's own rounding; a second product for the remainder would cost half as much tensor
 // time again.  Row sums are fp32 sums of the unrounded values.
-// Part of the exponentials runs on the FMA pipe (ex2_fma2): the special-function unit alone would need as long as
-// both products together (16 a clock for 128 x 128 x 2).
 #include <cuda.h>
 #include <cuda_fp16.h>
+
+#include <type_traits>
 
 #include "sm100_ptx.cuh"
 #include "store.cuh"
@@ -31,29 +39,38 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kM = 128, kN = 128;  // rows of a group, keys of a tile
-constexpr int kMaxSlots = 5, kRawSlots = 2;
-constexpr float kRescale = 8.f;
+constexpr int kM = 128;  // rows of a group
+__host__ __device__ constexpr int tile_keys(int d) { return d == 128 ? 80 : 96; }
 __host__ __device__ constexpr int threads(int fmt) { return fmt == H2O_KV8 ? 512 : 384; }
-__host__ __device__ constexpr int tile_bytes(int d) { return kN * d * 2; }
-__host__ __device__ constexpr int slots(int fmt, int d) { return d == 64 ? 5 : fmt == H2O_KV8 ? 4 : 5; }
+__host__ __device__ constexpr int tile_bytes(int d) { return tile_keys(d) * d * 2; }
+// Ring of stages, K and V of a tile in each.  Two groups that take tiles in turn use an even number: a warp that waits for
+// a tile then has seen the stage's tile before, so a parity cannot be mistaken for an older one.
+__host__ __device__ constexpr int stages(int fmt, int d) { return d == 64 ? 6 : fmt == H2O_KV8 ? 3 : 4; }
+__host__ __device__ constexpr int turn_stages(int fmt, int d) { return stages(fmt, d) & ~1; }
+constexpr int kMaxStages = 6, kRawStages = 2;  // (a stage of the code ring also holds K and V)
 __host__ __device__ constexpr int smem_bytes(int fmt, int d) {
-  return (2 + slots(fmt, d)) * tile_bytes(d) + (fmt == H2O_KV8 ? kRawSlots * kN * d : 0) + 1024;
+  return 2 * kM * d * 2 + 2 * stages(fmt, d) * tile_bytes(d) + (fmt == H2O_KV8 ? 2 * kRawStages * tile_keys(d) * d : 0) + 1024;
 }
-// registers of a thread: the block starts with regs_start() each; the softmax warps take what the others give back
+// Registers of a thread: the softmax warps take what the others give back.  8-bit: 512 threads start with 128 each =
+// 256 x 176 + 256 x 80; bfloat16: 384 start with 168 = 256 x 216 + 128 x 72.
 __host__ __device__ constexpr int regs_softmax(int fmt) { return fmt == H2O_KV8 ? 176 : 216; }
 __host__ __device__ constexpr int regs_other(int fmt) { return fmt == H2O_KV8 ? 80 : 72; }
+// Every kPolyEvery-th pair of exponentials runs on the FMA pipe.  4 x 2048 queries against 4096 keys, 32 heads: none 550,
+// one in eight 518, one in four 505, one in three 547, one in two 535 us.
+constexpr int kPolyEvery = 4;
 
 struct Shared {
   uint64_t q_full[2];
-  uint64_t kv_full[kMaxSlots], kv_empty[kMaxSlots];
-  uint64_t raw_full[kRawSlots], raw_empty[kRawSlots];
-  uint64_t s_full[2], p_full[2], o_final[2];
+  uint64_t kv_full[kMaxStages], kv_empty[kMaxStages];
+  uint64_t raw_full[kRawStages], raw_empty[kRawStages];
+  uint64_t s_full[2], s_read[2];   // S is complete / in the softmax threads' registers
+  uint64_t p_full[2], p_empty[2];  // P is complete / used, and O includes it
+  uint64_t o_final[2];
   uint64_t tail;  // the last V tile has been cleared behind the range
   uint32_t tmem_base;
   int abort_flag;
-  float row_factor[2 * kM];
-  __half scale[2][kN];  // 8-bit rows: the powers of two of the tile being converted
+  float row_factor[2 * kM];  // 8-bit rows: softmax scale times the query row's power of two
+  __half scale[2][2][96];    // 8-bit rows: the powers of two of K and V of the tile being converted
 };
 
 __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
@@ -90,6 +107,43 @@ __device__ __forceinline__ float2 ex2_fma2(float2 x) {
   p = __ffma2_rn(p, f, make_float2(1.0000001192092896f, 1.0000001192092896f));
   return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)),
                      __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+}
+
+constexpr float kRescale = 8.f;
+// A tile whose sum against the old reference exceeds this is done again against its own maximum: far inside the range of
+// fp32 and bf16; of f16 (largest 65504) for the 8-bit rows.
+template <int FMT>
+constexpr float kLargeSumOf = FMT == H2O_KV8 ? 4096.f : 1.0e12f;
+
+// Barrier of the eight softmax warps.
+__device__ __forceinline__ void softmax_sync() { asm volatile("barrier.cta.sync 3, 256;" ::: "memory"); }
+// N consecutive columns of the warp's 32 lanes from / to registers
+__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+template <int N>
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[N]) {
+#pragma unroll
+  for (int i = 0; i + 32 <= N; i += 32) tmem_ld32(addr + i, *reinterpret_cast<uint32_t(*)[32]>(&r[i]));
+  if constexpr (N % 32 != 0) tmem_ld16(addr + N / 32 * 32, *reinterpret_cast<uint32_t(*)[16]>(&r[N / 32 * 32]));
+}
+// Waits for loads under way into r; no use of r moves ahead of it.
+template <int N>
+__device__ __forceinline__ void tmem_wait_ld_of(uint32_t (&r)[N]) {
+  tmem_wait_ld();
+#pragma unroll
+  for (int i = 0; i < N; i += 8)
+    asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
+}
+template <int N>
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[N]) {
+  static_assert(N % 32 == 0 || N % 32 == 8 || N % 32 == 16, "");
+  if constexpr (N % 32 == 8) tmem_st8(addr + N / 32 * 32, &r[N / 32 * 32]);
+#pragma unroll
+  for (int i = 0; i + 32 <= N; i += 32) tmem_st32(addr + i, *reinterpret_cast<const uint32_t(*)[32]>(&r[i]));
+  if constexpr (N % 32 == 16) tmem_st16(addr + N / 32 * 32, *reinterpret_cast<const uint32_t(*)[16]>(&r[N / 32 * 32]));
 }
 
 // Barrier of the four converting warps that tells each of them whether all are well.
@@ -129,14 +183,19 @@ __global__ void __launch_bounds__(threads(FMT), 1)
 attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                  const __grid_constant__ AttendView a, int part_index) {
   constexpr bool kF16 = FMT == H2O_KV8;
-  constexpr int kTile = tile_bytes(D), kSlots = slots(FMT, D), kRaw = kN * D;
-  constexpr uint32_t kColO = 0, kColS = 256;  // O_g at 128 g, S_g / P_g at 256 + 128 g
+  constexpr int kN = tile_keys(D), kTile = tile_bytes(D), kQTile = kM * D * 2, kStages = stages(FMT, D), kRaw = kN * D;
+  constexpr float kLargeSum = kLargeSumOf<FMT>;
+  // tensor memory: O, S (starts on multiples of 32 columns) and P (of 8) of the two groups
+  constexpr uint32_t kColO = 0, kStepO = D, kColS = 2 * D, kStepS = 96, kColP = kColS + kStepS + kN, kStepP = kN / 2;
+  static_assert(kColP + 2 * kStepP <= 512, "tensor memory");
+  static_assert(smem_bytes(FMT, D) + sizeof(Shared) <= 227 * 1024, "shared memory of a block");
+  static_assert(kM * (D + 4) * 4 <= 2 * turn_stages(FMT, D) * kTile, "B's output fits the ring");
   extern __shared__ unsigned char dyn_raw[];
   __shared__ Shared sh;
   unsigned char* dyn = dyn_raw + ((1024u - (smem_u32(dyn_raw) & 1023u)) & 1023u);
   unsigned char* q_tiles = dyn;
-  unsigned char* ring = dyn + 2 * kTile;
-  unsigned char* raw = ring + kSlots * kTile;
+  unsigned char* ring = dyn + 2 * kQTile;
+  unsigned char* raw = ring + 2 * kStages * kTile;
 
   const AttendPart& part = a.part[part_index];
   const BlockWork w = block_work(a, part, blockIdx.x);
@@ -149,22 +208,26 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   if (!direct && key0 >= pr.len) return;  // (the join kernel does not read it)
   const int last_seen = seen_rows(part, pr, (r0 + n_rows - 1) / a.group);
   const int key1 = min(last_seen, key0 + part.chunk);
-  const int nt = max(0, (key1 - key0 + kN - 1) / kN);
-  const int n_groups = n_rows > kM ? 2 : 1;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // (the shuffle tells the compiler that the value is the same in all lanes: the issuing loops then stay in uniform registers)
+  const int nt = __shfl_sync(0xffffffffu, max(0, (key1 - key0 + kN - 1) / kN), 0);
+  const bool alt = __shfl_sync(0xffffffffu, n_rows, 0) <= kM;  // both groups on the same rows, tiles in turn
+  const int n_stages = alt ? turn_stages(FMT, D) : kStages;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
     for (int g = 0; g < 2; ++g) {
       mbar_init(&sh.q_full[g], 4);
       mbar_init(&sh.s_full[g], 1);
+      mbar_init(&sh.s_read[g], 4);
       mbar_init(&sh.p_full[g], 4);
+      mbar_init(&sh.p_empty[g], 1);
       mbar_init(&sh.o_final[g], 1);
     }
-    for (int i = 0; i < kSlots; ++i) {
-      mbar_init(&sh.kv_full[i], kF16 ? 4 : 1);
-      mbar_init(&sh.kv_empty[i], n_groups);
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&sh.kv_full[i], kF16 ? 4 : 1);  // (four converting warps)
+      mbar_init(&sh.kv_empty[i], alt ? 1 : 2);  // a product P V of each group that uses the tile
     }
-    for (int i = 0; i < kRawSlots; ++i) {
+    for (int i = 0; i < kRawStages; ++i) {
       mbar_init(&sh.raw_full[i], 1);
       mbar_init(&sh.raw_empty[i], 4);
     }
@@ -172,145 +235,170 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     sh.abort_flag = 0;
     fence_barrier_init();
   }
-  if (warp == 3) tmem_alloc(&sh.tmem_base, 512);
+  if (warp == 0) tmem_alloc(&sh.tmem_base, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = sh.tmem_base;
+  // the block has all of tensor memory, so it starts at 0: a constant keeps the operand addresses out of registers
+  constexpr uint32_t tmem = 0;
+  if (sh.tmem_base != 0 && threadIdx.x == 0) sh.abort_flag = 1;
   volatile int* abort_flag = &sh.abort_flag;
 
   if (warp < 4 || warp >= 12) {
     setmaxnreg_dec<regs_other(FMT)>();
     if (warp == 0) {
-      // ---- TMA: K_0, V_0, K_1, V_1, ... (16-bit rows: into the operand ring; 8-bit rows: into the code ring) ----
+      // ---- TMA: K_0, V_0, K_1, V_1, ... (16-bit rows: into the stages; 8-bit rows: into the code ring) ----
       if (lane == 0) {
-        constexpr int kS = kF16 ? kRawSlots : kSlots;
-        constexpr uint32_t bytes = kF16 ? kRaw : kTile;
-        uint64_t* full = kF16 ? sh.raw_full : sh.kv_full;
-        uint64_t* empty = kF16 ? sh.raw_empty : sh.kv_empty;
         int slot = 0;
         uint32_t phase = 1;
-        bool ok = true;
-        for (int r = 0; r < 2 * nt; ++r) {
-          ok = wait_or_abort(&empty[slot], phase, abort_flag);
-          if (!ok) break;
-          mbar_expect_tx(&full[slot], bytes);
-          tma_load_tile((kF16 ? raw : ring) + slot * bytes, (r & 1) ? &map_v : &map_k, w.head, (int)pr.row0 + key0 + (r >> 1) * kN, &full[slot]);
-          if (++slot == kS) {
-            slot = 0;
-            phase ^= 1;
+        const int row = (int)pr.row0 + key0;
+        if constexpr (kF16) {
+          for (int j = 0; j < nt; ++j) {
+            if (!wait_or_abort(&sh.raw_empty[slot], phase, abort_flag)) break;
+            mbar_expect_tx(&sh.raw_full[slot], 2 * kRaw);
+            tma_load_tile(raw + 2 * slot * kRaw, &map_k, w.head, row + j * kN, &sh.raw_full[slot]);
+            tma_load_tile(raw + (2 * slot + 1) * kRaw, &map_v, w.head, row + j * kN, &sh.raw_full[slot]);
+            if (++slot == kRawStages) {
+              slot = 0;
+              phase ^= 1;
+            }
+          }
+        } else {
+          for (int j = 0; j < nt; ++j) {
+            if (!wait_or_abort(&sh.kv_empty[slot], phase, abort_flag)) break;
+            mbar_expect_tx(&sh.kv_full[slot], 2 * kTile);
+            tma_load_tile(ring + 2 * slot * kTile, &map_k, w.head, row + j * kN, &sh.kv_full[slot]);
+            tma_load_tile(ring + (2 * slot + 1) * kTile, &map_v, w.head, row + j * kN, &sh.kv_full[slot]);
+            if (++slot == n_stages) {
+              slot = 0;
+              phase ^= 1;
+            }
           }
         }
       }
-    } else if (warp < 3 && warp <= n_groups) {
-      // ---- matrix instructions of group g (the whole warp walks, one elected lane issues) ----
+    } else if (warp < 3) {
+      // ---- S of group g (the whole warp walks, one elected lane issues) ----
       constexpr uint32_t fmt = kF16 ? kFmtF16 : kFmtBF16;
-      constexpr uint32_t idesc_s = instr_desc_f16(kM, kN, fmt, fmt, false, false);
-      constexpr uint32_t idesc_o = instr_desc_f16(kM, D, fmt, fmt, false, true);
-      const int g = warp - 1;
-      const uint32_t d_s = tmem + kColS + 128u * g, d_o = tmem + kColO + 128u * g;
-      const uint64_t dq = smem_desc_sw128(smem_u32(q_tiles + g * kTile), 16, 1024);
-      bool ok = nt == 0 || wait_or_abort(&sh.q_full[g], 0, abort_flag);
-      int slot = 0;
+      constexpr uint32_t idesc = instr_desc_f16(kM, kN, fmt, fmt, false, false);
+      const int g = warp - 1, first = alt ? g : 0, step = alt ? 2 : 1;
+      const uint32_t d_s = tmem + kColS + kStepS * g;
+      const uint64_t dq = smem_desc_sw128(smem_u32(q_tiles + (alt ? 0 : g) * kQTile), 16, 1024);
+      bool ok = first >= nt || wait_or_abort(&sh.q_full[alt ? 0 : g], 0, abort_flag);
+      int slot = first;
       uint32_t phase = 0;
-      auto next = [&] {
-        if (++slot == kSlots) {
-          slot = 0;
+      for (int j = first, n = 0; j < nt; j += step, ++n) {
+        if (slot >= n_stages) {
+          slot -= n_stages;
           phase ^= 1;
         }
-      };
-      for (int j = -1; j < nt; ++j) {
-        if (j >= 0) {  // O += P(j) V_j
-          ok = ok && wait_or_abort(&sh.kv_full[slot], phase, abort_flag);
-          if (!kF16 && j == nt - 1) {
-            // the range's last V tile: zeros behind it, by group A's warp
-            if (g == 0) {
-              const int there = key1 - key0 - j * kN;
-              const uint32_t tile = smem_u32(ring + slot * kTile);
-              ok = __all_sync(0xffffffffu, ok) != 0;
-              if (ok) {
-                for (int i = lane; i < (kN - there) * (D / 8); i += 32)
-                  st_shared16(operand_addr(tile, kN, there + i / (D / 8), i % (D / 8)), make_uint4(0, 0, 0, 0));
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.tail);
-              }
-            }
-            ok = ok && wait_or_abort(&sh.tail, 0, abort_flag);
+        ok = ok && wait_or_abort(&sh.kv_full[slot], phase, abort_flag);
+        if (n > 0) ok = ok && wait_or_abort(&sh.s_read[g], (uint32_t)(n - 1) & 1u, abort_flag);
+        ok = __all_sync(0xffffffffu, ok) != 0;
+        if (!ok) break;
+        tc_fence_after();
+        if (!kF16 && j == nt - 1) {
+          // the range's last V tile: zeros behind it, by group A's warp or the one that uses it
+          if (alt || g == 0) {
+            const int there = key1 - key0 - j * kN;
+            const uint32_t tile = smem_u32(ring + (2 * slot + 1) * kTile);
+            for (int x = lane; x < (kN - there) * (D / 8); x += 32)
+              st_shared16(operand_addr(tile, kN, there + x / (D / 8), x % (D / 8)), make_uint4(0, 0, 0, 0));
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.tail);
+          } else {
+            ok = __all_sync(0xffffffffu, wait_or_abort(&sh.tail, 0, abort_flag)) != 0;
+            if (!ok) break;
           }
-          ok = ok && wait_or_abort(&sh.p_full[g], (uint32_t)j & 1u, abort_flag);
-          ok = __all_sync(0xffffffffu, ok) != 0;
+        }
+        const uint64_t dk = smem_desc_sw128(smem_u32(ring + 2 * slot * kTile), 16, 1024);
+        if (elect_one()) {
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks) {
+            const uint32_t qoff = ((uint32_t)(ks >> 2) * (kM * 128) + (uint32_t)(ks & 3) * 32u) >> 4;
+            const uint32_t koff = ((uint32_t)(ks >> 2) * (kN * 128) + (uint32_t)(ks & 3) * 32u) >> 4;
+            if (ks == 0) mma_ss_lohi<false>(d_s, desc_lo(dq), desc_hi(dq), desc_lo(dk), desc_hi(dk), idesc);
+            else mma_ss_lohi<true>(d_s, desc_lo(dq) + qoff, desc_hi(dq), desc_lo(dk) + koff, desc_hi(dk), idesc);
+          }
+          mma_commit(&sh.s_full[g]);
+        }
+        __syncwarp();
+        slot += step;
+      }
+    } else if (warp == 3) {
+      // ---- O += P V of both groups, in the order A(0), B(0), A(1), ... (tiles in turn: A(0), B(1), A(2), ...) ----
+      constexpr uint32_t fmt = kF16 ? kFmtF16 : kFmtBF16;
+      constexpr uint32_t idesc = instr_desc_f16(kM, D, fmt, fmt, false, true);
+      bool ok = true;
+      int slot = 0;
+      for (int j = 0; j < nt && ok; ++j) {
+        const int n = alt ? j >> 1 : j;  // the group's own count
+        const uint64_t dv = smem_desc_sw128(smem_u32(ring + (2 * slot + 1) * kTile), kTile / 2, 1024);
+        for (int g = alt ? j & 1 : 0; g < (alt ? (j & 1) + 1 : 2); ++g) {
+          ok = __all_sync(0xffffffffu, wait_or_abort(&sh.p_full[g], (uint32_t)n & 1u, abort_flag)) != 0;
           if (!ok) break;
           tc_fence_after();
-          const uint64_t dv = smem_desc_sw128(smem_u32(ring + slot * kTile), kTile / 2, 1024);
+          const uint32_t d_o = tmem + kColO + kStepO * g, d_p = tmem + kColP + kStepP * g;
           if (elect_one()) {
-            if (j == 0) mma_ts_lohi<false>(d_o, d_s, desc_lo(dv), desc_hi(dv), idesc_o);
-            else mma_ts_lohi<true>(d_o, d_s, desc_lo(dv), desc_hi(dv), idesc_o);
+            if (n == 0) mma_ts_lohi<false>(d_o, d_p, desc_lo(dv), desc_hi(dv), idesc);
+            else mma_ts_lohi<true>(d_o, d_p, desc_lo(dv), desc_hi(dv), idesc);
 #pragma unroll
             for (int ks = 1; ks < kN / 16; ++ks)
-              mma_ts_lohi<true>(d_o, d_s + 8u * ks, desc_lo(dv) + ((2048u * ks) >> 4), desc_hi(dv), idesc_o);
+              mma_ts_lohi<true>(d_o, d_p + 8u * ks, desc_lo(dv) + ((2048u * ks) >> 4), desc_hi(dv), idesc);
+            mma_commit(&sh.p_empty[g]);
             mma_commit(&sh.kv_empty[slot]);
-            if (j == nt - 1) mma_commit(&sh.o_final[g]);
+            if (j + (alt ? 2 : 1) >= nt) mma_commit(&sh.o_final[g]);
           }
           __syncwarp();
-          next();
         }
-        if (j + 1 < nt) {  // S(j + 1) = Q K_{j+1}^T, over P(j): one thread's instructions run in order
-          ok = ok && wait_or_abort(&sh.kv_full[slot], phase, abort_flag);
-          ok = __all_sync(0xffffffffu, ok) != 0;
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t dk = smem_desc_sw128(smem_u32(ring + slot * kTile), 16, 1024);
-          if (elect_one()) {
-#pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-              const uint32_t off = ((uint32_t)(ks >> 2) * (kN * 128) + (uint32_t)(ks & 3) * 32u) >> 4;
-              if (ks == 0) mma_ss_lohi<false>(d_s, desc_lo(dq), desc_hi(dq), desc_lo(dk), desc_hi(dk), idesc_s);
-              else mma_ss_lohi<true>(d_s, desc_lo(dq) + off, desc_hi(dq), desc_lo(dk) + off, desc_hi(dk), idesc_s);
-            }
-            mma_commit(&sh.s_full[g]);
-            mma_commit(&sh.kv_empty[slot]);
-          }
-          __syncwarp();
-          next();
-        }
+        if (++slot == n_stages) slot = 0;
       }
     } else if (kF16 && warp >= 12) {
-      // ---- code tiles to f16 tiles: thread t takes chunk t % (D / 16) of every (2048 / D)-th row ----
+      // ---- code tiles to f16 tiles: thread t takes chunk t % (D / 16) of every (2048 / D)-th row, of K and of V ----
       constexpr int kChunks = D / 16, kStride = 128 / kChunks;
       const int t = threadIdx.x - 384, c = t % kChunks;
       const int64_t base = (int64_t)w.head * a.rows + pr.row0;
-      auto fetch = [&](int r) {
-        const int key = key0 + (r >> 1) * kN + t;
-        return key < key1 ? (uint32_t)((r & 1) ? a.v_scale : a.k_scale)[base + key] : 127u;
+      uint32_t byte_k = 127, byte_v = 127;  // the next tile's scales, one row to a thread
+      auto fetch = [&](int j) {
+        const int key = key0 + j * kN + t;
+        if (t < kN && key < key1) {
+          byte_k = a.k_scale[base + key];
+          byte_v = a.v_scale[base + key];
+        }
       };
-      uint32_t byte = nt > 0 ? fetch(0) : 0;
+      if (nt > 0) fetch(0);
       int slot = 0;
       uint32_t phase = 1;
-      for (int r = 0; r < 2 * nt; ++r) {
-        const int rs = r % kRawSlots;
-        sh.scale[r & 1][t] = __float2half_rn(kv8_scale(byte));
-        if (r + 1 < 2 * nt) byte = fetch(r + 1);
-        bool ok = wait_or_abort(&sh.raw_full[rs], (uint32_t)(r / kRawSlots) & 1u, abort_flag);
+      for (int j = 0; j < nt; ++j) {
+        const int rs = j % kRawStages;
+        if (t < kN) {
+          sh.scale[j & 1][0][t] = __float2half_rn(kv8_scale(byte_k));
+          sh.scale[j & 1][1][t] = __float2half_rn(kv8_scale(byte_v));
+        }
+        if (j + 1 < nt) fetch(j + 1);
+        bool ok = wait_or_abort(&sh.raw_full[rs], (uint32_t)(j / kRawStages) & 1u, abort_flag);
         ok = ok && wait_or_abort(&sh.kv_empty[slot], phase, abort_flag);
         ok = together(ok);  // (also publishes the scales; one answer for the four warps, so that none waits for another)
         if (ok) {
-          const uint32_t src = smem_u32(raw + rs * kRaw), dst = smem_u32(ring + slot * kTile);
-          const int there = min(kN, key1 - key0 - (r >> 1) * kN);
-#pragma unroll 4
-          for (int i = 0; i < kN / kStride; ++i) {
-            const int row = t / kChunks + i * kStride;
-            const uint32_t at = D == 128 ? src + row * 128 + ((c ^ (row & 7)) << 4) : src + row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
-            uint32_t x[4];
-            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at) : "memory");
-            const __half2 f = __half2half2(sh.scale[r & 1][row]);
-            uint4 y[2];
-            y[0] = make_uint4(codes_to_f16(x[0] & 0xffffu, f), codes_to_f16(x[0] >> 16, f), codes_to_f16(x[1] & 0xffffu, f), codes_to_f16(x[1] >> 16, f));
-            y[1] = make_uint4(codes_to_f16(x[2] & 0xffffu, f), codes_to_f16(x[2] >> 16, f), codes_to_f16(x[3] & 0xffffu, f), codes_to_f16(x[3] >> 16, f));
-            if (row >= there) y[0] = y[1] = make_uint4(0, 0, 0, 0);  // behind the range
-            const int first = (c >> 2) & 1;  // (lanes of the two halves start with different chunks: no bank conflict)
-            st_shared16(operand_addr(dst, kN, row, 2 * c + first), first ? y[1] : y[0]);
-            st_shared16(operand_addr(dst, kN, row, 2 * c + 1 - first), first ? y[0] : y[1]);
+          const int there = min(kN, key1 - key0 - j * kN);
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            const uint32_t src = smem_u32(raw + (2 * rs + kv) * kRaw), dst = smem_u32(ring + (2 * slot + kv) * kTile);
+#pragma unroll
+            for (int i = 0; i < kN / kStride; ++i) {
+              const int row = t / kChunks + i * kStride;
+              const uint32_t at = D == 128 ? src + row * 128 + ((c ^ (row & 7)) << 4) : src + row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
+              uint32_t x[4];
+              asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at) : "memory");
+              const __half2 f = __half2half2(sh.scale[j & 1][kv][row]);
+              uint4 y[2];
+              y[0] = make_uint4(codes_to_f16(x[0] & 0xffffu, f), codes_to_f16(x[0] >> 16, f), codes_to_f16(x[1] & 0xffffu, f), codes_to_f16(x[1] >> 16, f));
+              y[1] = make_uint4(codes_to_f16(x[2] & 0xffffu, f), codes_to_f16(x[2] >> 16, f), codes_to_f16(x[3] & 0xffffu, f), codes_to_f16(x[3] >> 16, f));
+              if (row >= there) y[0] = y[1] = make_uint4(0, 0, 0, 0);  // behind the range
+              const int first = (c >> 2) & 1;  // (lanes of the two halves start with different chunks: no bank conflict)
+              st_shared16(operand_addr(dst, kN, row, 2 * c + first), first ? y[1] : y[0]);
+              st_shared16(operand_addr(dst, kN, row, 2 * c + 1 - first), first ? y[0] : y[1]);
+            }
           }
           fence_proxy_async();
         }
@@ -320,7 +408,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           mbar_arrive(&sh.raw_empty[rs]);
           mbar_arrive(&sh.kv_full[slot]);
         }
-        if (++slot == kSlots) {
+        if (++slot == n_stages) {
           slot = 0;
           phase ^= 1;
         }
@@ -329,23 +417,30 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   } else {
     setmaxnreg_inc<regs_softmax(FMT)>();
     const int g = (warp - 4) >> 2, quarter = warp & 3;
-    if (g < n_groups) {
+    const int base = alt ? 0 : g * kM;  // the group's first row in the block
+    if (base < n_rows) {
       // ---- the group's query rows into shared memory: D / 8 lanes a row ----
-      {
+      if (nt > 0 && !(alt && g == 1)) {
         constexpr int kLanes = D / 8, kPer = 32 / kLanes;
         const int c = lane % kLanes;
-        const uint32_t tile = smem_u32(q_tiles + g * kTile);
-#pragma unroll 4
+        const uint32_t tile = smem_u32(q_tiles + g * kQTile);
+        // (all loads first: they share the memory with the first tiles, and a trip takes microseconds then)
+        uint4 x[32 / kPer];
+#pragma unroll
         for (int i = 0; i < 32 / kPer; ++i) {
-          const int rt = quarter * 32 + i * kPer + lane / kLanes, r = g * kM + rt;
-          uint4 x = make_uint4(0, 0, 0, 0);
+          const int r = base + quarter * 32 + i * kPer + lane / kLanes;
+          x[i] = make_uint4(0, 0, 0, 0);
           if (r < n_rows) {
             const int tok = (r0 + r) / a.group, hq = w.head * a.group + (r0 + r) - tok * a.group;
-            x = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (pr.t0 + tok) * a.q_stride + (int64_t)hq * D + c * 8);
+            x[i] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (pr.t0 + tok) * a.q_stride + (int64_t)hq * D + c * 8);
           }
+        }
+#pragma unroll
+        for (int i = 0; i < 32 / kPer; ++i) {
+          const int rt = quarter * 32 + i * kPer + lane / kLanes, r = base + rt;
           if constexpr (kF16) {
             float f[8];
-            Vec16<__nv_bfloat16>::unpack(x, f);
+            Vec16<__nv_bfloat16>::unpack(x[i], f);
             float big = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) big = fabsf(f[e]) < INFINITY ? fmaxf(big, fabsf(f[e])) : big;
@@ -353,100 +448,148 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             for (int o = kLanes / 2; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
             const int e2 = max(-100, min(126, (int)(__float_as_uint(big) >> 23) - 127));
             const float down = __uint_as_float((uint32_t)(127 - e2) << 23);
-            x = make_uint4(pack_half2(f[0] * down, f[1] * down), pack_half2(f[2] * down, f[3] * down),
-                           pack_half2(f[4] * down, f[5] * down), pack_half2(f[6] * down, f[7] * down));
+            x[i] = make_uint4(pack_half2(f[0] * down, f[1] * down), pack_half2(f[2] * down, f[3] * down),
+                              pack_half2(f[4] * down, f[5] * down), pack_half2(f[6] * down, f[7] * down));
             if (c == 0) sh.row_factor[r] = a.scale2 * __uint_as_float((uint32_t)(127 + e2) << 23);
           }
-          st_shared16(operand_addr(tile, kM, rt, c), x);
+          st_shared16(operand_addr(tile, kM, rt, c), x[i]);
         }
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.q_full[g]);
       }
-      // ---- softmax, one thread per row ----
-      const int rt = quarter * 32 + lane, r = g * kM + rt;
+      // (both groups on the same rows, 8-bit: B takes the row factors that A's warps left)
+      if (kF16 && alt) softmax_sync();
+
+      // ---- softmax ----
+      const int rt = quarter * 32 + lane, r = base + rt;
       const int tok = (r0 + r) / a.group;
       const int seen = min(key1, r < n_rows ? seen_rows(part, pr, tok) : key1);
-      const int all_seen = part.causal ? min(key1, seen_rows(part, pr, (r0 + g * kM) / a.group)) : key1;
+      const int all_seen = part.causal ? min(key1, seen_rows(part, pr, (r0 + base) / a.group)) : key1;
       const float factor = kF16 ? sh.row_factor[r] : a.scale2;
       const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
-      const uint32_t t_s = tmem + kColS + 128u * g + lane_addr, t_o = tmem + kColO + 128u * g + lane_addr;
+      const uint32_t t_s = tmem + kColS + kStepS * g + lane_addr, t_o = tmem + kColO + kStepO * g + lane_addr;
+      const uint32_t t_p = tmem + kColP + kStepP * g + lane_addr;
       float m = -INFINITY;
       float2 l2 = make_float2(0.f, 0.f);
       bool ok = true;
-      for (int j = 0; j < nt; ++j) {
-        ok = __all_sync(0xffffffffu, wait_or_abort(&sh.s_full[g], (uint32_t)j & 1u, abort_flag));
+      const int first = alt ? g : 0, step = alt ? 2 : 1;
+      using N0 = std::integral_constant<int, 0>;
+      using N1 = std::integral_constant<int, kN * 3 / 8>;
+      using N2 = std::integral_constant<int, kN / 2>;
+      for (int j = first, n = 0; j < nt; j += step, ++n) {
+        ok = __all_sync(0xffffffffu, wait_or_abort(&sh.s_full[g], (uint32_t)n & 1u, abort_flag));
         if (!ok) break;
         tc_fence_after();
-        uint32_t s[4][32];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld32(t_s + 32u * i, s[i]);
-        tmem_wait_ld();
         const int key = key0 + j * kN;
+        uint32_t s[kN], p[kN / 2];
+        tmem_load(t_s, s);
+        tmem_wait_ld_of(s);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.s_read[g]);
         if (key + kN > all_seen) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (key + 32 * i + e >= seen) s[i][e] = 0xff800000u;
+          for (int e = 0; e < kN; ++e)
+            if (key + e >= seen) s[e] = 0xff800000u;
         }
-        float top4[4];
+        // two 16-bit probabilities to a word of p, words FROM .. TO - 1; returns their sum
+        auto exponentials = [&](auto from, auto to) {
+          const float neg = m == -INFINITY ? 0.f : -m;
+          float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          top4[i] = __uint_as_float(s[i][0]);
+          for (int e = decltype(from)::value; e < decltype(to)::value; ++e) {
+            const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])),
+                                        make_float2(factor, factor), make_float2(neg, neg));
+            const float2 y = e % kPolyEvery == kPolyEvery - 1 ? ex2_fma2(x) : make_float2(ex2(x.x), ex2(x.y));
+            sum = __fadd2_rn(sum, y);
+            p[e] = kF16 ? pack_half2(y.x, y.y) : Vec16<__nv_bfloat16>::pack2(y.x, y.y);
+          }
+          return sum;
+        };
+        float2 sum = exponentials(N0{}, N1{});
+        // Has P(j - 1) been used (and does O include it)?  Asked ahead: the last exponentials hide the answer's way.
+        const bool used = n == 0 || mbar_test_wait(&sh.p_empty[g], (uint32_t)(n - 1) & 1u);
+        sum = __fadd2_rn(sum, exponentials(N1{}, N2{}));
+        if (!used) ok = wait_or_abort(&sh.p_empty[g], (uint32_t)(n - 1) & 1u, abort_flag);
+        const bool again = m == -INFINITY || sum.x + sum.y > kLargeSum;
+        if (__any_sync(0xffffffffu, again || !ok)) {
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          float top = -INFINITY;
 #pragma unroll
-          for (int e = 1; e + 1 < 32; e += 2) top4[i] = max3(top4[i], __uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
-          top4[i] = fmaxf(top4[i], __uint_as_float(s[i][31]));
-        }
-        // (the factor is positive: the maximum commutes with it)
-        const float top = fmaxf(max3(top4[0], top4[1], top4[2]), top4[3]) * factor;
-        const bool grows = top > m + kRescale;
-        if (__any_sync(0xffffffffu, grows)) {
-          const float mn = grows ? top : m;
+          for (int e = 0; e < kN; e += 2) top = max3(top, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+          top *= factor;  // (the factor is positive: the maximum commutes with it)
+          const float mn = top > m + kRescale ? top : m;
           const float alpha = mn == -INFINITY ? 1.f : ex2(m - mn);
           l2 = __fmul2_rn(l2, make_float2(alpha, alpha));
           m = mn;
-          if (j > 0) {
+          if (n > 0) {
+            tc_fence_after();
 #pragma unroll
-            for (int cc = 0; cc < D / 32; ++cc) {
-              uint32_t o[32];
-              tmem_ld32(t_o + 32u * cc, o);
+            for (int cc = 0; cc < D / 16; ++cc) {
+              uint32_t o[16];
+              tmem_ld16(t_o + 16u * cc, o);
               tmem_wait_ld();
 #pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-              tmem_st32(t_o + 32u * cc, o);
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+              tmem_st16(t_o + 16u * cc, o);
             }
           }
+          sum = exponentials(N0{}, N2{});
         }
-        const float neg = m == -INFINITY ? 0.f : -m;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          uint32_t pw[32];  // 64 keys, two to a column
-#pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const uint32_t(&src)[32] = s[2 * i + (e >> 4)];
-            const int at = 2 * (e & 15);
-            const float2 x = __ffma2_rn(make_float2(__uint_as_float(src[at]), __uint_as_float(src[at + 1])),
-                                        make_float2(factor, factor), make_float2(neg, neg));
-            const float2 p = (e & 3) == 3 ? ex2_fma2(x) : make_float2(ex2(x.x), ex2(x.y));
-            l2 = __fadd2_rn(l2, p);
-            pw[e] = kF16 ? pack_half2(p.x, p.y) : Vec16<__nv_bfloat16>::pack2(p.x, p.y);
-          }
-          tmem_st32(t_s + 32u * i, pw);
-        }
+        l2 = __fadd2_rn(l2, sum);
+        tc_fence_after();
+        tmem_store(t_p, p);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.p_full[g]);
       }
       // ---- result ----
-      if (ok && nt > 0) ok = __all_sync(0xffffffffu, wait_or_abort(&sh.o_final[g], 0, abort_flag));
-      if (ok) {
+      const float sum = l2.x + l2.y;
+      bool none = !ok || sum == 0.f || m == -INFINITY;
+      const bool wrote = nt > first;  // the group has an O
+      if (ok && wrote) ok = __all_sync(0xffffffffu, wait_or_abort(&sh.o_final[g], 0, abort_flag));
+      float* join = reinterpret_cast<float*>(q_tiles);  // [2][128]
+      if (alt) {  // B leaves m, sum (over Q) and O (over the K/V ring: both groups are done with them), A joins them
+        if (g == 1 && ok && nt > 0) ok = __all_sync(0xffffffffu, wait_or_abort(&sh.o_final[0], 0, abort_flag));
         tc_fence_after();
-        const float sum = l2.x + l2.y;
-        const bool none = sum == 0.f || m == -INFINITY;
-        const float inv = none ? 0.f : 1.f / sum;
-        const float lse2 = none ? -INFINITY : m + log2f(sum);
+        float* theirs = reinterpret_cast<float*>(ring) + rt * (D + 4);
+        if (g == 1) {
+          join[rt] = none ? -INFINITY : m;
+          join[kM + rt] = none ? 0.f : sum;
+#pragma unroll
+          for (int cc = 0; cc < D / 32; ++cc) {
+            uint32_t o[32];
+            if (wrote) {
+              tmem_ld32(t_o + 32u * cc, o);
+              tmem_wait_ld();
+            }
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              *reinterpret_cast<uint4*>(theirs + cc * 32 + e) = none ? make_uint4(0, 0, 0, 0) : make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          }
+        }
+        softmax_sync();
+      }
+      if (ok && !(alt && g == 1)) {
+        tc_fence_after();
+        float mine_w = none ? 0.f : 1.f, their_w = 0.f, total = none ? 0.f : sum, top = none ? -INFINITY : m;
+        const float* theirs = reinterpret_cast<const float*>(ring) + rt * (D + 4);
+        if (alt) {
+          const float mb = join[rt];
+          const float mx = fmaxf(top, mb);
+          if (mx > -INFINITY) {
+            mine_w = none ? 0.f : ex2(m - mx);
+            their_w = ex2(mb - mx);
+            total = mine_w * total + their_w * join[kM + rt];
+            top = mx;
+          }
+        }
+        none = total == 0.f;
+        const float inv = none ? 0.f : 1.f / total;
+        const float lse2 = none ? -INFINITY : top + log2f(total);
         const int64_t token = pr.t0 + tok;
         const int hq = w.head * a.group + (r0 + r) - tok * a.group;
         const int64_t at = ((int64_t)(part.slot0 + w.split) * a.q_rows + token) * a.heads * a.group + hq;
@@ -455,13 +598,21 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll
         for (int cc = 0; cc < D / 32; ++cc) {
           uint32_t o[32];
-          if (nt > 0) {
+          if (wrote) {
             tmem_ld32(t_o + 32u * cc, o);
             tmem_wait_ld();
           }
           if (r >= n_rows) continue;
+          if (alt) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = none ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv);
+            for (int e = 0; e < 32; ++e) {
+              const float own = mine_w == 0.f ? 0.f : mine_w * __uint_as_float(o[e]);
+              o[e] = __float_as_uint(fmaf(their_w, theirs[cc * 32 + e], own) * inv);
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = none ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv);
+          }
           if (direct) {
             uint32_t x[16];
 #pragma unroll
@@ -499,7 +650,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && sh.abort_flag && a.status) atomicCAS(a.status, 0, H2O_ERR_TIMEOUT);
-  if (warp == 3) {
+  if (warp == 0) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
