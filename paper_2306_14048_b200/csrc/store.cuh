@@ -19,7 +19,7 @@ struct h2o_store {
 
 namespace h2o {
 
-constexpr int kKv8 = H2O_KV8;
+constexpr int kMaxSplits = 64;  // of a part's keys
 
 struct AttendPart {
   const int64_t* begin;    // dev [problems]: first store row
@@ -116,6 +116,7 @@ constexpr int kFewBoxRows = 32;  // rows of a box of the store's tensor maps
 inline int many_box_rows(int dim) { return dim == 128 ? 80 : 96; }
 bool make_store_map(CUtensorMap_st* map, const h2o_store_config_t& c, const void* base, int box_rows);
 int attend_mma_row_tile(int64_t rows);
+int attend_mma_blocks_per_sm(int format, int tile);
 // part `first`, or (both) parts 0 and 1 in one launch
 cudaError_t launch_attend_mma(const AttendView& a, int first, bool both, const int* tile, int format, const void* map_k,
                               const void* map_v, cudaStream_t stream);

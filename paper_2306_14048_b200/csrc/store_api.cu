@@ -108,20 +108,26 @@ struct Plan {
 
 // More query rows than this (of one K/V head) run on the tcgen05 kernel, 256 to a block; up to it the mma.sync kernel
 // reads each key once.
-constexpr int kFewRows = 32;
+#ifndef KFEW
+#define KFEW 32
+#endif
+constexpr int kFewRows = KFEW;
 
-// Splits the keys of a part: `units` blocks per split, `room` blocks that run at once.  A block costs its keys plus
-// about `fixed` keys' time (start, merge, its result's trip through memory); blocks run in waves while there are few of
-// them.
-void split_part(h2o::AttendPart& p, int64_t units, int64_t room, int64_t fixed) {
-  const int64_t len = std::max(1, p.max_length);
+// Splits the keys of a part: `units` blocks per split, `room` blocks that run at once.  Costs in keys of one block: a block
+// costs its keys and `fixed` more (start, merge, its result's trip through memory), the joining kernel twice as much;
+// a block that has its SM to itself is taken to run twice as fast, and the last blocks to finish to leave a quarter of a
+// block's time unused.  Only the longest length is known here: the lengths of a batch's sequences (`ragged`) are taken
+// to average two thirds of it.
+void split_part(h2o::AttendPart& p, int64_t units, int64_t room, int64_t fixed, bool ragged) {
+  const int64_t len = std::max(1, p.max_length), num = ragged ? 2 : 3;
   int64_t best = -1;
-  for (int64_t n = 1; n <= 64; ++n) {
+  for (int64_t n = 1; n <= h2o::kMaxSplits; ++n) {
     const int64_t chunk = ((len + n - 1) / n + 127) / 128 * 128;
     const int64_t splits = (len + chunk - 1) / chunk;
-    const int64_t blocks = units * splits, waves = (blocks + room - 1) / room;
-    int64_t cost = waves <= 4 ? waves * (std::min(chunk, len) + fixed) : blocks * (std::min(chunk, len) + fixed) / room;
-    if (splits > 1) cost += fixed;
+    const int64_t one = std::min(chunk, len) + fixed;
+    const int64_t blocks = std::max(units, units * splits * num / 3);
+    int64_t cost = std::max(one / 2, (units * len * num / 3 + blocks * fixed) / room) + one / 4;
+    if (splits > 1) cost += 2 * fixed;
     if (best < 0 || cost < best) {
       best = cost;
       p.chunk = (int)chunk;
@@ -180,7 +186,11 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
                                               : h2o::attend_mma_row_tile(rows);
     p.row_tiles = (int)((rows + pl.tile[n] - 1) / pl.tile[n]);
     const int64_t units = (int64_t)p.row_tiles * a.heads * p.problems;
-    split_part(p, units, h2o::sm_count() * (pl.kernel[n] == Kernel::Tc ? 1 : 2), pl.kernel[n] == Kernel::Tc ? 512 : 256);
+    // Fixed costs: about 3 us at a block's share of the memory's 6.4 TB/s; of the tcgen05 kernel 8 us at 80 keys in 1 us.
+    const int key_bytes = 2 * a.dim * (c.format == H2O_KV8 ? 1 : c.format == H2O_BF16 ? 2 : 4);
+    const int per_sm = pl.kernel[n] == Kernel::Tc ? 1 : pl.kernel[n] == Kernel::Fma ? 2 : h2o::attend_mma_blocks_per_sm(c.format, pl.tile[n]);
+    const int64_t room = (int64_t)h2o::sm_count() * per_sm;
+    split_part(p, units, room, pl.kernel[n] == Kernel::Tc ? 640 : 19200000 / (room * key_bytes), !p.grouped);
     if (units * p.splits > INT32_MAX) pl.rc = H2O_ERR_UNSUPPORTED;
     p.slot0 = n == 0 ? 0 : a.part[0].splits;
     ++n;

@@ -1,5 +1,4 @@
-// Attention over a K/V store for float32 queries, on the fp32 FMA pipe (float32 or 8-bit rows, head_dim 64 and 128), and
-// the kernel that joins the parts of a split, for every type.
+// Attention over a K/V store for float32 queries, on the fp32 FMA pipe (float32 or 8-bit rows, head_dim 64 and 128).
 //
 // A block takes BM query rows (query tokens times the query heads of one K/V head) and walks over its keys 64 at a
 // time: S = Q K^T by register tiles, softmax with the running maximum and sum of each row, O += P V.
@@ -235,68 +234,6 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
   }
 }
 
-// Joins the chunks of every query row: weights 2^(lse_i - max), in the fixed order of the chunks.  One warp per row.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant__ AttendView a) {
-  const int seq = blockIdx.y;
-  const int lane = threadIdx.x & 31;
-  const int hq_all = a.heads * a.group;
-  const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int64_t t0 = first_token(a, seq);
-  const int nt = (int)clamp64(first_token(a, seq + 1) - t0, 0, a.max_q);
-  const int i = (int)(item / hq_all), hq = (int)(item - (int64_t)i * hq_all);
-  if (i >= nt) return;
-  const int64_t token = t0 + i;
-  constexpr int kPer = D / 32;
-  // chunks of this row: for each part, the first and how many were written
-  int slot[2] = {0, 0}, used[2] = {0, 0};
-  for (int k = 0; k < a.n_parts; ++k) {
-    const AttendPart& p = a.part[k];
-    int which = seq;
-    if (p.grouped) {
-      which = 0;
-      if (a.cu_group) {  // the group of this sequence: the last one that starts at or before it
-        int lo = 0, hi = a.n_groups;
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (a.cu_group[mid] <= seq) lo = mid;
-          else hi = mid;
-        }
-        which = lo;
-      }
-    }
-    const Problem pr = locate(a, p, which);
-    if (token < pr.t0 || token >= pr.t0 + pr.nt) return;  // beyond what the caller allowed for: left as it was
-    slot[k] = p.slot0;
-    used[k] = (pr.len + p.chunk - 1) / p.chunk;
-  }
-  const int64_t pitch = a.q_rows * hq_all, at = token * hq_all + hq;
-  float top = -INFINITY;
-  for (int k = 0; k < a.n_parts; ++k)
-    for (int s = 0; s < used[k]; ++s) top = fmaxf(top, a.part_lse[(slot[k] + s) * pitch + at]);
-  float total = 0.f, o[kPer];
-#pragma unroll
-  for (int e = 0; e < kPer; ++e) o[e] = 0.f;
-  for (int k = 0; k < a.n_parts; ++k)
-    for (int s = 0; s < used[k]; ++s) {
-      const int64_t j = (slot[k] + s) * pitch + at;
-      const float lse2 = a.part_lse[j];
-      if (lse2 == -INFINITY) continue;  // (a chunk without a visible key)
-      const float wgt = exp2f(lse2 - top);
-      total += wgt;
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) o[e] = fmaf(wgt, a.part_out[j * D + lane * kPer + e], o[e]);
-    }
-  const float inv = total == 0.f ? 0.f : 1.f / total;
-  T* to = static_cast<T*>(a.out) + token * a.out_stride + (int64_t)hq * D + lane * kPer;
-#pragma unroll
-  for (int e = 0; e < kPer; ++e) {
-    if constexpr (sizeof(T) == 4) to[e] = o[e] * inv;
-    else to[e] = __float2bfloat16(o[e] * inv);
-  }
-  if (a.lse && lane == 0) a.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
-}
-
 template <int FMT, int D, int BM>
 cudaError_t launch(const AttendView& a, int part, cudaStream_t stream) {
   constexpr int smem = (int)sizeof(Smem<D, BM>);
@@ -318,19 +255,6 @@ int attend_fma_row_tile(int64_t rows) { return rows <= 16 ? 16 : 64; }
 
 cudaError_t launch_attend_fma(const AttendView& a, int part, int tile, int format, cudaStream_t stream) {
   return format == H2O_F32 ? launch_shape<H2O_F32>(a, part, tile, stream) : launch_shape<H2O_KV8>(a, part, tile, stream);
-}
-
-cudaError_t launch_attend_join(const AttendView& a, int q_dtype, cudaStream_t stream) {
-  const int64_t rows = (int64_t)a.max_q * a.heads * a.group;
-  const dim3 grid((unsigned)((rows + 7) / 8), (unsigned)a.batch);
-  if (q_dtype == H2O_F32) {
-    if (a.dim == 128) attend_join_kernel<float, 128><<<grid, 256, 0, stream>>>(a);
-    else attend_join_kernel<float, 64><<<grid, 256, 0, stream>>>(a);
-  } else {
-    if (a.dim == 128) attend_join_kernel<__nv_bfloat16, 128><<<grid, 256, 0, stream>>>(a);
-    else attend_join_kernel<__nv_bfloat16, 64><<<grid, 256, 0, stream>>>(a);
-  }
-  return cudaGetLastError();
 }
 
 }  // namespace h2o

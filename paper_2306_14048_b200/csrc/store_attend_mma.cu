@@ -37,13 +37,18 @@ constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kKeys = kFewBoxRows;                  // keys of a tile
 constexpr uint32_t kSpin = 1u << 22;
 constexpr float kRescale = 8.f;
-constexpr int kRingBytes = 96 * 1024;                 // per block: two blocks on an SM
+// Shared memory of a block's rings (KB) and blocks on an SM, for blocks of up to 8 nt rows.  More blocks of smaller rings
+// where registers allow: 8-bit rows, whose conversion wants warps, 39.4 us with 2 blocks of 96 KB, 37.2 with 3 of 64, 34.5
+// with 4 of 48 (32 sequences of 1024 .. 4096 rows, 8 K/V heads of 4 query heads); bfloat16 rows 193.5 / 192.1 / 197.5 us
+// (64 sequences of up to 2048 rows, 32 heads).
+__host__ __device__ constexpr int ring_kb(int fmt, int nt) { return nt > 1 ? 96 : fmt == H2O_KV8 ? 48 : 64; }
+__host__ __device__ constexpr int blocks_per_sm(int fmt, int nt) { return 192 / ring_kb(fmt, nt); }
 constexpr int kMaxSlots = 8;
 
 __host__ __device__ constexpr int row_bytes(int fmt, int d) { return fmt == H2O_KV8 ? d : 2 * d; }
 __host__ __device__ constexpr int tile_bytes(int fmt, int d) { return kKeys * row_bytes(fmt, d); }
-__host__ __device__ constexpr int ring_slots(int fmt, int d) {
-  return kRingBytes / kWarps / tile_bytes(fmt, d) < kMaxSlots ? kRingBytes / kWarps / tile_bytes(fmt, d) : kMaxSlots;
+__host__ __device__ constexpr int ring_slots(int fmt, int d, int nt) {
+  return ring_kb(fmt, nt) * 1024 / kWarps / tile_bytes(fmt, d) < kMaxSlots ? ring_kb(fmt, nt) * 1024 / kWarps / tile_bytes(fmt, d) : kMaxSlots;
 }
 
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
@@ -88,10 +93,8 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ uint32_t codes_to_f16(uint32_t pair) {  // two e4m3 codes in the low 16 bits
-  uint32_t r;
-  asm("{\n\t.reg .b16 h;\n\tcvt.u16.u32 h, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(pair));
-  return r;
+__device__ __forceinline__ void codes_to_f16(uint32_t word, uint32_t& lo, uint32_t& hi) {  // four e4m3 codes
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(word));
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -121,11 +124,12 @@ __device__ __forceinline__ uint32_t chunk_addr(uint32_t tile, int r, int c) {
   else return tile + (c >> 3) * (kKeys * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
 }
 
-template <int FMT, int D, int NT>
+// NTB: the kernel's larger number of n-tiles, which the ring is made for.
+template <int FMT, int D, int NT, int NTB>
 __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* map_k, const CUtensorMap* map_v,
                                        const AttendPart& part, unsigned block, unsigned char* ring, Shared& sh) {
   constexpr bool kF16 = FMT == H2O_KV8;
-  constexpr int kTile = tile_bytes(FMT, D), kSlots = ring_slots(FMT, D), kSteps = D / 16, kRows = 8 * NT;
+  constexpr int kTile = tile_bytes(FMT, D), kSlots = ring_slots(FMT, D, NTB), kSteps = D / 16, kRows = 8 * NT;
   constexpr int kPitch = D + 4;  // floats per row of a warp's partial output
   static_assert(kRows * kPitch * 4 <= kSlots * kTile, "a warp's partial output fits its ring");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gl = lane >> 2, c4 = lane & 3;
@@ -301,10 +305,8 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
             for (int mt = 0; mt < 2; ++mt) {
               const uint32_t wl = t == 0 ? lo[mt].x : t == 1 ? lo[mt].y : t == 2 ? lo[mt].z : lo[mt].w;
               const uint32_t wh = t == 0 ? hi[mt].x : t == 1 ? hi[mt].y : t == 2 ? hi[mt].z : hi[mt].w;
-              ka[mt][0] = codes_to_f16(wl & 0xffffu);
-              ka[mt][1] = codes_to_f16(wh & 0xffffu);
-              ka[mt][2] = codes_to_f16(wl >> 16);
-              ka[mt][3] = codes_to_f16(wh >> 16);
+              codes_to_f16(wl, ka[mt][0], ka[mt][2]);
+              codes_to_f16(wh, ka[mt][1], ka[mt][3]);
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -429,7 +431,8 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
                 const uint32_t y = __byte_perm(x[2 * q + h], 0, 0x3120);
-                const uint32_t e0 = codes_to_f16(y & 0xffffu), e1 = codes_to_f16(y >> 16);
+                uint32_t e0, e1;
+                codes_to_f16(y, e0, e1);
                 const __half2 g0 = __hmul2(*reinterpret_cast<const __half2*>(&e0), h ? f1 : f0);
                 const __half2 g1 = __hmul2(*reinterpret_cast<const __half2*>(&e1), h ? f1 : f0);
                 va[2 * h] = *reinterpret_cast<const uint32_t*>(&g0);
@@ -511,7 +514,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
 // One launch for part `first` alone, with 8 NT0 rows to a block, or for parts 0 and 1 (a shared prefix: many rows and
 // few), with 8 NT0 and 8 NT1.
 template <int FMT, int D, int NT0, int NT1>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(FMT, NT0))
 attend_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                   const __grid_constant__ AttendView a, int first, unsigned blocks0) {
   extern __shared__ unsigned char dyn[];
@@ -519,15 +522,15 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   unsigned char* ring = dyn + ((1024u - (smem_u32(dyn) & 1023u)) & 1023u);
   if (NT0 == NT1 || blockIdx.x < blocks0) {
     const bool second = blockIdx.x >= blocks0;
-    attend<FMT, D, NT0>(a, &map_k, &map_v, a.part[second ? 1 : first], blockIdx.x - (second ? blocks0 : 0), ring, sh);
+    attend<FMT, D, NT0, NT0>(a, &map_k, &map_v, a.part[second ? 1 : first], blockIdx.x - (second ? blocks0 : 0), ring, sh);
   } else {
-    attend<FMT, D, NT1>(a, &map_k, &map_v, a.part[1], blockIdx.x - blocks0, ring, sh);
+    attend<FMT, D, NT1, NT0>(a, &map_k, &map_v, a.part[1], blockIdx.x - blocks0, ring, sh);
   }
 }
 
 template <int FMT, int D, int NT0, int NT1>
 cudaError_t launch(const AttendView& a, int first, bool both, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t stream) {
-  constexpr int smem = kWarps * ring_slots(FMT, D) * tile_bytes(FMT, D) + 1024;
+  constexpr int smem = kWarps * ring_slots(FMT, D, NT0) * tile_bytes(FMT, D) + 1024;
   static unsigned long long flags = 0;
   const void* f = reinterpret_cast<const void*>(attend_mma_kernel<FMT, D, NT0, NT1>);
   const cudaError_t e = ensure_dynamic_smem(f, smem, &flags);
@@ -554,6 +557,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
 }  // namespace
 
 int attend_mma_row_tile(int64_t rows) { return rows <= 8 ? 8 : rows <= 16 ? 16 : 32; }
+int attend_mma_blocks_per_sm(int format, int tile) { return blocks_per_sm(format, tile / 8); }
 
 // Rows of a store: {bytes or elements of up to 128 bytes, rows, pieces of a row, heads}; a box is `box_rows` rows of one
 // head, swizzled over as many bytes as its inner extent.

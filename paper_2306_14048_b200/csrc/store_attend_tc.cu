@@ -171,11 +171,12 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ uint32_t codes_to_f16(uint32_t pair, __half2 scale) {  // two e4m3 codes times a power of two
-  uint32_t r;
-  asm("{\n\t.reg .b16 h;\n\tcvt.u16.u32 h, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(pair));
-  const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&r), scale);
-  return *reinterpret_cast<const uint32_t*>(&h);
+// four e4m3 codes times a power of two
+__device__ __forceinline__ void codes_to_f16(uint32_t word, __half2 scale, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(word));
+  const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&lo), scale), y = __hmul2(*reinterpret_cast<const __half2*>(&hi), scale);
+  lo = *reinterpret_cast<const uint32_t*>(&x);
+  hi = *reinterpret_cast<const uint32_t*>(&y);
 }
 
 template <int FMT, int D>
@@ -212,6 +213,14 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   const int nt = __shfl_sync(0xffffffffu, max(0, (key1 - key0 + kN - 1) / kN), 0);
   const bool alt = __shfl_sync(0xffffffffu, n_rows, 0) <= kM;  // both groups on the same rows, tiles in turn
   const int n_stages = alt ? turn_stages(FMT, D) : kStages;
+  // token and query head of row r of the block: (first + r) / group by a multiplication (exact: first + r < 2^9, group <= 32)
+  const int tok0 = r0 / a.group, first_g = r0 - tok0 * a.group;
+  const uint32_t magic = (65536u + a.group - 1) / a.group;
+  auto split_row = [&](int r, int& tok, int& hq) {
+    const int d = (int)((uint32_t)(first_g + r) * magic >> 16);
+    tok = tok0 + d;
+    hq = w.head * a.group + first_g + r - d * a.group;
+  };
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -354,9 +363,10 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (++slot == n_stages) slot = 0;
       }
     } else if (kF16 && warp >= 12) {
-      // ---- code tiles to f16 tiles: thread t takes chunk t % (D / 16) of every (2048 / D)-th row, of K and of V ----
-      constexpr int kChunks = D / 16, kStride = 128 / kChunks;
-      const int t = threadIdx.x - 384, c = t % kChunks;
+      // ---- code tiles to f16 tiles, of K and of V: a thread takes 16 codes at a time ----
+      // Eight neighbouring threads take four chunks of two rows (rows of 128 codes: the low four of one, the high four of
+      // the other), which keeps both the loads and the stores free of bank conflicts.
+      const int t = threadIdx.x - 384;
       const int64_t base = (int64_t)w.head * a.rows + pr.row0;
       uint32_t byte_k = 127, byte_v = 127;  // the next tile's scales, one row to a thread
       auto fetch = [&](int j) {
@@ -380,24 +390,33 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         ok = ok && wait_or_abort(&sh.kv_empty[slot], phase, abort_flag);
         ok = together(ok);  // (also publishes the scales; one answer for the four warps, so that none waits for another)
         if (ok) {
-          const int there = min(kN, key1 - key0 - j * kN);
+          const int there = key1 - key0 - j * kN;
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
             const uint32_t src = smem_u32(raw + (2 * rs + kv) * kRaw), dst = smem_u32(ring + (2 * slot + kv) * kTile);
 #pragma unroll
-            for (int i = 0; i < kN / kStride; ++i) {
-              const int row = t / kChunks + i * kStride;
+            for (int i = 0; i < kN * D / 16 / 128; ++i) {
+              int row, c;
+              if constexpr (D == 128) {
+                const int q = i * 16 + (t >> 3), odd = (t >> 2) & 1;  // pair of rows q / 2
+                row = (q & ~1) + odd;
+                c = (t & 3) + 4 * (odd ^ (q & 1));
+              } else {
+                row = i * 32 + (t >> 2);
+                c = t & 3;
+              }
               const uint32_t at = D == 128 ? src + row * 128 + ((c ^ (row & 7)) << 4) : src + row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
               uint32_t x[4];
               asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at) : "memory");
               const __half2 f = __half2half2(sh.scale[j & 1][kv][row]);
-              uint4 y[2];
-              y[0] = make_uint4(codes_to_f16(x[0] & 0xffffu, f), codes_to_f16(x[0] >> 16, f), codes_to_f16(x[1] & 0xffffu, f), codes_to_f16(x[1] >> 16, f));
-              y[1] = make_uint4(codes_to_f16(x[2] & 0xffffu, f), codes_to_f16(x[2] >> 16, f), codes_to_f16(x[3] & 0xffffu, f), codes_to_f16(x[3] >> 16, f));
-              if (row >= there) y[0] = y[1] = make_uint4(0, 0, 0, 0);  // behind the range
-              const int first = (c >> 2) & 1;  // (lanes of the two halves start with different chunks: no bank conflict)
-              st_shared16(operand_addr(dst, kN, row, 2 * c + first), first ? y[1] : y[0]);
-              st_shared16(operand_addr(dst, kN, row, 2 * c + 1 - first), first ? y[0] : y[1]);
+              uint4 lo, hi;
+              codes_to_f16(x[0], f, lo.x, lo.y);
+              codes_to_f16(x[1], f, lo.z, lo.w);
+              codes_to_f16(x[2], f, hi.x, hi.y);
+              codes_to_f16(x[3], f, hi.z, hi.w);
+              if (there < kN && row >= there) lo = hi = make_uint4(0, 0, 0, 0);  // behind the range
+              st_shared16(operand_addr(dst, kN, row, 2 * c), lo);
+              st_shared16(operand_addr(dst, kN, row, 2 * c + 1), hi);
             }
           }
           fence_proxy_async();
@@ -431,7 +450,8 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           const int r = base + quarter * 32 + i * kPer + lane / kLanes;
           x[i] = make_uint4(0, 0, 0, 0);
           if (r < n_rows) {
-            const int tok = (r0 + r) / a.group, hq = w.head * a.group + (r0 + r) - tok * a.group;
+            int tok, hq;
+            split_row(r, tok, hq);
             x[i] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (pr.t0 + tok) * a.q_stride + (int64_t)hq * D + c * 8);
           }
         }
@@ -463,7 +483,8 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 
       // ---- softmax ----
       const int rt = quarter * 32 + lane, r = base + rt;
-      const int tok = (r0 + r) / a.group;
+      int tok, hq;
+      split_row(r, tok, hq);
       const int seen = min(key1, r < n_rows ? seen_rows(part, pr, tok) : key1);
       const int all_seen = part.causal ? min(key1, seen_rows(part, pr, (r0 + base) / a.group)) : key1;
       const float factor = kF16 ? sh.row_factor[r] : a.scale2;
@@ -591,7 +612,6 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         const float inv = none ? 0.f : 1.f / total;
         const float lse2 = none ? -INFINITY : top + log2f(total);
         const int64_t token = pr.t0 + tok;
-        const int hq = w.head * a.group + (r0 + r) - tok * a.group;
         const int64_t at = ((int64_t)(part.slot0 + w.split) * a.q_rows + token) * a.heads * a.group + hq;
         __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out) + token * a.out_stride + (int64_t)hq * D;
         const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.out_stride * 2)) & 31u) == 0;
