@@ -17,8 +17,6 @@ namespace h2o {
 
 namespace {
 
-constexpr float kE4m3Max = 448.f;
-
 // Exponent e of a row whose largest finite magnitude is `a`: with a = m * 2^k, 1 <= m < 2, 448 = 1.75 * 2^8.
 __device__ __forceinline__ int kv8_exponent(float a) {
   const uint32_t b = __float_as_uint(a);
@@ -27,88 +25,136 @@ __device__ __forceinline__ int kv8_exponent(float a) {
   return max(-15, min(7, e));
 }
 
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&f)[8]);
-template <>
-__device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, float (&f)[8]) {
-  Vec16<__nv_bfloat16>::load(p, f);
+// 16 consecutive channels of an input or output row.  Inputs are read once: a streaming load leaves the second-level cache
+// to the scattered rows of the store.
+__device__ __forceinline__ void load16(const __nv_bfloat16* p, float (&f)[16]) {
+  float lo[8], hi[8];
+  Vec16<__nv_bfloat16>::unpack(__ldcs(reinterpret_cast<const uint4*>(p)), lo);
+  Vec16<__nv_bfloat16>::unpack(__ldcs(reinterpret_cast<const uint4*>(p) + 1), hi);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    f[i] = lo[i];
+    f[8 + i] = hi[i];
+  }
 }
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, float (&f)[8]) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-  f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+__device__ __forceinline__ void load16(const float* p, float (&f)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 a = __ldcs(reinterpret_cast<const float4*>(p + 4 * i));
+    f[4 * i] = a.x; f[4 * i + 1] = a.y; f[4 * i + 2] = a.z; f[4 * i + 3] = a.w;
+  }
 }
-template <typename T>
-__device__ __forceinline__ void store8(T* p, const float (&f)[8]);
-template <>
-__device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16* p, const float (&f)[8]) {
-  Vec16<__nv_bfloat16>::store(p, f);
+__device__ __forceinline__ void store16(__nv_bfloat16* p, const float (&f)[16]) {
+  float lo[8], hi[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    lo[i] = f[i];
+    hi[i] = f[8 + i];
+  }
+  Vec16<__nv_bfloat16>::store(p, lo);
+  Vec16<__nv_bfloat16>::store(p + 8, hi);
 }
-template <>
-__device__ __forceinline__ void store8<float>(float* p, const float (&f)[8]) {
-  *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+__device__ __forceinline__ void store16(float* p, const float (&f)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(p + 4 * i) = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
 }
 
 struct RowsArgs {
   uint8_t *k8, *v8, *ks, *vs;
   void *k, *v;
   const int64_t* rows;
-  int64_t first_row, n, stride, capacity;
-  int heads;
+  int64_t first_row, stride, capacity;
+  int n, heads;
 };
 
-// D / 8 neighbouring threads take one row of one head (8 channels each): K for z = 0, V for z = 1.
-template <typename T, int D, bool WRITE>
-__global__ void __launch_bounds__(256) store_rows_kernel(RowsArgs a) {
-  constexpr int kLanes = D / 8;
-  const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes;  // token * heads + head
-  const int lane = threadIdx.x % kLanes;
-  if (item >= a.n * a.heads) return;  // (whole groups of kLanes threads)
-  const int64_t token = item / a.heads;
-  const int head = (int)(item - token * a.heads);
-  const int64_t row = a.rows ? a.rows[token] : a.first_row + token;
-  if (row < 0 || row >= a.capacity) return;
-  T* x = static_cast<T*>(blockIdx.z ? a.v : a.k) + token * a.stride + (int64_t)head * D + lane * 8;
-  uint8_t* codes = (blockIdx.z ? a.v8 : a.k8) + ((int64_t)head * a.capacity + row) * D + lane * 8;
-  uint8_t* scale = (blockIdx.z ? a.vs : a.ks) + (int64_t)head * a.capacity + row;
-  float f[8];
-  if constexpr (WRITE) {
-    load8<T>(x, f);
-    float m = 0.f;
+constexpr int kRowThreads = 256;
+
+// Bound by memory.  A thread has 16 channels of one head (blockIdx.x, threadIdx.x) and TOKENS tokens in a row
+// (blockIdx.y): a whole vector of codes, and the loads of all its tokens under way together.  K for z = 0, V for z = 1.
+template <typename T, int D, int TOKENS, bool WRITE>
+__global__ void __launch_bounds__(kRowThreads) store_rows_kernel(RowsArgs a) {
+  constexpr int kLanes = D / 16;  // neighbouring threads of a head's row
+  const int column = blockIdx.x * kRowThreads + threadIdx.x;
+  if (column >= a.heads * kLanes) return;  // (whole groups of kLanes threads)
+  const int head = column / kLanes, lane = column % kLanes;
+  const int first = blockIdx.y * TOKENS;
+  T* const x = static_cast<T*>(blockIdx.z ? a.v : a.k) + (int64_t)column * 16;
+  uint8_t* const codes = (blockIdx.z ? a.v8 : a.k8) + (int64_t)head * a.capacity * D + lane * 16;
+  uint8_t* const scales = (blockIdx.z ? a.vs : a.ks) + (int64_t)head * a.capacity;
+  int64_t row[TOKENS];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float b = fabsf(f[i]);
-      m = b < INFINITY ? fmaxf(m, b) : m;  // (false for NaN)
-    }
-    const unsigned mask = (kLanes == 16 ? 0xffffu : 0xffu) << ((threadIdx.x & 31) / kLanes * kLanes);  // this row's threads
-#pragma unroll
-    for (int o = kLanes / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(mask, m, o));
-    const int e = kv8_exponent(m);
-    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-    uint32_t w[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const __nv_fp8x2_storage_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * i] * inv, f[4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-      const __nv_fp8x2_storage_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * i + 2] * inv, f[4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
-      w[i] = (uint32_t)lo | ((uint32_t)hi << 16);
-    }
-    *reinterpret_cast<uint2*>(codes) = make_uint2(w[0], w[1]);
-    if (lane == 0) *scale = (uint8_t)(e + 127);
-  } else {
-    const uint2 w = *reinterpret_cast<const uint2*>(codes);
-    const float s = kv8_scale(*scale);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t pair = ((i < 2 ? w.x : w.y) >> (16 * (i & 1))) & 0xffffu;
-      const __half2 h = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)pair, __NV_E4M3));
-      const float2 g = __half22float2(h);
-      f[2 * i] = g.x * s;
-      f[2 * i + 1] = g.y * s;
-    }
-    store8<T>(x, f);
+  for (int i = 0; i < TOKENS; ++i) {
+    const int token = first + i;
+    row[i] = token >= a.n ? -1 : a.rows ? a.rows[token] : a.first_row + token;
+    if (row[i] >= a.capacity) row[i] = -1;
   }
+  if constexpr (WRITE) {
+    float f[TOKENS][16];
+#pragma unroll
+    for (int i = 0; i < TOKENS; ++i)
+      if (row[i] >= 0) load16(x + (first + i) * a.stride, f[i]);
+    const unsigned mask = ((1u << kLanes) - 1u) << ((threadIdx.x & 31) / kLanes * kLanes);  // this row's threads
+#pragma unroll
+    for (int i = 0; i < TOKENS; ++i) {
+      if (row[i] < 0) continue;  // (the same for all threads of a row)
+      float m = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float b = fabsf(f[i][e]);
+        m = b < INFINITY ? fmaxf(m, b) : m;  // (false for NaN)
+      }
+#pragma unroll
+      for (int o = kLanes / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(mask, m, o));
+      const int e2 = kv8_exponent(m);
+      const float inv = __uint_as_float((uint32_t)(127 - e2) << 23);
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float* g = &f[i][4 * e];
+        const __nv_fp8x2_storage_t lo = __nv_cvt_float2_to_fp8x2(make_float2(g[0] * inv, g[1] * inv), __NV_SATFINITE, __NV_E4M3);
+        const __nv_fp8x2_storage_t hi = __nv_cvt_float2_to_fp8x2(make_float2(g[2] * inv, g[3] * inv), __NV_SATFINITE, __NV_E4M3);
+        w[e] = (uint32_t)lo | ((uint32_t)hi << 16);
+      }
+      *reinterpret_cast<uint4*>(codes + row[i] * D) = make_uint4(w[0], w[1], w[2], w[3]);
+      if (lane == 0) scales[row[i]] = (uint8_t)(e2 + 127);
+    }
+  } else {
+    uint4 w[TOKENS];
+    uint32_t byte[TOKENS];
+#pragma unroll
+    for (int i = 0; i < TOKENS; ++i)
+      if (row[i] >= 0) {
+        w[i] = *reinterpret_cast<const uint4*>(codes + row[i] * D);
+        byte[i] = scales[row[i]];
+      }
+#pragma unroll
+    for (int i = 0; i < TOKENS; ++i) {
+      if (row[i] < 0) continue;
+      const float s = kv8_scale(byte[i]);
+      const uint32_t words[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+      float f[16];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t pair = (words[e >> 1] >> (16 * (e & 1))) & 0xffffu;
+        const float2 g = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)pair, __NV_E4M3)));
+        f[2 * e] = g.x * s;
+        f[2 * e + 1] = g.y * s;
+      }
+      store16(x + (first + i) * a.stride, f);
+    }
+  }
+}
+
+template <typename T, int D, bool WRITE>
+cudaError_t launch_tokens(const RowsArgs& a, cudaStream_t stream) {
+  const unsigned columns = (unsigned)(((int64_t)a.heads * (D / 16) + kRowThreads - 1) / kRowThreads);
+  // several tokens to a thread where there are blocks enough all the same
+  constexpr int kMany = sizeof(T) == 2 ? 4 : 2;
+  if ((int64_t)columns * 2 * a.n / kMany >= 8 * sm_count())
+    store_rows_kernel<T, D, kMany, WRITE><<<dim3(columns, (unsigned)((a.n + kMany - 1) / kMany), 2), kRowThreads, 0, stream>>>(a);
+  else
+    store_rows_kernel<T, D, 1, WRITE><<<dim3(columns, (unsigned)a.n, 2), kRowThreads, 0, stream>>>(a);
+  return cudaGetLastError();
 }
 
 template <bool WRITE>
@@ -119,24 +165,25 @@ cudaError_t launch_rows(const h2o_store_config_t& c, void* k, void* v, int dtype
   a.v8 = static_cast<uint8_t*>(c.v);
   a.ks = c.k_scale;
   a.vs = c.v_scale;
-  a.k = k;
-  a.v = v;
   a.rows = rows;
-  a.first_row = first_row;
-  a.n = n;
   a.stride = stride;
   a.capacity = c.rows;
   a.heads = c.n_heads;
-  const int64_t threads = n * c.n_heads * (c.head_dim / 8);
-  const dim3 grid((unsigned)((threads + 255) / 256), 1, 2);
-  if (dtype == H2O_F32) {
-    if (c.head_dim == 128) store_rows_kernel<float, 128, WRITE><<<grid, 256, 0, stream>>>(a);
-    else store_rows_kernel<float, 64, WRITE><<<grid, 256, 0, stream>>>(a);
-  } else {
-    if (c.head_dim == 128) store_rows_kernel<__nv_bfloat16, 128, WRITE><<<grid, 256, 0, stream>>>(a);
-    else store_rows_kernel<__nv_bfloat16, 64, WRITE><<<grid, 256, 0, stream>>>(a);
+  const int64_t elem = dtype == H2O_F32 ? 4 : 2;
+  constexpr int64_t kMost = 65535;  // tokens of a launch (the grid's second dimension)
+  for (int64_t at = 0; at < n; at += kMost) {
+    a.n = (int)(n - at < kMost ? n - at : kMost);
+    a.k = static_cast<char*>(k) + at * stride * elem;
+    a.v = static_cast<char*>(v) + at * stride * elem;
+    a.rows = rows ? rows + at : nullptr;
+    a.first_row = first_row + at;
+    const cudaError_t e = dtype == H2O_F32
+                              ? (c.head_dim == 128 ? launch_tokens<float, 128, WRITE>(a, stream) : launch_tokens<float, 64, WRITE>(a, stream))
+                              : (c.head_dim == 128 ? launch_tokens<__nv_bfloat16, 128, WRITE>(a, stream)
+                                                   : launch_tokens<__nv_bfloat16, 64, WRITE>(a, stream));
+    if (e != cudaSuccess) return e;
   }
-  return cudaGetLastError();
+  return cudaSuccess;
 }
 
 }  // namespace

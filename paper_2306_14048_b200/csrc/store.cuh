@@ -113,7 +113,7 @@ cudaError_t launch_store_read(const h2o_store_config_t& c, void* k, void* v, int
 int attend_fma_row_tile(int64_t rows);  // rows of a tile for problems of up to `rows` rows
 cudaError_t launch_attend_fma(const AttendView& a, int part, int tile, int format, cudaStream_t stream);
 constexpr int kFewBoxRows = 32;  // rows of a box of the store's tensor maps
-inline int many_box_rows(int dim) { return dim == 128 ? 80 : 96; }
+int many_box_rows(int format, int dim);
 bool make_store_map(CUtensorMap_st* map, const h2o_store_config_t& c, const void* base, int box_rows);
 int attend_mma_row_tile(int64_t rows);
 int attend_mma_blocks_per_sm(int format, int tile);

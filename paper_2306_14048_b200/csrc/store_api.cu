@@ -106,12 +106,11 @@ struct Plan {
   int rc;
 };
 
-// More query rows than this (of one K/V head) run on the tcgen05 kernel, 256 to a block; up to it the mma.sync kernel
-// reads each key once.
-#ifndef KFEW
-#define KFEW 32
-#endif
-constexpr int kFewRows = KFEW;
+// More query rows than this (of one K/V head) run on the tcgen05 kernel, 256 to a block; up to it the mma.sync kernel,
+// which reads each key once as well and has less to set up.  One sequence of 16384 rows, mma.sync against tcgen05 (us):
+// bfloat16, 8 heads of 128, 16 query rows 30 / 26, 20 rows 36 / 26; 32 heads 61 / 65 and 69 / 65; 16 heads of 64: 28 / 37
+// and 37 / 37.  8-bit, 8 heads of 128, 32 query rows 26 / 28; 32 heads 61 / 73.
+int few_rows(int format) { return format == H2O_KV8 ? 32 : 16; }
 
 // Splits the keys of a part: `units` blocks per split, `room` blocks that run at once.  Costs in keys of one block: a block
 // costs its keys and `fixed` more (start, merge, its result's trip through memory), the joining kernel twice as much;
@@ -180,7 +179,7 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
     p.causal = prefix && k == 1;
     p.problems = p.grouped ? n_groups : a.batch;
     const int64_t rows = std::min<int64_t>((p.grouped ? (int64_t)a.max_group * a.max_q : a.max_q), a.q_rows) * a.group;
-    pl.kernel[n] = q->dtype == H2O_F32 ? Kernel::Fma : rows > kFewRows ? Kernel::Tc : Kernel::Mma;
+    pl.kernel[n] = q->dtype == H2O_F32 ? Kernel::Fma : rows > few_rows(c.format) ? Kernel::Tc : Kernel::Mma;
     pl.tile[n] = pl.kernel[n] == Kernel::Fma  ? h2o::attend_fma_row_tile(rows)
                  : pl.kernel[n] == Kernel::Tc ? h2o::kManyRowTile
                                               : h2o::attend_mma_row_tile(rows);
@@ -276,7 +275,7 @@ int h2o_store_create(h2o_store_t** out, const h2o_store_config_t* cfg) {
       const void* base;
       int box;
     } const maps[4] = {{s->few_k, cfg->k, h2o::kFewBoxRows}, {s->few_v, cfg->v, h2o::kFewBoxRows},
-                       {s->many_k, cfg->k, h2o::many_box_rows(cfg->head_dim)}, {s->many_v, cfg->v, h2o::many_box_rows(cfg->head_dim)}};
+                       {s->many_k, cfg->k, h2o::many_box_rows(cfg->format, cfg->head_dim)}, {s->many_v, cfg->v, h2o::many_box_rows(cfg->format, cfg->head_dim)}};
     for (const auto& m : maps)
       if (!h2o::make_store_map(reinterpret_cast<CUtensorMap_st*>(m.map), s->cfg, m.base, m.box)) {
         delete s;

@@ -546,8 +546,11 @@ cudaError_t launch_rows(const AttendView& a, int first, bool both, const int* ti
   const int t0 = tile[first], t1 = both ? tile[1] : t0;
   if (t0 == 8) return launch<FMT, D, 1, 1>(a, first, both, map_k, map_v, st);
   if (t0 == 16) return t1 == 8 ? launch<FMT, D, 2, 1>(a, first, both, map_k, map_v, st) : launch<FMT, D, 2, 2>(a, first, both, map_k, map_v, st);
-  if (t1 == 8) return launch<FMT, D, 4, 1>(a, first, both, map_k, map_v, st);
-  return t1 == 16 ? launch<FMT, D, 4, 2>(a, first, both, map_k, map_v, st) : launch<FMT, D, 4, 4>(a, first, both, map_k, map_v, st);
+  if constexpr (FMT == H2O_KV8) {  // (bfloat16 rows: more than 16 query rows run on the tcgen05 kernel)
+    if (t1 == 8) return launch<FMT, D, 4, 1>(a, first, both, map_k, map_v, st);
+    return t1 == 16 ? launch<FMT, D, 4, 2>(a, first, both, map_k, map_v, st) : launch<FMT, D, 4, 4>(a, first, both, map_k, map_v, st);
+  }
+  return cudaErrorInvalidValue;
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,

@@ -2,7 +2,7 @@
 // accumulators in tensor memory; bfloat16 queries, bfloat16 or 8-bit rows, head_dim 64 or 128.
 //
 // A block takes up to 256 query rows (query tokens times the query heads of one K/V head) as two groups of 128, A and
-// B, which share every key tile (80 keys for head_dim 128, 96 for 64); up to 128 rows are given to both groups, which
+// B, which share every key tile (80 keys for head_dim 128, 96 or 64 for 64); up to 128 rows are given to both groups, which
 // then take the tiles in turn and join their results at the end.  Per group g and key tile j:
 //   S_g(j) = Q_g K_j^T     into tensor memory, from there into the softmax threads' registers, which frees S_g at once:
 //                          S_g(j + 1) runs while the exponentials of tile j are computed
@@ -12,9 +12,9 @@
 // and tiles of 128 keys the chain S - exponentials - P V of a group is serial: 3700 cycles per tile of both groups for
 // 2048 of tensor work.  Measured (4 x 2048 queries against 4096 keys, 32 heads): 593 us that way, 505 us this way (1090
 // TFLOP/s); tiles of 64 keys with S prefetched into registers and P in two buffers 650 us; two threads to a row 725 us.
-// Roles: warp 0 TMA and tensor memory, warps 1 and 2 issue S of A and B (they also clear what lies behind the range in
-// its last V tile: 0 * NaN must not reach the sums), warp 3 issues P V of both, warps 4..7 and 8..11 the softmax of A and
-// B, one thread per row; with 8-bit rows warps 12..15 turn code tiles into f16 tiles.  A wait on a barrier costs 300 to
+// Roles: warp 0 TMA, warps 1 and 2 issue S of A and B (they also clear what lies behind the range in
+// its last V tile: 0 * NaN must not reach the sums), warp 3 issues P V of both and owns tensor memory, warps 4..7 and 8..11 the softmax of A and
+// B, one thread per row; with 8-bit rows warps 12..15 and 16..19 turn code tiles of K and of V into f16 tiles.  A wait on a barrier costs 300 to
 // 400 cycles here even when it is complete (it queues behind the exponentials), so the issuers have few: K and V of a tile
 // arrive on one barrier, and P V waits for P alone, which comes after S and so after the tile.  Their loops run on
 // values the compiler knows to be uniform (constant tensor-memory addresses, counts from a shuffle): 575 -> 550 us.
@@ -40,21 +40,23 @@ namespace {
 using namespace ptx;
 
 constexpr int kM = 128;  // rows of a group
-__host__ __device__ constexpr int tile_keys(int d) { return d == 128 ? 80 : 96; }
-__host__ __device__ constexpr int threads(int fmt) { return fmt == H2O_KV8 ? 512 : 384; }
-__host__ __device__ constexpr int tile_bytes(int d) { return tile_keys(d) * d * 2; }
-// Ring of stages, K and V of a tile in each.  Two groups that take tiles in turn use an even number: a warp that waits for
-// a tile then has seen the stage's tile before, so a parity cannot be mistaken for an older one.
+// (8-bit rows of 64 channels: what fits the softmax threads' 144 registers)
+__host__ __device__ constexpr int tile_keys(int fmt, int d) { return d == 128 ? 80 : fmt == H2O_KV8 ? 64 : 96; }
+__host__ __device__ constexpr int threads(int fmt) { return fmt == H2O_KV8 ? 640 : 384; }
+__host__ __device__ constexpr int tile_bytes(int fmt, int d) { return tile_keys(fmt, d) * d * 2; }
+// Ring of stages, K and V of a tile in each.  Two groups that take tiles in turn use an even number where TMA fills the
+// stages: a warp that waits for a tile then has seen the stage's tile before, so a parity cannot be mistaken for an older
+// one.  (Converted tiles complete in order, so a warp that has seen its last tile may count on all before it.)
 __host__ __device__ constexpr int stages(int fmt, int d) { return d == 64 ? 6 : fmt == H2O_KV8 ? 3 : 4; }
-__host__ __device__ constexpr int turn_stages(int fmt, int d) { return stages(fmt, d) & ~1; }
+__host__ __device__ constexpr int turn_stages(int fmt, int d) { return fmt == H2O_KV8 ? stages(fmt, d) : stages(fmt, d) & ~1; }
 constexpr int kMaxStages = 6, kRawStages = 2;  // (a stage of the code ring also holds K and V)
 __host__ __device__ constexpr int smem_bytes(int fmt, int d) {
-  return 2 * kM * d * 2 + 2 * stages(fmt, d) * tile_bytes(d) + (fmt == H2O_KV8 ? 2 * kRawStages * tile_keys(d) * d : 0) + 1024;
+  return 2 * kM * d * 2 + 2 * stages(fmt, d) * tile_bytes(fmt, d) + (fmt == H2O_KV8 ? 2 * kRawStages * tile_keys(fmt, d) * d : 0) + 1024;
 }
-// Registers of a thread: the softmax warps take what the others give back.  8-bit: 512 threads start with 128 each =
-// 256 x 176 + 256 x 80; bfloat16: 384 start with 168 = 256 x 216 + 128 x 72.
-__host__ __device__ constexpr int regs_softmax(int fmt) { return fmt == H2O_KV8 ? 176 : 216; }
-__host__ __device__ constexpr int regs_other(int fmt) { return fmt == H2O_KV8 ? 80 : 72; }
+// Registers of a thread: the softmax warps take what the others give back.  8-bit: 640 threads start with 96 each =
+// 256 x 144 + 384 x 64; bfloat16: 384 start with 168 = 256 x 216 + 128 x 72.
+__host__ __device__ constexpr int regs_softmax(int fmt) { return fmt == H2O_KV8 ? 144 : 216; }
+__host__ __device__ constexpr int regs_other(int fmt) { return fmt == H2O_KV8 ? 64 : 72; }
 // Every kPolyEvery-th pair of exponentials runs on the FMA pipe.  4 x 2048 queries against 4096 keys, 32 heads: none 550,
 // one in eight 518, one in four 505, one in three 547, one in two 535 us.
 constexpr int kPolyEvery = 4;
@@ -146,16 +148,16 @@ __device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[N]
   if constexpr (N % 32 == 16) tmem_st16(addr + N / 32 * 32, *reinterpret_cast<const uint32_t(*)[16]>(&r[N / 32 * 32]));
 }
 
-// Barrier of the four converting warps that tells each of them whether all are well.
-__device__ __forceinline__ bool together(bool ok) {
+// Barrier of the four warps that convert K (kv = 0) or V (1), that tells each of them whether all are well.
+__device__ __forceinline__ bool together(bool ok, int kv) {
   uint32_t all;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.u32 p, %1, 0;\n\t"
-      "barrier.cta.red.and.aligned.pred q, 2, 128, p;\n\t"
+      "barrier.cta.red.and.pred q, %2, 128, p;\n\t"
       "selp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(all)
-      : "r"(ok ? 1u : 0u)
+      : "r"(ok ? 1u : 0u), "r"(1 + kv)
       : "memory");
   return all != 0;
 }
@@ -184,7 +186,7 @@ __global__ void __launch_bounds__(threads(FMT), 1)
 attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                  const __grid_constant__ AttendView a, int part_index) {
   constexpr bool kF16 = FMT == H2O_KV8;
-  constexpr int kN = tile_keys(D), kTile = tile_bytes(D), kQTile = kM * D * 2, kStages = stages(FMT, D), kRaw = kN * D;
+  constexpr int kN = tile_keys(FMT, D), kTile = tile_bytes(FMT, D), kQTile = kM * D * 2, kStages = stages(FMT, D), kRaw = kN * D;
   constexpr float kLargeSum = kLargeSumOf<FMT>;
   // tensor memory: O, S (starts on multiples of 32 columns) and P (of 8) of the two groups
   constexpr uint32_t kColO = 0, kStepO = D, kColS = 2 * D, kStepS = 96, kColP = kColS + kStepS + kN, kStepP = kN / 2;
@@ -223,6 +225,35 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   };
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
+  // The query rows are asked for before the first tiles, into the softmax warps' registers: behind the tiles' traffic a trip
+  // to memory takes microseconds.
+  const bool softmax_warp = warp >= 4 && warp < 12;
+  const int grp = (warp >> 2) - 1, base = alt ? 0 : grp * kM;  // a softmax warp's group, and the group's first row in the block
+  constexpr int kLanes = D / 8, kPer = 32 / kLanes;            // lanes to a query row, rows to a load
+  uint4 qx[32 / kPer];
+  auto load_query = [&] {
+#pragma unroll
+    for (int i = 0; i < 32 / kPer; ++i) {
+      const int r = base + (warp & 3) * 32 + i * kPer + lane / kLanes;
+      qx[i] = make_uint4(0, 0, 0, 0);
+      if (r < n_rows) {
+        int tok, hq;
+        split_row(r, tok, hq);
+        qx[i] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (pr.t0 + tok) * a.q_stride + (int64_t)hq * D + lane % kLanes * 8);
+      }
+    }
+  };
+  const bool loads_query = softmax_warp && nt > 0 && base < n_rows && !(alt && grp == 1);
+  if (loads_query) load_query();
+  const int row0 = (int)pr.row0 + key0;
+  auto load_tile = [&](int j, int slot) {  // K and V of tile j (16-bit rows: into a stage; 8-bit rows: into the code ring)
+    uint64_t* full = kF16 ? &sh.raw_full[slot] : &sh.kv_full[slot];
+    unsigned char* to = kF16 ? raw + 2 * slot * kRaw : ring + 2 * slot * kTile;
+    mbar_expect_tx(full, kF16 ? 2 * kRaw : 2 * kTile);
+    tma_load_tile(to, &map_k, w.head, row0 + j * kN, full);
+    tma_load_tile(to + (kF16 ? kRaw : kTile), &map_v, w.head, row0 + j * kN, full);
+  };
+  const int n_load = kF16 ? kRawStages : n_stages;  // stages of the ring that TMA fills
   if (threadIdx.x == 0) {
     for (int g = 0; g < 2; ++g) {
       mbar_init(&sh.q_full[g], 4);
@@ -233,18 +264,18 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       mbar_init(&sh.o_final[g], 1);
     }
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(&sh.kv_full[i], kF16 ? 4 : 1);  // (four converting warps)
+      mbar_init(&sh.kv_full[i], kF16 ? 8 : 1);  // (eight converting warps)
       mbar_init(&sh.kv_empty[i], alt ? 1 : 2);  // a product P V of each group that uses the tile
     }
     for (int i = 0; i < kRawStages; ++i) {
       mbar_init(&sh.raw_full[i], 1);
-      mbar_init(&sh.raw_empty[i], 4);
+      mbar_init(&sh.raw_empty[i], 8);
     }
     mbar_init(&sh.tail, 1);
     sh.abort_flag = 0;
     fence_barrier_init();
   }
-  if (warp == 0) tmem_alloc(&sh.tmem_base, 512);
+  if (warp == 3) tmem_alloc(&sh.tmem_base, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -256,32 +287,16 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   if (warp < 4 || warp >= 12) {
     setmaxnreg_dec<regs_other(FMT)>();
     if (warp == 0) {
-      // ---- TMA: K_0, V_0, K_1, V_1, ... (16-bit rows: into the stages; 8-bit rows: into the code ring) ----
+      // ---- TMA ----
       if (lane == 0) {
         int slot = 0;
         uint32_t phase = 1;
-        const int row = (int)pr.row0 + key0;
-        if constexpr (kF16) {
-          for (int j = 0; j < nt; ++j) {
-            if (!wait_or_abort(&sh.raw_empty[slot], phase, abort_flag)) break;
-            mbar_expect_tx(&sh.raw_full[slot], 2 * kRaw);
-            tma_load_tile(raw + 2 * slot * kRaw, &map_k, w.head, row + j * kN, &sh.raw_full[slot]);
-            tma_load_tile(raw + (2 * slot + 1) * kRaw, &map_v, w.head, row + j * kN, &sh.raw_full[slot]);
-            if (++slot == kRawStages) {
-              slot = 0;
-              phase ^= 1;
-            }
-          }
-        } else {
-          for (int j = 0; j < nt; ++j) {
-            if (!wait_or_abort(&sh.kv_empty[slot], phase, abort_flag)) break;
-            mbar_expect_tx(&sh.kv_full[slot], 2 * kTile);
-            tma_load_tile(ring + 2 * slot * kTile, &map_k, w.head, row + j * kN, &sh.kv_full[slot]);
-            tma_load_tile(ring + (2 * slot + 1) * kTile, &map_v, w.head, row + j * kN, &sh.kv_full[slot]);
-            if (++slot == n_stages) {
-              slot = 0;
-              phase ^= 1;
-            }
+        for (int j = 0; j < nt; ++j) {
+          if (!wait_or_abort(kF16 ? &sh.raw_empty[slot] : &sh.kv_empty[slot], phase, abort_flag)) break;
+          load_tile(j, slot);
+          if (++slot == n_load) {
+            slot = 0;
+            phase ^= 1;
           }
         }
       }
@@ -363,61 +378,58 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (++slot == n_stages) slot = 0;
       }
     } else if (kF16 && warp >= 12) {
-      // ---- code tiles to f16 tiles, of K and of V: a thread takes 16 codes at a time ----
+      // ---- code tiles to f16 tiles, four warps for K and four for V: a thread takes 16 codes at a time ----
       // Eight neighbouring threads take four chunks of two rows (rows of 128 codes: the low four of one, the high four of
       // the other), which keeps both the loads and the stores free of bank conflicts.
-      const int t = threadIdx.x - 384;
+      const int kv = (warp - 12) >> 2, t = threadIdx.x - 384 - 128 * kv;
       const int64_t base = (int64_t)w.head * a.rows + pr.row0;
-      uint32_t byte_k = 127, byte_v = 127;  // the next tile's scales, one row to a thread
+      const uint8_t* scales = kv ? a.v_scale : a.k_scale;
+      uint32_t byte = 127;  // of the next tile, one row to a thread
       auto fetch = [&](int j) {
         const int key = key0 + j * kN + t;
-        if (t < kN && key < key1) {
-          byte_k = a.k_scale[base + key];
-          byte_v = a.v_scale[base + key];
-        }
+        if (t < kN && key < key1) byte = scales[base + key];
       };
       if (nt > 0) fetch(0);
       int slot = 0;
       uint32_t phase = 1;
+      bool raw_there = false, slot_free = false;
       for (int j = 0; j < nt; ++j) {
         const int rs = j % kRawStages;
-        if (t < kN) {
-          sh.scale[j & 1][0][t] = __float2half_rn(kv8_scale(byte_k));
-          sh.scale[j & 1][1][t] = __float2half_rn(kv8_scale(byte_v));
-        }
+        if (t < kN) sh.scale[j & 1][kv][t] = __float2half_rn(kv8_scale(byte));
         if (j + 1 < nt) fetch(j + 1);
-        bool ok = wait_or_abort(&sh.raw_full[rs], (uint32_t)(j / kRawStages) & 1u, abort_flag);
-        ok = ok && wait_or_abort(&sh.kv_empty[slot], phase, abort_flag);
-        ok = together(ok);  // (also publishes the scales; one answer for the four warps, so that none waits for another)
+        bool ok = raw_there || wait_or_abort(&sh.raw_full[rs], (uint32_t)(j / kRawStages) & 1u, abort_flag);
+        ok = ok && (slot_free || wait_or_abort(&sh.kv_empty[slot], phase, abort_flag));
+        ok = together(ok, kv);  // (also publishes the scales; one answer for the four warps, so that none waits for another)
         if (ok) {
+          // the next tile's waits, asked ahead (the conversion hides the answers' way)
+          const int rn = (j + 1) % kRawStages, sn = slot + 1 == n_stages ? 0 : slot + 1;
+          raw_there = j + 1 < nt && mbar_test_wait(&sh.raw_full[rn], (uint32_t)((j + 1) / kRawStages) & 1u);
+          slot_free = mbar_test_wait(&sh.kv_empty[sn], sn == 0 ? phase ^ 1u : phase);
           const int there = key1 - key0 - j * kN;
+          const uint32_t src = smem_u32(raw + (2 * rs + kv) * kRaw), dst = smem_u32(ring + (2 * slot + kv) * kTile);
 #pragma unroll
-          for (int kv = 0; kv < 2; ++kv) {
-            const uint32_t src = smem_u32(raw + (2 * rs + kv) * kRaw), dst = smem_u32(ring + (2 * slot + kv) * kTile);
-#pragma unroll
-            for (int i = 0; i < kN * D / 16 / 128; ++i) {
-              int row, c;
-              if constexpr (D == 128) {
-                const int q = i * 16 + (t >> 3), odd = (t >> 2) & 1;  // pair of rows q / 2
-                row = (q & ~1) + odd;
-                c = (t & 3) + 4 * (odd ^ (q & 1));
-              } else {
-                row = i * 32 + (t >> 2);
-                c = t & 3;
-              }
-              const uint32_t at = D == 128 ? src + row * 128 + ((c ^ (row & 7)) << 4) : src + row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
-              uint32_t x[4];
-              asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at) : "memory");
-              const __half2 f = __half2half2(sh.scale[j & 1][kv][row]);
-              uint4 lo, hi;
-              codes_to_f16(x[0], f, lo.x, lo.y);
-              codes_to_f16(x[1], f, lo.z, lo.w);
-              codes_to_f16(x[2], f, hi.x, hi.y);
-              codes_to_f16(x[3], f, hi.z, hi.w);
-              if (there < kN && row >= there) lo = hi = make_uint4(0, 0, 0, 0);  // behind the range
-              st_shared16(operand_addr(dst, kN, row, 2 * c), lo);
-              st_shared16(operand_addr(dst, kN, row, 2 * c + 1), hi);
+          for (int i = 0; i < kN * D / 16 / 128; ++i) {
+            int row, c;
+            if constexpr (D == 128) {
+              const int q = i * 16 + (t >> 3), odd = (t >> 2) & 1;  // pair of rows q / 2
+              row = (q & ~1) + odd;
+              c = (t & 3) + 4 * (odd ^ (q & 1));
+            } else {
+              row = i * 32 + (t >> 2);
+              c = t & 3;
             }
+            const uint32_t at = D == 128 ? src + row * 128 + ((c ^ (row & 7)) << 4) : src + row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
+            uint32_t x[4];
+            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at) : "memory");
+            const __half2 f = __half2half2(sh.scale[j & 1][kv][row]);
+            uint4 lo, hi;
+            codes_to_f16(x[0], f, lo.x, lo.y);
+            codes_to_f16(x[1], f, lo.z, lo.w);
+            codes_to_f16(x[2], f, hi.x, hi.y);
+            codes_to_f16(x[3], f, hi.z, hi.w);
+            if (there < kN && row >= there) lo = hi = make_uint4(0, 0, 0, 0);  // behind the range
+            st_shared16(operand_addr(dst, kN, row, 2 * c), lo);
+            st_shared16(operand_addr(dst, kN, row, 2 * c + 1), hi);
           }
           fence_proxy_async();
         }
@@ -435,32 +447,17 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     }
   } else {
     setmaxnreg_inc<regs_softmax(FMT)>();
-    const int g = (warp - 4) >> 2, quarter = warp & 3;
-    const int base = alt ? 0 : g * kM;  // the group's first row in the block
+    const int g = grp, quarter = warp & 3;
     if (base < n_rows) {
-      // ---- the group's query rows into shared memory: D / 8 lanes a row ----
-      if (nt > 0 && !(alt && g == 1)) {
-        constexpr int kLanes = D / 8, kPer = 32 / kLanes;
+      if (loads_query) {
         const int c = lane % kLanes;
         const uint32_t tile = smem_u32(q_tiles + g * kQTile);
-        // (all loads first: they share the memory with the first tiles, and a trip takes microseconds then)
-        uint4 x[32 / kPer];
 #pragma unroll
         for (int i = 0; i < 32 / kPer; ++i) {
-          const int r = base + quarter * 32 + i * kPer + lane / kLanes;
-          x[i] = make_uint4(0, 0, 0, 0);
-          if (r < n_rows) {
-            int tok, hq;
-            split_row(r, tok, hq);
-            x[i] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (pr.t0 + tok) * a.q_stride + (int64_t)hq * D + c * 8);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 32 / kPer; ++i) {
-          const int rt = quarter * 32 + i * kPer + lane / kLanes, r = base + rt;
+          const int rt = quarter * 32 + i * kPer + lane / kLanes;
           if constexpr (kF16) {
             float f[8];
-            Vec16<__nv_bfloat16>::unpack(x[i], f);
+            Vec16<__nv_bfloat16>::unpack(qx[i], f);
             float big = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) big = fabsf(f[e]) < INFINITY ? fmaxf(big, fabsf(f[e])) : big;
@@ -468,11 +465,11 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             for (int o = kLanes / 2; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
             const int e2 = max(-100, min(126, (int)(__float_as_uint(big) >> 23) - 127));
             const float down = __uint_as_float((uint32_t)(127 - e2) << 23);
-            x[i] = make_uint4(pack_half2(f[0] * down, f[1] * down), pack_half2(f[2] * down, f[3] * down),
-                              pack_half2(f[4] * down, f[5] * down), pack_half2(f[6] * down, f[7] * down));
-            if (c == 0) sh.row_factor[r] = a.scale2 * __uint_as_float((uint32_t)(127 + e2) << 23);
+            qx[i] = make_uint4(pack_half2(f[0] * down, f[1] * down), pack_half2(f[2] * down, f[3] * down),
+                               pack_half2(f[4] * down, f[5] * down), pack_half2(f[6] * down, f[7] * down));
+            if (c == 0) sh.row_factor[base + rt] = a.scale2 * __uint_as_float((uint32_t)(127 + e2) << 23);
           }
-          st_shared16(operand_addr(tile, kM, rt, c), x[i]);
+          st_shared16(operand_addr(tile, kM, rt, c), qx[i]);
         }
         fence_proxy_async();
         __syncwarp();
@@ -491,6 +488,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
       const uint32_t t_s = tmem + kColS + kStepS * g + lane_addr, t_o = tmem + kColO + kStepO * g + lane_addr;
       const uint32_t t_p = tmem + kColP + kStepP * g + lane_addr;
+      const bool idle = base + quarter * 32 >= n_rows;
       float m = -INFINITY;
       float2 l2 = make_float2(0.f, 0.f);
       bool ok = true;
@@ -501,6 +499,15 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       for (int j = first, n = 0; j < nt; j += step, ++n) {
         ok = __all_sync(0xffffffffu, wait_or_abort(&sh.s_full[g], (uint32_t)n & 1u, abort_flag));
         if (!ok) break;
+        if (idle) {  // none of the warp's rows exists: whatever P holds there goes into rows of O that nobody reads
+          if (n > 0) ok = __all_sync(0xffffffffu, wait_or_abort(&sh.p_empty[g], (uint32_t)(n - 1) & 1u, abort_flag));
+          if (!ok) break;
+          if (lane == 0) {
+            mbar_arrive(&sh.s_read[g]);
+            mbar_arrive(&sh.p_full[g]);
+          }
+          continue;
+        }
         tc_fence_after();
         const int key = key0 + j * kN;
         uint32_t s[kN], p[kN / 2];
@@ -670,7 +677,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && sh.abort_flag && a.status) atomicCAS(a.status, 0, H2O_ERR_TIMEOUT);
-  if (warp == 0) {
+  if (warp == 3) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -687,6 +694,8 @@ cudaError_t launch(const AttendView& a, int part, const CUtensorMap& k, const CU
 }
 
 }  // namespace
+
+int many_box_rows(int format, int dim) { return tile_keys(format, dim); }
 
 cudaError_t launch_attend_tc(const AttendView& a, int part, int format, const void* map_k, const void* map_v, cudaStream_t st) {
   const CUtensorMap& k = *static_cast<const CUtensorMap*>(map_k);
