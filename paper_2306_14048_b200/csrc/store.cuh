@@ -46,7 +46,11 @@ struct AttendView {
   const void *k, *v;
   const uint8_t *k_scale, *v_scale;  // 8-bit rows only
   int64_t rows, row_stride;
-  float *part_out, *part_lse;  // [slots][q_rows][heads * group](dim), null when the kernel writes the result itself
+  float *part_out, *part_lse;  // [slots][q_rows][heads * group](dim), null when nothing goes through them
+  // early: part 1's kernel is launched to start before part 0's has ended.  finish (with early): part 1, unsplit, writes the
+  // results, joined with what part 0 left; otherwise every part leaves its chunks for the joining kernel, or there is one
+  // unsplit part that writes the results.
+  int early, finish;
   int32_t* status;
   int n_parts;
   AttendPart part[2];
@@ -83,6 +87,44 @@ __device__ __forceinline__ int seen_rows(const AttendPart& p, const Problem& r, 
   return p.causal ? max(0, r.len - (r.nt - 1 - i)) : r.len;
 }
 
+// The group of a sequence: the last one that starts at or before it.
+__device__ __forceinline__ int group_of(const AttendView& a, int seq) {
+  if (!a.cu_group) return 0;
+  int lo = 0, hi = a.n_groups;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a.cu_group[mid] <= seq) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// What part 0 left for the query tokens of one sequence (a.finish): its chunks' results, joined with part 1's own.
+struct Prefix {
+  int used;         // chunks
+  int64_t t0, t1;   // tokens that part 0 has worked on: others are left as they were
+  __device__ __forceinline__ int64_t at(const AttendView& a, int s, int64_t token, int hq) const {
+    return ((int64_t)(a.part[0].slot0 + s) * a.q_rows + token) * a.heads * a.group + hq;
+  }
+};
+__device__ __forceinline__ Prefix prefix_of(const AttendView& a, int seq) {
+  const Problem pr = locate(a, a.part[0], group_of(a, seq));
+  return Prefix{(pr.len + a.part[0].chunk - 1) / a.part[0].chunk, pr.t0, pr.t0 + pr.nt};
+}
+// The largest of the chunks' logarithms and `top`; then the sum of the chunks' weights relative to it.
+__device__ __forceinline__ float prefix_top(const AttendView& a, const Prefix& f, int64_t token, int hq, float top) {
+  for (int s = 0; s < f.used; ++s) top = fmaxf(top, a.part_lse[f.at(a, s, token, hq)]);
+  return top;
+}
+__device__ __forceinline__ float prefix_sum(const AttendView& a, const Prefix& f, int64_t token, int hq, float top) {
+  float sum = 0.f;
+  for (int s = 0; s < f.used; ++s) sum += exp2f(a.part_lse[f.at(a, s, token, hq)] - top);
+  return sum;
+}
+// Waits until the kernels before this one have ended (nothing to wait for in an ordinary launch).
+__device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // What one thread block works on: row tile fastest, then head, split, problem.
 struct BlockWork {
   int problem, head, split, row_tile;
@@ -104,6 +146,22 @@ inline int64_t part_blocks(const AttendView& a, const AttendPart& p) {
 // The value of a scale byte (a biased exponent).  Only bytes 112 .. 134 are ever written; others, in rows nobody
 // has written, are cut to that range.
 __device__ __forceinline__ float kv8_scale(uint32_t byte) { return __uint_as_float(min(max(byte, 112u), 134u) << 23); }
+
+// Launches `kernel`, `early`: it may start before the kernel in front of it has ended.
+template <typename... Args>
+cudaError_t launch_kernel(void (*kernel)(Args...), dim3 grid, int threads, int smem, cudaStream_t stream, bool early, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = early ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 
 // Launchers.
 cudaError_t launch_store_write(const h2o_store_config_t& c, const void* k, const void* v, int dtype, int64_t stride,

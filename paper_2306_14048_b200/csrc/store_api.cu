@@ -195,8 +195,13 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
     ++n;
   }
   a.n_parts = n;
-  const int64_t slots = (int64_t)a.part[0].splits + (n == 2 ? a.part[1].splits : 0);
-  if (slots > 1) {
+  // The second part's kernel, where it is one of its own, starts before the first one's has ended: neither needs the
+  // other's results until the end.  Prompts' own rows, unsplit, then join what the first part left themselves (32 prompts
+  // of up to 200 tokens: 415 -> 348 us); single tokens' blocks are many and short, and leave that to the joining kernel.
+  a.early = n == 2 && pl.kernel[0] == Kernel::Tc;
+  a.finish = a.early && a.part[1].splits == 1 && pl.kernel[1] == Kernel::Tc;
+  const int64_t slots = (int64_t)a.part[0].splits + (n == 2 && !a.finish ? a.part[1].splits : 0);
+  if (slots > 1 || a.finish) {
     const size_t rows = (size_t)slots * a.q_rows * a.heads * a.group;
     pl.lse_offset = align_up(rows * a.dim * sizeof(float));
     pl.scratch = pl.lse_offset + align_up(rows * sizeof(float));
@@ -222,7 +227,7 @@ int run_plan(const h2o_store_t* store, const h2o_queries_t* q, Plan& pl, void* s
     else if (pl.kernel[k] == Kernel::Tc) e = h2o::launch_attend_tc(pl.a, k, format, store->many_k, store->many_v, st);
     else e = h2o::launch_attend_mma(pl.a, k, both, pl.tile, format, store->few_k, store->few_v, st);
   }
-  if (e == cudaSuccess && pl.scratch > 0) e = h2o::launch_attend_join(pl.a, q->dtype, st);
+  if (e == cudaSuccess && pl.scratch > 0 && !pl.a.finish) e = h2o::launch_attend_join(pl.a, q->dtype, st);
   if (e != cudaSuccess) {
     cudaGetLastError();
     return H2O_ERR_CUDA;

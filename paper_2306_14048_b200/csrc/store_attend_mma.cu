@@ -475,6 +475,9 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   constexpr int kLanes = D / 4;  // threads of a row, four channels each
   for (int r = threadIdx.x / kLanes; r < n_rows; r += kThreads / kLanes) {
     const int c = (threadIdx.x % kLanes) * 4;
+    const int tok = (r0 + r) / a.group;
+    const int64_t token = pr.t0 + tok;
+    const int hq = w.head * a.group + (r0 + r) - tok * a.group;
     float top = -INFINITY;
 #pragma unroll
     for (int x = 0; x < kWarps; ++x) top = fmaxf(top, sh.m[x][r]);
@@ -494,9 +497,6 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
     const bool none = sum == 0.f;
     const float inv = none ? 0.f : 1.f / sum;
     const float lse2 = none ? -INFINITY : top + log2f(sum);
-    const int tok = (r0 + r) / a.group;
-    const int64_t token = pr.t0 + tok;
-    const int hq = w.head * a.group + (r0 + r) - tok * a.group;
     if (direct) {
       uint2 word;
       word.x = Vec16<__nv_bfloat16>::pack2(v.x * inv, v.y * inv);
@@ -520,12 +520,15 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   extern __shared__ unsigned char dyn[];
   __shared__ Shared sh;
   unsigned char* ring = dyn + ((1024u - (smem_u32(dyn) & 1023u)) & 1023u);
+  let_next_start();  // (the joining kernel waits for this one's end; others are launched to start after it)
   if (NT0 == NT1 || blockIdx.x < blocks0) {
     const bool second = blockIdx.x >= blocks0;
     attend<FMT, D, NT0, NT0>(a, &map_k, &map_v, a.part[second ? 1 : first], blockIdx.x - (second ? blocks0 : 0), ring, sh);
   } else {
     attend<FMT, D, NT1, NT0>(a, &map_k, &map_v, a.part[1], blockIdx.x - blocks0, ring, sh);
   }
+  // a launch that started early does not end before the one in front of it, whatever its blocks have to do
+  if (a.early && blockIdx.x == 0) wait_for_earlier();
 }
 
 template <int FMT, int D, int NT0, int NT1>
@@ -536,8 +539,8 @@ cudaError_t launch(const AttendView& a, int first, bool both, const CUtensorMap&
   const cudaError_t e = ensure_dynamic_smem(f, smem, &flags);
   if (e != cudaSuccess) return e;
   const int64_t b0 = part_blocks(a, a.part[first]), b1 = both ? part_blocks(a, a.part[1]) : 0;
-  attend_mma_kernel<FMT, D, NT0, NT1><<<(unsigned)(b0 + b1), kThreads, smem, stream>>>(map_k, map_v, a, first, (unsigned)b0);
-  return cudaGetLastError();
+  return launch_kernel(attend_mma_kernel<FMT, D, NT0, NT1>, dim3((unsigned)(b0 + b1)), kThreads, smem, stream, a.early != 0, map_k, map_v, a,
+                       first, (unsigned)b0);
 }
 
 template <int FMT, int D>

@@ -200,14 +200,18 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   unsigned char* ring = dyn + 2 * kQTile;
   unsigned char* raw = ring + 2 * kStages * kTile;
 
+  let_next_start();
+  const bool finish = a.finish && part_index == 1;
   const AttendPart& part = a.part[part_index];
   const BlockWork w = block_work(a, part, blockIdx.x);
   const Problem pr = locate(a, part, w.problem);
   const int rows = pr.nt * a.group, r0 = w.row_tile * (2 * kM);
+  // (a launch that started early does not end before the one in front of it, whatever its blocks have to do)
+  if (a.early && part_index == 1 && blockIdx.x == 0) wait_for_earlier();
   if (r0 >= rows) return;
   const int n_rows = min(2 * kM, rows - r0);
   const int key0 = w.split * part.chunk;
-  const bool direct = a.part_out == nullptr;
+  const bool direct = a.part_out == nullptr || finish;
   if (!direct && key0 >= pr.len) return;  // (the join kernel does not read it)
   const int last_seen = seen_rows(part, pr, (r0 + n_rows - 1) / a.group);
   const int key1 = min(last_seen, key0 + part.chunk);
@@ -576,7 +580,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       }
       // ---- result ----
       const float sum = l2.x + l2.y;
-      bool none = !ok || sum == 0.f || m == -INFINITY;
+      bool none = !ok || sum == 0.f;  // (NaN is not none)
       const bool wrote = nt > first;  // the group has an O
       if (ok && wrote) ok = __all_sync(0xffffffffu, wait_or_abort(&sh.o_final[g], 0, abort_flag));
       float* join = reinterpret_cast<float*>(q_tiles);  // [2][128]
@@ -607,18 +611,31 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         const float* theirs = reinterpret_cast<const float*>(ring) + rt * (D + 4);
         if (alt) {
           const float mb = join[rt];
-          const float mx = fmaxf(top, mb);
-          if (mx > -INFINITY) {
-            mine_w = none ? 0.f : ex2(m - mx);
-            their_w = ex2(mb - mx);
-            total = mine_w * total + their_w * join[kM + rt];
+          top = fmaxf(top, mb);
+          const float to = top == -INFINITY ? 0.f : top;
+          mine_w = none ? 0.f : ex2(m - to);
+          their_w = ex2(mb - to);
+          total = mine_w * total + their_w * join[kM + rt];
+        }
+        const int64_t token = pr.t0 + tok;
+        Prefix prefix{0, 0, 0};
+        bool write = r < n_rows;
+        if (finish) {
+          wait_for_earlier();
+          prefix = prefix_of(a, w.problem);
+          write = write && token >= prefix.t0 && token < prefix.t1;
+          if (write) {
+            const float mx = prefix_top(a, prefix, token, hq, top);
+            const float scale = top == -INFINITY ? 0.f : ex2(top - mx);
+            mine_w *= scale;
+            their_w *= scale;
+            total = total * scale + (mx == -INFINITY ? 0.f : prefix_sum(a, prefix, token, hq, mx));
             top = mx;
           }
         }
         none = total == 0.f;
         const float inv = none ? 0.f : 1.f / total;
         const float lse2 = none ? -INFINITY : top + log2f(total);
-        const int64_t token = pr.t0 + tok;
         const int64_t at = ((int64_t)(part.slot0 + w.split) * a.q_rows + token) * a.heads * a.group + hq;
         __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out) + token * a.out_stride + (int64_t)hq * D;
         const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.out_stride * 2)) & 31u) == 0;
@@ -629,16 +646,25 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             tmem_ld32(t_o + 32u * cc, o);
             tmem_wait_ld();
           }
-          if (r >= n_rows) continue;
-          if (alt) {
+          if (!write) continue;
+          // (a weight of 0 belongs to an O that was never written)
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float own = mine_w == 0.f ? 0.f : mine_w * __uint_as_float(o[e]);
-              o[e] = __float_as_uint(fmaf(their_w, theirs[cc * 32 + e], own) * inv);
+          for (int e = 0; e < 32; ++e) {
+            float x = mine_w == 0.f ? 0.f : mine_w * __uint_as_float(o[e]);
+            if (alt) x = fmaf(their_w, theirs[cc * 32 + e], x);
+            o[e] = __float_as_uint(x * inv);
+          }
+          for (int s = 0; s < prefix.used; ++s) {  // (finish) part 0's chunks
+            const int64_t from = prefix.at(a, s, token, hq);
+            const float wgt = none ? 0.f : exp2f(a.part_lse[from] - top) * inv;
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const float4 v = *reinterpret_cast<const float4*>(a.part_out + from * D + cc * 32 + e);
+              o[e] = __float_as_uint(fmaf(wgt, v.x, __uint_as_float(o[e])));
+              o[e + 1] = __float_as_uint(fmaf(wgt, v.y, __uint_as_float(o[e + 1])));
+              o[e + 2] = __float_as_uint(fmaf(wgt, v.z, __uint_as_float(o[e + 2])));
+              o[e + 3] = __float_as_uint(fmaf(wgt, v.w, __uint_as_float(o[e + 3])));
             }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = none ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv);
           }
           if (direct) {
             uint32_t x[16];
@@ -667,7 +693,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             }
           }
         }
-        if (r < n_rows) {
+        if (write) {
           if (!direct) a.part_lse[at] = lse2;
           else if (a.lse) a.lse[token * a.heads * a.group + hq] = lse2 * 0.6931471805599453f;
         }
@@ -689,8 +715,8 @@ cudaError_t launch(const AttendView& a, int part, const CUtensorMap& k, const CU
   static unsigned long long flags = 0;
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(attend_tc_kernel<FMT, D>), smem, &flags);
   if (e != cudaSuccess) return e;
-  attend_tc_kernel<FMT, D><<<(unsigned)part_blocks(a, a.part[part]), threads(FMT), smem, stream>>>(k, v, a, part);
-  return cudaGetLastError();
+  return launch_kernel(attend_tc_kernel<FMT, D>, dim3((unsigned)part_blocks(a, a.part[part])), threads(FMT), smem, stream,
+                       a.early != 0 && part == 1, k, v, a, part);
 }
 
 }  // namespace

@@ -14,8 +14,7 @@ constexpr int kMaxSlots = 2 * kMaxSplits;  // two parts
 template <typename T, int D>
 __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant__ AttendView a) {
   // (launched while the kernels that leave the chunks may still run)
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  wait_for_earlier();
   constexpr int kPer = D / 32;
   const int seq = blockIdx.y;
   const int lane = threadIdx.x & 31;
@@ -32,19 +31,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
   for (int k = 0; k < 2; ++k) {
     if (k >= a.n_parts) break;
     const AttendPart& p = a.part[k];
-    int which = seq;
-    if (p.grouped) {
-      which = 0;
-      if (a.cu_group) {  // the group of this sequence: the last one that starts at or before it
-        int lo = 0, hi = a.n_groups;
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (a.cu_group[mid] <= seq) lo = mid;
-          else hi = mid;
-        }
-        which = lo;
-      }
-    }
+    const int which = p.grouped ? group_of(a, seq) : seq;
     const Problem pr = locate(a, p, which);
     if (token < pr.t0 || token >= pr.t0 + pr.nt) return;  // beyond what the caller allowed for: left as it was
     slot[k] = p.slot0;
@@ -110,16 +97,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
 template <typename T, int D>
 cudaError_t launch(const AttendView& a, cudaStream_t stream) {
   const int64_t rows = (int64_t)a.max_q * a.heads * a.group;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((rows + 7) / 8), (unsigned)a.batch);
-  cfg.blockDim = dim3(256);
-  cfg.stream = stream;
-  cudaLaunchAttribute early[1];
-  early[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  early[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = early;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attend_join_kernel<T, D>, a);
+  return launch_kernel(attend_join_kernel<T, D>, dim3((unsigned)((rows + 7) / 8), (unsigned)a.batch), 256, 0, stream, true, a);
 }
 
 }  // namespace

@@ -269,6 +269,27 @@ def test_cross_extreme_values(pkg, fmt, q_dtype, n):
             ref.compare(lse[sl], want[1], want[3], "lse %d" % b)
 
 
+@pytest.mark.parametrize("fmt,q_dtype", FORMATS)
+@pytest.mark.parametrize("n", [1, 70, 150])
+@pytest.mark.parametrize("at", [0, 200, 299])
+def test_cross_nan_keys(pkg, fmt, q_dtype, n, at):
+    """A NaN key gives NaN to every query that sees it, wherever it lies; its neighbours in the store give nothing."""
+    dim = 128
+    k, v = (_rows(s, 600, 1, dim, DT.get(fmt, torch.bfloat16), spread=False) for s in (2, 3))
+    k[at, 0, 77] = math.nan
+    if at == 0:
+        k[:300, 0, 77] = math.nan  # nothing but NaN
+    store, k64, v64 = _make(pkg, fmt, k, v)
+    q = torch.randn((2 * n, 1, dim), generator=_gen(4)).to(DT[q_dtype]).cuda()
+    out, lse = torch.empty_like(q), torch.empty((2 * n, 1), dtype=torch.float32, device="cuda")
+    kw = {} if n == 1 else {"cu_q": _i32([0, n, 2 * n]), "max_q": n}
+    store.cross_attend(q, _i64([0, 300]), _i32([300, 299]), out, max_len=300, lse=lse, **kw)
+    assert torch.isnan(out[:n]).all() and torch.isnan(lse[:n]).all()
+    want = ref.attend(q[n:].double().cpu().numpy(), k64[300:599], v64[300:599], [299] * n, float(np.float32(1 / math.sqrt(dim))), fmt, q_dtype)
+    ref.compare(out[n:], want[0], want[2], "out")
+    ref.compare(lse[n:], want[1], want[3], "lse")
+
+
 @pytest.mark.parametrize("fmt,q_dtype", [("kv8", "bf16"), ("kv8", "f32"), ("bf16", "bf16")])
 @pytest.mark.parametrize("n", [1, 70])
 def test_cross_queries_and_values_of_far_apart_magnitudes(pkg, fmt, q_dtype, n):
