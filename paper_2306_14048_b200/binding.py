@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -181,7 +182,7 @@ def _load() -> ctypes.CDLL:
     lib.h2o_debug_set_prefill_events.argtypes = [vp, c.POINTER(vp)]
     lib.h2o_debug_bounds_checked.restype = c.c_int
     lib.h2o_debug_bounds_checked.argtypes = []
-    qp, rp = c.POINTER(h2o_queries_t), c.POINTER(h2o_ranges_t)
+    qp = rp = vp  # h2o_queries_t / h2o_ranges_t: by reference, or as packed bytes
     lib.h2o_store_create.restype = c.c_int
     lib.h2o_store_create.argtypes = [c.POINTER(vp), c.POINTER(h2o_store_config_t)]
     lib.h2o_store_destroy.restype = c.c_int
@@ -421,6 +422,10 @@ class H2OCache:
 
 
 _DTYPES = {torch.float32: H2O_F32, torch.bfloat16: H2O_BF16}
+# h2o_queries_t and h2o_ranges_t as bytes: a step's host time counts, and packing costs a third of filling a Structure
+_pack_queries = struct.Struct("@PPPPqqqfiiii0P").pack
+_pack_ranges = struct.Struct("@PPi0P").pack
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _bad(why: str):
@@ -460,6 +465,8 @@ class H2OStore:
                 _bad("rows of k and v must have one stride and dense heads")
         self.format = H2O_KV8 if eight else _DTYPES[k.dtype]
         self.device = k.device
+        self._index = k.device.index
+        self._need = {}  # scratch bytes by the sizes of a call
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
         torch.cuda.current_stream(self.device).synchronize()  # the zero is there, whatever stream comes next
@@ -481,51 +488,52 @@ class H2OStore:
         return cls(k, torch.zeros_like(k), scale, scale.clone())
 
     # ---- argument checks ----
-    def _stream(self, stream) -> int:
-        return int((torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream)
-
     def _rows(self, k, v, rows, first_row):
-        if k.shape != v.shape or k.dtype != v.dtype or k.dim() != 3 or k.shape[1:] != (self.n_heads, self.head_dim):
-            _bad("k and v must be [tokens, %d, %d] of one dtype" % (self.n_heads, self.head_dim))
-        if k.dtype not in _DTYPES or k.device != self.device or v.device != self.device:
-            _bad("k and v must be float32 or bfloat16 on %s" % self.device)
-        n = k.shape[0]
-        if k.stride() != v.stride() or (n and (k.stride(2) != 1 or k.stride(1) != self.head_dim)):
+        shape = k.shape
+        if len(shape) != 3 or v.shape != shape or shape[1] != self.n_heads or shape[2] != self.head_dim:
+            _bad("k and v must be [tokens, %d, %d]" % (self.n_heads, self.head_dim))
+        dtype = _DTYPES.get(k.dtype)
+        if dtype is None or v.dtype is not k.dtype or k.get_device() != self._index or v.get_device() != self._index:
+            _bad("k and v must both be float32 or bfloat16 on %s" % self.device)
+        n, stride = shape[0], k.stride()
+        if stride != v.stride() or (n and (stride[2] != 1 or stride[1] != self.head_dim)):
             _bad("k and v must have one token stride and dense heads")
-        if rows is not None and (rows.dtype != torch.int64 or rows.shape != (n,) or rows.device != self.device or not rows.is_contiguous()):
+        if rows is not None and (rows.dtype is not torch.int64 or rows.shape != (n,) or rows.get_device() != self._index or not rows.is_contiguous()):
             _bad("rows must be a contiguous int64 [tokens] on %s" % self.device)
-        return (k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], n, k.stride(0) if n > 1 else 0,
-                None if rows is None else rows.data_ptr(), int(first_row))
+        return (self._h, k.data_ptr(), v.data_ptr(), dtype, n, stride[0] if n > 1 else 0,
+                None if rows is None else rows.data_ptr(), first_row)
 
     def _queries(self, q, out, cu_q, max_q, lse, softmax_scale, batch):
-        heads = q.shape[1] if q.dim() == 3 else 0
-        if q.dim() != 3 or q.shape[2] != self.head_dim or heads < self.n_heads or heads % self.n_heads:
+        shape = q.shape
+        if len(shape) != 3 or shape[2] != self.head_dim or shape[1] < self.n_heads or shape[1] % self.n_heads:
             _bad("q must be [tokens, multiple of %d, %d]" % (self.n_heads, self.head_dim))
-        if out.shape != q.shape or out.dtype != q.dtype or q.dtype not in _DTYPES:
+        tokens, heads, dim = shape
+        dtype = _DTYPES.get(q.dtype)
+        if dtype is None or out.dtype is not q.dtype or out.shape != shape:
             _bad("q and out must be float32 or bfloat16 of one shape and dtype")
-        if q.device != self.device or out.device != self.device:
+        if q.get_device() != self._index or out.get_device() != self._index:
             _bad("q and out must be on %s" % self.device)
-        if q.numel() and (q.stride(2) != 1 or q.stride(1) != self.head_dim or out.stride(2) != 1 or out.stride(1) != self.head_dim):
+        s, o = q.stride(), out.stride()
+        if tokens and (s[2] != 1 or s[1] != dim or o[2] != 1 or o[1] != dim):
             _bad("q and out must have dense heads")
-        tokens = q.shape[0]
         if cu_q is None:
             if max_q != 1 or tokens < batch:
                 _bad("without cu_q there is one token per sequence")
-        elif cu_q.dtype != torch.int32 or cu_q.shape != (batch + 1,) or cu_q.device != self.device or not cu_q.is_contiguous():
+        elif cu_q.dtype is not torch.int32 or cu_q.shape != (batch + 1,) or cu_q.get_device() != self._index or not cu_q.is_contiguous():
             _bad("cu_q must be a contiguous int32 [batch + 1] on %s" % self.device)
-        if lse is not None and (lse.dtype != torch.float32 or lse.shape != (tokens, heads) or lse.device != self.device or not lse.is_contiguous()):
+        if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (tokens, heads) or lse.get_device() != self._index or not lse.is_contiguous()):
             _bad("lse must be a contiguous float32 [tokens, heads] on %s" % self.device)
-        return h2o_queries_t(q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
-                             None if cu_q is None else cu_q.data_ptr(), tokens, q.stride(0) if tokens > 1 else 0,
-                             out.stride(0) if tokens > 1 else 0, softmax_scale, _DTYPES[q.dtype], heads // self.n_heads,
-                             batch, max_q)
+        group = heads // self.n_heads
+        return (_pack_queries(q.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(), 0 if cu_q is None else cu_q.data_ptr(),
+                              tokens, s[0] if tokens > 1 else 0, o[0] if tokens > 1 else 0, softmax_scale, dtype, group, batch, max_q),
+                (tokens, group, dtype, batch, max_q))
 
     def _ranges(self, begin, length, most, count):
-        if begin.dtype != torch.int64 or length.dtype != torch.int32 or begin.shape != (count,) or length.shape != (count,):
+        if begin.dtype is not torch.int64 or length.dtype is not torch.int32 or begin.shape != (count,) or length.shape != (count,):
             _bad("begin must be int64 and length int32, one entry per range")
-        if begin.device != self.device or length.device != self.device or not begin.is_contiguous() or not length.is_contiguous():
+        if begin.get_device() != self._index or length.get_device() != self._index or not begin.is_contiguous() or not length.is_contiguous():
             _bad("begin and length must be contiguous on %s" % self.device)
-        return h2o_ranges_t(begin.data_ptr(), length.data_ptr(), most)
+        return _pack_ranges(begin.data_ptr(), length.data_ptr(), most)
 
     def _scratch(self, nbytes, stream):
         """A piece of scratch of this call's own, on its stream; torch's blocks are 512-byte aligned."""
@@ -534,47 +542,74 @@ class H2OStore:
         with torch.cuda.stream(stream):
             return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
+    def _needs(self, sizes, nbytes):
+        """Remembers how much scratch a call of these sizes needs (a function of the sizes alone, which a call that went
+        through has shown to be valid)."""
+        if sizes not in self._need:
+            if len(self._need) >= 1024:
+                self._need.clear()
+            self._need[sizes] = nbytes
+
     # ---- calls ----
     def write(self, k, v, rows=None, first_row=0, stream=None):
         """Quantise k, v [tokens, heads, head_dim] into store rows ``rows`` (int64, device) or first_row, first_row + 1, ..."""
-        _check(lib.h2o_store_write(self._h, *self._rows(k, v, rows, first_row), self._stream(stream)), "h2o_store_write")
+        code = lib.h2o_store_write(*self._rows(k, v, rows, first_row), _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "h2o_store_write")
 
     def read(self, k, v, rows=None, first_row=0, stream=None):
         """Read store rows back into k, v [tokens, heads, head_dim]."""
-        _check(lib.h2o_store_read(self._h, *self._rows(k, v, rows, first_row), self._stream(stream)), "h2o_store_read")
+        code = lib.h2o_store_read(*self._rows(k, v, rows, first_row), _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "h2o_store_read")
 
     def cross_attend(self, q, begin, length, out, max_len, cu_q=None, max_q=1, lse=None, softmax_scale=0.0, stream=None):
         """Sequence b's query tokens attend store rows begin[b] .. begin[b] + length[b] - 1.  q, out: [tokens, query
         heads, head_dim]; cu_q: int32 [batch + 1] first token of each sequence (None: token b is sequence b); max_q,
         max_len: upper bounds; lse: float32 [tokens, query heads] or None."""
-        batch = begin.shape[0]
-        qs = ctypes.byref(self._queries(q, out, cu_q, max_q, lse, softmax_scale, batch))
-        rs = ctypes.byref(self._ranges(begin, length, max_len, batch))
-        need = lib.h2o_cross_scratch_bytes(self._h, qs, rs)
+        batch = begin.shape[0] if begin.dim() == 1 else -1
+        qs, sizes = self._queries(q, out, cu_q, max_q, lse, softmax_scale, batch)
+        rs = self._ranges(begin, length, max_len, batch)
+        sizes += (max_len,)
+        need = self._need.get(sizes)
+        if need is None:
+            need = lib.h2o_cross_scratch_bytes(self._h, qs, rs)
         scratch = self._scratch(need, stream) if need else None
-        _check(lib.h2o_cross_attend(self._h, qs, rs, scratch.data_ptr() if need else None, need, self._stream(stream)),
-               "h2o_cross_attend")
+        code = lib.h2o_cross_attend(self._h, qs, rs, scratch.data_ptr() if need else None, need,
+                                    _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "h2o_cross_attend")
+        self._needs(sizes, need)
 
     def prefix_attend(self, q, prefix_begin, prefix_len, own_begin, own_len, out, max_prefix, max_own, cu_group=None,
                       max_group=0, cu_q=None, max_q=1, lse=None, softmax_scale=0.0, stream=None):
         """Groups of consecutive sequences (cu_group: int32 [groups + 1], None: one group) share the store rows
         prefix_begin[g] .. + prefix_len[g] - 1; sequence b's own rows are own_begin[b] .. + own_len[b] - 1, the last
         of them those of its query tokens.  max_group: upper bound of a group's sequences (0: the batch)."""
-        batch, groups = own_begin.shape[0], prefix_begin.shape[0]
+        batch = own_begin.shape[0] if own_begin.dim() == 1 else -1
+        groups = prefix_begin.shape[0] if prefix_begin.dim() == 1 else -1
         if cu_group is None:
             if groups != 1:
                 _bad("several groups need cu_group")
-        elif cu_group.dtype != torch.int32 or cu_group.shape != (groups + 1,) or cu_group.device != self.device or not cu_group.is_contiguous():
-            _bad("cu_group must be a contiguous int32 [groups + 1] on %s" % self.device)
-        qs = ctypes.byref(self._queries(q, out, cu_q, max_q, lse, softmax_scale, batch))
-        ps = ctypes.byref(self._ranges(prefix_begin, prefix_len, max_prefix, groups))
-        os_ = ctypes.byref(self._ranges(own_begin, own_len, max_own, batch))
-        cg = None if cu_group is None else cu_group.data_ptr()
+            cg = None
+        else:
+            if cu_group.dtype is not torch.int32 or cu_group.shape != (groups + 1,) or cu_group.get_device() != self._index or not cu_group.is_contiguous():
+                _bad("cu_group must be a contiguous int32 [groups + 1] on %s" % self.device)
+            cg = cu_group.data_ptr()
+        qs, sizes = self._queries(q, out, cu_q, max_q, lse, softmax_scale, batch)
+        ps = self._ranges(prefix_begin, prefix_len, max_prefix, groups)
+        os_ = self._ranges(own_begin, own_len, max_own, batch)
         most = max_group or max(1, batch)
-        need = lib.h2o_prefix_scratch_bytes(self._h, qs, ps, groups, cg, most, os_)
+        sizes += (max_prefix, max_own, groups, most)
+        need = self._need.get(sizes)
+        if need is None:
+            need = lib.h2o_prefix_scratch_bytes(self._h, qs, ps, groups, cg, most, os_)
         scratch = self._scratch(need, stream) if need else None
-        _check(lib.h2o_prefix_attend(self._h, qs, ps, groups, cg, most, os_, scratch.data_ptr() if need else None, need,
-                                     self._stream(stream)), "h2o_prefix_attend")
+        code = lib.h2o_prefix_attend(self._h, qs, ps, groups, cg, most, os_, scratch.data_ptr() if need else None, need,
+                                     _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "h2o_prefix_attend")
+        self._needs(sizes, need)
 
     def status(self) -> int:
         """H2O_OK, or the H2O_ERR_* a kernel recorded (synchronises)."""

@@ -120,7 +120,7 @@ int few_rows(int format) { return format == H2O_KV8 ? 32 : 16; }
 void split_part(h2o::AttendPart& p, int64_t units, int64_t room, int64_t fixed, bool ragged) {
   const int64_t len = std::max(1, p.max_length), num = ragged ? 2 : 3;
   int64_t best = -1;
-  for (int64_t n = 1; n <= h2o::kMaxSplits; ++n) {
+  for (int64_t n = 1; n <= h2o::kMaxSplits && (n == 1 || units * n <= 16 * room); ++n) {
     const int64_t chunk = ((len + n - 1) / n + 127) / 128 * 128;
     const int64_t splits = (len + chunk - 1) / chunk;
     const int64_t one = std::min(chunk, len) + fixed;
@@ -180,16 +180,17 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
     p.problems = p.grouped ? n_groups : a.batch;
     const int64_t rows = std::min<int64_t>((p.grouped ? (int64_t)a.max_group * a.max_q : a.max_q), a.q_rows) * a.group;
     pl.kernel[n] = q->dtype == H2O_F32 ? Kernel::Fma : rows > few_rows(c.format) ? Kernel::Tc : Kernel::Mma;
-    pl.tile[n] = pl.kernel[n] == Kernel::Fma  ? h2o::attend_fma_row_tile(rows)
+    pl.tile[n] = pl.kernel[n] == Kernel::Fma  ? h2o::attend_fma_row_tile(rows, (int64_t)a.heads * p.problems)
                  : pl.kernel[n] == Kernel::Tc ? h2o::kManyRowTile
                                               : h2o::attend_mma_row_tile(rows);
     p.row_tiles = (int)((rows + pl.tile[n] - 1) / pl.tile[n]);
     const int64_t units = (int64_t)p.row_tiles * a.heads * p.problems;
-    // Fixed costs: about 3 us at a block's share of the memory's 6.4 TB/s; of the tcgen05 kernel 8 us at 80 keys in 1 us.
+    // Fixed costs: about 3 us at a block's share of the memory's 6.4 TB/s; of the tcgen05 kernel 8 us at 80 keys in 1 us, of
+    // the FMA kernel 2 us at 64 keys in 3.5.
     const int key_bytes = 2 * a.dim * (c.format == H2O_KV8 ? 1 : c.format == H2O_BF16 ? 2 : 4);
     const int per_sm = pl.kernel[n] == Kernel::Tc ? 1 : pl.kernel[n] == Kernel::Fma ? 2 : h2o::attend_mma_blocks_per_sm(c.format, pl.tile[n]);
     const int64_t room = (int64_t)h2o::sm_count() * per_sm;
-    split_part(p, units, room, pl.kernel[n] == Kernel::Tc ? 640 : 19200000 / (room * key_bytes), !p.grouped);
+    split_part(p, units, room, pl.kernel[n] == Kernel::Tc ? 640 : pl.kernel[n] == Kernel::Fma ? 36 : 19200000 / (room * key_bytes), !p.grouped);
     if (units * p.splits > INT32_MAX) pl.rc = H2O_ERR_UNSUPPORTED;
     p.slot0 = n == 0 ? 0 : a.part[0].splits;
     ++n;
