@@ -13,8 +13,8 @@
 // The handle: host memory only.
 struct h2o_store {
   h2o_store_config_t cfg;  // strides filled in
-  // tensor maps of the rows (opaque here): boxes for few and for many query rows
-  alignas(64) unsigned char few_k[128], few_v[128], many_k[128], many_v[128];
+  // tensor maps of the rows (opaque here): boxes for few query rows, and for many in blocks of one and of two groups
+  alignas(64) unsigned char few_k[128], few_v[128], one_k[128], one_v[128], two_k[128], two_v[128];
 };
 
 namespace h2o {
@@ -171,15 +171,16 @@ cudaError_t launch_store_read(const h2o_store_config_t& c, void* k, void* v, int
 int attend_fma_row_tile(int64_t rows, int64_t problems);
 cudaError_t launch_attend_fma(const AttendView& a, int part, int tile, int format, cudaStream_t stream);
 constexpr int kFewBoxRows = 32;  // rows of a box of the store's tensor maps
-int many_box_rows(int format, int dim);
 bool make_store_map(CUtensorMap_st* map, const h2o_store_config_t& c, const void* base, int box_rows);
 int attend_mma_row_tile(int64_t rows);
 int attend_mma_blocks_per_sm(int format, int tile);
 // part `first`, or (both) parts 0 and 1 in one launch
 cudaError_t launch_attend_mma(const AttendView& a, int first, bool both, const int* tile, int format, const void* map_k,
                               const void* map_v, cudaStream_t stream);
-constexpr int kManyRowTile = 256;
-cudaError_t launch_attend_tc(const AttendView& a, int part, int format, const void* map_k, const void* map_v, cudaStream_t stream);
+int attend_tc_box_rows(int format, int dim, int groups);
+// `groups` of 128 query rows to a block
+cudaError_t launch_attend_tc(const AttendView& a, int part, int groups, int format, const void* map_k, const void* map_v,
+                             cudaStream_t stream);
 cudaError_t launch_attend_join(const AttendView& a, int q_dtype, cudaStream_t stream);
 
 }  // namespace h2o

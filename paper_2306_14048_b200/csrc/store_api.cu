@@ -94,7 +94,8 @@ int check_ranges(const h2o_ranges_t* r) {
   return H2O_OK;
 }
 
-enum class Kernel { Fma, Mma, Tc };
+enum class Kernel { Fma, Mma, Tc1, Tc2 };  // (tcgen05: one or two groups of 128 rows to a block)
+bool is_tc(Kernel k) { return k == Kernel::Tc1 || k == Kernel::Tc2; }
 
 // What a call launches and how much scratch it needs.
 struct Plan {
@@ -111,6 +112,11 @@ struct Plan {
 // bfloat16, 8 heads of 128, 16 query rows 30 / 26, 20 rows 36 / 26; 32 heads 61 / 65 and 69 / 65; 16 heads of 64: 28 / 37
 // and 37 / 37.  8-bit, 8 heads of 128, 32 query rows 26 / 28; 32 heads 61 / 73.
 int few_rows(int format) { return format == H2O_KV8 ? 32 : 16; }
+
+#ifndef SHORTK
+#define SHORTK 512
+#endif
+constexpr int kShortKeys = SHORTK;
 
 // Splits the keys of a part: `units` blocks per split, `room` blocks that run at once.  Costs in keys of one block: a block
 // costs its keys and `fixed` more (start, merge, its result's trip through memory), the joining kernel twice as much;
@@ -179,18 +185,24 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
     p.causal = prefix && k == 1;
     p.problems = p.grouped ? n_groups : a.batch;
     const int64_t rows = std::min<int64_t>((p.grouped ? (int64_t)a.max_group * a.max_q : a.max_q), a.q_rows) * a.group;
-    pl.kernel[n] = q->dtype == H2O_F32 ? Kernel::Fma : rows > few_rows(c.format) ? Kernel::Tc : Kernel::Mma;
-    pl.tile[n] = pl.kernel[n] == Kernel::Fma  ? h2o::attend_fma_row_tile(rows, (int64_t)a.heads * p.problems)
-                 : pl.kernel[n] == Kernel::Tc ? h2o::kManyRowTile
-                                              : h2o::attend_mma_row_tile(rows);
+    if (q->dtype == H2O_F32) {
+      pl.kernel[n] = Kernel::Fma;
+      pl.tile[n] = h2o::attend_fma_row_tile(rows, (int64_t)a.heads * p.problems);
+    } else if (rows <= few_rows(c.format)) {
+      pl.kernel[n] = Kernel::Mma;
+      pl.tile[n] = h2o::attend_mma_row_tile(rows);
+    } else {
+      pl.kernel[n] = c.format == H2O_BF16 && p.max_length <= kShortKeys ? Kernel::Tc1 : Kernel::Tc2;
+      pl.tile[n] = pl.kernel[n] == Kernel::Tc1 ? 128 : 256;
+    }
     p.row_tiles = (int)((rows + pl.tile[n] - 1) / pl.tile[n]);
     const int64_t units = (int64_t)p.row_tiles * a.heads * p.problems;
     // Fixed costs: about 3 us at a block's share of the memory's 6.4 TB/s; of the tcgen05 kernel 8 us at 80 keys in 1 us, of
     // the FMA kernel 2 us at 64 keys in 3.5.
     const int key_bytes = 2 * a.dim * (c.format == H2O_KV8 ? 1 : c.format == H2O_BF16 ? 2 : 4);
-    const int per_sm = pl.kernel[n] == Kernel::Tc ? 1 : pl.kernel[n] == Kernel::Fma ? 2 : h2o::attend_mma_blocks_per_sm(c.format, pl.tile[n]);
+    const int per_sm = pl.kernel[n] == Kernel::Tc2 ? 1 : pl.kernel[n] == Kernel::Tc1 || pl.kernel[n] == Kernel::Fma ? 2 : h2o::attend_mma_blocks_per_sm(c.format, pl.tile[n]);
     const int64_t room = (int64_t)h2o::sm_count() * per_sm;
-    split_part(p, units, room, pl.kernel[n] == Kernel::Tc ? 640 : pl.kernel[n] == Kernel::Fma ? 36 : 19200000 / (room * key_bytes), !p.grouped);
+    split_part(p, units, room, is_tc(pl.kernel[n]) ? 640 : pl.kernel[n] == Kernel::Fma ? 36 : 19200000 / (room * key_bytes), !p.grouped);
     if (units * p.splits > INT32_MAX) pl.rc = H2O_ERR_UNSUPPORTED;
     p.slot0 = n == 0 ? 0 : a.part[0].splits;
     ++n;
@@ -199,8 +211,8 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
   // The second part's kernel, where it is one of its own, starts before the first one's has ended: neither needs the
   // other's results until the end.  Prompts' own rows, unsplit, then join what the first part left themselves (32 prompts
   // of up to 200 tokens: 415 -> 348 us); single tokens' blocks are many and short, and leave that to the joining kernel.
-  a.early = n == 2 && pl.kernel[0] == Kernel::Tc;
-  a.finish = a.early && a.part[1].splits == 1 && pl.kernel[1] == Kernel::Tc;
+  a.early = n == 2 && is_tc(pl.kernel[0]);
+  a.finish = a.early && a.part[1].splits == 1 && is_tc(pl.kernel[1]);
   const int64_t slots = (int64_t)a.part[0].splits + (n == 2 && !a.finish ? a.part[1].splits : 0);
   if (slots > 1 || a.finish) {
     const size_t rows = (size_t)slots * a.q_rows * a.heads * a.group;
@@ -225,7 +237,8 @@ int run_plan(const h2o_store_t* store, const h2o_queries_t* q, Plan& pl, void* s
   const bool both = pl.a.n_parts == 2 && pl.kernel[0] == Kernel::Mma && pl.kernel[1] == Kernel::Mma;
   for (int k = 0; k < (both ? 1 : pl.a.n_parts) && e == cudaSuccess; ++k) {
     if (pl.kernel[k] == Kernel::Fma) e = h2o::launch_attend_fma(pl.a, k, pl.tile[k], format, st);
-    else if (pl.kernel[k] == Kernel::Tc) e = h2o::launch_attend_tc(pl.a, k, format, store->many_k, store->many_v, st);
+    else if (pl.kernel[k] == Kernel::Tc2) e = h2o::launch_attend_tc(pl.a, k, 2, format, store->two_k, store->two_v, st);
+    else if (pl.kernel[k] == Kernel::Tc1) e = h2o::launch_attend_tc(pl.a, k, 1, format, store->one_k, store->one_v, st);
     else e = h2o::launch_attend_mma(pl.a, k, both, pl.tile, format, store->few_k, store->few_v, st);
   }
   if (e == cudaSuccess && pl.scratch > 0 && !pl.a.finish) e = h2o::launch_attend_join(pl.a, q->dtype, st);
@@ -280,8 +293,12 @@ int h2o_store_create(h2o_store_t** out, const h2o_store_config_t* cfg) {
       unsigned char* map;
       const void* base;
       int box;
-    } const maps[4] = {{s->few_k, cfg->k, h2o::kFewBoxRows}, {s->few_v, cfg->v, h2o::kFewBoxRows},
-                       {s->many_k, cfg->k, h2o::many_box_rows(cfg->format, cfg->head_dim)}, {s->many_v, cfg->v, h2o::many_box_rows(cfg->format, cfg->head_dim)}};
+    } const maps[6] = {{s->few_k, cfg->k, h2o::kFewBoxRows},
+                       {s->few_v, cfg->v, h2o::kFewBoxRows},
+                       {s->one_k, cfg->k, h2o::attend_tc_box_rows(cfg->format, cfg->head_dim, 1)},
+                       {s->one_v, cfg->v, h2o::attend_tc_box_rows(cfg->format, cfg->head_dim, 1)},
+                       {s->two_k, cfg->k, h2o::attend_tc_box_rows(cfg->format, cfg->head_dim, 2)},
+                       {s->two_v, cfg->v, h2o::attend_tc_box_rows(cfg->format, cfg->head_dim, 2)}};
     for (const auto& m : maps)
       if (!h2o::make_store_map(reinterpret_cast<CUtensorMap_st*>(m.map), s->cfg, m.base, m.box)) {
         delete s;

@@ -40,23 +40,24 @@ namespace {
 using namespace ptx;
 
 constexpr int kM = 128;  // rows of a group
-// (8-bit rows of 64 channels: what fits the softmax threads' 144 registers)
-__host__ __device__ constexpr int tile_keys(int fmt, int d) { return d == 128 ? 80 : fmt == H2O_KV8 ? 64 : 96; }
-__host__ __device__ constexpr int threads(int fmt) { return fmt == H2O_KV8 ? 640 : 384; }
-__host__ __device__ constexpr int tile_bytes(int fmt, int d) { return tile_keys(fmt, d) * d * 2; }
+// G: groups of a block, 2, or 1 (bfloat16 rows only: half the block, two of them on an SM).
+// (8-bit rows of 64 channels: what fits the softmax threads' 144 registers; one group: what fits half an SM's shared memory)
+__host__ __device__ constexpr int tile_keys(int fmt, int d, int g) { return g == 1 ? 64 : d == 128 ? 80 : fmt == H2O_KV8 ? 64 : 96; }
+__host__ __device__ constexpr int threads(int fmt, int g) { return fmt == H2O_KV8 ? 640 : 128 + 128 * g; }
+__host__ __device__ constexpr int tile_bytes(int fmt, int d, int g) { return tile_keys(fmt, d, g) * d * 2; }
 // Ring of stages, K and V of a tile in each.  Two groups that take tiles in turn use an even number where TMA fills the
 // stages: a warp that waits for a tile then has seen the stage's tile before, so a parity cannot be mistaken for an older
 // one.  (Converted tiles complete in order, so a warp that has seen its last tile may count on all before it.)
-__host__ __device__ constexpr int stages(int fmt, int d) { return d == 64 ? 6 : fmt == H2O_KV8 ? 3 : 4; }
-__host__ __device__ constexpr int turn_stages(int fmt, int d) { return fmt == H2O_KV8 ? stages(fmt, d) : stages(fmt, d) & ~1; }
+__host__ __device__ constexpr int stages(int fmt, int d, int g) { return g == 1 ? (d == 64 ? 4 : 2) : d == 64 ? 6 : fmt == H2O_KV8 ? 3 : 4; }
+__host__ __device__ constexpr int turn_stages(int fmt, int d, int g) { return fmt == H2O_KV8 ? stages(fmt, d, g) : stages(fmt, d, g) & ~1; }
 constexpr int kMaxStages = 6, kRawStages = 2;  // (a stage of the code ring also holds K and V)
-__host__ __device__ constexpr int smem_bytes(int fmt, int d) {
-  return 2 * kM * d * 2 + 2 * stages(fmt, d) * tile_bytes(fmt, d) + (fmt == H2O_KV8 ? 2 * kRawStages * tile_keys(fmt, d) * d : 0) + 1024;
+__host__ __device__ constexpr int smem_bytes(int fmt, int d, int g) {
+  return g * kM * d * 2 + 2 * stages(fmt, d, g) * tile_bytes(fmt, d, g) + (fmt == H2O_KV8 ? 2 * kRawStages * tile_keys(fmt, d, g) * d : 0) + 1024;
 }
 // Registers of a thread: the softmax warps take what the others give back.  8-bit: 640 threads start with 96 each =
-// 256 x 144 + 384 x 64; bfloat16: 384 start with 168 = 256 x 216 + 128 x 72.
-__host__ __device__ constexpr int regs_softmax(int fmt) { return fmt == H2O_KV8 ? 144 : 216; }
-__host__ __device__ constexpr int regs_other(int fmt) { return fmt == H2O_KV8 ? 64 : 72; }
+// 256 x 144 + 384 x 64; bfloat16: 384 start with 168 = 256 x 216 + 128 x 72; one group: 256 with 128 = 128 x 176 + 128 x 80.
+__host__ __device__ constexpr int regs_softmax(int fmt, int g) { return fmt == H2O_KV8 ? 144 : g == 1 ? 176 : 216; }
+__host__ __device__ constexpr int regs_other(int fmt, int g) { return fmt == H2O_KV8 ? 64 : g == 1 ? 80 : 72; }
 // Every kPolyEvery-th pair of exponentials runs on the FMA pipe.  4 x 2048 queries against 4096 keys, 32 heads: none 550,
 // one in eight 518, one in four 505, one in three 547, one in two 535 us.
 constexpr int kPolyEvery = 4;
@@ -117,6 +118,13 @@ constexpr float kRescale = 8.f;
 template <int FMT>
 constexpr float kLargeSumOf = FMT == H2O_KV8 ? 4096.f : 1.0e12f;
 
+// 32-byte global load: a whole sector, where neighbouring threads read rows far apart (the address is 32-byte aligned)
+__device__ __forceinline__ void ld_global_256(const float* p, float4& a, float4& b) {
+  asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=f"(a.x), "=f"(a.y), "=f"(a.z), "=f"(a.w), "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w)
+               : "l"(p)
+               : "memory");
+}
 // Barrier of the eight softmax warps.
 __device__ __forceinline__ void softmax_sync() { asm volatile("barrier.cta.sync 3, 256;" ::: "memory"); }
 // N consecutive columns of the warp's 32 lanes from / to registers
@@ -181,44 +189,70 @@ __device__ __forceinline__ void codes_to_f16(uint32_t word, __half2 scale, uint3
   hi = *reinterpret_cast<const uint32_t*>(&y);
 }
 
-template <int FMT, int D>
-__global__ void __launch_bounds__(threads(FMT), 1)
+// FINISH: part 1 of a shared prefix, which joins what part 0 left (an instance of its own: the rest is 5 % faster without).
+template <int FMT, int D, int G, bool FINISH>
+__global__ void __launch_bounds__(threads(FMT, G), 3 - G)
 attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                  const __grid_constant__ AttendView a, int part_index) {
   constexpr bool kF16 = FMT == H2O_KV8;
-  constexpr int kN = tile_keys(FMT, D), kTile = tile_bytes(FMT, D), kQTile = kM * D * 2, kStages = stages(FMT, D), kRaw = kN * D;
+  constexpr int kN = tile_keys(FMT, D, G), kTile = tile_bytes(FMT, D, G), kQTile = kM * D * 2, kStages = stages(FMT, D, G), kRaw = kN * D;
   constexpr float kLargeSum = kLargeSumOf<FMT>;
-  // tensor memory: O, S (starts on multiples of 32 columns) and P (of 8) of the two groups
-  constexpr uint32_t kColO = 0, kStepO = D, kColS = 2 * D, kStepS = 96, kColP = kColS + kStepS + kN, kStepP = kN / 2;
-  static_assert(kColP + 2 * kStepP <= 512, "tensor memory");
-  static_assert(smem_bytes(FMT, D) + sizeof(Shared) <= 227 * 1024, "shared memory of a block");
-  static_assert(kM * (D + 4) * 4 <= 2 * turn_stages(FMT, D) * kTile, "B's output fits the ring");
+  // tensor memory: O, S (starts on multiples of 32 columns) and P (of 8) of the groups
+  constexpr uint32_t kColO = 0, kStepO = D, kColS = G * D, kStepS = 96, kColP = kColS + kStepS * (G - 1) + kN, kStepP = kN / 2;
+  constexpr uint32_t kCols = G == 2 ? 512 : 256;
+  static_assert(kColP + G * kStepP <= kCols, "tensor memory");
+  static_assert(smem_bytes(FMT, D, G) + sizeof(Shared) + (G == 1 ? 1024 : 0) <= (G == 1 ? 114 : 227) * 1024, "shared memory of a block");
+  static_assert(G == 1 || kM * (D + 4) * 4 <= 2 * turn_stages(FMT, D, G) * kTile, "B's output fits the ring");
   extern __shared__ unsigned char dyn_raw[];
   __shared__ Shared sh;
   unsigned char* dyn = dyn_raw + ((1024u - (smem_u32(dyn_raw) & 1023u)) & 1023u);
   unsigned char* q_tiles = dyn;
-  unsigned char* ring = dyn + 2 * kQTile;
+  unsigned char* ring = dyn + G * kQTile;
   unsigned char* raw = ring + 2 * kStages * kTile;
 
   let_next_start();
-  const bool finish = a.finish && part_index == 1;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  // what does not depend on the block's work, while the others look that up
+  if (threadIdx.x == 0) {
+    prefetch_tensormap(&map_k);
+    prefetch_tensormap(&map_v);
+    for (int g = 0; g < 2; ++g) {
+      mbar_init(&sh.q_full[g], 4);
+      mbar_init(&sh.s_full[g], 1);
+      mbar_init(&sh.s_read[g], 4);
+      mbar_init(&sh.p_full[g], 4);
+      mbar_init(&sh.p_empty[g], 1);
+      mbar_init(&sh.o_final[g], 1);
+    }
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&sh.kv_full[i], kF16 ? 8 : 1);  // (eight converting warps)
+      mbar_init(&sh.kv_empty[i], G);  // a product P V of each group
+    }
+    for (int i = 0; i < kRawStages; ++i) {
+      mbar_init(&sh.raw_full[i], 1);
+      mbar_init(&sh.raw_empty[i], 8);
+    }
+    mbar_init(&sh.tail, 1);
+    sh.abort_flag = 0;
+    fence_barrier_init();
+  }
   const AttendPart& part = a.part[part_index];
   const BlockWork w = block_work(a, part, blockIdx.x);
   const Problem pr = locate(a, part, w.problem);
-  const int rows = pr.nt * a.group, r0 = w.row_tile * (2 * kM);
+  const int rows = pr.nt * a.group, r0 = w.row_tile * (G * kM);
   // (a launch that started early does not end before the one in front of it, whatever its blocks have to do)
   if (a.early && part_index == 1 && blockIdx.x == 0) wait_for_earlier();
   if (r0 >= rows) return;
-  const int n_rows = min(2 * kM, rows - r0);
+  const int n_rows = min(G * kM, rows - r0);
   const int key0 = w.split * part.chunk;
-  const bool direct = a.part_out == nullptr || finish;
+  const bool direct = a.part_out == nullptr || FINISH;
   if (!direct && key0 >= pr.len) return;  // (the join kernel does not read it)
   const int last_seen = seen_rows(part, pr, (r0 + n_rows - 1) / a.group);
   const int key1 = min(last_seen, key0 + part.chunk);
   // (the shuffle tells the compiler that the value is the same in all lanes: the issuing loops then stay in uniform registers)
   const int nt = __shfl_sync(0xffffffffu, max(0, (key1 - key0 + kN - 1) / kN), 0);
-  const bool alt = __shfl_sync(0xffffffffu, n_rows, 0) <= kM;  // both groups on the same rows, tiles in turn
-  const int n_stages = alt ? turn_stages(FMT, D) : kStages;
+  const bool alt = G == 2 && __shfl_sync(0xffffffffu, n_rows, 0) <= kM;  // both groups on the same rows, tiles in turn
+  const int n_stages = alt ? turn_stages(FMT, D, G) : kStages;
   // token and query head of row r of the block: (first + r) / group by a multiplication (exact: first + r < 2^9, group <= 32)
   const int tok0 = r0 / a.group, first_g = r0 - tok0 * a.group;
   const uint32_t magic = (65536u + a.group - 1) / a.group;
@@ -227,11 +261,9 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     tok = tok0 + d;
     hq = w.head * a.group + first_g + r - d * a.group;
   };
-  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-
   // The query rows are asked for before the first tiles, into the softmax warps' registers: behind the tiles' traffic a trip
   // to memory takes microseconds.
-  const bool softmax_warp = warp >= 4 && warp < 12;
+  const bool softmax_warp = warp >= 4 && warp < 4 + 4 * G;
   const int grp = (warp >> 2) - 1, base = alt ? 0 : grp * kM;  // a softmax warp's group, and the group's first row in the block
   constexpr int kLanes = D / 8, kPer = 32 / kLanes;            // lanes to a query row, rows to a load
   uint4 qx[32 / kPer];
@@ -258,38 +290,19 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     tma_load_tile(to + (kF16 ? kRaw : kTile), &map_v, w.head, row0 + j * kN, full);
   };
   const int n_load = kF16 ? kRawStages : n_stages;  // stages of the ring that TMA fills
-  if (threadIdx.x == 0) {
-    for (int g = 0; g < 2; ++g) {
-      mbar_init(&sh.q_full[g], 4);
-      mbar_init(&sh.s_full[g], 1);
-      mbar_init(&sh.s_read[g], 4);
-      mbar_init(&sh.p_full[g], 4);
-      mbar_init(&sh.p_empty[g], 1);
-      mbar_init(&sh.o_final[g], 1);
-    }
-    for (int i = 0; i < kStages; ++i) {
-      mbar_init(&sh.kv_full[i], kF16 ? 8 : 1);  // (eight converting warps)
-      mbar_init(&sh.kv_empty[i], alt ? 1 : 2);  // a product P V of each group that uses the tile
-    }
-    for (int i = 0; i < kRawStages; ++i) {
-      mbar_init(&sh.raw_full[i], 1);
-      mbar_init(&sh.raw_empty[i], 8);
-    }
-    mbar_init(&sh.tail, 1);
-    sh.abort_flag = 0;
-    fence_barrier_init();
-  }
-  if (warp == 3) tmem_alloc(&sh.tmem_base, 512);
+  if (warp == 3) tmem_alloc(&sh.tmem_base, kCols);
   tc_fence_before();
-  __syncthreads();
+  // (warp 0 has initialised the barriers and needs nothing of the others: its first copies start at once)
+  if (warp == 0) asm volatile("barrier.cta.arrive 4, %0;" ::"n"(threads(FMT, G)) : "memory");
+  else asm volatile("barrier.cta.sync 4, %0;" ::"n"(threads(FMT, G)) : "memory");
   tc_fence_after();
-  // the block has all of tensor memory, so it starts at 0: a constant keeps the operand addresses out of registers
-  constexpr uint32_t tmem = 0;
-  if (sh.tmem_base != 0 && threadIdx.x == 0) sh.abort_flag = 1;
+  // a block of two groups has all of tensor memory, which starts at 0: a constant keeps the operand addresses out of registers
+  const uint32_t tmem = G == 2 ? 0u : __shfl_sync(0xffffffffu, sh.tmem_base, 0);
+  if (G == 2 && warp == 3 && lane == 0 && sh.tmem_base != 0) sh.abort_flag = 1;
   volatile int* abort_flag = &sh.abort_flag;
 
-  if (warp < 4 || warp >= 12) {
-    setmaxnreg_dec<regs_other(FMT)>();
+  if (!softmax_warp) {
+    setmaxnreg_dec<regs_other(FMT, G)>();
     if (warp == 0) {
       // ---- TMA ----
       if (lane == 0) {
@@ -304,7 +317,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           }
         }
       }
-    } else if (warp < 3) {
+    } else if (warp < 1 + G) {
       // ---- S of group g (the whole warp walks, one elected lane issues) ----
       constexpr uint32_t fmt = kF16 ? kFmtF16 : kFmtBF16;
       constexpr uint32_t idesc = instr_desc_f16(kM, kN, fmt, fmt, false, false);
@@ -362,7 +375,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       for (int j = 0; j < nt && ok; ++j) {
         const int n = alt ? j >> 1 : j;  // the group's own count
         const uint64_t dv = smem_desc_sw128(smem_u32(ring + (2 * slot + 1) * kTile), kTile / 2, 1024);
-        for (int g = alt ? j & 1 : 0; g < (alt ? (j & 1) + 1 : 2); ++g) {
+        for (int g = alt ? j & 1 : 0; g < (alt ? (j & 1) + 1 : G); ++g) {
           ok = __all_sync(0xffffffffu, wait_or_abort(&sh.p_full[g], (uint32_t)n & 1u, abort_flag)) != 0;
           if (!ok) break;
           tc_fence_after();
@@ -375,6 +388,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
               mma_ts_lohi<true>(d_o, d_p + 8u * ks, desc_lo(dv) + ((2048u * ks) >> 4), desc_hi(dv), idesc);
             mma_commit(&sh.p_empty[g]);
             mma_commit(&sh.kv_empty[slot]);
+            if (alt) mma_commit(&sh.kv_empty[slot]);  // (for the group that does not use the tile)
             if (j + (alt ? 2 : 1) >= nt) mma_commit(&sh.o_final[g]);
           }
           __syncwarp();
@@ -450,7 +464,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       }
     }
   } else {
-    setmaxnreg_inc<regs_softmax(FMT)>();
+    setmaxnreg_inc<regs_softmax(FMT, G)>();
     const int g = grp, quarter = warp & 3;
     if (base < n_rows) {
       if (loads_query) {
@@ -481,6 +495,10 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       }
       // (both groups on the same rows, 8-bit: B takes the row factors that A's warps left)
       if (kF16 && alt) softmax_sync();
+
+      // (looked up while the first tile is on its way)
+      Prefix prefix{0, 0, 0};
+      if constexpr (FINISH) prefix = prefix_of(a, w.problem);
 
       // ---- softmax ----
       const int rt = quarter * 32 + lane, r = base + rt;
@@ -580,7 +598,8 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       }
       // ---- result ----
       const float sum = l2.x + l2.y;
-      bool none = !ok || sum == 0.f;  // (NaN is not none)
+      // no key seen: the sum is 0, or what ex2_fma2 makes of -infinity; but NaN is a result
+      bool none = !ok || sum == 0.f || (m == -INFINITY && sum == sum);
       const bool wrote = nt > first;  // the group has an O
       if (ok && wrote) ok = __all_sync(0xffffffffu, wait_or_abort(&sh.o_final[g], 0, abort_flag));
       float* join = reinterpret_cast<float*>(q_tiles);  // [2][128]
@@ -618,11 +637,9 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           total = mine_w * total + their_w * join[kM + rt];
         }
         const int64_t token = pr.t0 + tok;
-        Prefix prefix{0, 0, 0};
         bool write = r < n_rows;
-        if (finish) {
+        if constexpr (FINISH) {
           wait_for_earlier();
-          prefix = prefix_of(a, w.problem);
           write = write && token >= prefix.t0 && token < prefix.t1;
           if (write) {
             const float mx = prefix_top(a, prefix, token, hq, top);
@@ -638,9 +655,25 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         const float lse2 = none ? -INFINITY : top + log2f(total);
         const int64_t at = ((int64_t)(part.slot0 + w.split) * a.q_rows + token) * a.heads * a.group + hq;
         __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out) + token * a.out_stride + (int64_t)hq * D;
+        // part 0's first chunk (mostly the only one), 64 channels of it asked for at a time
+        [[maybe_unused]] float4 first[FINISH ? 16 : 1];
+        [[maybe_unused]] float first_w = 0.f;
+        if constexpr (FINISH) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) first[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (write && prefix.used > 0 && !none) first_w = exp2f(a.part_lse[prefix.at(a, 0, token, hq)] - top) * inv;
+        }
+        auto load_first = [&](int cc) {
+          const float* from = a.part_out + prefix.at(a, 0, token, hq) * D + cc * 32;
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) ld_global_256(from + 4 * i, first[i], first[i + 1]);
+        };
         const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.out_stride * 2)) & 31u) == 0;
 #pragma unroll
         for (int cc = 0; cc < D / 32; ++cc) {
+          if constexpr (FINISH) {
+            if (cc % 2 == 0 && write && prefix.used > 0) load_first(cc);
+          }
           uint32_t o[32];
           if (wrote) {
             tmem_ld32(t_o + 32u * cc, o);
@@ -654,16 +687,20 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             if (alt) x = fmaf(their_w, theirs[cc * 32 + e], x);
             o[e] = __float_as_uint(x * inv);
           }
-          for (int s = 0; s < prefix.used; ++s) {  // (finish) part 0's chunks
-            const int64_t from = prefix.at(a, s, token, hq);
-            const float wgt = none ? 0.f : exp2f(a.part_lse[from] - top) * inv;
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              const float4 v = *reinterpret_cast<const float4*>(a.part_out + from * D + cc * 32 + e);
+          if constexpr (FINISH) {  // part 0's chunks
+            auto add = [&](int e, float wgt, const float4& v) {
               o[e] = __float_as_uint(fmaf(wgt, v.x, __uint_as_float(o[e])));
               o[e + 1] = __float_as_uint(fmaf(wgt, v.y, __uint_as_float(o[e + 1])));
               o[e + 2] = __float_as_uint(fmaf(wgt, v.z, __uint_as_float(o[e + 2])));
               o[e + 3] = __float_as_uint(fmaf(wgt, v.w, __uint_as_float(o[e + 3])));
+            };
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) add(e, first_w, first[(cc % 2) * 8 + e / 4]);
+            for (int s = 1; s < prefix.used; ++s) {
+              const int64_t from = prefix.at(a, s, token, hq);
+              const float wgt = none ? 0.f : exp2f(a.part_lse[from] - top) * inv;
+#pragma unroll
+              for (int e = 0; e < 32; e += 4) add(e, wgt, *reinterpret_cast<const float4*>(a.part_out + from * D + cc * 32 + e));
             }
           }
           if (direct) {
@@ -705,29 +742,34 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   if (threadIdx.x == 0 && sh.abort_flag && a.status) atomicCAS(a.status, 0, H2O_ERR_TIMEOUT);
   if (warp == 3) {
     tc_fence_after();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc(tmem, kCols);
   }
 }
 
-template <int FMT, int D>
-cudaError_t launch(const AttendView& a, int part, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t stream) {
-  constexpr int smem = smem_bytes(FMT, D);
+template <int FMT, int D, int G, bool FINISH>
+cudaError_t launch_finish(const AttendView& a, int part, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t stream) {
+  constexpr int smem = smem_bytes(FMT, D, G);
   static unsigned long long flags = 0;
-  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(attend_tc_kernel<FMT, D>), smem, &flags);
+  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(attend_tc_kernel<FMT, D, G, FINISH>), smem, &flags);
   if (e != cudaSuccess) return e;
-  return launch_kernel(attend_tc_kernel<FMT, D>, dim3((unsigned)part_blocks(a, a.part[part])), threads(FMT), smem, stream,
+  return launch_kernel(attend_tc_kernel<FMT, D, G, FINISH>, dim3((unsigned)part_blocks(a, a.part[part])), threads(FMT, G), smem, stream,
                        a.early != 0 && part == 1, k, v, a, part);
+}
+template <int FMT, int D, int G>
+cudaError_t launch(const AttendView& a, int part, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t st) {
+  return a.finish && part == 1 ? launch_finish<FMT, D, G, true>(a, part, k, v, st) : launch_finish<FMT, D, G, false>(a, part, k, v, st);
 }
 
 }  // namespace
 
-int many_box_rows(int format, int dim) { return tile_keys(format, dim); }
+int attend_tc_box_rows(int format, int dim, int groups) { return tile_keys(format, dim, groups); }
 
-cudaError_t launch_attend_tc(const AttendView& a, int part, int format, const void* map_k, const void* map_v, cudaStream_t st) {
+cudaError_t launch_attend_tc(const AttendView& a, int part, int groups, int format, const void* map_k, const void* map_v, cudaStream_t st) {
   const CUtensorMap& k = *static_cast<const CUtensorMap*>(map_k);
   const CUtensorMap& v = *static_cast<const CUtensorMap*>(map_v);
-  if (format == H2O_KV8) return a.dim == 128 ? launch<H2O_KV8, 128>(a, part, k, v, st) : launch<H2O_KV8, 64>(a, part, k, v, st);
-  return a.dim == 128 ? launch<H2O_BF16, 128>(a, part, k, v, st) : launch<H2O_BF16, 64>(a, part, k, v, st);
+  if (format == H2O_KV8) return a.dim == 128 ? launch<H2O_KV8, 128, 2>(a, part, k, v, st) : launch<H2O_KV8, 64, 2>(a, part, k, v, st);
+  if (groups == 1) return a.dim == 128 ? launch<H2O_BF16, 128, 1>(a, part, k, v, st) : launch<H2O_BF16, 64, 1>(a, part, k, v, st);
+  return a.dim == 128 ? launch<H2O_BF16, 128, 2>(a, part, k, v, st) : launch<H2O_BF16, 64, 2>(a, part, k, v, st);
 }
 
 }  // namespace h2o

@@ -241,7 +241,7 @@ def test_cross_more_sequences_than_blocks(pkg, fmt, q_dtype):
 
 
 @pytest.mark.parametrize("fmt,q_dtype", FORMATS)
-@pytest.mark.parametrize("n", [1, 70])
+@pytest.mark.parametrize("n", [1, 70, 150])
 def test_cross_extreme_values(pkg, fmt, q_dtype, n):
     """NaN among the keys reaches the queries that see it and no others; logits of -infinity count for nothing; large
     logits do not overflow."""
