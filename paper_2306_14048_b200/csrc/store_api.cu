@@ -200,9 +200,10 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
     // Fixed costs: about 3 us at a block's share of the memory's 6.4 TB/s; of the tcgen05 kernel 8 us at 80 keys in 1 us, of
     // the FMA kernel 2 us at 64 keys in 3.5.
     const int key_bytes = 2 * a.dim * (c.format == H2O_KV8 ? 1 : c.format == H2O_BF16 ? 2 : 4);
-    const int per_sm = pl.kernel[n] == Kernel::Tc2 ? 1 : pl.kernel[n] == Kernel::Tc1 || pl.kernel[n] == Kernel::Fma ? 2 : h2o::attend_mma_blocks_per_sm(c.format, pl.tile[n]);
+    const bool tiles = pl.kernel[n] == Kernel::Fma && pl.tile[n] >= 16;
+    const int per_sm = pl.kernel[n] == Kernel::Tc2 ? 1 : pl.kernel[n] == Kernel::Tc1 || tiles ? 2 : pl.kernel[n] == Kernel::Fma ? 4 : h2o::attend_mma_blocks_per_sm(c.format, pl.tile[n]);
     const int64_t room = (int64_t)h2o::sm_count() * per_sm;
-    split_part(p, units, room, is_tc(pl.kernel[n]) ? 640 : pl.kernel[n] == Kernel::Fma ? 36 : 19200000 / (room * key_bytes), !p.grouped);
+    split_part(p, units, room, is_tc(pl.kernel[n]) ? 640 : tiles ? 36 : 19200000 / (room * key_bytes), !p.grouped);
     if (units * p.splits > INT32_MAX) pl.rc = H2O_ERR_UNSUPPORTED;
     p.slot0 = n == 0 ? 0 : a.part[0].splits;
     ++n;

@@ -1,6 +1,7 @@
-// Attention over a K/V store for float32 queries, on the fp32 FMA pipe (float32 or 8-bit rows, head_dim 64 and 128).
+// Attention over a K/V store for float32 queries, on the fp32 FMA pipe (float32 or 8-bit rows, head_dim 64 and 128): a kernel
+// for up to four query rows (a decoding step) and one for more.
 //
-// A block takes BM query rows (query tokens times the query heads of one K/V head) and walks over its keys 64 at a
+// More: a block takes BM query rows (query tokens times the query heads of one K/V head) and walks over its keys 64 at a
 // time: S = Q K^T by register tiles, softmax with the running maximum and sum of each row, O += P V.
 // 256 threads as 16 x 16: thread (x, y) has rows y * RM .. + RM - 1, keys x + 16 j of a tile, output columns
 // 4 x + 64 j .. + 3, so a row's statistics are shuffles within 16 lanes and its probabilities pass between them
@@ -235,6 +236,171 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
   }
 }
 
+// Up to R query rows: bound by reading K and V once.  Four warps take 8 or 16 keys of the block's chunk in turn, straight
+// from memory into registers: a lane has four channels of a key (D = 128: a warp one key to a load, D = 64: two).  The 8
+// partial dot products of a lane become sums over the key's lanes by halving exchanges (9 or 8 shuffles instead of
+// 8 x 5), which leaves every key's logit with a few lanes; the probabilities go back by one shuffle per key.  K and V of a
+// step are asked for together, 16 vectors a lane: 16 warps keep 128 KB of an SM under way.
+constexpr int kFewThreads = 128, kFewWarps = 4, kLoads = 8;
+
+template <int FMT, int D>
+__device__ __forceinline__ float4 load_row4(const void* base, const uint8_t* scale, const AttendView& a, int head, int64_t row, int c) {
+  if constexpr (FMT == H2O_F32) {
+    return __ldcs(reinterpret_cast<const float4*>(static_cast<const float*>(base) + row * a.row_stride + (int64_t)head * D + c));
+  } else {
+    const int64_t at = (int64_t)head * a.rows + row;
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(base) + at * D + c);
+    const float s = kv8_scale(scale[at]);
+    return make_float4(e4m3(w & 255u) * s, e4m3((w >> 8) & 255u) * s, e4m3((w >> 16) & 255u) * s, e4m3(w >> 24) * s);
+  }
+}
+
+template <int FMT, int D, int R>
+__global__ void __launch_bounds__(kFewThreads) attend_few_kernel(const __grid_constant__ AttendView a, int part_index) {
+  constexpr int kLanes = D / 4, kPer = 32 / kLanes, kKeys = kLoads * kPer;  // lanes of a key, keys of a load, of a step
+  __shared__ float sh_m[kFewWarps][R], sh_l[kFewWarps][R];
+  __shared__ __align__(16) float sh_o[kFewWarps][R][D];
+  const AttendPart& part = a.part[part_index];
+  const BlockWork w = block_work(a, part, blockIdx.x);
+  const Problem pr = locate(a, part, w.problem);
+  const int rows = pr.nt * a.group, r0 = w.row_tile * R;
+  if (r0 >= rows) return;
+  const int n_rows = min(R, rows - r0);
+  const int key0 = w.split * part.chunk;
+  const bool direct = a.part_out == nullptr;
+  if (!direct && key0 >= pr.len) return;  // (the join kernel does not read it)
+  const int key1 = min(seen_rows(part, pr, (r0 + n_rows - 1) / a.group), key0 + part.chunk);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int c = lane % kLanes * 4, sub = lane / kLanes;  // the lane's channels, its key of a load
+
+  float4 q[R];
+  int seen[R];
+  float m[R], l[R];
+  float4 o[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const bool there = r < n_rows;
+    const int tok = there ? (r0 + r) / a.group : 0;
+    const int64_t hq = (int64_t)w.head * a.group + (there ? r0 + r - tok * a.group : 0);
+    q[r] = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (pr.t0 + tok) * a.q_stride + hq * D + c);
+    seen[r] = there ? min(key1, seen_rows(part, pr, tok)) : 0;
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+    o[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  // the key of a step whose logit this lane ends up with (a few lanes the same one)
+  const int mine = kPer == 1 ? lane >> 2 : 2 * ((lane >> 1) & 7) + (lane >> 4);
+  for (int key = key0 + warp * kKeys; key < key1; key += kFewWarps * kKeys) {
+    float4 kk[kLoads], vv[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int x = key + i * kPer + sub;
+      const bool there = x < key1;  // (what lies behind the range may be anything)
+      kk[i] = there ? load_row4<FMT, D>(a.k, a.k_scale, a, w.head, pr.row0 + x, c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      vv[i] = there ? load_row4<FMT, D>(a.v, a.v_scale, a, w.head, pr.row0 + x, c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    float s[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float d[kLoads];
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) d[i] = fmaf(q[r].w, kk[i].w, fmaf(q[r].z, kk[i].z, fmaf(q[r].y, kk[i].y, q[r].x * kk[i].x)));
+      // a lane keeps the half of its values that its bit names and gives the other half away
+      int bit = kLanes / 2;
+#pragma unroll
+      for (int n = kLoads / 2; n > 0; n >>= 1, bit >>= 1) {
+        const bool upper = (lane & bit) != 0;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+          const float give = upper ? d[i] : d[i + n], keep = upper ? d[i + n] : d[i];
+          d[i] = keep + __shfl_xor_sync(0xffffffffu, give, bit);
+        }
+      }
+#pragma unroll
+      for (; bit > 0; bit >>= 1) d[0] += __shfl_xor_sync(0xffffffffu, d[0], bit);
+      s[r] = key + mine < seen[r] ? d[0] * a.scale2 : -INFINITY;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (__any_sync(0xffffffffu, s[r] > m[r] + 8.f)) {  // the reference maximum follows lazily
+        const float mn = fmaxf(m[r], warp_max(s[r]));
+        const float alpha = mn == -INFINITY ? 1.f : exp2f(m[r] - mn);
+        m[r] = mn;
+        l[r] *= alpha;
+        o[r].x *= alpha;
+        o[r].y *= alpha;
+        o[r].z *= alpha;
+        o[r].w *= alpha;
+      }
+      const float p = exp2f(s[r] - (m[r] == -INFINITY ? 0.f : m[r]));
+      l[r] += p;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const float pi = __shfl_sync(0xffffffffu, p, kPer == 1 ? 4 * i : 16 * sub + 2 * i);
+        o[r].x = fmaf(pi, vv[i].x, o[r].x);
+        o[r].y = fmaf(pi, vv[i].y, o[r].y);
+        o[r].z = fmaf(pi, vv[i].z, o[r].z);
+        o[r].w = fmaf(pi, vv[i].w, o[r].w);
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const float sum = warp_sum(l[r]) * (kKeys / 32.f);  // (32 / kKeys lanes have counted each key)
+    if (kPer == 2) {
+      o[r].x += __shfl_xor_sync(0xffffffffu, o[r].x, 16);
+      o[r].y += __shfl_xor_sync(0xffffffffu, o[r].y, 16);
+      o[r].z += __shfl_xor_sync(0xffffffffu, o[r].z, 16);
+      o[r].w += __shfl_xor_sync(0xffffffffu, o[r].w, 16);
+    }
+    if (sub == 0) store4(&sh_o[warp][r][c], o[r]);
+    if (lane == 0) {
+      sh_m[warp][r] = m[r];
+      sh_l[warp][r] = sum;
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n_rows * kLanes; i += kFewThreads) {
+    const int r = i / kLanes, cc = i % kLanes * 4;
+    float top = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < kFewWarps; ++x) top = fmaxf(top, sh_m[x][r]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int x = 0; x < kFewWarps; ++x) {
+      const float wgt = exp2f(sh_m[x][r] - base);
+      const float4 y = *reinterpret_cast<const float4*>(&sh_o[x][r][cc]);
+      sum += wgt * sh_l[x][r];
+      v.x = fmaf(wgt, y.x, v.x);
+      v.y = fmaf(wgt, y.y, v.y);
+      v.z = fmaf(wgt, y.z, v.z);
+      v.w = fmaf(wgt, y.w, v.w);
+    }
+    const bool none = sum == 0.f;
+    const float inv = none ? 0.f : 1.f / sum;
+    const float lse2 = none ? -INFINITY : top + log2f(sum);
+    v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+    const int tok = (r0 + r) / a.group;
+    const int64_t token = pr.t0 + tok;
+    const int hq = w.head * a.group + (r0 + r) - tok * a.group;
+    if (direct) {
+      store4(static_cast<float*>(a.out) + token * a.out_stride + (int64_t)hq * D + cc, v);
+      if (a.lse && cc == 0) a.lse[token * a.heads * a.group + hq] = lse2 * 0.6931471805599453f;
+    } else {
+      const int64_t at = ((int64_t)(part.slot0 + w.split) * a.q_rows + token) * a.heads * a.group + hq;
+      store4(a.part_out + at * D + cc, v);
+      if (cc == 0) a.part_lse[at] = lse2;
+    }
+  }
+}
+
+template <int FMT, int D, int R>
+cudaError_t launch_few(const AttendView& a, int part, cudaStream_t stream) {
+  attend_few_kernel<FMT, D, R><<<(unsigned)part_blocks(a, a.part[part]), kFewThreads, 0, stream>>>(a, part);
+  return cudaGetLastError();
+}
 template <int FMT, int D, int BM>
 cudaError_t launch(const AttendView& a, int part, cudaStream_t stream) {
   constexpr int smem = (int)sizeof(Smem<D, BM>);
@@ -244,20 +410,29 @@ cudaError_t launch(const AttendView& a, int part, cudaStream_t stream) {
   attend_fma_kernel<FMT, D, BM><<<(unsigned)part_blocks(a, a.part[part]), kThreads, smem, stream>>>(a, part);
   return cudaGetLastError();
 }
-template <int FMT>
+template <int FMT, int D>
 cudaError_t launch_shape(const AttendView& a, int part, int tile, cudaStream_t stream) {
-  if (a.dim == 128) return tile == 16 ? launch<FMT, 128, 16>(a, part, stream) : launch<FMT, 128, 64>(a, part, stream);
-  return tile == 16 ? launch<FMT, 64, 16>(a, part, stream) : launch<FMT, 64, 64>(a, part, stream);
+  switch (tile) {
+    case 1: return launch_few<FMT, D, 1>(a, part, stream);
+    case 2: return launch_few<FMT, D, 2>(a, part, stream);
+    case 4: return launch_few<FMT, D, 4>(a, part, stream);
+    case 16: return launch<FMT, D, 16>(a, part, stream);
+    default: return launch<FMT, D, 64>(a, part, stream);
+  }
 }
 
 }  // namespace
 
-// Rows of a tile for `problems` problems of up to `rows` rows: 64, whose products are bound by the FMA pipe, where that
-// makes blocks enough to fill the device, else 16 (131 query tokens, 515 keys, 16 heads of two sequences: 22.8 -> 8.8 us).
-int attend_fma_row_tile(int64_t rows, int64_t problems) { return (rows + 63) / 64 * problems < 2 * sm_count() ? 16 : 64; }
+// Rows of a tile for `problems` problems of up to `rows` rows: 1, 2 or 4 in the kernel for few; else 64, whose products are
+// bound by shared memory, where that makes blocks enough to fill the device, or 16.
+int attend_fma_row_tile(int64_t rows, int64_t problems) {
+  if (rows <= 4) return rows <= 2 ? (int)rows : 4;
+  return (rows + 63) / 64 * problems < 2 * sm_count() ? 16 : 64;
+}
 
 cudaError_t launch_attend_fma(const AttendView& a, int part, int tile, int format, cudaStream_t stream) {
-  return format == H2O_F32 ? launch_shape<H2O_F32>(a, part, tile, stream) : launch_shape<H2O_KV8>(a, part, tile, stream);
+  if (format == H2O_F32) return a.dim == 128 ? launch_shape<H2O_F32, 128>(a, part, tile, stream) : launch_shape<H2O_F32, 64>(a, part, tile, stream);
+  return a.dim == 128 ? launch_shape<H2O_KV8, 128>(a, part, tile, stream) : launch_shape<H2O_KV8, 64>(a, part, tile, stream);
 }
 
 }  // namespace h2o
