@@ -402,19 +402,20 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const int kv = (warp - 12) >> 2, t = threadIdx.x - 384 - 128 * kv;
       const int64_t base = (int64_t)w.head * a.rows + pr.row0;
       const uint8_t* scales = kv ? a.v_scale : a.k_scale;
-      uint32_t byte = 127;  // of the next tile, one row to a thread
+      // of the next two tiles, one row to a thread: behind the tiles' traffic a load takes longer than a tile
       auto fetch = [&](int j) {
         const int key = key0 + j * kN + t;
-        if (t < kN && key < key1) byte = scales[base + key];
+        return t < kN && key < key1 ? (uint32_t)scales[base + key] : 127u;
       };
-      if (nt > 0) fetch(0);
+      uint32_t byte = fetch(0), byte_next = fetch(1);
       int slot = 0;
       uint32_t phase = 1;
       bool raw_there = false, slot_free = false;
       for (int j = 0; j < nt; ++j) {
         const int rs = j % kRawStages;
         if (t < kN) sh.scale[j & 1][kv][t] = __float2half_rn(kv8_scale(byte));
-        if (j + 1 < nt) fetch(j + 1);
+        byte = byte_next;
+        byte_next = fetch(j + 2);
         bool ok = raw_there || wait_or_abort(&sh.raw_full[rs], (uint32_t)(j / kRawStages) & 1u, abort_flag);
         ok = ok && (slot_free || wait_or_abort(&sh.kv_empty[slot], phase, abort_flag));
         ok = together(ok, kv);  // (also publishes the scales; one answer for the four warps, so that none waits for another)
@@ -682,10 +683,14 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           if (!write) continue;
           // (a weight of 0 belongs to an O that was never written)
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            float x = mine_w == 0.f ? 0.f : mine_w * __uint_as_float(o[e]);
-            if (alt) x = fmaf(their_w, theirs[cc * 32 + e], x);
-            o[e] = __float_as_uint(x * inv);
+          for (int e = 0; e < 32; e += 4) {
+            const float4 y = alt ? *reinterpret_cast<const float4*>(theirs + cc * 32 + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+            const float ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+              const float x = mine_w == 0.f ? 0.f : mine_w * __uint_as_float(o[e + b]);
+              o[e + b] = __float_as_uint((alt ? fmaf(their_w, ys[b], x) : x) * inv);
+            }
           }
           if constexpr (FINISH) {  // part 0's chunks
             auto add = [&](int e, float wgt, const float4& v) {

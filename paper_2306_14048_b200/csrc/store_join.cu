@@ -13,8 +13,6 @@ constexpr int kMaxSlots = 2 * kMaxSplits;  // two parts
 
 template <typename T, int D>
 __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant__ AttendView a) {
-  // (launched while the kernels that leave the chunks may still run)
-  wait_for_earlier();
   constexpr int kPer = D / 32;
   const int seq = blockIdx.y;
   const int lane = threadIdx.x & 31;
@@ -23,20 +21,24 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
   const int64_t t0 = first_token(a, seq);
   const int nt = (int)clamp64(first_token(a, seq + 1) - t0, 0, a.max_q);
   const int i = (int)(item / hq_all), hq = (int)(item - (int64_t)i * hq_all);
-  if (i >= nt) return;
+  bool live = i < nt;
   const int64_t token = t0 + i;
   // chunks of this row: for each part, the first and how many were written
   int slot[2] = {0, 0}, used[2] = {0, 0};
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    if (k >= a.n_parts) break;
+    if (k >= a.n_parts || !live) break;
     const AttendPart& p = a.part[k];
     const int which = p.grouped ? group_of(a, seq) : seq;
     const Problem pr = locate(a, p, which);
-    if (token < pr.t0 || token >= pr.t0 + pr.nt) return;  // beyond what the caller allowed for: left as it was
+    if (token < pr.t0 || token >= pr.t0 + pr.nt) live = false;  // beyond what the caller allowed for: left as it was
     slot[k] = p.slot0;
     used[k] = (pr.len + p.chunk - 1) / p.chunk;
   }
+  // (Launched while the kernels that leave the chunks may still run: what does not depend on them is looked up before.  All
+  // wait, so that this kernel never ends before them.)
+  wait_for_earlier();
+  if (!live) return;
   const int n = used[0] + used[1];
   const int64_t pitch = a.q_rows * hq_all, at = token * hq_all + hq;
   auto place = [&](int s) { return (int64_t)(s < used[0] ? slot[0] + s : slot[1] + s - used[0]) * pitch + at; };
