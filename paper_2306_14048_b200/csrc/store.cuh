@@ -168,7 +168,7 @@ cudaError_t launch_store_write(const h2o_store_config_t& c, const void* k, const
                                int64_t n, const int64_t* rows, int64_t first_row, cudaStream_t stream);
 cudaError_t launch_store_read(const h2o_store_config_t& c, void* k, void* v, int dtype, int64_t stride, int64_t n,
                               const int64_t* rows, int64_t first_row, cudaStream_t stream);
-int attend_fma_row_tile(int64_t rows, int64_t problems);
+int attend_fma_row_tile(int64_t rows);
 cudaError_t launch_attend_fma(const AttendView& a, int part, int tile, int format, cudaStream_t stream);
 constexpr int kFewBoxRows = 32;  // rows of a box of the store's tensor maps
 bool make_store_map(CUtensorMap_st* map, const h2o_store_config_t& c, const void* base, int box_rows);

@@ -187,7 +187,7 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
     const int64_t rows = std::min<int64_t>((p.grouped ? (int64_t)a.max_group * a.max_q : a.max_q), a.q_rows) * a.group;
     if (q->dtype == H2O_F32) {
       pl.kernel[n] = Kernel::Fma;
-      pl.tile[n] = h2o::attend_fma_row_tile(rows, (int64_t)a.heads * p.problems);
+      pl.tile[n] = h2o::attend_fma_row_tile(rows);
     } else if (rows <= few_rows(c.format)) {
       pl.kernel[n] = Kernel::Mma;
       pl.tile[n] = h2o::attend_mma_row_tile(rows);
