@@ -51,6 +51,7 @@ struct AttendView {
   // results, joined with what part 0 left; otherwise every part leaves its chunks for the joining kernel, or there is one
   // unsplit part that writes the results.
   int early, finish;
+  int walk;  // 1: part 1's blocks take the prefix as well, and nothing else is launched (few rows of the mma.sync kernel)
   int32_t* status;
   int n_parts;
   AttendPart part[2];
@@ -174,7 +175,7 @@ constexpr int kFewBoxRows = 32;  // rows of a box of the store's tensor maps
 bool make_store_map(CUtensorMap_st* map, const h2o_store_config_t& c, const void* base, int box_rows);
 int attend_mma_row_tile(int64_t rows);
 int attend_mma_blocks_per_sm(int format, int tile);
-// part `first`, or (both) parts 0 and 1 in one launch
+// part `first`, or (both) parts 0 and 1 in one launch, or (a.walk) part 1 with the prefix
 cudaError_t launch_attend_mma(const AttendView& a, int first, bool both, const int* tile, int format, const void* map_k,
                               const void* map_v, cudaStream_t stream);
 int attend_tc_box_rows(int format, int dim, int groups);

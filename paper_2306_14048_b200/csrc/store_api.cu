@@ -113,10 +113,16 @@ struct Plan {
 // and 37 / 37.  8-bit, 8 heads of 128, 32 query rows 26 / 28; 32 heads 61 / 73.
 int few_rows(int format) { return format == H2O_KV8 ? 32 : 16; }
 
-#ifndef SHORTK
-#define SHORTK 512
-#endif
-constexpr int kShortKeys = SHORTK;
+// Up to this many keys in a range the tcgen05 kernel takes 128 rows to a block, two blocks to an SM, so that one's start
+// and end run beside the other's tiles (bfloat16; the 8-bit kernel's shared memory holds one).  Own rows of 64 prompts of up
+// to 200 tokens behind a shared prefix: 117 -> 89 us; beside it, 515 keys for 32 heads of 131 tokens: 100 -> 108.
+constexpr int kShortKeys = 512;
+
+// Prefix and own rows together up to this many keys: each sequence's blocks read the prefix again (from the second-level
+// cache) rather than leave chunks for a joining kernel.  Device time of a call, joined / walked, prefix 300, up to 60 own
+// rows, 4 sequences, 8 heads of 128: 7.8 / 6.2 us, 8-bit 8.5 / 8.2; 660 keys: 6.6 / 7.4; and a launch less, 15 / 12 us a call.
+// Up to two blocks to an SM: prefix 400, 16 heads, 16 sequences: 11.7 / 8.4; 32 sequences, 8-bit: 16.4 / 17.7.
+constexpr int kWalkKeys = 512;
 
 // Splits the keys of a part: `units` blocks per split, `room` blocks that run at once.  Costs in keys of one block: a block
 // costs its keys and `fixed` more (start, merge, its result's trip through memory), the joining kernel twice as much;
@@ -209,6 +215,14 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
     ++n;
   }
   a.n_parts = n;
+  if (n == 2 && pl.kernel[0] == Kernel::Mma && pl.kernel[1] == Kernel::Mma && pl.tile[1] == 8 &&
+      (int64_t)a.part[0].max_length + a.part[1].max_length <= kWalkKeys &&
+      (int64_t)a.part[1].problems * a.part[1].row_tiles * a.heads <= 2 * h2o::sm_count()) {
+    a.walk = 1;
+    a.part[1].splits = 1;
+    a.part[1].chunk = std::max(1, a.part[1].max_length);
+    return pl;
+  }
   // The second part's kernel, where it is one of its own, starts before the first one's has ended: neither needs the
   // other's results until the end.  Prompts' own rows, unsplit, then join what the first part left themselves (32 prompts
   // of up to 200 tokens: 415 -> 348 us); single tokens' blocks are many and short, and leave that to the joining kernel.
@@ -235,8 +249,8 @@ int run_plan(const h2o_store_t* store, const h2o_queries_t* q, Plan& pl, void* s
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   const int format = store->cfg.format;
-  const bool both = pl.a.n_parts == 2 && pl.kernel[0] == Kernel::Mma && pl.kernel[1] == Kernel::Mma;
-  for (int k = 0; k < (both ? 1 : pl.a.n_parts) && e == cudaSuccess; ++k) {
+  const bool both = pl.a.n_parts == 2 && !pl.a.walk && pl.kernel[0] == Kernel::Mma && pl.kernel[1] == Kernel::Mma;
+  for (int k = 0; k < (both || pl.a.walk ? 1 : pl.a.n_parts) && e == cudaSuccess; ++k) {
     if (pl.kernel[k] == Kernel::Fma) e = h2o::launch_attend_fma(pl.a, k, pl.tile[k], format, st);
     else if (pl.kernel[k] == Kernel::Tc2) e = h2o::launch_attend_tc(pl.a, k, 2, format, store->two_k, store->two_v, st);
     else if (pl.kernel[k] == Kernel::Tc1) e = h2o::launch_attend_tc(pl.a, k, 1, format, store->one_k, store->one_v, st);

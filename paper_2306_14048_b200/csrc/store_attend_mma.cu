@@ -124,8 +124,9 @@ __device__ __forceinline__ uint32_t chunk_addr(uint32_t tile, int r, int c) {
   else return tile + (c >> 3) * (kKeys * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
 }
 
-// NTB: the kernel's larger number of n-tiles, which the ring is made for.
-template <int FMT, int D, int NT, int NTB>
+// NTB: the kernel's larger number of n-tiles, which the ring is made for.  WALK: the block takes its sequence's prefix
+// (part 0's range) and then its own rows, and writes the result: no chunks, no joining kernel.
+template <int FMT, int D, int NT, int NTB, bool WALK>
 __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* map_k, const CUtensorMap* map_v,
                                        const AttendPart& part, unsigned block, unsigned char* ring, Shared& sh) {
   constexpr bool kF16 = FMT == H2O_KV8;
@@ -145,13 +146,18 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   const int key1 = min(last_seen, key0 + part.chunk);
   const int first_seen = part.causal ? seen_rows(part, pr, r0 / a.group) : last_seen;
 
-  // ---- this warp's tiles: key0 + 32 (warp + 4 j) ----
-  const int n_tiles = max(0, (key1 - key0 + kKeys - 1) / kKeys);
+  [[maybe_unused]] Problem prefix{0, 0, 0, 0};
+  if constexpr (WALK) prefix = locate(a, a.part[0], group_of(a, w.problem));
+  const int pre = WALK ? prefix.len : 0, pre_tiles = (pre + kKeys - 1) / kKeys;
+
+  // ---- this warp's tiles: warp + 4 j of the prefix's and then the chunk's ----
+  const int n_tiles = pre_tiles + max(0, (key1 - key0 + kKeys - 1) / kKeys);
   const int mine = n_tiles > warp ? (n_tiles - warp + kWarps - 1) / kWarps : 0;
   unsigned char* my_ring = ring + warp * (kSlots * kTile);
   uint64_t* full = sh.full[warp];
   auto issue = [&](int i) {  // item i: K of tile i / 2, then its V; lane 0 only
-    const int row = (int)pr.row0 + key0 + (warp + kWarps * (i >> 1)) * kKeys;
+    const int t = warp + kWarps * (i >> 1);
+    const int row = WALK && t < pre_tiles ? (int)prefix.row0 + t * kKeys : (int)pr.row0 + key0 + (t - pre_tiles) * kKeys;
     mbar_expect_tx(&full[i % kSlots], kTile);
     tma_4d(my_ring + (i % kSlots) * kTile, (i & 1) ? map_v : map_k, row, w.head, &full[i % kSlots]);
   };
@@ -238,9 +244,11 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   // 8-bit rows: the scale bytes of the warp's next tile, one key per lane
   uint32_t scale_k = 127, scale_v = 127;
   auto fetch_scales = [&](int j) {
-    const int key = key0 + (warp + kWarps * j) * kKeys + lane;
-    if (key < key1) {
-      const int64_t at = (int64_t)w.head * a.rows + pr.row0 + key;
+    const int t = warp + kWarps * j;
+    const bool in_prefix = WALK && t < pre_tiles;
+    const int key = (in_prefix ? t : t - pre_tiles) * kKeys + (in_prefix ? 0 : key0) + lane;
+    if (key < (in_prefix ? pre : key1)) {
+      const int64_t at = (int64_t)w.head * a.rows + (in_prefix ? prefix.row0 : pr.row0) + key;
       scale_k = a.k_scale[at];
       scale_v = a.v_scale[at];
     }
@@ -250,8 +258,10 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   }
 
   for (int j = 0; j < mine; ++j) {
-    const int tile_key = key0 + (warp + kWarps * j) * kKeys;
-    const int there = min(kKeys, key1 - tile_key);
+    const int tile_no = warp + kWarps * j;
+    const bool in_prefix = WALK && tile_no < pre_tiles;
+    const int tile_key = in_prefix ? tile_no * kKeys : key0 + (tile_no - pre_tiles) * kKeys, end = in_prefix ? pre : key1;
+    const int there = min(kKeys, end - tile_key);
     if constexpr (kF16) {
       sh.k_factor[warp][lane] = kv8_scale(scale_k);
       sh.v_factor[warp][lane] = __float2half_rn(kv8_scale(scale_v));
@@ -323,7 +333,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
       if (lane == 0 && i + kSlots < 2 * mine) issue(i + kSlots);
     }
     // ---- logits (base 2); lane: keys gl, gl + 8 (+ 16 mt), rows 2 c4, 2 c4 + 1 (+ 8 nt) ----
-    const bool masked = tile_key + kKeys > min(first_seen, key1);
+    const bool masked = tile_key + kKeys > (in_prefix ? pre : min(first_seen, key1));
     bool grows = false;
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
@@ -341,7 +351,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
           x *= factor[nt][e & 1];
           if (masked) {
             const int key = tile_key + mt * 16 + gl + 8 * (e >> 1);
-            if (key >= min(seen[nt][e & 1], key1)) x = -INFINITY;
+            if (key >= (in_prefix ? pre : min(seen[nt][e & 1], key1))) x = -INFINITY;
           }
           s[mt][nt][e] = x;
           grows |= x > m[nt][e & 1] + kRescale;
@@ -396,8 +406,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
       if (!wait(&full[slot], (uint32_t)(i / kSlots) & 1u)) timed_out = true;
       const uint32_t tile = smem_u32(my_ring + slot * kTile);
       if (there < kKeys) {
-        // rows behind the range may hold anything, and 0 * NaN must not reach the sums (a chunk's last tile only:
-        // nothing is loaded over it afterwards)
+        // rows behind the range may hold anything, and 0 * NaN must not reach the sums
         for (int x = lane; x < (kKeys - there) * (row_bytes(FMT, D) / 16); x += 32) {
           const uint32_t at = chunk_addr<FMT, D>(tile, there + x / (row_bytes(FMT, D) / 16), x % (row_bytes(FMT, D) / 16));
           asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(at), "r"(0) : "memory");
@@ -444,6 +453,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
           }
         }
       }
+      if (WALK && there < kKeys) fence_proxy_async();  // (the zeros come before the copy that may go over them)
       __syncwarp();
       if (lane == 0 && i + kSlots < 2 * mine) issue(i + kSlots);
     }
@@ -478,6 +488,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
     const int tok = (r0 + r) / a.group;
     const int64_t token = pr.t0 + tok;
     const int hq = w.head * a.group + (r0 + r) - tok * a.group;
+    if (WALK && (token < prefix.t0 || token >= prefix.t0 + prefix.nt)) continue;  // beyond what the caller allowed for
     float top = -INFINITY;
 #pragma unroll
     for (int x = 0; x < kWarps; ++x) top = fmaxf(top, sh.m[x][r]);
@@ -513,7 +524,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
 
 // One launch for part `first` alone, with 8 NT0 rows to a block, or for parts 0 and 1 (a shared prefix: many rows and
 // few), with 8 NT0 and 8 NT1.
-template <int FMT, int D, int NT0, int NT1>
+template <int FMT, int D, int NT0, int NT1, bool WALK>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(FMT, NT0))
 attend_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                   const __grid_constant__ AttendView a, int first, unsigned blocks0) {
@@ -523,29 +534,30 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   let_next_start();  // (the joining kernel waits for this one's end; others are launched to start after it)
   if (NT0 == NT1 || blockIdx.x < blocks0) {
     const bool second = blockIdx.x >= blocks0;
-    attend<FMT, D, NT0, NT0>(a, &map_k, &map_v, a.part[second ? 1 : first], blockIdx.x - (second ? blocks0 : 0), ring, sh);
+    attend<FMT, D, NT0, NT0, WALK>(a, &map_k, &map_v, a.part[second ? 1 : first], blockIdx.x - (second ? blocks0 : 0), ring, sh);
   } else {
-    attend<FMT, D, NT1, NT0>(a, &map_k, &map_v, a.part[1], blockIdx.x - blocks0, ring, sh);
+    attend<FMT, D, NT1, NT0, false>(a, &map_k, &map_v, a.part[1], blockIdx.x - blocks0, ring, sh);
   }
   // a launch that started early does not end before the one in front of it, whatever its blocks have to do
   if (a.early && blockIdx.x == 0) wait_for_earlier();
 }
 
-template <int FMT, int D, int NT0, int NT1>
+template <int FMT, int D, int NT0, int NT1, bool WALK = false>
 cudaError_t launch(const AttendView& a, int first, bool both, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t stream) {
   constexpr int smem = kWarps * ring_slots(FMT, D, NT0) * tile_bytes(FMT, D) + 1024;
   static unsigned long long flags = 0;
-  const void* f = reinterpret_cast<const void*>(attend_mma_kernel<FMT, D, NT0, NT1>);
+  const void* f = reinterpret_cast<const void*>(attend_mma_kernel<FMT, D, NT0, NT1, WALK>);
   const cudaError_t e = ensure_dynamic_smem(f, smem, &flags);
   if (e != cudaSuccess) return e;
   const int64_t b0 = part_blocks(a, a.part[first]), b1 = both ? part_blocks(a, a.part[1]) : 0;
-  return launch_kernel(attend_mma_kernel<FMT, D, NT0, NT1>, dim3((unsigned)(b0 + b1)), kThreads, smem, stream, a.early != 0, map_k, map_v, a,
+  return launch_kernel(attend_mma_kernel<FMT, D, NT0, NT1, WALK>, dim3((unsigned)(b0 + b1)), kThreads, smem, stream, a.early != 0, map_k, map_v, a,
                        first, (unsigned)b0);
 }
 
 template <int FMT, int D>
 cudaError_t launch_rows(const AttendView& a, int first, bool both, const int* tile, const CUtensorMap& map_k, const CUtensorMap& map_v,
                         cudaStream_t st) {
+  if (a.walk) return launch<FMT, D, 1, 1, true>(a, 1, false, map_k, map_v, st);
   const int t0 = tile[first], t1 = both ? tile[1] : t0;
   if (t0 == 8) return launch<FMT, D, 1, 1>(a, first, both, map_k, map_v, st);
   if (t0 == 16) return t1 == 8 ? launch<FMT, D, 2, 1>(a, first, both, map_k, map_v, st) : launch<FMT, D, 2, 2>(a, first, both, map_k, map_v, st);
