@@ -10,14 +10,16 @@
 //   O_g   += P_g(j) V_j    P is the tensor-memory operand, V the MN-major shared-memory operand
 // The tile size is what tensor memory holds of O (2 x 128 columns), S (2 x 80) and P (2 x 40).  With S and P in one place
 // and tiles of 128 keys the chain S - exponentials - P V of a group is serial: 3700 cycles per tile of both groups for
-// 2048 of tensor work.  Measured (4 x 2048 queries against 4096 keys, 32 heads): 593 us that way, 505 us this way (1090
-// TFLOP/s); tiles of 64 keys with S prefetched into registers and P in two buffers 650 us; two threads to a row 725 us.
-// Roles: warp 0 TMA, warps 1 and 2 issue S of A and B (they also clear what lies behind the range in
-// its last V tile: 0 * NaN must not reach the sums), warp 3 issues P V of both and owns tensor memory, warps 4..7 and 8..11 the softmax of A and
-// B, one thread per row; with 8-bit rows warps 12..15 and 16..19 turn code tiles of K and of V into f16 tiles.  A wait on a barrier costs 300 to
-// 400 cycles here even when it is complete (it queues behind the exponentials), so the issuers have few: K and V of a tile
-// arrive on one barrier, and P V waits for P alone, which comes after S and so after the tile.  Their loops run on
-// values the compiler knows to be uniform (constant tensor-memory addresses, counts from a shuffle): 575 -> 550 us.
+// 2048 of tensor work.  4 x 2048 queries against 4096 keys, 32 heads: 593 us that way, 505 us this way when it was
+// first built, 469 us now (1170 TFLOP/s; 540 us, 1020 TFLOP/s, once the power limit has lowered the clock).  Tiles of 64 keys
+// with S prefetched into registers and P in two buffers took 650 us, two threads to a row 725 us.
+// Roles: warp 0 TMA; warps 1 and 2 issue S of A and B (they also clear what lies behind the range in its last V tile:
+// 0 * NaN must not reach the sums); warp 3 issues P V of both and owns tensor memory; warps 4..7 and 8..11 are the softmax
+// of A and B, one thread per row; with 8-bit rows warps 12..15 and 16..19 turn code tiles of K and of V into f16 tiles.
+// A wait on a barrier costs 300 to 400 cycles here even when it is complete (it queues behind the exponentials), so the
+// issuers have few: K and V of a tile arrive on one barrier, and P V waits for P alone, which comes after S and so after
+// the tile.  Their loops run on values the compiler knows to be uniform (constant tensor-memory addresses, counts from a
+// shuffle): 575 -> 550 us.
 // The reference m of a row is the maximum of its first tile.  Later tiles compute their exponentials against it without
 // looking for a maximum: only when a tile's sum comes out large (kLargeSum) the tile is done again with the new
 // maximum and O is rescaled.  A value far above the reference costs no precision in floating point, only range.
@@ -58,9 +60,9 @@ __host__ __device__ constexpr int smem_bytes(int fmt, int d, int g) {
 // 256 x 144 + 384 x 64; bfloat16: 384 start with 168 = 256 x 216 + 128 x 72; one group: 256 with 128 = 128 x 176 + 128 x 80.
 __host__ __device__ constexpr int regs_softmax(int fmt, int g) { return fmt == H2O_KV8 ? 144 : g == 1 ? 176 : 216; }
 __host__ __device__ constexpr int regs_other(int fmt, int g) { return fmt == H2O_KV8 ? 64 : g == 1 ? 80 : 72; }
-// Every kPolyEvery-th pair of exponentials runs on the FMA pipe.  4 x 2048 queries against 4096 keys, 32 heads: none 550,
-// one in eight 518, one in four 505, one in three 547, one in two 535 us.
-constexpr int kPolyEvery = 4;
+// Every kPolyEvery-th pair of exponentials runs on the FMA pipe.  4 x 2048 queries against 4096 keys, 32 heads: none 482,
+// one in sixteen 484, one in eight 469, one in four 490 us (before the power limit lowers the clock).
+constexpr int kPolyEvery = 8;
 
 struct Shared {
   uint64_t q_full[2];
@@ -95,10 +97,17 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 // exp2 of two values on the FMA pipe: nearest integer by the 1.5 * 2^23 trick, degree-5 polynomial of 2^f on
-// [-0.5, 0.5] (1.8e-7 relative, as good as ex2.approx), exponent added with integer arithmetic.  Below -126: ~1e-38.
+// [-0.5, 0.5] (1.8e-7 relative, as good as ex2.approx), times 2^n put together with integer arithmetic.  Below -126:
+// ~1e-38; NaN stays NaN; above kPolyMax the result means nothing.
+constexpr float kPolyMax = 100.f;
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ float2 ex2_fma2(float2 x) {
-  x.x = fmaxf(x.x, -126.f);
-  x.y = fmaxf(x.y, -126.f);
+  x.x = max_or_nan(x.x, -126.f);
+  x.y = max_or_nan(x.y, -126.f);
   const float2 t = __fadd2_rn(x, make_float2(12582912.f, 12582912.f));
   const float2 n = __fadd2_rn(t, make_float2(-12582912.f, -12582912.f));
   const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
@@ -108,8 +117,8 @@ __device__ __forceinline__ float2 ex2_fma2(float2 x) {
   p = __ffma2_rn(p, f, make_float2(0.24022118747234344f, 0.24022118747234344f));
   p = __ffma2_rn(p, f, make_float2(0.6931470036506653f, 0.6931470036506653f));
   p = __ffma2_rn(p, f, make_float2(1.0000001192092896f, 1.0000001192092896f));
-  return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)),
-                     __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+  return __fmul2_rn(p, make_float2(__uint_as_float((__float_as_uint(t.x) << 23) + 0x3f800000u),
+                                   __uint_as_float((__float_as_uint(t.y) << 23) + 0x3f800000u)));
 }
 
 constexpr float kRescale = 8.f;
@@ -548,14 +557,18 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         auto exponentials = [&](auto from, auto to) {
           const float neg = m == -INFINITY ? 0.f : -m;
           float2 sum = make_float2(0.f, 0.f);
+          float top = -INFINITY;  // of the exponents ex2_fma2 gets
 #pragma unroll
           for (int e = decltype(from)::value; e < decltype(to)::value; ++e) {
             const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])),
                                         make_float2(factor, factor), make_float2(neg, neg));
-            const float2 y = e % kPolyEvery == kPolyEvery - 1 ? ex2_fma2(x) : make_float2(ex2(x.x), ex2(x.y));
+            const bool poly = e % kPolyEvery == kPolyEvery - 1;
+            if (poly) top = max3(top, x.x, x.y);
+            const float2 y = poly ? ex2_fma2(x) : make_float2(ex2(x.x), ex2(x.y));
             sum = __fadd2_rn(sum, y);
             p[e] = kF16 ? pack_half2(y.x, y.y) : Vec16<__nv_bfloat16>::pack2(y.x, y.y);
           }
+          if (top > kPolyMax) sum.x = INFINITY;
           return sum;
         };
         float2 sum = exponentials(N0{}, N1{});

@@ -534,3 +534,201 @@ def test_decoder_layer_with_cache_store_and_prefix(pkg):
             want = ref.attend(nq[b:b + 1].double().numpy(), np.concatenate([k64[p0:p0 + p1], mine[b][0]]),
                               np.concatenate([v64[p0:p0 + p1], mine[b][1]]), [p1 + step + 1], scale, "kv8", "bf16")
             ref.compare(o[b:b + 1], want[0], want[2], "sample")
+
+
+# (query tokens of the sequences, their own rows, sequences of the groups, their prefixes), by how they are worked on:
+# few rows and keys in one launch; few rows in chunks; many rows of a group and few of a sequence; many of both, with the
+# prefix in one piece and in several
+SHAPES = [
+    ([2, 4, 0, 3], [2, 70, 9, 33], [2, 2], [33, 440]),
+    ([1, 3, 2, 4], [1, 64, 2, 300], [2, 2], [2100, 31]),
+    ([1] * 40, list(range(40)), [25, 15], [1500, 700]),
+    ([40, 17, 64, 33], [40, 20, 200, 33], [3, 1], [96, 65]),
+    ([60, 130, 33], [200, 130, 40], [3], [5000]),
+]
+
+
+def _prefix_case(pkg, fmt, q_dtype, dim, shape, seed, group=2, heads=1):
+    """Tensors of such a call, with `call` and `check`; the sequences' own ranges and the prefixes may be changed."""
+    q_len, own, members, pre = shape
+    begin, rows = _layout(pre + own, seed + 1)
+    k, v = (_rows(seed + s, rows, heads, dim, DT.get(fmt, torch.bfloat16)) for s in (2, 3))
+    store, k64, v64 = _make(pkg, fmt, k, v)
+    cu, cg = (np.concatenate([[0], np.cumsum(x)]).tolist() for x in (q_len, members))
+    hq = heads * group
+    r = dict(q=(torch.randn((cu[-1] + 1, hq, dim), generator=_gen(seed + 4)) * 1.5).to(DT[q_dtype]).cuda(), store=store,
+             pb=_i64(begin[:len(pre)]), pl=_i32(pre), ob=_i64(begin[len(pre):]), ol=_i32(own), cu=_i32(cu), cg=_i32(cg))
+    r["out"], r["lse"] = torch.full_like(r["q"], 5.0), torch.full((cu[-1] + 1, hq), 5.0, dtype=torch.float32, device="cuda")
+
+    def call(stream=None, **kw):
+        most = dict(max_prefix=max(pre), max_own=max(own), max_q=max(q_len), max_group=max(members))
+        most.update(kw)
+        store.prefix_attend(r["q"], r["pb"], r["pl"], r["ob"], r["ol"], r["out"], cu_group=r["cg"], cu_q=r["cu"], lse=r["lse"],
+                            stream=stream, **most)
+
+    def check(untouched=()):
+        assert store.status() == 0
+        pb, pl, ob, ol = (r[x].tolist() for x in ("pb", "pl", "ob", "ol"))
+        which = np.repeat(np.arange(len(members)), members)
+        for b, n in enumerate(q_len):
+            sl, g = slice(cu[b], cu[b] + n), which[b]
+            if b in untouched:
+                assert (r["out"][sl] == 5.0).all() and (r["lse"][sl] == 5.0).all()
+                continue
+            kk, vv = (np.concatenate([x[pb[g]:pb[g] + pl[g]], x[ob[b]:ob[b] + ol[b]]]) for x in (k64, v64))
+            seen = [pl[g] + max(0, ol[b] - (n - 1 - i)) for i in range(n)]
+            want = ref.attend(r["q"][sl].double().cpu().numpy(), kk, vv, seen, float(np.float32(1 / math.sqrt(dim))), fmt, q_dtype)
+            ref.compare(r["out"][sl], want[0], want[2], "out of sequence %d" % b)
+            ref.compare(r["lse"][sl], want[1], want[3], "lse of sequence %d" % b)
+        assert (r["out"][cu[-1]:] == 5.0).all() and (r["lse"][cu[-1]:] == 5.0).all()
+
+    return r, call, check
+
+
+@pytest.mark.parametrize("fmt,q_dtype", FORMATS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_prefix_shapes(pkg, fmt, q_dtype, dim, shape):
+    _, call, check = _prefix_case(pkg, fmt, q_dtype, dim, SHAPES[shape], 30 + shape, heads=2)
+    call()
+    check()
+
+
+@pytest.mark.parametrize("fmt,q_dtype", FORMATS)
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_prefix_graphs_replayed_at_once(pkg, fmt, q_dtype, shape):
+    """Two captured calls on two streams at the same time, and eager ones on a third, with other ranges than captured."""
+    runs = []
+    for i in range(2):
+        r, call, check = _prefix_case(pkg, fmt, q_dtype, 128, SHAPES[shape], 50 + i)
+        r["stream"], graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        r["stream"].wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(r["stream"]):
+            call()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=r["stream"]):
+            call()
+        runs.append((r, graph, check))
+    third = torch.cuda.Stream()
+    e, eager, check_eager = _prefix_case(pkg, fmt, q_dtype, 128, SHAPES[shape], 70)
+    for i, (r, _, _) in enumerate(runs):
+        r["pl"].sub_(torch.tensor([7 + 20 * i] + [i] * (len(r["pl"]) - 1), device="cuda", dtype=torch.int32))
+        r["ol"].sub_(1 + i).clamp_(min=0)
+        r["out"].fill_(5.0), r["lse"].fill_(5.0)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for r, graph, _ in runs:
+            with torch.cuda.stream(r["stream"]):
+                graph.replay()
+        eager(stream=third)
+    torch.cuda.synchronize()
+    for _, _, check in runs:
+        check()
+    check_eager()
+
+
+@pytest.mark.parametrize("fmt,q_dtype", FORMATS)
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_prefix_ranges_may_be_the_same(pkg, fmt, q_dtype, shape):
+    """All sequences with one own range, which lies in the prefix, and all groups with one prefix."""
+    r, call, check = _prefix_case(pkg, fmt, q_dtype, 64, SHAPES[shape], 90)
+    r["pb"].fill_(0), r["pl"].fill_(31)
+    r["ob"].fill_(5), r["ol"].copy_(r["ol"].clamp(max=25))
+    call()
+    check()
+
+
+@pytest.mark.parametrize("fmt,q_dtype", FORMATS)
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_prefix_beyond_what_the_call_allows_for(pkg, fmt, q_dtype, shape):
+    """Longer ranges are cut, sequences and tokens beyond the bounds are left out; nothing else changes."""
+    r, call, check = _prefix_case(pkg, fmt, q_dtype, 128, SHAPES[shape], 110)
+    pre, own = int(r["pl"].max()) - 9, int(r["ol"].max()) // 2
+    call(max_prefix=pre, max_own=own)
+    r["pl"].clamp_(max=pre), r["ol"].clamp_(max=own)  # (for the check)
+    check()
+    q_len, _, members, _ = SHAPES[shape]
+    if max(q_len) == 1:
+        r["out"].fill_(5.0), r["lse"].fill_(5.0)
+        call(max_group=members[0] - 2)
+        check(untouched=(members[0] - 2, members[0] - 1))
+    else:  # the last token of the longest sequence
+        r["out"].fill_(5.0), r["lse"].fill_(5.0)
+        call(max_q=max(q_len) - 1)
+        b = int(np.argmax(q_len))
+        last = int(r["cu"][b + 1]) - 1
+        assert (r["out"][last] == 5.0).all() and (r["lse"][last] == 5.0).all()
+        assert (r["out"][:last] != 5.0).any(-1).all()
+
+
+
+@pytest.mark.parametrize("fmt,q_dtype", FORMATS)
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_prefix_of_nothing(pkg, fmt, q_dtype, shape):
+    r, call, check = _prefix_case(pkg, fmt, q_dtype, 64, SHAPES[shape], 130)
+    r["pl"].zero_(), r["ol"].zero_()
+    for kw in (dict(), dict(max_prefix=0), dict(max_own=0), dict(max_prefix=0, max_own=0)):
+        r["out"].fill_(5.0), r["lse"].fill_(5.0)
+        call(**kw)
+        check()
+
+
+@pytest.mark.parametrize("fmt,q_dtype", FORMATS)
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_prefix_nan_stays_with_its_group(pkg, fmt, q_dtype, shape):
+    """A NaN among the first group's prefix: every query of that group is NaN, no other; then one among a sequence's own."""
+    q_len, own, members, pre = SHAPES[shape]
+    for where in ("prefix", "own"):
+        r, call, check = _prefix_case(pkg, fmt, q_dtype, 128, SHAPES[shape], 150)
+        at = int(r["pb"][0]) + pre[0] // 2 if where == "prefix" else int(r["ob"][1])
+        if fmt == "kv8":
+            r["store"].k[:, at, 3] = 0x7F
+        else:
+            r["store"].k[at, :, 3] = math.nan
+        call()
+        hit = range(members[0]) if where == "prefix" else [1]
+        for b in hit:  # (every token sees row 0 of its own range, where it has one)
+            sl = slice(int(r["cu"][b]), int(r["cu"][b + 1]))
+            assert torch.isnan(r["out"][sl]).all() and torch.isnan(r["lse"][sl]).all()
+            r["out"][sl], r["lse"][sl] = 5.0, 5.0
+        check(untouched=list(hit))
+
+
+def test_broadcast_store_rows_are_refused(pkg):
+    one = torch.zeros((1, 2, 64), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError):
+        pkg.H2OStore(one.expand(9, 2, 64), one.expand(9, 2, 64))
+
+
+@pytest.mark.parametrize("fmt,q_dtype", FORMATS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n,length", [(1, 300), (70, 300), (70, 700), (150, 700)])
+def test_cross_one_key_at_every_place(pkg, fmt, q_dtype, dim, n, length):
+    """The same store row at every place of a range: NaN there gives NaN everywhere; a logit there that is hundreds above
+    all before it takes the whole weight."""
+    at, batch = 800, 97
+    g = _gen(7)
+    u = torch.nn.functional.normalize(torch.randn(dim, generator=g), dim=0)
+    q = ((torch.randn((n, 1, dim), generator=g) * 0.05 + 6.0 * u).to(DT[q_dtype])).repeat(batch, 1, 1).cuda()
+    begin = [at - 7 * i if i % 2 else at - i for i in range(batch)]
+    kw = {} if n == 1 else {"cu_q": _i32([n * i for i in range(batch + 1)]), "max_q": n}
+    for what in ("nan", 400.0, 1100.0, 20000.0):
+        k, v = (_rows(s, 1600, 1, dim, DT.get(fmt, torch.bfloat16), spread=False) for s in (2, 3))
+        if what == "nan":
+            k[at, 0, 5] = math.nan
+        else:
+            k[at, 0] = (u * what / 6.0 * math.sqrt(dim)).to(k.dtype)  # a logit of about `what`
+        store, k64, v64 = _make(pkg, fmt, k, v)
+        out, lse = torch.empty_like(q), torch.empty((batch * n, 1), dtype=torch.float32, device="cuda")
+        store.cross_attend(q, _i64(begin), _i32([length] * batch), out, max_len=length, lse=lse, **kw)
+        for b in range(batch):
+            sl, here = slice(b * n, b * n + n), at < begin[b] + length
+            if here and what == "nan":
+                assert torch.isnan(out[sl]).all() and torch.isnan(lse[sl]).all(), b
+            elif here:  # the others' weights are below e^-100
+                x = (q[b * n:b * n + n, 0].double().cpu().numpy() @ k64[at, 0]) * float(np.float32(1 / math.sqrt(dim)))
+                assert x.min() > 200.0
+                want = np.broadcast_to(v64[at], (n, 1, dim))
+                ref.compare(out[sl], want, np.abs(want) * 2.0 ** -7 + 1e-30, "out %d" % b)
+                size = (np.abs(q[sl, 0].double().cpu().numpy()) @ np.abs(k64[at, 0])) * float(np.float32(1 / math.sqrt(dim)))
+                ref.compare(lse[sl, 0], x, size * (dim + 8) * 2.0 ** -23, "lse %d" % b)
