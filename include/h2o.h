@@ -462,7 +462,8 @@ typedef struct {
  * and the own rows but the last n_b - 1 - i.  The prefix is read once for all the queries of a group.
  *
  * A query without a single key (empty ranges), or whose every logit is -infinity, gets out 0 and lse -infinity.
- * What lies outside a range is not read into any result (it may hold NaN).  Rows of q behind the last sequence leave
+ * What lies outside a range is not read into any result (it may hold NaN).  Inside a sequence's own range a value that
+ * is not finite may reach all of its query tokens, the earlier ones too (a weight of 0 times it).  Rows of q behind the last sequence leave
  * out and lse as they were.  max_q, max_length and max_group (sequences in a group) size the launch: they must be
  * upper bounds; tokens, rows and sequences beyond them are left out, and ranges are cut to the store's rows.
  * cu_q, cu_group, begin and length are read on the device when the kernels run, so a captured graph follows them.

@@ -461,7 +461,7 @@ class H2OStore:
             if k_scale is not None or v_scale is not None:
                 _bad("scales belong to 8-bit rows")
             self.rows, self.n_heads, self.head_dim = k.shape
-            if k.stride() != v.stride() or k.stride(2) != 1 or k.stride(1) != self.head_dim:
+            if k.stride() != v.stride() or k.stride(2) != 1 or k.stride(1) != self.head_dim or (self.rows > 1 and k.stride(0) == 0):
                 _bad("rows of k and v must have one stride and dense heads")
         self.format = H2O_KV8 if eight else _DTYPES[k.dtype]
         self.device = k.device
@@ -496,7 +496,7 @@ class H2OStore:
         if dtype is None or v.dtype is not k.dtype or k.get_device() != self._index or v.get_device() != self._index:
             _bad("k and v must both be float32 or bfloat16 on %s" % self.device)
         n, stride = shape[0], k.stride()
-        if stride != v.stride() or (n and (stride[2] != 1 or stride[1] != self.head_dim)):
+        if stride != v.stride() or (n and (stride[2] != 1 or stride[1] != self.head_dim)) or (n > 1 and stride[0] == 0):
             _bad("k and v must have one token stride and dense heads")
         if rows is not None and (rows.dtype is not torch.int64 or rows.shape != (n,) or rows.get_device() != self._index or not rows.is_contiguous()):
             _bad("rows must be a contiguous int64 [tokens] on %s" % self.device)
@@ -516,6 +516,8 @@ class H2OStore:
         s, o = q.stride(), out.stride()
         if tokens and (s[2] != 1 or s[1] != dim or o[2] != 1 or o[1] != dim):
             _bad("q and out must have dense heads")
+        if tokens > 1 and (s[0] == 0 or o[0] == 0):  # (0 means dense to the library)
+            _bad("q and out must not be broadcast over the tokens")
         if cu_q is None:
             if max_q != 1 or tokens < batch:
                 _bad("without cu_q there is one token per sequence")

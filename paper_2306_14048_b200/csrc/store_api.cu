@@ -40,7 +40,7 @@ int check_store(const h2o_store_config_t* c) {
   if (c->format == H2O_KV8) {
     if (!c->k_scale || !c->v_scale) return H2O_ERR_INVALID_ARG;
     if (c->row_stride != 0) return H2O_ERR_INVALID_ARG;
-    if (c->rows * c->n_heads > INT32_MAX) return H2O_ERR_UNSUPPORTED;  // rows of all heads: one tensor-map coordinate
+    if (c->rows * c->n_heads > INT32_MAX) return H2O_ERR_UNSUPPORTED;  // rows of all heads are counted in 32 bits
   } else {
     if (c->row_stride != 0 && (c->row_stride < dense || c->row_stride % 8 != 0)) return H2O_ERR_INVALID_ARG;
     if (c->row_stride > (1ll << 36)) return H2O_ERR_UNSUPPORTED;

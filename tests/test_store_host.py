@@ -168,3 +168,19 @@ def test_reference_quantiser_against_torch():
     want = torch.ldexp(y.double(), e.unsqueeze(-1)).numpy()
     np.testing.assert_array_equal(ref.values(code, scale), want)
     assert float(torch.finfo(torch.float8_e4m3fn).max) == 448.0
+
+
+def test_broadcast_tensors_are_refused(b):
+    """An expanded tensor has a token stride of 0, which the library would read as dense."""
+    from types import SimpleNamespace
+
+    me = SimpleNamespace(_index=-1, head_dim=64, n_heads=2, device="cpu", _h=None)  # (-1: where CPU tensors say they are)
+    wide, one = torch.zeros(5, 2, 64), torch.zeros(1, 2, 64)
+    queries = lambda q, out: b.H2OStore._queries(me, q, out, None, 1, None, 0.0, 5)
+    rows = lambda k: b.H2OStore._rows(me, k, k, None, 0)
+    queries(wide, wide.clone())
+    rows(wide), rows(one)
+    for call in (lambda: queries(one.expand(5, 2, 64), wide), lambda: queries(wide, one.expand(5, 2, 64)),
+                 lambda: queries(wide[:, :1].expand(5, 2, 64), wide), lambda: rows(one.expand(5, 2, 64))):
+        with pytest.raises(ValueError):
+            call()
