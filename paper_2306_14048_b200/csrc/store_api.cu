@@ -128,12 +128,12 @@ constexpr int kWalkKeys = 512;
 // costs its keys and `fixed` more (start, merge, its result's trip through memory), the joining kernel twice as much;
 // a block that has its SM to itself is taken to run twice as fast, and the last blocks to finish to leave a quarter of a
 // block's time unused.  Only the longest length is known here: the lengths of a batch's sequences (`ragged`) are taken
-// to average two thirds of it.
-void split_part(h2o::AttendPart& p, int64_t units, int64_t room, int64_t fixed, bool ragged) {
+// to average two thirds of it.  Chunks are multiples of `step` keys, what a block takes at a time.
+void split_part(h2o::AttendPart& p, int64_t units, int64_t room, int64_t fixed, int64_t step, bool ragged) {
   const int64_t len = std::max(1, p.max_length), num = ragged ? 2 : 3;
   int64_t best = -1;
   for (int64_t n = 1; n <= h2o::kMaxSplits && (n == 1 || units * n <= 16 * room); ++n) {
-    const int64_t chunk = ((len + n - 1) / n + 127) / 128 * 128;
+    const int64_t chunk = ((len + n - 1) / n + step - 1) / step * step;
     const int64_t splits = (len + chunk - 1) / chunk;
     const int64_t one = std::min(chunk, len) + fixed;
     const int64_t blocks = std::max(units, units * splits * num / 3);
@@ -144,7 +144,7 @@ void split_part(h2o::AttendPart& p, int64_t units, int64_t room, int64_t fixed, 
       p.chunk = (int)chunk;
       p.splits = (int)splits;
     }
-    if (chunk == 128) break;
+    if (chunk == step) break;
   }
 }
 
@@ -209,7 +209,8 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
     const bool tiles = pl.kernel[n] == Kernel::Fma && pl.tile[n] >= 16;
     const int per_sm = pl.kernel[n] == Kernel::Tc2 ? 1 : pl.kernel[n] == Kernel::Tc1 || tiles ? 2 : pl.kernel[n] == Kernel::Fma ? 4 : h2o::attend_mma_blocks_per_sm(c.format, pl.tile[n]);
     const int64_t room = (int64_t)h2o::sm_count() * per_sm;
-    split_part(p, units, room, is_tc(pl.kernel[n]) ? 640 : tiles ? 36 : 19200000 / (room * key_bytes), !p.grouped);
+    split_part(p, units, room, is_tc(pl.kernel[n]) ? 640 : tiles ? 36 : 19200000 / (room * key_bytes),
+               tiles ? 64 : 128, !p.grouped);
     if (units * p.splits > INT32_MAX) pl.rc = H2O_ERR_UNSUPPORTED;
     p.slot0 = n == 0 ? 0 : a.part[0].splits;
     ++n;

@@ -7,7 +7,7 @@
 // 4 x + 64 j .. + 3, so a row's statistics are shuffles within 16 lanes and its probabilities pass between them
 // through shared memory without a block barrier.  K of the next tile is fetched (cp.async, float32 rows) during
 // P V, V during the next S.  Bound by shared memory: 8 vector loads (32 wavefronts) feed 64 multiply-adds of a warp.
-// 4 x 512 queries against 2048 keys, 16 heads of 128: 630 us, 27 TFLOP/s.
+// 4 x 512 queries against 2048 keys, 16 heads of 128: 590 us, 29 TFLOP/s.
 #include "store.cuh"
 
 namespace h2o {
@@ -124,82 +124,88 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
     load_k(key0);
     load_v(key0);
   }
+  // A warp without rows only copies (32 sequences behind a prefix of 4096: 126 -> 102 us; full tiles 2 % slower).
+  const bool works = (int)(threadIdx.x >> 5) * 2 * RM < n_rows;
   for (int key = key0; key < key1; key += kBN) {
     cp_wait<1>();  // K of this tile (V's copies may still be under way)
     __syncthreads();
-    float s[RM][kJ];
+    if (works) {
+      float s[RM][kJ];
 #pragma unroll
-    for (int i = 0; i < RM; ++i)
+      for (int i = 0; i < RM; ++i)
 #pragma unroll
-      for (int j = 0; j < kJ; ++j) s[i][j] = 0.f;
+        for (int j = 0; j < kJ; ++j) s[i][j] = 0.f;
 #pragma unroll 4
-    for (int c = 0; c < D; c += 4) {
-      float4 kk[kJ];
+      for (int c = 0; c < D; c += 4) {
+        float4 kk[kJ];
 #pragma unroll
-      for (int j = 0; j < kJ; ++j) kk[j] = *reinterpret_cast<const float4*>(&sh.k[x + 16 * j][c]);
+        for (int j = 0; j < kJ; ++j) kk[j] = *reinterpret_cast<const float4*>(&sh.k[x + 16 * j][c]);
 #pragma unroll
-      for (int i = 0; i < RM; ++i) {
-        const float4 qq = *reinterpret_cast<const float4*>(&sh.q[y * RM + i][c]);
+        for (int i = 0; i < RM; ++i) {
+          const float4 qq = *reinterpret_cast<const float4*>(&sh.q[y * RM + i][c]);
 #pragma unroll
-        for (int j = 0; j < kJ; ++j) {
-          s[i][j] = fmaf(qq.x, kk[j].x, s[i][j]);
-          s[i][j] = fmaf(qq.y, kk[j].y, s[i][j]);
-          s[i][j] = fmaf(qq.z, kk[j].z, s[i][j]);
-          s[i][j] = fmaf(qq.w, kk[j].w, s[i][j]);
+          for (int j = 0; j < kJ; ++j) {
+            s[i][j] = fmaf(qq.x, kk[j].x, s[i][j]);
+            s[i][j] = fmaf(qq.y, kk[j].y, s[i][j]);
+            s[i][j] = fmaf(qq.z, kk[j].z, s[i][j]);
+            s[i][j] = fmaf(qq.w, kk[j].w, s[i][j]);
+          }
         }
       }
-    }
 #pragma unroll
-    for (int i = 0; i < RM; ++i) {
-      float top = -INFINITY;
+      for (int i = 0; i < RM; ++i) {
+        float top = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < kJ; ++j) {
-        const int kx = key + x + 16 * j;
-        s[i][j] = kx < seen[i] && kx < key1 ? s[i][j] * a.scale2 : -INFINITY;
-        top = fmaxf(top, s[i][j]);
-      }
+        for (int j = 0; j < kJ; ++j) {
+          const int kx = key + x + 16 * j;
+          s[i][j] = kx < seen[i] && kx < key1 ? s[i][j] * a.scale2 : -INFINITY;
+          top = fmaxf(top, s[i][j]);
+        }
 #pragma unroll
-      for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-      const float mn = fmaxf(m[i], top);
-      const float base = mn == -INFINITY ? 0.f : mn;  // nothing seen so far: every exponential is 0
-      const float alpha = exp2f(m[i] - base);
-      float sum = 0.f;
+        for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const float mn = fmaxf(m[i], top);
+        const float base = mn == -INFINITY ? 0.f : mn;  // nothing seen so far: every exponential is 0
+        const float alpha = exp2f(m[i] - base);
+        float sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < kJ; ++j) {
-        const float p = exp2f(s[i][j] - base);
-        sum += p;
-        sh.p[y * RM + i][x + 16 * j] = p;
-      }
-      l[i] = l[i] * alpha + sum;
-      m[i] = mn;
+        for (int j = 0; j < kJ; ++j) {
+          const float p = exp2f(s[i][j] - base);
+          sum += p;
+          sh.p[y * RM + i][x + 16 * j] = p;
+        }
+        l[i] = l[i] * alpha + sum;
+        m[i] = mn;
 #pragma unroll
-      for (int j = 0; j < NC; ++j) {
-        o[i][j].x *= alpha;
-        o[i][j].y *= alpha;
-        o[i][j].z *= alpha;
-        o[i][j].w *= alpha;
+        for (int j = 0; j < NC; ++j) {
+          o[i][j].x *= alpha;
+          o[i][j].y *= alpha;
+          o[i][j].z *= alpha;
+          o[i][j].w *= alpha;
+        }
       }
     }
     cp_wait<0>();
     __syncthreads();  // V is there, K has been read
     if (key + kBN < key1) load_k(key + kBN);
+    if (works) {
 #pragma unroll 2
-    for (int kk = 0; kk < kBN; kk += 4) {
-      float4 pp[RM];
+      for (int kk = 0; kk < kBN; kk += 4) {
+        float4 pp[RM];
 #pragma unroll
-      for (int i = 0; i < RM; ++i) pp[i] = *reinterpret_cast<const float4*>(&sh.p[y * RM + i][kk]);
+        for (int i = 0; i < RM; ++i) pp[i] = *reinterpret_cast<const float4*>(&sh.p[y * RM + i][kk]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < 4; ++e) {
 #pragma unroll
-        for (int j = 0; j < NC; ++j) {
-          const float4 vv = *reinterpret_cast<const float4*>(&sh.v[kk + e][4 * x + 64 * j]);
+          for (int j = 0; j < NC; ++j) {
+            const float4 vv = *reinterpret_cast<const float4*>(&sh.v[kk + e][4 * x + 64 * j]);
 #pragma unroll
-          for (int i = 0; i < RM; ++i) {
-            const float p = e == 0 ? pp[i].x : e == 1 ? pp[i].y : e == 2 ? pp[i].z : pp[i].w;
-            o[i][j].x = fmaf(p, vv.x, o[i][j].x);
-            o[i][j].y = fmaf(p, vv.y, o[i][j].y);
-            o[i][j].z = fmaf(p, vv.z, o[i][j].z);
-            o[i][j].w = fmaf(p, vv.w, o[i][j].w);
+            for (int i = 0; i < RM; ++i) {
+              const float p = e == 0 ? pp[i].x : e == 1 ? pp[i].y : e == 2 ? pp[i].z : pp[i].w;
+              o[i][j].x = fmaf(p, vv.x, o[i][j].x);
+              o[i][j].y = fmaf(p, vv.y, o[i][j].y);
+              o[i][j].z = fmaf(p, vv.z, o[i][j].z);
+              o[i][j].w = fmaf(p, vv.w, o[i][j].w);
+            }
           }
         }
       }
@@ -424,7 +430,7 @@ cudaError_t launch_shape(const AttendView& a, int part, int tile, cudaStream_t s
 }  // namespace
 
 // Rows of a tile for problems of up to `rows` rows: 1, 2 or 4 in the kernel for few; else 16 or 64 (fewer rows make more
-// shared-memory loads per product: 131 query tokens, 515 keys, 16 heads run in 24.4 us in tiles of 16, in 22.7 in tiles of 64).
+// shared-memory loads per product: 131 query tokens, 515 keys, 16 heads ran in 24.4 us in tiles of 16, 22.7 in tiles of 64).
 int attend_fma_row_tile(int64_t rows) { return rows <= 2 ? (int)rows : rows <= 4 ? 4 : rows <= 16 ? 16 : 64; }
 
 cudaError_t launch_attend_fma(const AttendView& a, int part, int tile, int format, cudaStream_t stream) {
