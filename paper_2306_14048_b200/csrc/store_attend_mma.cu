@@ -37,12 +37,13 @@ constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kKeys = kFewBoxRows;                  // keys of a tile
 constexpr uint32_t kSpin = 1u << 22;
 constexpr float kRescale = 8.f;
-// Shared memory of a block's rings (KB) and blocks on an SM, for blocks of up to 8 nt rows.  More blocks of smaller rings
-// where registers allow: 8-bit rows, whose conversion wants warps, 39.4 us with 2 blocks of 96 KB, 37.2 with 3 of 64, 34.5
-// with 4 of 48 (32 sequences of 1024 .. 4096 rows, 8 K/V heads of 4 query heads); bfloat16 rows 193.5 / 192.1 / 197.5 us
-// (64 sequences of up to 2048 rows, 32 heads).
+// Shared memory of a block's rings (KB), and blocks on an SM that its registers and the splitting of the keys count on (one
+// more fits where the code takes fewer), for blocks of up to 8 nt rows.  bfloat16, one query row (64 sequences of up to 2048
+// rows, 32 heads / 32 of 4096, 4 heads of 8 query heads / 64 behind a prefix of 8192): 96 KB and 2 blocks 193 / 37.8 / 88.6
+// us, 64 and 2 195.5 / 35.3 / 86.2, 64 and 3 195.5 / 37.1 / 86.0.  8-bit rows, whose conversion wants warps (32 sequences of
+// up to 4096, 8 heads of 4 / 64 of 2048, 32 heads of 64): 64 and 3 40.7 / 68.5, 48 and 3 39.8 / 62.3, 48 and 4 41 / 62.1.
 __host__ __device__ constexpr int ring_kb(int fmt, int nt) { return nt > 1 ? 96 : fmt == H2O_KV8 ? 48 : 64; }
-__host__ __device__ constexpr int blocks_per_sm(int fmt, int nt) { return 192 / ring_kb(fmt, nt); }
+__host__ __device__ constexpr int blocks_per_sm(int fmt, int nt) { return nt == 1 && fmt == H2O_KV8 ? 3 : 2; }
 constexpr int kMaxSlots = 8;
 
 __host__ __device__ constexpr int row_bytes(int fmt, int d) { return fmt == H2O_KV8 ? d : 2 * d; }
@@ -106,13 +107,14 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+template <int NT>  // the kernel's larger number of n-tiles
 struct Shared {
   uint64_t full[kWarps][kMaxSlots];
-  float m[kWarps][32], l[kWarps][32];  // the warps' statistics, per row
-  float row_factor[32];                // softmax scale times log2(e) (times the row's power of two)
+  float m[kWarps][8 * NT], l[kWarps][8 * NT];  // the warps' statistics, per row
+  float row_factor[8 * NT];                // softmax scale times log2(e) (times the row's power of two)
   float k_factor[kWarps][kKeys];       // 8-bit rows: K's power of two of each key of the warp's tile
   __half v_factor[kWarps][kKeys];
-  uint2 q[4][8][32];                   // query operand, [n-tile][k-step][lane]
+  uint2 q[NT][8][32];                   // query operand, [n-tile][k-step][lane]
 };
 
 // The address of 16-byte chunk `c` of row `r` of a tile, as TMA swizzles it (tiles are 1024-byte aligned).
@@ -128,7 +130,7 @@ __device__ __forceinline__ uint32_t chunk_addr(uint32_t tile, int r, int c) {
 // (part 0's range) and then its own rows, and writes the result: no chunks, no joining kernel.
 template <int FMT, int D, int NT, int NTB, bool WALK>
 __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* map_k, const CUtensorMap* map_v,
-                                       const AttendPart& part, unsigned block, unsigned char* ring, Shared& sh) {
+                                       const AttendPart& part, unsigned block, unsigned char* ring, Shared<NTB>& sh) {
   constexpr bool kF16 = FMT == H2O_KV8;
   constexpr int kTile = tile_bytes(FMT, D), kSlots = ring_slots(FMT, D, NTB), kSteps = D / 16, kRows = 8 * NT;
   constexpr int kPitch = D + 4;  // floats per row of a warp's partial output
@@ -529,7 +531,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(FMT, NT0))
 attend_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                   const __grid_constant__ AttendView a, int first, unsigned blocks0) {
   extern __shared__ unsigned char dyn[];
-  __shared__ Shared sh;
+  __shared__ Shared<NT0> sh;
   unsigned char* ring = dyn + ((1024u - (smem_u32(dyn) & 1023u)) & 1023u);
   let_next_start();  // (the joining kernel waits for this one's end; others are launched to start after it)
   if (NT0 == NT1 || blockIdx.x < blocks0) {
