@@ -571,12 +571,16 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           if (top > kPolyMax) sum.x = INFINITY;
           return sum;
         };
-        float2 sum = exponentials(N0{}, N1{});
-        // Has P(j - 1) been used (and does O include it)?  Asked ahead: the last exponentials hide the answer's way.
-        const bool used = n == 0 || mbar_test_wait(&sh.p_empty[g], (uint32_t)(n - 1) & 1u);
-        sum = __fadd2_rn(sum, exponentials(N1{}, N2{}));
-        if (!used) ok = wait_or_abort(&sh.p_empty[g], (uint32_t)(n - 1) & 1u, abort_flag);
-        const bool again = m == -INFINITY || sum.x + sum.y > kLargeSum;
+        float2 sum = make_float2(0.f, 0.f);
+        bool again = true;  // (the first tile: its maximum first)
+        if (n > 0) {
+          sum = exponentials(N0{}, N1{});
+          // Has P(j - 1) been used (and does O include it)?  Asked ahead: the last exponentials hide the answer's way.
+          const bool used = mbar_test_wait(&sh.p_empty[g], (uint32_t)(n - 1) & 1u);
+          sum = __fadd2_rn(sum, exponentials(N1{}, N2{}));
+          if (!used) ok = wait_or_abort(&sh.p_empty[g], (uint32_t)(n - 1) & 1u, abort_flag);
+          again = m == -INFINITY || sum.x + sum.y > kLargeSum;
+        }
         if (__any_sync(0xffffffffu, again || !ok)) {
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
