@@ -406,6 +406,8 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       }
     } else if (kF16 && warp >= 12) {
       // ---- code tiles to f16 tiles, four warps for K and four for V: a thread takes 16 codes at a time ----
+      // (Two sets of four warps that take tiles in turn: 50.4 us against 47.3 for 16 sequences of 4 query heads behind a prefix of
+      // 32768, 8 heads; a third stage of codes: no difference.)
       // Eight neighbouring threads take four chunks of two rows (rows of 128 codes: the low four of one, the high four of
       // the other), which keeps both the loads and the stores free of bank conflicts.
       const int kv = (warp - 12) >> 2, t = threadIdx.x - 384 - 128 * kv;
