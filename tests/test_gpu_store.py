@@ -732,3 +732,41 @@ def test_cross_one_key_at_every_place(pkg, fmt, q_dtype, dim, n, length):
                 ref.compare(out[sl], want, np.abs(want) * 2.0 ** -7 + 1e-30, "out %d" % b)
                 size = (np.abs(q[sl, 0].double().cpu().numpy()) @ np.abs(k64[at, 0])) * float(np.float32(1 / math.sqrt(dim)))
                 ref.compare(lse[sl, 0], x, size * (dim + 8) * 2.0 ** -23, "lse %d" % b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,dim,tokens,scattered", [(2, 64, 65607, True), (1, 128, 65538, False), (5, 128, 4999, True)])
+def test_write_and_read_many_tokens(pkg, dtype, heads, dim, tokens, scattered):
+    """Several tokens to a thread with a remainder, and more tokens than one launch takes."""
+    rows = tokens + 5
+    k, v = (_rows(s, tokens, heads, dim, DT[dtype]) for s in (1, 2))
+    store = pkg.H2OStore.empty_kv8(rows, heads, dim)
+    for t in (store.k, store.v, store.k_scale, store.v_scale):
+        t.fill_(0x77)
+    to = torch.randperm(rows, generator=_gen(3))[:tokens] if scattered else torch.arange(3, tokens + 3)
+    at = dict(rows=to.cuda()) if scattered else dict(first_row=3)
+    store.write(k.cuda(), v.cuda(), **at)
+    back = [torch.empty((tokens, heads, dim), dtype=torch.float32, device="cuda") for _ in range(2)]
+    store.read(*back, **at)
+    for x, code, scale, got in ((k, store.k, store.k_scale, back[0]), (v, store.v, store.v_scale, back[1])):
+        c, s = ref.quantise(x)
+        want = np.full((heads, rows, dim), 0x77, np.uint8), np.full((heads, rows), 0x77, np.uint8)
+        want[0][:, to], want[1][:, to] = c, s
+        assert np.array_equal(code.cpu().numpy(), want[0]) and np.array_equal(scale.cpu().numpy(), want[1])
+        np.testing.assert_array_equal(got.double().cpu().numpy(), ref.values(c, s).transpose(1, 0, 2))
+
+
+@pytest.mark.parametrize("fmt,q_dtype", FORMATS)
+@pytest.mark.parametrize("n", [1, 3, 40])
+def test_store_of_one_row_and_the_last_rows(pkg, fmt, q_dtype, n):
+    """A store of a single row; and ranges that end with the store, inside a tile."""
+    for rows, length in ((1, 1), (37, 37), (131, 5)):
+        k, v = (_rows(s, rows, 2, 64, DT.get(fmt, torch.bfloat16)) for s in (1, 2))
+        store, k64, v64 = _make(pkg, fmt, k, v)
+        q = torch.randn((n, 2, 64), generator=_gen(3)).to(DT[q_dtype]).cuda()
+        out = torch.empty_like(q)
+        kw = {} if n == 1 else {"cu_q": _i32([0, n]), "max_q": n}
+        store.cross_attend(q, _i64([rows - length]), _i32([length]), out, max_len=length, **kw)
+        want = ref.attend(q.double().cpu().numpy(), k64[rows - length:], v64[rows - length:], [length] * n,
+                          float(np.float32(1 / math.sqrt(64))), fmt, q_dtype)
+        ref.compare(out, want[0], want[2], "out")
