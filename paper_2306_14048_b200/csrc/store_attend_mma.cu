@@ -15,7 +15,9 @@
 // The reference maximum moves only when a logit exceeds it by 8 (base 2), which a warp vote finds: in steady state no
 // shuffle and no rescaling.  Sums are kept per lane and added at the end.
 //
-// bfloat16 rows: P = bf16 hi + bf16 lo (two products), so that its rounding (2^-9) does not add to the output's.
+// bfloat16 rows: P = bf16 hi + bf16 lo (two products), so that its rounding (2^-8) does not add to the output's.  hi lies
+// below P, so lo is positive like P: a value of infinity in V then gives that infinity in both products (a lo of 0 or
+// less would make them NaN together).  What is left out is below 2^-15 of P: hi leaves 2^-7, of which lo rounds 2^-8 away.
 // 8-bit rows: e4m3 codes become f16 exactly and P is one f16 (11 bits).  K's power of two multiplies the score; V's
 // multiplies the codes (exact in f16 by the format's range; in P it would push small probabilities into subnormals).
 // The query rows become f16 by a power of two of their own that brings the largest value into [1, 2).  Which
@@ -102,6 +104,8 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// The largest bf16 number below p (0 for 0), in the upper half of the word; NaN stays NaN.
+__device__ __forceinline__ uint32_t below(float p) { return (max(__float_as_uint(p), 1u) - 1u) & 0xffff0000u; }
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -395,10 +399,9 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
           if constexpr (kF16) {
             ph[mt][nt][h] = transpose8x8(pack_half2(p0, p1));
           } else {
-            const __nv_bfloat162 hi = __floats2bfloat162_rn(p0, p1);
-            const float2 back = __bfloat1622float2(hi);
-            ph[mt][nt][h] = transpose8x8(*reinterpret_cast<const uint32_t*>(&hi));
-            pl[mt][nt][h] = transpose8x8(Vec16<__nv_bfloat16>::pack2(p0 - back.x, p1 - back.y));
+            const uint32_t h0 = below(p0), h1 = below(p1);
+            ph[mt][nt][h] = transpose8x8(__byte_perm(h0, h1, 0x7632));
+            pl[mt][nt][h] = transpose8x8(Vec16<__nv_bfloat16>::pack2(p0 - __uint_as_float(h0), p1 - __uint_as_float(h1)));
           }
         }
     }

@@ -1,0 +1,103 @@
+"""The K/V store operators on a B200 at values where a rounding, a mask or a factor can show: infinite values, hidden keys,
+small probabilities in long ranges, softmax scales at the ends of fp32."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import store_reference as ref
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+FORMATS = [("f32", "f32"), ("bf16", "bf16"), ("kv8", "bf16"), ("kv8", "f32")]
+
+
+@pytest.fixture(scope="module")
+def pkg():
+    import paper_2306_14048_b200 as p
+
+    assert torch.cuda.is_available(), "these tests need a CUDA device; there is no CPU fallback"
+    return p
+
+
+def _normal(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed))
+
+
+def _i64(x):
+    return torch.tensor(x, dtype=torch.int64, device="cuda")
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _store(pkg, fmt, k, v):
+    if fmt == "kv8":
+        (ck, sk), (cv, sv) = ref.quantise(k), ref.quantise(v)
+        store = pkg.H2OStore(*[torch.from_numpy(x).cuda() for x in (ck, cv, sk, sv)])
+        return store, ref.values(ck, sk).transpose(1, 0, 2), ref.values(cv, sv).transpose(1, 0, 2)
+    return pkg.H2OStore(k.cuda(), v.cuda()), k.double().numpy(), v.double().numpy()
+
+
+def _attend(store, q, begin, length, n, scale=0.0):
+    """Sequences of n tokens each; out and lse."""
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], dtype=torch.float32, device="cuda")
+    kw = {} if n == 1 else {"cu_q": _i32([n * i for i in range(len(begin) + 1)]), "max_q": n}
+    store.cross_attend(q, _i64(begin), _i32(length), out, max_len=max(length), lse=lse, softmax_scale=scale, **kw)
+    assert store.status() == 0
+    return out, lse
+
+
+@pytest.mark.parametrize("fmt", ["f32", "bf16"])  # (8-bit rows have no infinities)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n,length", [(1, 50), (1, 3000), (4, 50), (16, 50), (16, 900), (17, 50), (150, 50), (150, 700)])
+def test_infinite_values_stay_infinite(pkg, fmt, dim, n, length):
+    """A value of +-infinity with a positive probability gives that infinity, whatever the number of query rows; both signs
+    in one channel, or a NaN, give NaN.  The sequences: a single key (probability 1), keys of equal logits (probabilities that
+    are powers of two), random ones."""
+    rows = 4 + 64 + length
+    k, v = (_normal(s, rows, 1, dim).to(DT[fmt]) for s in (1, 2))
+    k[:68] = 0
+    k[68:] *= 0.3
+    v[1, 0, 3], v[1, 0, 4] = math.inf, -math.inf
+    v[20, 0, 5], v[30, 0, 6], v[31, 0, 6] = math.inf, math.inf, -math.inf
+    v[68 + length // 3, 0, ::7], v[68 + length // 2, 0, 1::7] = math.inf, -math.inf
+    v[rows - 1, 0, 1], v[rows - 1, 0, 2] = math.inf, math.nan
+    store, k64, v64 = _store(pkg, fmt, k, v)
+    begin, ln = [1, 4, 68], [1, 64, length]
+    q = _normal(3, 3 * n, 1, dim).to(DT[fmt]).cuda()
+    out, lse = _attend(store, q, begin, ln, n)
+    for b in range(3):
+        sl = slice(b * n, b * n + n)
+        with np.errstate(invalid="ignore"):
+            want = ref.attend(q[sl].double().cpu().numpy(), k64[begin[b]:begin[b] + ln[b]], v64[begin[b]:begin[b] + ln[b]],
+                              [ln[b]] * n, float(np.float32(1 / math.sqrt(dim))), fmt, fmt)
+            ref.compare(out[sl], want[0], want[2], "out of sequence %d" % b)
+        ref.compare(lse[sl], want[1], want[3], "lse of sequence %d" % b)
+
+
+@pytest.mark.parametrize("fmt", ["f32", "bf16"])
+@pytest.mark.parametrize("group,n", [(1, 4), (8, 2), (1, 12), (2, 6)])
+def test_infinite_own_values_behind_a_prefix(pkg, fmt, group, n):
+    """The same among the own rows of sequences that share a prefix: infinite in the last row, so for the last token."""
+    dim, pre, own, batch = 64, 40, 30, 3
+    rows = pre + own * batch
+    k, v = (_normal(s, rows, 1, dim).to(DT[fmt]) for s in (1, 2))
+    for b in range(batch):
+        v[pre + own * (b + 1) - 1, 0, 5 + b] = math.inf
+    store, k64, v64 = _store(pkg, fmt, k, v)
+    q = _normal(3, batch * n, group, dim).to(DT[fmt]).cuda()
+    for most in (pre, 5000):  # (the bound of a prefix decides how the call is cut)
+        out = torch.empty_like(q)
+        store.prefix_attend(q, _i64([0]), _i32([pre]), _i64([pre + own * b for b in range(batch)]), _i32([own] * batch), out,
+                            max_prefix=most, max_own=own, cu_q=_i32([n * b for b in range(batch + 1)]), max_q=n)
+        assert store.status() == 0
+        for b in range(batch):
+            at = pre + own * b
+            kk, vv = (np.concatenate([x[:pre], x[at:at + own]]) for x in (k64, v64))
+            last = b * n + n - 1
+            want = ref.attend(q[last:last + 1].double().cpu().numpy(), kk, vv, [pre + own], float(np.float32(1 / math.sqrt(dim))), fmt, fmt)
+            assert np.isposinf(want[0][0, :, 5 + b]).all()
+            ref.compare(out[last:last + 1], want[0], want[2], "last token of sequence %d" % b)
