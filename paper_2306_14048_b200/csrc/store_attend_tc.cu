@@ -97,8 +97,9 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 // exp2 of two values on the FMA pipe: nearest integer by the 1.5 * 2^23 trick, degree-5 polynomial of 2^f on
-// [-0.5, 0.5] (1.8e-7 relative, as good as ex2.approx), times 2^n put together with integer arithmetic.  Below -126:
-// ~1e-38; NaN stays NaN; above kPolyMax the result means nothing.
+// [-0.5, 0.5] (1.8e-7 relative, as good as ex2.approx), times 2^n put together with integer arithmetic.  Below -126.5,
+// -infinity (a key that is not seen) included: 0, as the exponent field of 2^-127 is; NaN stays NaN; above kPolyMax the
+// result means nothing.
 constexpr float kPolyMax = 100.f;
 __device__ __forceinline__ float max_or_nan(float a, float b) {
   float r;
@@ -106,8 +107,8 @@ __device__ __forceinline__ float max_or_nan(float a, float b) {
   return r;
 }
 __device__ __forceinline__ float2 ex2_fma2(float2 x) {
-  x.x = max_or_nan(x.x, -126.f);
-  x.y = max_or_nan(x.y, -126.f);
+  x.x = max_or_nan(x.x, -127.f);
+  x.y = max_or_nan(x.y, -127.f);
   const float2 t = __fadd2_rn(x, make_float2(12582912.f, 12582912.f));
   const float2 n = __fadd2_rn(t, make_float2(-12582912.f, -12582912.f));
   const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
@@ -618,8 +619,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       }
       // ---- result ----
       const float sum = l2.x + l2.y;
-      // no key seen: the sum is 0, or what ex2_fma2 makes of -infinity; but NaN is a result
-      bool none = !ok || sum == 0.f || (m == -INFINITY && sum == sum);
+      bool none = !ok || sum == 0.f;  // no key seen (NaN is a result)
       const bool wrote = nt > first;  // the group has an O
       if (ok && wrote) ok = __all_sync(0xffffffffu, wait_or_abort(&sh.o_final[g], 0, abort_flag));
       float* join = reinterpret_cast<float*>(q_tiles);  // [2][128]

@@ -101,3 +101,40 @@ def test_infinite_own_values_behind_a_prefix(pkg, fmt, group, n):
             want = ref.attend(q[last:last + 1].double().cpu().numpy(), kk, vv, [pre + own], float(np.float32(1 / math.sqrt(dim))), fmt, fmt)
             assert np.isposinf(want[0][0, :, 5 + b]).all()
             ref.compare(out[last:last + 1], want[0], want[2], "last token of sequence %d" % b)
+
+
+@pytest.mark.parametrize("fmt,q_dtype", FORMATS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("group,n,own", [(1, 5, 30), (1, 16, 40), (1, 40, 100), (2, 90, 200), (1, 150, 700), (1, 300, 300)])
+def test_hidden_keys_weigh_nothing(pkg, fmt, q_dtype, dim, group, n, own):
+    """Values of the largest magnitudes in the rows of later tokens: tokens before them see nothing of it."""
+    pre, rows = 20, 20 + own
+    big = 57344.0 if fmt == "kv8" else 3.0e38
+    k, v = (_normal(s, rows, 1, dim).to(DT.get(fmt, torch.bfloat16)) for s in (1, 2))
+    v[rows - n + 1:] = big  # the rows of all tokens but the first
+    store, k64, v64 = _store(pkg, fmt, k, v)
+    q = _normal(3, n, group, dim).to(DT[q_dtype]).cuda()
+    for most in (pre, 5000):
+        out, lse = torch.empty_like(q), torch.empty((n, group), dtype=torch.float32, device="cuda")
+        store.prefix_attend(q, _i64([0]), _i32([pre]), _i64([pre]), _i32([own]), out, max_prefix=most, max_own=own, cu_q=_i32([0, n]),
+                            max_q=n, lse=lse)
+        assert store.status() == 0
+        want = ref.attend(q[:1].double().cpu().numpy(), k64, v64, [rows - n + 1], float(np.float32(1 / math.sqrt(dim))), fmt, q_dtype)
+        ref.compare(out[:1], want[0], want[2], "first token")
+        ref.compare(lse[:1], want[1], want[3], "lse of the first token")
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n,length", [(1, 60), (16, 60), (17, 60), (150, 60), (150, 700)])
+def test_keys_with_logits_of_minus_infinity_weigh_nothing(pkg, dim, n, length):
+    k, v = (_normal(s, length, 1, dim).bfloat16() for s in (1, 2))
+    off = torch.arange(length) % 3 != 0
+    k[off, 0, 0] = -math.inf
+    v[off] = 3.0e38
+    store, k64, v64 = _store(pkg, "bf16", k, v)
+    q = _normal(3, n, 1, dim).abs().bfloat16().cuda()
+    out, lse = _attend(store, q, [0], [length], n)
+    on = ~off.numpy()
+    want = ref.attend(q.double().cpu().numpy(), k64[on], v64[on], [int(on.sum())] * n, float(np.float32(1 / math.sqrt(dim))), "bf16", "bf16")
+    ref.compare(out, want[0], want[2], "out")
+    ref.compare(lse, want[1], want[3], "lse")
