@@ -12,8 +12,8 @@
 // With rows on M a single row would leave 15 of 16 lanes' work unused; on N it is 7 of 8, and the accumulator of a row
 // is half as many registers.  P leaves S^T's accumulators transposed (movmatrix), with no trip through shared memory.
 //
-// The reference maximum moves only when a logit exceeds it by 8 (base 2), which a warp vote finds: in steady state no
-// shuffle and no rescaling.  Sums are kept per lane and added at the end.
+// The reference maximum (8-bit rows: 7 less) moves only when a logit exceeds it by 8 (base 2), which a warp vote finds: in
+// steady state no shuffle and no rescaling.  Sums are kept per lane and added at the end.
 //
 // bfloat16 rows: P = bf16 hi + bf16 lo (two products), so that its rounding (2^-8) does not add to the output's.  hi lies
 // below P, so lo is positive like P: a value of infinity in V then gives that infinity in both products (a lo of 0 or
@@ -39,6 +39,10 @@ constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kKeys = kFewBoxRows;                  // keys of a tile
 constexpr uint32_t kSpin = 1u << 22;
 constexpr float kRescale = 8.f;
+// 8-bit rows: how far (base 2) the reference lies below the maximum.  In f16 whatever is below 2^-25 becomes 0: with at least
+// 2^7 for the largest probability that is 2^-32 of it, so 2^20 such keys that go missing weigh 2^-12.  The largest
+// is 2^(7 + 8), inside f16's range.
+constexpr float kHeadF16 = 7.f;
 // Shared memory of a block's rings (KB), and blocks on an SM that its registers and the splitting of the keys count on (one
 // more fits where the code takes fewer), for blocks of up to 8 nt rows.  bfloat16, one query row (64 sequences of up to 2048
 // rows, 32 heads / 32 of 4096, 4 heads of 8 query heads / 64 behind a prefix of 8192): 96 KB and 2 blocks 193 / 37.8 / 88.6
@@ -136,6 +140,7 @@ template <int FMT, int D, int NT, int NTB, bool WALK>
 __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* map_k, const CUtensorMap* map_v,
                                        const AttendPart& part, unsigned block, unsigned char* ring, Shared<NTB>& sh) {
   constexpr bool kF16 = FMT == H2O_KV8;
+  constexpr float kHead = kF16 ? kHeadF16 : 0.f;
   constexpr int kTile = tile_bytes(FMT, D), kSlots = ring_slots(FMT, D, NTB), kSteps = D / 16, kRows = 8 * NT;
   constexpr int kPitch = D + 4;  // floats per row of a warp's partial output
   static_assert(kRows * kPitch * 4 <= kSlots * kTile, "a warp's partial output fits its ring");
@@ -360,7 +365,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
             if (key >= (in_prefix ? pre : min(seen[nt][e & 1], key1))) x = -INFINITY;
           }
           s[mt][nt][e] = x;
-          grows |= x > m[nt][e & 1] + kRescale;
+          grows |= x > m[nt][e & 1] + (kRescale + kHead);
         }
     }
     if (__any_sync(0xffffffffu, grows)) {
@@ -372,7 +377,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-          const float mn = fmaxf(m[nt][e], top);
+          const float mn = fmaxf(m[nt][e], top - kHead);
           const float alpha = mn == -INFINITY ? 1.f : ex2(m[nt][e] - mn);
           l[nt][e] *= alpha;
           m[nt][e] = mn;

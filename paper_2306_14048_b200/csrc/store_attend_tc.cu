@@ -20,9 +20,9 @@
 // issuers have few: K and V of a tile arrive on one barrier, and P V waits for P alone, which comes after S and so after
 // the tile.  Their loops run on values the compiler knows to be uniform (constant tensor-memory addresses, counts from a
 // shuffle): 575 -> 550 us.
-// The reference m of a row is the maximum of its first tile.  Later tiles compute their exponentials against it without
-// looking for a maximum: only when a tile's sum comes out large (kLargeSum) the tile is done again with the new
-// maximum and O is rescaled.  A value far above the reference costs no precision in floating point, only range.
+// The reference m of a row is the maximum of its first tile (8-bit rows: 7 less).  Later tiles compute their exponentials
+// against it without looking for a maximum: only when a tile's sum comes out large (kLargeSum) the tile is done again with
+// the new maximum and O is rescaled.  A value far above the reference costs no precision in floating point, only range.
 //
 // Rounding: P is one bf16 (8-bit rows: one f16).  Its error, 2^-9 relative per key and of either sign, averages over
 // the keys to about that of the output's own rounding; a second product for the remainder would cost half as much tensor
@@ -126,7 +126,12 @@ constexpr float kRescale = 8.f;
 // A tile whose sum against the old reference exceeds this is done again against its own maximum: far inside the range of
 // fp32 and bf16; of f16 (largest 65504) for the 8-bit rows.
 template <int FMT>
-constexpr float kLargeSumOf = FMT == H2O_KV8 ? 4096.f : 1.0e12f;
+constexpr float kLargeSumOf = FMT == H2O_KV8 ? 32768.f : 1.0e12f;
+// How far (base 2) the reference lies below the maximum it was taken from.  In f16 whatever is below 2^-25 becomes 0: with 2^7
+// for the largest probability that is 2^-32 of it, so 2^20 such keys that go missing weigh 2^-12.  A first tile's sum
+// (80 x 2^7) and what is done again (2^7 x 2^kRescale) stay below the limit.
+template <int FMT>
+constexpr float kHeadOf = FMT == H2O_KV8 ? 7.f : 0.f;
 
 // 32-byte global load: a whole sector, where neighbouring threads read rows far apart (the address is 32-byte aligned)
 __device__ __forceinline__ void ld_global_256(const float* p, float4& a, float4& b) {
@@ -206,7 +211,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                  const __grid_constant__ AttendView a, int part_index) {
   constexpr bool kF16 = FMT == H2O_KV8;
   constexpr int kN = tile_keys(FMT, D, G), kTile = tile_bytes(FMT, D, G), kQTile = kM * D * 2, kStages = stages(FMT, D, G), kRaw = kN * D;
-  constexpr float kLargeSum = kLargeSumOf<FMT>;
+  constexpr float kLargeSum = kLargeSumOf<FMT>, kHead = kHeadOf<FMT>;
   // tensor memory: O, S (starts on multiples of 32 columns) and P (of 8) of the groups
   constexpr uint32_t kColO = 0, kStepO = D, kColS = G * D, kStepS = 96, kColP = kColS + kStepS * (G - 1) + kN, kStepP = kN / 2;
   constexpr uint32_t kCols = G == 2 ? 512 : 256;
@@ -591,7 +596,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll
           for (int e = 0; e < kN; e += 2) top = max3(top, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
           top *= factor;  // (the factor is positive: the maximum commutes with it)
-          const float mn = top > m + kRescale ? top : m;
+          const float mn = top - kHead > m + kRescale ? top - kHead : m;
           const float alpha = mn == -INFINITY ? 1.f : ex2(m - mn);
           l2 = __fmul2_rn(l2, make_float2(alpha, alpha));
           m = mn;

@@ -138,3 +138,37 @@ def test_keys_with_logits_of_minus_infinity_weigh_nothing(pkg, dim, n, length):
     want = ref.attend(q.double().cpu().numpy(), k64[on], v64[on], [int(on.sum())] * n, float(np.float32(1 / math.sqrt(dim))), "bf16", "bf16")
     ref.compare(out, want[0], want[2], "out")
     ref.compare(lse, want[1], want[3], "lse")
+
+
+@pytest.mark.parametrize("q_dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("at", [0, 130000])
+@pytest.mark.parametrize("tokens,n", [(700, 1), (20000, 20000)])
+def test_many_small_probabilities_add_up_on_8_bit_rows(pkg, q_dtype, at, tokens, n):
+    """One key with a logit of 26 (base 2) above 2^18 others: each of those weighs 2^-26, all of them 2^-8.  So many query
+    rows that the keys are not split.
+
+    Tolerance: the probabilities are f16 operands, off by 2^-11 relative or 2^-25 of their unit where they are subnormal;
+    the unit is at most 2^-7 of the largest weight that it has met.  So 2^-32 per key, 2^-11 and the output's 2^-8 of the
+    result, and 2^-16 for sums and exponentials."""
+    if n > 1 and q_dtype == "f32":
+        tokens = n = 300  # (the kernel for float32 queries has no such operand and is slow)
+    length, dim = 1 << 18, 64
+    code = torch.zeros((1, length, dim), dtype=torch.uint8, device="cuda")
+    scale = torch.full((1, length), 127, dtype=torch.uint8, device="cuda")
+    vcode = torch.full_like(code, 0x38)  # 1.0
+    code[0, at, 0], vcode[0, at] = 0x38, 0
+    store = pkg.H2OStore(code, vcode, scale, scale.clone())
+    q = torch.zeros((tokens, 1, dim), dtype=DT[q_dtype], device="cuda")
+    q[:, 0, 0] = 26.0
+    c = math.log(2.0)
+    if n == 1:
+        out, lse = _attend(store, q, [0] * tokens, [length] * tokens, 1, c)
+    else:
+        out, lse = _attend(store, q, [0], [length], n, c)
+    x = 26.0 * float(np.float32(c))
+    others = (length - 1) * math.exp(-x)
+    want = others / (1.0 + others)
+    got = out.double()
+    tol = length * 2.0 ** -32 + want * (2.0 ** -11 + 2.0 ** -8 + 2.0 ** -16)
+    assert (got - want).abs().max().item() <= tol, ((got - want).abs().max().item(), tol, want)
+    assert (lse.double() - (x + math.log1p(others))).abs().max().item() <= 2.0 ** -16 * x
