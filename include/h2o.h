@@ -439,7 +439,7 @@ typedef struct {
   const int32_t* cu_q; /* dev [batch + 1]: sequence b has tokens cu_q[b] .. cu_q[b + 1] - 1; NULL: token b alone */
   int64_t q_rows;      /* tokens in q and out                                                                */
   int64_t q_stride, out_stride; /* elements between tokens, 0: dense; multiples of 8                          */
-  float softmax_scale; /* c; <= 0 selects 1/sqrt(head_dim)                                                   */
+  float softmax_scale; /* c, at most 2e38; <= 0 selects 1/sqrt(head_dim)                                     */
   int32_t dtype;       /* of q and out: the store's format; H2O_F32 or H2O_BF16 for an H2O_KV8 store          */
   int32_t query_group; /* query heads per K/V head, 1 .. 32                                                  */
   int32_t batch;       /* sequences, 0 .. 65535                                                              */

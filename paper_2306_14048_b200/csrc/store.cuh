@@ -148,6 +148,12 @@ inline int64_t part_blocks(const AttendView& a, const AttendPart& p) {
 // has written, are cut to that range.
 __device__ __forceinline__ float kv8_scale(uint32_t byte) { return __uint_as_float(min(max(byte, 112u), 134u) << 23); }
 
+// Softmax scale (times log2(e)) times the power of two of an f16 query row.  Kept a normal number: a factor of 0 would make
+// NaN of a hidden key's -infinity, an infinite one of a logit of 0.  (Below the smallest one every logit is 0 up to 2^-100.)
+__device__ __forceinline__ float f16_row_factor(float scale2, int e2) {
+  return fminf(fmaxf(scale2 * __uint_as_float((uint32_t)(127 + e2) << 23), 1.17549435e-38f), 3.40282347e38f);
+}
+
 // Launches `kernel`, `early`: it may start before the kernel in front of it has ended.
 template <typename... Args>
 cudaError_t launch_kernel(void (*kernel)(Args...), dim3 grid, int threads, int smem, cudaStream_t stream, bool early, Args... args) {

@@ -65,11 +65,14 @@ int check_rows(const h2o_store_t* store, const void* k, const void* v, int dtype
   return H2O_OK;
 }
 
+// The softmax scale for logits in base 2.
+float base2(float scale) { return (float)((double)scale * 1.4426950408889634074); }
+
 int check_queries(const h2o_store_t* store, const h2o_queries_t* q) {
   if (!store || !q) return H2O_ERR_INVALID_ARG;
   if (q->batch < 0 || q->q_rows < 0 || q->max_q < 0 || q->q_stride < 0 || q->out_stride < 0) return H2O_ERR_INVALID_ARG;
   if (q->query_group < 1 || q->query_group > kMaxGroup) return q->query_group < 1 ? H2O_ERR_INVALID_ARG : H2O_ERR_UNSUPPORTED;
-  if (std::isnan(q->softmax_scale) || std::isinf(q->softmax_scale)) return H2O_ERR_INVALID_ARG;
+  if (std::isnan(q->softmax_scale) || std::isinf(base2(q->softmax_scale))) return H2O_ERR_INVALID_ARG;
   const h2o_store_config_t& c = store->cfg;
   if (q->dtype != H2O_F32 && q->dtype != H2O_BF16) return H2O_ERR_UNSUPPORTED;
   if (c.format != H2O_KV8 && q->dtype != c.format) return H2O_ERR_UNSUPPORTED;
@@ -171,7 +174,7 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
   a.max_q = std::min<int64_t>(q->max_q, q->q_rows);
   a.max_group = std::min(max_group, q->batch);
   const float scale = q->softmax_scale > 0.f ? q->softmax_scale : 1.0f / std::sqrt((float)a.dim);
-  a.scale2 = (float)((double)scale * 1.4426950408889634074);
+  a.scale2 = base2(scale);
   a.k = c.k;
   a.v = c.v;
   a.k_scale = c.k_scale;

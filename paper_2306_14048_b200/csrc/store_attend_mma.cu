@@ -221,7 +221,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
         b.y = pack_half2(__uint_as_float(raw[ks].y << 16) * down, __uint_as_float(raw[ks].y & 0xffff0000u) * down);
         sh.q[nt][ks][lane] = b;
       }
-      if (c4 == 0) sh.row_factor[r] = a.scale2 * __uint_as_float((uint32_t)(127 + e2) << 23);
+      if (c4 == 0) sh.row_factor[r] = f16_row_factor(a.scale2, e2);
     }
   }
   __syncthreads();

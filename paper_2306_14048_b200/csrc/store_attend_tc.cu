@@ -503,7 +503,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             const float down = __uint_as_float((uint32_t)(127 - e2) << 23);
             qx[i] = make_uint4(pack_half2(f[0] * down, f[1] * down), pack_half2(f[2] * down, f[3] * down),
                                pack_half2(f[4] * down, f[5] * down), pack_half2(f[6] * down, f[7] * down));
-            if (c == 0) sh.row_factor[base + rt] = a.scale2 * __uint_as_float((uint32_t)(127 + e2) << 23);
+            if (c == 0) sh.row_factor[base + rt] = f16_row_factor(a.scale2, e2);
           }
           st_shared16(operand_addr(tile, kM, rt, c), qx[i]);
         }

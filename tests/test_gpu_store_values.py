@@ -172,3 +172,22 @@ def test_many_small_probabilities_add_up_on_8_bit_rows(pkg, q_dtype, at, tokens,
     tol = length * 2.0 ** -32 + want * (2.0 ** -11 + 2.0 ** -8 + 2.0 ** -16)
     assert (got - want).abs().max().item() <= tol, ((got - want).abs().max().item(), tol, want)
     assert (lse.double() - (x + math.log1p(others))).abs().max().item() <= 2.0 ** -16 * x
+
+
+@pytest.mark.parametrize("fmt,q_dtype", FORMATS)
+@pytest.mark.parametrize("scale", [1e-16, 1e-30, 1e-38, 2e-45])
+@pytest.mark.parametrize("n", [1, 20, 70, 150])
+def test_tiny_softmax_scales(pkg, fmt, q_dtype, scale, n):
+    """Logits of 0 up to rounding: every key weighs the same, and what lies behind the range nothing.  Queries of zeros, tiny
+    ones and ordinary ones."""
+    dim, length = 64, 37
+    k, v = (_normal(s, length + 60, 1, dim).to(DT.get(fmt, torch.bfloat16)) for s in (1, 2))
+    store, k64, v64 = _store(pkg, fmt, k, v)
+    q = _normal(3, 3 * n, 1, dim)
+    q[:n] = 0.0
+    q[n:2 * n] *= 2.0 ** -110
+    q = q.to(DT[q_dtype]).cuda()
+    out, lse = _attend(store, q, [0] * 3, [length] * 3, n, scale)
+    want = ref.attend(q.double().cpu().numpy(), k64[:length], v64[:length], [length] * (3 * n), float(np.float32(scale)), fmt, q_dtype)
+    ref.compare(out, want[0], want[2], "out")
+    ref.compare(lse, want[1], want[3], "lse")
