@@ -417,6 +417,12 @@ typedef struct {
 } h2o_store_config_t;
 int h2o_store_create(h2o_store_t** out, const h2o_store_config_t* cfg);
 int h2o_store_destroy(h2o_store_t* store); /* the handle only; NULL is accepted */
+/*
+ * Diagnostic: the attention kernels of later calls on this store poll a wait `polls` times before it gives up (0: it gives up at
+ * once; < 0 or beyond the default: the default).  A block whose wait gives up waits for its own copies and products under
+ * way, leaves H2O_ERR_TIMEOUT in the status word and returns; outputs of such a call mean nothing, the context stays usable.
+ */
+int h2o_debug_store_set_polls(h2o_store_t* store, int32_t polls);
 
 /*
  * Quantise n_tokens rows as they are written into an H2O_KV8 store / read rows of one back (H2O_ERR_UNSUPPORTED for

@@ -53,6 +53,7 @@ EXPORTED = (
     "h2o_prefill_scratch_layout",
     "h2o_store_create",
     "h2o_store_destroy",
+    "h2o_debug_store_set_polls",
     "h2o_store_write",
     "h2o_store_read",
     "h2o_cross_scratch_bytes",
@@ -187,6 +188,8 @@ def _load() -> ctypes.CDLL:
     lib.h2o_store_create.argtypes = [c.POINTER(vp), c.POINTER(h2o_store_config_t)]
     lib.h2o_store_destroy.restype = c.c_int
     lib.h2o_store_destroy.argtypes = [vp]
+    lib.h2o_debug_store_set_polls.restype = c.c_int
+    lib.h2o_debug_store_set_polls.argtypes = [vp, c.c_int32]
     for f in (lib.h2o_store_write, lib.h2o_store_read):
         f.restype = c.c_int
         f.argtypes = [vp, vp, vp, c.c_int32, c.c_int64, c.c_int64, vp, c.c_int64, vp]

@@ -13,6 +13,7 @@
 // The handle: host memory only.
 struct h2o_store {
   h2o_store_config_t cfg;  // strides filled in
+  uint32_t polls;          // of a wait before it gives up
   // tensor maps of the rows (opaque here): boxes for few query rows, and for many in blocks of one and of two groups
   alignas(64) unsigned char few_k[128], few_v[128], one_k[128], one_v[128], two_k[128], two_v[128];
 };
@@ -20,6 +21,9 @@ struct h2o_store {
 namespace h2o {
 
 constexpr int kMaxSplits = 64;  // of a part's keys
+// Polls of a wait before it gives up (tens of milliseconds; what is waited for takes microseconds), and of the waits for a
+// block's own copies and products that end a block that has given up.
+constexpr uint32_t kStorePolls = 1u << 22;
 
 struct AttendPart {
   const int64_t* begin;    // dev [problems]: first store row
@@ -53,6 +57,7 @@ struct AttendView {
   int early, finish;
   int walk;  // 1: part 1's blocks take the prefix as well, and nothing else is launched (few rows of the mma.sync kernel)
   int32_t* status;
+  uint32_t polls;  // of a wait before it gives up
   int n_parts;
   AttendPart part[2];
 };

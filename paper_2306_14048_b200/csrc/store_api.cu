@@ -182,6 +182,7 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
   a.rows = c.rows;
   a.row_stride = c.row_stride;
   a.status = c.status;
+  a.polls = store->polls;
   int n = 0;
   for (int k = 0; k < 2; ++k) {
     const h2o_ranges_t* r = k == 0 ? prefix : own;
@@ -305,6 +306,7 @@ int h2o_store_create(h2o_store_t** out, const h2o_store_config_t* cfg) {
   h2o_store* s = new (std::nothrow) h2o_store();
   if (!s) return H2O_ERR_INVALID_ARG;
   s->cfg = *cfg;
+  s->polls = h2o::kStorePolls;
   if (s->cfg.row_stride == 0) s->cfg.row_stride = (int64_t)cfg->n_heads * cfg->head_dim;
   // the kernels for bfloat16 queries read the rows by TMA
   if (cfg->format != H2O_F32) {
@@ -330,6 +332,12 @@ int h2o_store_create(h2o_store_t** out, const h2o_store_config_t* cfg) {
 
 int h2o_store_destroy(h2o_store_t* store) {
   delete store;
+  return H2O_OK;
+}
+
+int h2o_debug_store_set_polls(h2o_store_t* store, int32_t polls) {
+  if (!store) return H2O_ERR_INVALID_ARG;
+  store->polls = polls < 0 ? h2o::kStorePolls : std::min((uint32_t)polls, h2o::kStorePolls);
   return H2O_OK;
 }
 

@@ -37,7 +37,6 @@ using namespace ptx;
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kKeys = kFewBoxRows;                  // keys of a tile
-constexpr uint32_t kSpin = 1u << 22;
 constexpr float kRescale = 8.f;
 // 8-bit rows: how far (base 2) the reference lies below the maximum.  In f16 whatever is below 2^-25 becomes 0: with at least
 // 2^7 for the largest probability that is 2^-32 of it, so 2^20 such keys that go missing weigh 2^-12.  The largest
@@ -58,8 +57,8 @@ __host__ __device__ constexpr int ring_slots(int fmt, int d, int nt) {
   return ring_kb(fmt, nt) * 1024 / kWarps / tile_bytes(fmt, d) < kMaxSlots ? ring_kb(fmt, nt) * 1024 / kWarps / tile_bytes(fmt, d) : kMaxSlots;
 }
 
-__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
-  for (uint32_t it = 0; it < kSpin; ++it)
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, uint32_t polls) {
+  for (uint32_t it = 0; it < polls; ++it)
     if (mbar_try_wait(bar, parity)) return true;
   return false;
 }
@@ -119,6 +118,7 @@ template <int NT>  // the kernel's larger number of n-tiles
 struct Shared {
   uint64_t full[kWarps][kMaxSlots];
   float m[kWarps][8 * NT], l[kWarps][8 * NT];  // the warps' statistics, per row
+  int gave_up;                          // a wait of some warp has
   float row_factor[8 * NT];                // softmax scale times log2(e) (times the row's power of two)
   float k_factor[kWarps][kKeys];       // 8-bit rows: K's power of two of each key of the warp's tile
   __half v_factor[kWarps][kKeys];
@@ -172,6 +172,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
     mbar_expect_tx(&full[i % kSlots], kTile);
     tma_4d(my_ring + (i % kSlots) * kTile, (i & 1) ? map_v : map_k, row, w.head, &full[i % kSlots]);
   };
+  if (threadIdx.x == 0) sh.gave_up = 0;
   if (lane == 0) {
     for (int s = 0; s < kSlots; ++s) mbar_init(&full[s], 1);
     fence_barrier_init();
@@ -251,7 +252,10 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[ct][nt][e] = 0.f;
   }
-  bool timed_out = false;
+  // Items this lane would ask for; -1 - i once its wait for item i has given up.  Nothing is asked for from then on (lane 0
+  // asks, and has seen every item before arrive), and the warp leaves the loop at the next vote: a vote for each wait costs
+  // an 8-bit step as much again as this (39.4 us without, 40.0 and 40.3).
+  int limit = 2 * mine;
   // 8-bit rows: the scale bytes of the warp's next tile, one key per lane
   uint32_t scale_k = 127, scale_v = 127;
   auto fetch_scales = [&](int j) {
@@ -268,7 +272,8 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
     if (mine > 0) fetch_scales(0);
   }
 
-  for (int j = 0; j < mine; ++j) {
+  int j = 0;
+  for (; j < mine; ++j) {
     const int tile_no = warp + kWarps * j;
     const bool in_prefix = WALK && tile_no < pre_tiles;
     const int tile_key = in_prefix ? tile_no * kKeys : key0 + (tile_no - pre_tiles) * kKeys, end = in_prefix ? pre : key1;
@@ -289,7 +294,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
         for (int e = 0; e < 4; ++e) s[mt][nt][e] = 0.f;
     {
       const int i = 2 * j, slot = i % kSlots;
-      if (!wait(&full[slot], (uint32_t)(i / kSlots) & 1u)) timed_out = true;
+      if (!wait(&full[slot], (uint32_t)(i / kSlots) & 1u, a.polls) && limit >= 0) limit = -1 - i;
       const uint32_t tile = smem_u32(my_ring + slot * kTile);
       if constexpr (!kF16) {
 #pragma unroll
@@ -341,7 +346,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
         }
       }
       __syncwarp();
-      if (lane == 0 && i + kSlots < 2 * mine) issue(i + kSlots);
+      if (lane == 0 && i + kSlots < limit) issue(i + kSlots);
     }
     // ---- logits (base 2); lane: keys gl, gl + 8 (+ 16 mt), rows 2 c4, 2 c4 + 1 (+ 8 nt) ----
     const bool masked = tile_key + kKeys > (in_prefix ? pre : min(first_seen, key1));
@@ -368,7 +373,8 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
           grows |= x > m[nt][e & 1] + (kRescale + kHead);
         }
     }
-    if (__any_sync(0xffffffffu, grows)) {
+    if (__any_sync(0xffffffffu, grows || limit < 0)) {
+      if (__any_sync(0xffffffffu, limit < 0)) break;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -413,7 +419,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
     // ---- O^T += V^T P^T ----
     {
       const int i = 2 * j + 1, slot = i % kSlots;
-      if (!wait(&full[slot], (uint32_t)(i / kSlots) & 1u)) timed_out = true;
+      if (!wait(&full[slot], (uint32_t)(i / kSlots) & 1u, a.polls) && limit >= 0) limit = -1 - i;
       const uint32_t tile = smem_u32(my_ring + slot * kTile);
       if (there < kKeys) {
         // rows behind the range may hold anything, and 0 * NaN must not reach the sums
@@ -465,10 +471,18 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
       }
       if (WALK && there < kKeys) fence_proxy_async();  // (the zeros come before the copy that may go over them)
       __syncwarp();
-      if (lane == 0 && i + kSlots < 2 * mine) issue(i + kSlots);
+      if (lane == 0 && i + kSlots < limit) issue(i + kSlots);
     }
   }
-  if (timed_out && a.status) atomicCAS(a.status, 0, H2O_ERR_TIMEOUT);
+  if (__any_sync(0xffffffffu, limit < 0)) {
+    if (lane == 0) {  // the block does not end before the copies under way
+      const int taken = limit < 0 ? -1 - limit : min(2 * mine, 2 * j + 1);
+      for (int i = taken; i < min(2 * mine, taken + kSlots); ++i) wait(&full[i % kSlots], (uint32_t)(i / kSlots) & 1u, kStorePolls);
+      sh.gave_up = 1;
+      if (a.status) atomicCAS(a.status, 0, H2O_ERR_TIMEOUT);
+    }
+    __syncwarp();
+  }
 
   // ---- the warps' results, joined through shared memory (each warp over its own ring) ----
   float* my_o = reinterpret_cast<float*>(my_ring);
@@ -492,6 +506,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
       }
     }
   __syncthreads();
+  if (sh.gave_up) return;  // (the same for the whole block)
   constexpr int kLanes = D / 4;  // threads of a row, four channels each
   for (int r = threadIdx.x / kLanes; r < n_rows; r += kThreads / kLanes) {
     const int c = (threadIdx.x % kLanes) * 4;

@@ -72,14 +72,17 @@ struct Shared {
   uint64_t p_full[2], p_empty[2];  // P is complete / used, and O includes it
   uint64_t o_final[2];
   uint64_t tail;  // the last V tile has been cleared behind the range
+  uint64_t ended;  // of a block that gives up: the products of warps 1 to 3 have ended
   uint32_t tmem_base;
   int abort_flag;
+  int loads;  // tiles that TMA has been asked for
   float row_factor[2 * kM];  // 8-bit rows: softmax scale times the query row's power of two
   __half scale[2][2][96];    // 8-bit rows: the powers of two of K and V of the tile being converted
 };
 
-__device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  for (uint32_t it = 0; it < kSpinLimit; ++it) {
+// Up to `polls` polls, or until another wait of the block has given up.
+__device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint32_t polls) {
+  for (uint32_t it = 0; it < polls; ++it) {
     if (mbar_try_wait(bar, parity)) return true;
     if ((it & 1023u) == 1023u && *abort_flag) return false;
   }
@@ -248,6 +251,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       mbar_init(&sh.raw_empty[i], 8);
     }
     mbar_init(&sh.tail, 1);
+    mbar_init(&sh.ended, 3);
     sh.abort_flag = 0;
     fence_barrier_init();
   }
@@ -321,16 +325,17 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     if (warp == 0) {
       // ---- TMA ----
       if (lane == 0) {
-        int slot = 0;
+        int slot = 0, j = 0;
         uint32_t phase = 1;
-        for (int j = 0; j < nt; ++j) {
-          if (!wait_or_abort(kF16 ? &sh.raw_empty[slot] : &sh.kv_empty[slot], phase, abort_flag)) break;
+        for (; j < nt; ++j) {
+          if (!wait_or_abort(kF16 ? &sh.raw_empty[slot] : &sh.kv_empty[slot], phase, abort_flag, a.polls)) break;
           load_tile(j, slot);
           if (++slot == n_load) {
             slot = 0;
             phase ^= 1;
           }
         }
+        sh.loads = j;
       }
     } else if (warp < 1 + G) {
       // ---- S of group g (the whole warp walks, one elected lane issues) ----
@@ -339,7 +344,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const int g = warp - 1, first = alt ? g : 0, step = alt ? 2 : 1;
       const uint32_t d_s = tmem + kColS + kStepS * g;
       const uint64_t dq = smem_desc_sw128(smem_u32(q_tiles + (alt ? 0 : g) * kQTile), 16, 1024);
-      bool ok = first >= nt || wait_or_abort(&sh.q_full[alt ? 0 : g], 0, abort_flag);
+      bool ok = first >= nt || wait_or_abort(&sh.q_full[alt ? 0 : g], 0, abort_flag, a.polls);
       int slot = first;
       uint32_t phase = 0;
       for (int j = first, n = 0; j < nt; j += step, ++n) {
@@ -347,8 +352,8 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           slot -= n_stages;
           phase ^= 1;
         }
-        ok = ok && wait_or_abort(&sh.kv_full[slot], phase, abort_flag);
-        if (n > 0) ok = ok && wait_or_abort(&sh.s_read[g], (uint32_t)(n - 1) & 1u, abort_flag);
+        ok = ok && wait_or_abort(&sh.kv_full[slot], phase, abort_flag, a.polls);
+        if (n > 0) ok = ok && wait_or_abort(&sh.s_read[g], (uint32_t)(n - 1) & 1u, abort_flag, a.polls);
         ok = __all_sync(0xffffffffu, ok) != 0;
         if (!ok) break;
         tc_fence_after();
@@ -363,7 +368,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.tail);
           } else {
-            ok = __all_sync(0xffffffffu, wait_or_abort(&sh.tail, 0, abort_flag)) != 0;
+            ok = __all_sync(0xffffffffu, wait_or_abort(&sh.tail, 0, abort_flag, a.polls)) != 0;
             if (!ok) break;
           }
         }
@@ -391,7 +396,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         const int n = alt ? j >> 1 : j;  // the group's own count
         const uint64_t dv = smem_desc_sw128(smem_u32(ring + (2 * slot + 1) * kTile), kTile / 2, 1024);
         for (int g = alt ? j & 1 : 0; g < (alt ? (j & 1) + 1 : G); ++g) {
-          ok = __all_sync(0xffffffffu, wait_or_abort(&sh.p_full[g], (uint32_t)n & 1u, abort_flag)) != 0;
+          ok = __all_sync(0xffffffffu, wait_or_abort(&sh.p_full[g], (uint32_t)n & 1u, abort_flag, a.polls)) != 0;
           if (!ok) break;
           tc_fence_after();
           const uint32_t d_o = tmem + kColO + kStepO * g, d_p = tmem + kColP + kStepP * g;
@@ -433,8 +438,8 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (t < kN) sh.scale[j & 1][kv][t] = __float2half_rn(kv8_scale(byte));
         byte = byte_next;
         byte_next = fetch(j + 2);
-        bool ok = raw_there || wait_or_abort(&sh.raw_full[rs], (uint32_t)(j / kRawStages) & 1u, abort_flag);
-        ok = ok && (slot_free || wait_or_abort(&sh.kv_empty[slot], phase, abort_flag));
+        bool ok = raw_there || wait_or_abort(&sh.raw_full[rs], (uint32_t)(j / kRawStages) & 1u, abort_flag, a.polls);
+        ok = ok && (slot_free || wait_or_abort(&sh.kv_empty[slot], phase, abort_flag, a.polls));
         ok = together(ok, kv);  // (also publishes the scales; one answer for the four warps, so that none waits for another)
         if (ok) {
           // the next tile's waits, asked ahead (the conversion hides the answers' way)
@@ -537,10 +542,10 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       using N1 = std::integral_constant<int, kN * 3 / 8>;
       using N2 = std::integral_constant<int, kN / 2>;
       for (int j = first, n = 0; j < nt; j += step, ++n) {
-        ok = __all_sync(0xffffffffu, wait_or_abort(&sh.s_full[g], (uint32_t)n & 1u, abort_flag));
+        ok = __all_sync(0xffffffffu, wait_or_abort(&sh.s_full[g], (uint32_t)n & 1u, abort_flag, a.polls));
         if (!ok) break;
         if (idle) {  // none of the warp's rows exists: whatever P holds there goes into rows of O that nobody reads
-          if (n > 0) ok = __all_sync(0xffffffffu, wait_or_abort(&sh.p_empty[g], (uint32_t)(n - 1) & 1u, abort_flag));
+          if (n > 0) ok = __all_sync(0xffffffffu, wait_or_abort(&sh.p_empty[g], (uint32_t)(n - 1) & 1u, abort_flag, a.polls));
           if (!ok) break;
           if (lane == 0) {
             mbar_arrive(&sh.s_read[g]);
@@ -586,7 +591,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           // Has P(j - 1) been used (and does O include it)?  Asked ahead: the last exponentials hide the answer's way.
           const bool used = mbar_test_wait(&sh.p_empty[g], (uint32_t)(n - 1) & 1u);
           sum = __fadd2_rn(sum, exponentials(N1{}, N2{}));
-          if (!used) ok = wait_or_abort(&sh.p_empty[g], (uint32_t)(n - 1) & 1u, abort_flag);
+          if (!used) ok = wait_or_abort(&sh.p_empty[g], (uint32_t)(n - 1) & 1u, abort_flag, a.polls);
           again = m == -INFINITY || sum.x + sum.y > kLargeSum;
         }
         if (__any_sync(0xffffffffu, again || !ok)) {
@@ -626,10 +631,10 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const float sum = l2.x + l2.y;
       bool none = !ok || sum == 0.f;  // no key seen (NaN is a result)
       const bool wrote = nt > first;  // the group has an O
-      if (ok && wrote) ok = __all_sync(0xffffffffu, wait_or_abort(&sh.o_final[g], 0, abort_flag));
+      if (ok && wrote) ok = __all_sync(0xffffffffu, wait_or_abort(&sh.o_final[g], 0, abort_flag, a.polls));
       float* join = reinterpret_cast<float*>(q_tiles);  // [2][128]
       if (alt) {  // B leaves m, sum (over Q) and O (over the K/V ring: both groups are done with them), A joins them
-        if (g == 1 && ok && nt > 0) ok = __all_sync(0xffffffffu, wait_or_abort(&sh.o_final[0], 0, abort_flag));
+        if (g == 1 && ok && nt > 0) ok = __all_sync(0xffffffffu, wait_or_abort(&sh.o_final[0], 0, abort_flag, a.polls));
         tc_fence_after();
         float* theirs = reinterpret_cast<float*>(ring) + rt * (D + 4);
         if (g == 1) {
@@ -648,6 +653,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           }
         }
         softmax_sync();
+        ok = __all_sync(0xffffffffu, ok && !*abort_flag) != 0;  // (A's result needs B's)
       }
       if (ok && !(alt && g == 1)) {
         tc_fence_after();
@@ -768,7 +774,20 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   }
   tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && sh.abort_flag && a.status) atomicCAS(a.status, 0, H2O_ERR_TIMEOUT);
+  if (sh.abort_flag) {  // the block ends after its copies and products under way (each waited for with a limit)
+    if (warp == 0) {
+      for (int j = max(0, sh.loads - n_load); j < sh.loads; ++j) {
+        uint64_t* full = kF16 ? &sh.raw_full[j % n_load] : &sh.kv_full[j % n_load];
+        for (uint32_t it = 0; it < kStorePolls && !mbar_try_wait(full, (uint32_t)(j / n_load) & 1u); ++it) {}
+      }
+      if (lane == 0 && a.status) atomicCAS(a.status, 0, H2O_ERR_TIMEOUT);
+    } else if (warp <= 3) {
+      if (elect_one()) mma_commit(&sh.ended);
+      __syncwarp();
+      for (uint32_t it = 0; it < kStorePolls && !mbar_try_wait(&sh.ended, 0); ++it) {}
+    }
+    __syncthreads();
+  }
   if (warp == 3) {
     tc_fence_after();
     tmem_dealloc(tmem, kCols);

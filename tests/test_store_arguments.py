@@ -43,3 +43,10 @@ def test_softmax_scales_that_leave_fp32_are_refused(b, scale, rc):
     if rc == -1:
         assert b.lib.h2o_prefix_attend(h, ctypes.byref(q), ctypes.byref(r), 1, None, 1, ctypes.byref(r), None, 0, None) == rc
         assert b.lib.h2o_cross_scratch_bytes(h, ctypes.byref(q), ctypes.byref(r)) == 0
+
+
+def test_poll_limit_needs_a_store(b):
+    assert b.lib.h2o_debug_store_set_polls(None, 5) == -1
+    h, _ = _handle(b)
+    for polls in (0, 7, -1, 2 ** 31 - 1):
+        assert b.lib.h2o_debug_store_set_polls(h, polls) == 0
