@@ -611,7 +611,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             for (int cc = 0; cc < D / 16; ++cc) {
               uint32_t o[16];
               tmem_ld16(t_o + 16u * cc, o);
-              tmem_wait_ld();
+              tmem_wait_ld_of(o);
 #pragma unroll
               for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
               tmem_st16(t_o + 16u * cc, o);
@@ -645,7 +645,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             uint32_t o[32];
             if (wrote) {
               tmem_ld32(t_o + 32u * cc, o);
-              tmem_wait_ld();
+              tmem_wait_ld_of(o);
             }
 #pragma unroll
             for (int e = 0; e < 32; e += 4)
@@ -708,7 +708,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           uint32_t o[32];
           if (wrote) {
             tmem_ld32(t_o + 32u * cc, o);
-            tmem_wait_ld();
+            tmem_wait_ld_of(o);
           }
           if (!write) continue;
           // (a weight of 0 belongs to an O that was never written)
