@@ -110,17 +110,20 @@ inline cudaError_t ensure_dynamic_smem(const void* func, int bytes, unsigned lon
   return e;
 }
 
-// SMs of the current device (asked once per device; the dispatch thresholds of the launchers scale with it).
-inline int sm_count() {
+// SMs of a device (asked once per device; the dispatch thresholds of the launchers scale with it), and of the current one.
+inline int sm_count(int dev) {
   static int cached[64] = {};
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+  if (dev < 0 || dev >= 64) return 148;
   if (cached[dev] == 0) {
     int n = 0;
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 148;
     cached[dev] = n;
   }
   return cached[dev];
+}
+inline int sm_count() {
+  int dev = 0;
+  return cudaGetDevice(&dev) == cudaSuccess ? sm_count(dev) : 148;
 }
 
 // Launchers (each returns the cudaError_t of its launch).

@@ -156,6 +156,7 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
   Plan pl;
   std::memset(&pl, 0, sizeof(pl));
   const h2o_store_config_t& c = store->cfg;
+  const int sms = h2o::sm_count(c.device);
   h2o::AttendView& a = pl.a;
   a.q = q->q;
   a.out = q->out;
@@ -212,7 +213,7 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
     const int key_bytes = 2 * a.dim * (c.format == H2O_KV8 ? 1 : c.format == H2O_BF16 ? 2 : 4);
     const bool tiles = pl.kernel[n] == Kernel::Fma && pl.tile[n] >= 16;
     const int per_sm = pl.kernel[n] == Kernel::Tc2 ? 1 : pl.kernel[n] == Kernel::Tc1 || tiles ? 2 : pl.kernel[n] == Kernel::Fma ? 4 : h2o::attend_mma_blocks_per_sm(c.format, pl.tile[n]);
-    const int64_t room = (int64_t)h2o::sm_count() * per_sm;
+    const int64_t room = (int64_t)sms * per_sm;
     split_part(p, units, room, is_tc(pl.kernel[n]) ? 640 : tiles ? 36 : 19200000 / (room * key_bytes),
                tiles ? 64 : 128, !p.grouped);
     if (units * p.splits > INT32_MAX) pl.rc = H2O_ERR_UNSUPPORTED;
@@ -222,7 +223,7 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
   a.n_parts = n;
   if (n == 2 && pl.kernel[0] == Kernel::Mma && pl.kernel[1] == Kernel::Mma && pl.tile[1] == 8 &&
       (int64_t)a.part[0].max_length + a.part[1].max_length <= kWalkKeys &&
-      (int64_t)a.part[1].problems * a.part[1].row_tiles * a.heads <= 2 * h2o::sm_count()) {
+      (int64_t)a.part[1].problems * a.part[1].row_tiles * a.heads <= 2 * sms) {
     a.walk = 1;
     a.part[1].splits = 1;
     a.part[1].chunk = std::max(1, a.part[1].max_length);
