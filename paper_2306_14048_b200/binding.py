@@ -435,6 +435,14 @@ def _bad(why: str):
     raise ValueError("H2OStore: " + why)
 
 
+def _rows_alike(k, v, rows, heads, dim):
+    """Strides of k and v [rows, heads, dim]: dense heads and one row stride, as far as there is more than one of them.  A
+    broadcast over the rows is refused (a stride of 0 means dense to the library)."""
+    if rows == 0 or (k == v and k[2] == 1 and k[1] == dim and k[0] > 0):
+        return True
+    return k[2] == v[2] == 1 and (heads == 1 or k[1] == v[1] == dim) and (rows == 1 or k[0] == v[0] > 0)
+
+
 class H2OStore:
     """K/V rows that many queries read and nothing evicts (h2o_store_*): an encoder's states, a prompt that a batch
     shares, a sequence's own tokens.
@@ -464,7 +472,7 @@ class H2OStore:
             if k_scale is not None or v_scale is not None:
                 _bad("scales belong to 8-bit rows")
             self.rows, self.n_heads, self.head_dim = k.shape
-            if k.stride() != v.stride() or k.stride(2) != 1 or k.stride(1) != self.head_dim or (self.rows > 1 and k.stride(0) == 0):
+            if not _rows_alike(k.stride(), v.stride(), *k.shape):
                 _bad("rows of k and v must have one stride and dense heads")
         self.format = H2O_KV8 if eight else _DTYPES[k.dtype]
         self.device = k.device
@@ -499,7 +507,7 @@ class H2OStore:
         if dtype is None or v.dtype is not k.dtype or k.get_device() != self._index or v.get_device() != self._index:
             _bad("k and v must both be float32 or bfloat16 on %s" % self.device)
         n, stride = shape[0], k.stride()
-        if stride != v.stride() or (n and (stride[2] != 1 or stride[1] != self.head_dim)) or (n > 1 and stride[0] == 0):
+        if not _rows_alike(stride, v.stride(), *shape):
             _bad("k and v must have one token stride and dense heads")
         if rows is not None and (rows.dtype is not torch.int64 or rows.shape != (n,) or rows.get_device() != self._index or not rows.is_contiguous()):
             _bad("rows must be a contiguous int64 [tokens] on %s" % self.device)
@@ -517,7 +525,7 @@ class H2OStore:
         if q.get_device() != self._index or out.get_device() != self._index:
             _bad("q and out must be on %s" % self.device)
         s, o = q.stride(), out.stride()
-        if tokens and (s[2] != 1 or s[1] != dim or o[2] != 1 or o[1] != dim):
+        if tokens and (s[2] != 1 or o[2] != 1 or (heads > 1 and (s[1] != dim or o[1] != dim))):
             _bad("q and out must have dense heads")
         if tokens > 1 and (s[0] == 0 or o[0] == 0):  # (0 means dense to the library)
             _bad("q and out must not be broadcast over the tokens")
