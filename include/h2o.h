@@ -394,7 +394,8 @@ const char* h2o_strerror(int code);
  *   format H2O_F32, H2O_BF16: k, v dev [rows, n_heads, head_dim], `row_stride` elements from row to row (0: dense;
  *     a multiple of 8 otherwise).  The caller writes these rows itself.
  *   format H2O_KV8: k, v dev uint8 [n_heads, rows, head_dim] e4m3 codes and k_scale, v_scale dev uint8
- *     [n_heads, rows], dense: value = code * 2^(scale - 127).  Written by h2o_store_write.
+ *     [n_heads, rows], dense: value = code * 2^(scale - 127).  Written by h2o_store_write, whose scales are 112 .. 134;
+ *     of a caller's own, one below counts as 112 and one above as 134 (the values would not fit f16).
  *
  * H2O_KV8 quantisation, per row of a head (this library's own): a = the largest finite magnitude; e = the smallest
  * integer in [-15, 7] with a <= 448 * 2^e; code = x * 2^-e rounded to e4m3 (nearest, ties to even), magnitudes beyond

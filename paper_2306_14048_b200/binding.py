@@ -448,7 +448,8 @@ class H2OStore:
     shares, a sequence's own tokens.
 
     ``k``, ``v``: float32 or bfloat16 [rows, heads, head_dim] (rows may be strided), or uint8 e4m3 codes
-    [heads, rows, head_dim] with ``k_scale``, ``v_scale`` uint8 [heads, rows].  The tensors stay the caller's (this
+    [heads, rows, head_dim] with ``k_scale``, ``v_scale`` uint8 [heads, rows] (value = code * 2^(scale - 127), scales
+    outside 112 .. 134 as the nearer of the two).  The tensors stay the caller's (this
     object keeps a reference) and are read where they lie.  Methods mirror the C calls: ``write`` ->
     h2o_store_write, ``read`` -> h2o_store_read, ``cross_attend`` -> h2o_cross_attend, ``prefix_attend`` ->
     h2o_prefix_attend, ``close`` -> h2o_store_destroy.  Results go to tensors that the caller passes; scratch comes

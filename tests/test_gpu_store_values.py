@@ -191,3 +191,25 @@ def test_tiny_softmax_scales(pkg, fmt, q_dtype, scale, n):
     want = ref.attend(q.double().cpu().numpy(), k64[:length], v64[:length], [length] * (3 * n), float(np.float32(scale)), fmt, q_dtype)
     ref.compare(out, want[0], want[2], "out")
     ref.compare(lse, want[1], want[3], "lse")
+
+
+@pytest.mark.parametrize("q_dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n", [1, 20, 70, 150])
+def test_scale_bytes_outside_the_format_count_as_the_nearest_inside(pkg, q_dtype, dim, n):
+    """A caller's own codes and scales: every byte as a scale, read back and attended."""
+    rows = 256
+    g = torch.Generator().manual_seed(5)
+    code = torch.randint(0, 0x7F, (2, 1, rows, dim), generator=g, dtype=torch.uint8) | (torch.randint(0, 2, (2, 1, rows, dim), generator=g, dtype=torch.uint8) << 7)
+    byte = torch.stack([torch.randperm(256, generator=g), torch.randperm(256, generator=g)]).to(torch.uint8).view(2, 1, rows)
+    store = pkg.H2OStore(code[0].cuda(), code[1].cuda(), byte[0].cuda(), byte[1].cuda())
+    k64, v64 = (ref.values(code[i], byte[i].clamp(112, 134)).transpose(1, 0, 2) for i in range(2))
+    back = [torch.empty((rows, 1, dim), dtype=DT[q_dtype], device="cuda") for _ in range(2)]
+    store.read(*back)
+    for got, want in zip(back, (k64, v64)):
+        np.testing.assert_array_equal(got.double().cpu().numpy(), want)
+    q = (_normal(4, n, 1, dim) * 1e-4).to(DT[q_dtype]).cuda()
+    out, lse = _attend(store, q, [0], [rows], n)
+    want = ref.attend(q.double().cpu().numpy(), k64, v64, [rows] * n, float(np.float32(1 / math.sqrt(dim))), "kv8", q_dtype)
+    ref.compare(out, want[0], want[2], "out")
+    ref.compare(lse, want[1], want[3], "lse")
