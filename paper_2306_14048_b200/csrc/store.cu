@@ -73,6 +73,7 @@ struct RowsArgs {
   const int64_t* rows;
   int64_t first_row, stride, capacity;
   int n, heads;
+  int32_t* status;
 };
 
 constexpr int kRowThreads = 256;
@@ -95,6 +96,9 @@ __global__ void __launch_bounds__(kRowThreads) store_rows_kernel(RowsArgs a) {
     const int token = first + i;
     row[i] = token >= a.n ? -1 : a.rows ? a.rows[token] : a.first_row + token;
     if (row[i] >= a.capacity) row[i] = -1;
+    if (row[i] >= 0 && !(H2O_IN_RANGE(row[i], a.capacity, a.status) && H2O_IN_RANGE(head, a.heads, a.status) &&
+                         H2O_IN_RANGE(column * 16 + 15, a.stride, a.status)))
+      row[i] = -1;
   }
   if constexpr (WRITE) {
     Raw16<T> raw[TOKENS];
@@ -180,6 +184,7 @@ cudaError_t launch_rows(const h2o_store_config_t& c, void* k, void* v, int dtype
   a.stride = stride;
   a.capacity = c.rows;
   a.heads = c.n_heads;
+  a.status = c.status;
   const int64_t elem = dtype == H2O_F32 ? 4 : 2;
   constexpr int64_t kMost = 65535;  // tokens of a launch (the grid's second dimension)
   for (int64_t at = 0; at < n; at += kMost) {

@@ -51,6 +51,7 @@ struct AttendView {
   const uint8_t *k_scale, *v_scale;  // 8-bit rows only
   int64_t rows, row_stride;
   float *part_out, *part_lse;  // [slots][q_rows][heads * group](dim), null when nothing goes through them
+  int slots;
   // early: part 1's kernel is launched to start before part 0's has ended.  finish (with early): part 1, unsplit, writes the
   // results, joined with what part 0 left; otherwise every part leaves its chunks for the joining kernel, or there is one
   // unsplit part that writes the results.
@@ -88,6 +89,16 @@ __device__ __forceinline__ Problem locate(const AttendView& a, const AttendPart&
   r.len = (int)clamp64(p.length[i], 0, min((int64_t)p.max_length, a.rows - r.row0));
   return r;
 }
+// In the checked build: may these be used?  (Elsewhere always.)
+__device__ __forceinline__ bool token_ok(const AttendView& a, int64_t token, int hq) {
+  return H2O_IN_RANGE(token, a.q_rows, a.status) && H2O_IN_RANGE(hq, a.heads * a.group, a.status);
+}
+__device__ __forceinline__ bool row_ok(const AttendView& a, int head, int64_t row) {
+  return H2O_IN_RANGE(row, a.rows, a.status) && H2O_IN_RANGE(head, a.heads, a.status);
+}
+__device__ __forceinline__ bool partial_ok(const AttendView& a, int64_t at) {
+  return H2O_IN_RANGE(at, a.slots * a.q_rows * a.heads * a.group, a.status);
+}
 // Rows of a problem that its query token `i` sees.
 __device__ __forceinline__ int seen_rows(const AttendPart& p, const Problem& r, int i) {
   return p.causal ? max(0, r.len - (r.nt - 1 - i)) : r.len;
@@ -119,12 +130,14 @@ __device__ __forceinline__ Prefix prefix_of(const AttendView& a, int seq) {
 }
 // The largest of the chunks' logarithms and `top`; then the sum of the chunks' weights relative to it.
 __device__ __forceinline__ float prefix_top(const AttendView& a, const Prefix& f, int64_t token, int hq, float top) {
-  for (int s = 0; s < f.used; ++s) top = fmaxf(top, a.part_lse[f.at(a, s, token, hq)]);
+  for (int s = 0; s < f.used; ++s)
+    if (partial_ok(a, f.at(a, s, token, hq))) top = fmaxf(top, a.part_lse[f.at(a, s, token, hq)]);
   return top;
 }
 __device__ __forceinline__ float prefix_sum(const AttendView& a, const Prefix& f, int64_t token, int hq, float top) {
   float sum = 0.f;
-  for (int s = 0; s < f.used; ++s) sum += exp2f(a.part_lse[f.at(a, s, token, hq)] - top);
+  for (int s = 0; s < f.used; ++s)
+    if (partial_ok(a, f.at(a, s, token, hq))) sum += exp2f(a.part_lse[f.at(a, s, token, hq)] - top);
   return sum;
 }
 // Waits until the kernels before this one have ended (nothing to wait for in an ordinary launch).
@@ -149,8 +162,8 @@ inline int64_t part_blocks(const AttendView& a, const AttendPart& p) {
   return (int64_t)p.row_tiles * a.heads * p.splits * p.problems;
 }
 
-// The value of a scale byte (a biased exponent).  Only bytes 112 .. 134 are ever written; others, in rows nobody
-// has written, are cut to that range.
+// The value of a scale byte (a biased exponent).  Only bytes 112 .. 134 are ever written here; others, in rows nobody has
+// written or of a caller's own, are cut to that range, where every code times the scale is an f16 number.
 __device__ __forceinline__ float kv8_scale(uint32_t byte) { return __uint_as_float(min(max(byte, 112u), 134u) << 23); }
 
 // Softmax scale (times log2(e)) times the power of two of an f16 query row.  Kept a normal number: a factor of 0 would make

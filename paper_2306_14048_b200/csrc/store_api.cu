@@ -236,6 +236,7 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
   a.finish = a.early && a.part[1].splits == 1 && is_tc(pl.kernel[1]);
   const int64_t slots = (int64_t)a.part[0].splits + (n == 2 && !a.finish ? a.part[1].splits : 0);
   if (slots > 1 || a.finish) {
+    a.slots = (int)slots;
     const size_t rows = (size_t)slots * a.q_rows * a.heads * a.group;
     pl.lse_offset = align_up(rows * a.dim * sizeof(float));
     pl.scratch = pl.lse_offset + align_up(rows * sizeof(float));

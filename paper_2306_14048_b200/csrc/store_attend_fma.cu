@@ -49,7 +49,7 @@ __device__ __forceinline__ void load_tile(float* dst, const void* base, const ui
     for (int i = threadIdx.x; i < kBN * kV; i += kThreads) {
       const int r = i / kV, c = (i % kV) * 4;
       float* to = dst + r * PITCH + c;
-      if (r < n) cp_async16(to, static_cast<const float*>(base) + (row0 + r) * a.row_stride + (int64_t)head * D + c);
+      if (r < n && row_ok(a, head, row0 + r)) cp_async16(to, static_cast<const float*>(base) + (row0 + r) * a.row_stride + (int64_t)head * D + c);
       else *reinterpret_cast<float4*>(to) = make_float4(0.f, 0.f, 0.f, 0.f);
     }
   } else {
@@ -58,7 +58,7 @@ __device__ __forceinline__ void load_tile(float* dst, const void* base, const ui
       const int r = i / kV, c = (i % kV) * 16;
       uint4 w = make_uint4(0, 0, 0, 0);
       float s = 0.f;
-      if (r < n) {
+      if (r < n && row_ok(a, head, row0 + r)) {
         const int64_t at = (int64_t)head * a.rows + row0 + r;
         w = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(base) + at * D + c);
         s = kv8_scale(scale[at]);
@@ -99,7 +99,8 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
     float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r < n_rows) {
       const int tok = (r0 + r) / a.group, g = (r0 + r) - tok * a.group;
-      f = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (pr.t0 + tok) * a.q_stride + ((int64_t)w.head * a.group + g) * D + c);
+      if (token_ok(a, pr.t0 + tok, w.head * a.group + g))
+        f = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (pr.t0 + tok) * a.q_stride + ((int64_t)w.head * a.group + g) * D + c);
     }
     *reinterpret_cast<float4*>(&sh.q[r][c]) = f;
   }
@@ -223,6 +224,7 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
     const int tok = (r0 + r) / a.group;
     const int64_t token = pr.t0 + tok;
     const int hq = w.head * a.group + (r0 + r) - tok * a.group;
+    if (!token_ok(a, token, hq)) continue;
     const bool none = sum == 0.f;
     const float inv = none ? 0.f : 1.f / sum;
     const float lse2 = none ? -INFINITY : m[i] + log2f(sum);
@@ -234,6 +236,7 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
       if (a.lse && x == 0) a.lse[token * a.heads * a.group + hq] = lse2 * 0.6931471805599453f;
     } else {
       const int64_t at = ((int64_t)(part.slot0 + w.split) * a.q_rows + token) * a.heads * a.group + hq;
+      if (!partial_ok(a, at)) continue;
 #pragma unroll
       for (int j = 0; j < NC; ++j)
         store4(a.part_out + at * D + 4 * x + 64 * j, make_float4(o[i][j].x * inv, o[i][j].y * inv, o[i][j].z * inv, o[i][j].w * inv));
@@ -251,6 +254,7 @@ constexpr int kFewThreads = 128, kFewWarps = 4, kLoads = 8;
 
 template <int FMT, int D>
 __device__ __forceinline__ float4 load_row4(const void* base, const uint8_t* scale, const AttendView& a, int head, int64_t row, int c) {
+  if (!row_ok(a, head, row)) return make_float4(0.f, 0.f, 0.f, 0.f);
   if constexpr (FMT == H2O_F32) {
     return __ldcs(reinterpret_cast<const float4*>(static_cast<const float*>(base) + row * a.row_stride + (int64_t)head * D + c));
   } else {
@@ -288,7 +292,9 @@ __global__ void __launch_bounds__(kFewThreads) attend_few_kernel(const __grid_co
     const bool there = r < n_rows;
     const int tok = there ? (r0 + r) / a.group : 0;
     const int64_t hq = (int64_t)w.head * a.group + (there ? r0 + r - tok * a.group : 0);
-    q[r] = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (pr.t0 + tok) * a.q_stride + hq * D + c);
+    q[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (token_ok(a, pr.t0 + tok, (int)hq))
+      q[r] = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (pr.t0 + tok) * a.q_stride + hq * D + c);
     seen[r] = there ? min(key1, seen_rows(part, pr, tok)) : 0;
     m[r] = -INFINITY;
     l[r] = 0.f;
@@ -391,11 +397,13 @@ __global__ void __launch_bounds__(kFewThreads) attend_few_kernel(const __grid_co
     const int tok = (r0 + r) / a.group;
     const int64_t token = pr.t0 + tok;
     const int hq = w.head * a.group + (r0 + r) - tok * a.group;
+    if (!token_ok(a, token, hq)) continue;
     if (direct) {
       store4(static_cast<float*>(a.out) + token * a.out_stride + (int64_t)hq * D + cc, v);
       if (a.lse && cc == 0) a.lse[token * a.heads * a.group + hq] = lse2 * 0.6931471805599453f;
     } else {
       const int64_t at = ((int64_t)(part.slot0 + w.split) * a.q_rows + token) * a.heads * a.group + hq;
+      if (!partial_ok(a, at)) continue;
       store4(a.part_out + at * D + cc, v);
       if (cc == 0) a.part_lse[at] = lse2;
     }

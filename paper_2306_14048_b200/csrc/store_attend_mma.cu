@@ -168,7 +168,8 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   uint64_t* full = sh.full[warp];
   auto issue = [&](int i) {  // item i: K of tile i / 2, then its V; lane 0 only
     const int t = warp + kWarps * (i >> 1);
-    const int row = WALK && t < pre_tiles ? (int)prefix.row0 + t * kKeys : (int)pr.row0 + key0 + (t - pre_tiles) * kKeys;
+    int row = WALK && t < pre_tiles ? (int)prefix.row0 + t * kKeys : (int)pr.row0 + key0 + (t - pre_tiles) * kKeys;
+    if (!row_ok(a, w.head, row)) row = 0;
     mbar_expect_tx(&full[i % kSlots], kTile);
     tma_4d(my_ring + (i % kSlots) * kTile, (i & 1) ? map_v : map_k, row, w.head, &full[i % kSlots]);
   };
@@ -183,7 +184,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   // ---- the query operand: lane (gl, c4) of n-tile nt holds row 8 nt + gl (the warps share the n-tiles) ----
   for (int nt = warp; nt < NT; nt += kWarps) {
     const int r = nt * 8 + gl;
-    const bool there = r < n_rows;
+    const bool there = r < n_rows && token_ok(a, pr.t0 + (r0 + r) / a.group, w.head * a.group + (r0 + r) % a.group);
     const int tok = there ? (r0 + r) / a.group : 0;
     const __nv_bfloat16* qr = static_cast<const __nv_bfloat16*>(a.q) + (pr.t0 + tok) * a.q_stride +
                               ((int64_t)w.head * a.group + (there ? r0 + r - tok * a.group : 0)) * D;
@@ -262,7 +263,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
     const int t = warp + kWarps * j;
     const bool in_prefix = WALK && t < pre_tiles;
     const int key = (in_prefix ? t : t - pre_tiles) * kKeys + (in_prefix ? 0 : key0) + lane;
-    if (key < (in_prefix ? pre : key1)) {
+    if (key < (in_prefix ? pre : key1) && row_ok(a, w.head, (in_prefix ? prefix.row0 : pr.row0) + key)) {
       const int64_t at = (int64_t)w.head * a.rows + (in_prefix ? prefix.row0 : pr.row0) + key;
       scale_k = a.k_scale[at];
       scale_v = a.v_scale[at];
@@ -514,6 +515,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
     const int64_t token = pr.t0 + tok;
     const int hq = w.head * a.group + (r0 + r) - tok * a.group;
     if (WALK && (token < prefix.t0 || token >= prefix.t0 + prefix.nt)) continue;  // beyond what the caller allowed for
+    if (!token_ok(a, token, hq)) continue;
     float top = -INFINITY;
 #pragma unroll
     for (int x = 0; x < kWarps; ++x) top = fmaxf(top, sh.m[x][r]);
@@ -541,6 +543,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
       if (a.lse && c == 0) a.lse[token * a.heads * a.group + hq] = lse2 * 0.6931471805599453f;
     } else {
       const int64_t at = ((int64_t)(part.slot0 + w.split) * a.q_rows + token) * a.heads * a.group + hq;
+      if (!partial_ok(a, at)) continue;
       *reinterpret_cast<float4*>(a.part_out + at * D + c) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
       if (c == 0) a.part_lse[at] = lse2;
     }

@@ -294,7 +294,8 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       if (r < n_rows) {
         int tok, hq;
         split_row(r, tok, hq);
-        qx[i] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (pr.t0 + tok) * a.q_stride + (int64_t)hq * D + lane % kLanes * 8);
+        if (token_ok(a, pr.t0 + tok, hq))
+          qx[i] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (pr.t0 + tok) * a.q_stride + (int64_t)hq * D + lane % kLanes * 8);
       }
     }
   };
@@ -305,8 +306,9 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     uint64_t* full = kF16 ? &sh.raw_full[slot] : &sh.kv_full[slot];
     unsigned char* to = kF16 ? raw + 2 * slot * kRaw : ring + 2 * slot * kTile;
     mbar_expect_tx(full, kF16 ? 2 * kRaw : 2 * kTile);
-    tma_load_tile(to, &map_k, w.head, row0 + j * kN, full);
-    tma_load_tile(to + (kF16 ? kRaw : kTile), &map_v, w.head, row0 + j * kN, full);
+    const int row = row_ok(a, w.head, row0 + j * kN) ? row0 + j * kN : 0;
+    tma_load_tile(to, &map_k, w.head, row, full);
+    tma_load_tile(to + (kF16 ? kRaw : kTile), &map_v, w.head, row, full);
   };
   const int n_load = kF16 ? kRawStages : n_stages;  // stages of the ring that TMA fills
   if (warp == 3) tmem_alloc(&sh.tmem_base, kCols);
@@ -427,7 +429,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       // of the next two tiles, one row to a thread: behind the tiles' traffic a load takes longer than a tile
       auto fetch = [&](int j) {
         const int key = key0 + j * kN + t;
-        return t < kN && key < key1 ? (uint32_t)scales[base + key] : 127u;
+        return t < kN && key < key1 && row_ok(a, w.head, pr.row0 + key) ? (uint32_t)scales[base + key] : 127u;
       };
       uint32_t byte = fetch(0), byte_next = fetch(1);
       int slot = 0;
@@ -668,7 +670,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           total = mine_w * total + their_w * join[kM + rt];
         }
         const int64_t token = pr.t0 + tok;
-        bool write = r < n_rows;
+        bool write = r < n_rows && token_ok(a, token, hq);
         if constexpr (FINISH) {
           wait_for_earlier();
           write = write && token >= prefix.t0 && token < prefix.t1;
@@ -685,6 +687,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         const float inv = none ? 0.f : 1.f / total;
         const float lse2 = none ? -INFINITY : top + log2f(total);
         const int64_t at = ((int64_t)(part.slot0 + w.split) * a.q_rows + token) * a.heads * a.group + hq;
+        if (!direct) write = write && partial_ok(a, at);
         __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out) + token * a.out_stride + (int64_t)hq * D;
         // part 0's first chunk (mostly the only one), 64 channels of it asked for at a time
         [[maybe_unused]] float4 first[FINISH ? 16 : 1];
@@ -692,6 +695,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if constexpr (FINISH) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) first[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+          write = write && (prefix.used == 0 || partial_ok(a, prefix.at(a, prefix.used - 1, token, hq)));
           if (write && prefix.used > 0 && !none) first_w = exp2f(a.part_lse[prefix.at(a, 0, token, hq)] - top) * inv;
         }
         auto load_first = [&](int cc) {

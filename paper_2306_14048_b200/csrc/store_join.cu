@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
   // (Launched while the kernels that leave the chunks may still run: what does not depend on them is looked up before.  All
   // wait, so that this kernel never ends before them.)
   wait_for_earlier();
-  if (!live) return;
+  if (!live || !token_ok(a, token, hq)) return;
   const int n = used[0] + used[1];
   const int64_t pitch = a.q_rows * hq_all, at = token * hq_all + hq;
   auto place = [&](int s) { return (int64_t)(s < used[0] ? slot[0] + s : slot[1] + s - used[0]) * pitch + at; };
@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
 #pragma unroll
   for (int k = 0; k < kMaxSlots / 32; ++k) {
     const int s = 32 * k + lane;
-    lse[k] = s < n ? a.part_lse[place(s)] : -INFINITY;
+    lse[k] = s < n && partial_ok(a, place(s)) ? a.part_lse[place(s)] : -INFINITY;
     top = fmaxf(top, lse[k]);
   }
   top = warp_max(top);
@@ -67,6 +67,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
 #pragma unroll 4
     for (int s = 0; s < here; ++s) {
       const float w = __shfl_sync(0xffffffffu, lse[k], s);
+      if (!partial_ok(a, place(32 * k + s))) continue;
       const float* from = a.part_out + place(32 * k + s) * D + lane * kPer;
       if constexpr (kPer == 4) {
         const float4 v = *reinterpret_cast<const float4*>(from);
