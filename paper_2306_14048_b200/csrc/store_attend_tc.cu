@@ -126,10 +126,10 @@ __device__ __forceinline__ float2 ex2_fma2(float2 x) {
 }
 
 constexpr float kRescale = 8.f;
-// A tile whose sum against the old reference exceeds this is done again against its own maximum: far inside the range of
-// fp32 and bf16; of f16 (largest 65504) for the 8-bit rows.
+// A tile whose sum against the old reference exceeds this is done again against its own maximum: inside f16's range (largest
+// 65504) for the 8-bit rows; for bfloat16 rows so that O, which is divided by its sum at the end, holds values up to 2^100.
 template <int FMT>
-constexpr float kLargeSumOf = FMT == H2O_KV8 ? 32768.f : 1.0e12f;
+constexpr float kLargeSumOf = FMT == H2O_KV8 ? 32768.f : 1048576.f;
 // How far (base 2) the reference lies below the maximum it was taken from.  In f16 whatever is below 2^-25 becomes 0: with 2^7
 // for the largest probability that is 2^-32 of it, so 2^20 such keys that go missing weigh 2^-12.  A first tile's sum
 // (80 x 2^7) and what is done again (2^7 x 2^kRescale) stay below the limit.

@@ -213,3 +213,23 @@ def test_scale_bytes_outside_the_format_count_as_the_nearest_inside(pkg, q_dtype
     want = ref.attend(q.double().cpu().numpy(), k64, v64, [rows] * n, float(np.float32(1 / math.sqrt(dim))), "kv8", q_dtype)
     ref.compare(out, want[0], want[2], "out")
     ref.compare(lse, want[1], want[3], "lse")
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n", [1, 16, 17, 150, 300])
+@pytest.mark.parametrize("steps", [6, 12, 39])
+def test_large_values_and_growing_logits_do_not_overflow(pkg, dim, n, steps):
+    """Values of 2^99, and single keys whose logits are `steps` (base 2), twice that, ... above the others': sums are kept
+    relative to a maximum that may lag, but not by so much that fp32 ends."""
+    length = 500
+    k, v = torch.zeros((length, 1, dim)), torch.full((length, 1, dim), 2.0 ** 99)
+    k[150::100, 0, 0] = steps * torch.arange(1.0, 5.0)
+    v[::2] *= -0.5
+    store, k64, v64 = _store(pkg, "bf16", k.bfloat16(), v.bfloat16())
+    q = torch.zeros((n, 1, dim), dtype=torch.bfloat16, device="cuda")
+    q[:, 0, 0] = 1.0
+    c = math.log(2.0)
+    out, lse = _attend(store, q, [0], [length], n, c)
+    want = ref.attend(q.double().cpu().numpy(), k64, v64, [length] * n, float(np.float32(c)), "bf16", "bf16")
+    ref.compare(out, want[0], want[2], "out")
+    ref.compare(lse, want[1], want[3], "lse")
