@@ -473,6 +473,10 @@ typedef struct {
  * is not finite may reach all of its query tokens, the earlier ones too (a weight of 0 times it).  Rows of q behind the last sequence leave
  * out and lse as they were.  max_q, max_length and max_group (sequences in a group) size the launch: they must be
  * upper bounds; tokens, rows and sequences beyond them are left out, and ranges are cut to the store's rows.
+ * Precision: logits, maxima, sums and lse in fp32.  float32 queries: probabilities too.  bfloat16 queries on bfloat16 rows: up to
+ * 16 query rows of a K/V head (tokens times query_group; for a prefix, of all sequences of a group together) probabilities
+ * keep 15 bits, beyond that they are bfloat16 (2^-8 relative), whose errors average out over the keys.  bfloat16 queries on 8-bit rows:
+ * probabilities and queries are f16 (2^-11), the queries by a power of two of their own.  Values up to 2^100 do not overflow.
  * cu_q, cu_group, begin and length are read on the device when the kernels run, so a captured graph follows them.
  * scratch: dev, 256-byte aligned, at least the size the matching function returns for the same arguments (possibly 0:
  * then NULL will do); used by the work this call enqueues only, with any contents.  0 also for invalid arguments.

@@ -11,8 +11,8 @@
 // The tile size is what tensor memory holds of O (2 x 128 columns), S (2 x 80) and P (2 x 40).  With S and P in one place
 // and tiles of 128 keys the chain S - exponentials - P V of a group is serial: 3700 cycles per tile of both groups for
 // 2048 of tensor work.  4 x 2048 queries against 4096 keys, 32 heads: 593 us that way, 505 us this way when it was
-// first built, 469 us now (1170 TFLOP/s; 540 us, 1020 TFLOP/s, once the power limit has lowered the clock).  Tiles of 64 keys
-// with S prefetched into registers and P in two buffers took 650 us, two threads to a row 725 us.
+// first built, 469 us now (1170 TFLOP/s) before the power limit lowers the clock and 530 to 550 us (1000 to 1040) after.
+// Tiles of 64 keys with S prefetched into registers and P in two buffers took 650 us, two threads to a row 725 us.
 // Roles: warp 0 TMA; warps 1 and 2 issue S of A and B (they also clear what lies behind the range in its last V tile:
 // 0 * NaN must not reach the sums); warp 3 issues P V of both and owns tensor memory; warps 4..7 and 8..11 are the softmax
 // of A and B, one thread per row; with 8-bit rows warps 12..15 and 16..19 turn code tiles of K and of V into f16 tiles.
@@ -24,9 +24,9 @@
 // against it without looking for a maximum: only when a tile's sum comes out large (kLargeSum) the tile is done again with
 // the new maximum and O is rescaled.  A value far above the reference costs no precision in floating point, only range.
 //
-// Rounding: P is one bf16 (8-bit rows: one f16).  Its error, 2^-9 relative per key and of either sign, averages over
-// the keys to about that of the output's own rounding; a second product for the remainder would cost half as much tensor
-// time again.  Row sums are fp32 sums of the unrounded values.
+// Rounding: P is one bf16 (8-bit rows: one f16).  Its error, up to 2^-8 relative per key and of either sign, averages over
+// the keys to about that of the output's own rounding, which is up to 2^-8 as well; a second product for the remainder would
+// cost half as much tensor time again.  Row sums are fp32 sums of the unrounded values.
 #include <cuda.h>
 #include <cuda_fp16.h>
 
