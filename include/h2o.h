@@ -490,6 +490,109 @@ int h2o_prefix_attend(h2o_store_t* store, const h2o_queries_t* queries, const h2
                       const int32_t* cu_group, int32_t max_group, const h2o_ranges_t* own, void* scratch,
                       size_t scratch_bytes, void* stream);
 
+/*
+ * Rotary positions: a pair of channels (a, b) of a head, turned by the angle t = position * frequency of the pair,
+ *   a' = a cos t - b sin t,  b' = b cos t + a sin t;
+ * the channels behind rotary_dim stay as they are.  Each pair takes its position from one of `axes` axes (a text's one; a
+ * video's time, height and width).  Angles are formed in 64 bits (positions of a stream of millions of tokens keep their
+ * fraction of a turn), sines and cosines in fp32, the products in fp32, rounded once.
+ */
+typedef struct {
+  const double* frequency; /* dev [rotary_dim / 2] radians per position                                        */
+  const uint8_t* axis;     /* dev [rotary_dim / 2] axis of each pair, or NULL: axis 0; one beyond the last counts as it */
+  int32_t rotary_dim;      /* even, 2 .. head_dim                                                              */
+  int32_t axes;            /* 1 .. 8                                                                           */
+  int32_t pairs;           /* 0: channels i and i + rotary_dim / 2 (halves); 1: channels 2 i and 2 i + 1       */
+  int32_t device;          /* CUDA device ordinal                                                              */
+} h2o_rotary_t;
+/*
+ * x: dev [n_tokens, n_heads, head_dim] of `dtype` (H2O_F32 or H2O_BF16) -> out, the same shape; out may be x itself, but must not
+ * overlap it otherwise.  head_dim: a multiple of 8, up to 512.  Strides in elements between tokens (0: dense; multiples of 8
+ * otherwise), 16-byte aligned.  positions: dev int64 [axes][n_tokens], `position_stride` entries from axis to axis (0: n_tokens).
+ * inverse: turns by -t, which takes the rotation back and is its transposed map: the gradient with respect to x of what a
+ * rotation computes is the inverse rotation of the gradient.
+ */
+int h2o_rotate(const h2o_rotary_t* rotary, const void* x, void* out, int32_t dtype, int64_t n_tokens, int32_t n_heads,
+               int32_t head_dim, int64_t x_stride, int64_t out_stride, const int64_t* positions, int64_t position_stride,
+               int32_t inverse, void* stream);
+
+/*
+ * Paged K/V cache: rows in pages of a pool that many sequences share, so that a sequence grows without being moved and gives
+ * pages back one by one.  Beside the caches above (budgets, eviction by score) it serves the rule that streaming inputs are
+ * compared with, a window of recent tokens and the first few (sinks), and ordinary attention to everything.  The handle
+ * describes caller-owned memory, which must stay valid until h2o_pages_destroy.  Calls on one handle may run on several
+ * streams at once as far as their memory allows: every call has its own scratch, and the caller orders appends against reads.
+ *
+ * k, v: dev, element (page, row, head, channel) at page * page_stride + row * row_stride + head * head_stride + channel.
+ */
+typedef struct h2o_pages h2o_pages_t; /* opaque, host-side */
+typedef struct {
+  int32_t n_heads;    /* K/V heads, >= 1                                                                   */
+  int32_t head_dim;   /* 64 or 128                                                                         */
+  int32_t format;     /* H2O_F32 or H2O_BF16                                                               */
+  int32_t device;     /* CUDA device ordinal                                                               */
+  int32_t n_pages;    /* pages of the pool, >= 1                                                           */
+  int32_t page_size;  /* rows of a page, a multiple of 8, up to 65536                                      */
+  int64_t page_stride, row_stride, head_stride; /* elements, multiples of 8, at least head_dim; all 0: dense
+                                                   [n_pages, page_size, n_heads, head_dim]                 */
+  void *k, *v;        /* dev, 16-byte aligned                                                              */
+  int32_t* status;    /* dev, one int32 the caller has set to 0, or NULL: where a kernel's bounded wait that gives up leaves
+                         H2O_ERR_TIMEOUT                                                                   */
+} h2o_pages_config_t;
+int h2o_pages_create(h2o_pages_t** out, const h2o_pages_config_t* cfg);
+int h2o_pages_destroy(h2o_pages_t* pages); /* the handle only; NULL is accepted */
+int h2o_debug_pages_set_polls(h2o_pages_t* pages, int32_t polls); /* as h2o_debug_store_set_polls */
+
+/*
+ * Sequences in a paged cache: row x of sequence b is row x % page_size of page table[b * table_stride + x / page_size].  The
+ * arrays are read on the device when the kernels run, so a captured graph follows them.  An entry outside 0 .. n_pages - 1 is
+ * no page: nothing is written for a token that belongs there, and its rows read as zeros (keys and values of 0, which count
+ * in a softmax); entries of rows that no query sees may hold anything.  A call's new tokens are the last rows of their
+ * sequence: token i of n_b is row length[b] - n_b + i.
+ */
+typedef struct {
+  const int32_t* table;  /* dev [batch][table_stride]                                                      */
+  const int32_t* length; /* dev [batch]: rows of each sequence, its new tokens included                    */
+  int64_t table_stride;  /* entries between sequences, 0: max_pages                                        */
+  int32_t max_pages;     /* entries a sequence has; rows behind them do not exist                          */
+  int32_t max_length;    /* upper bound of the lengths; longer ones are cut to it                          */
+} h2o_sequences_t;
+
+/* New tokens on their way into the cache, and the queries that go with them. */
+typedef struct {
+  const void *k, *v;   /* dev [n_tokens, n_heads, head_dim] of the pages' format                           */
+  const void* q;       /* dev [n_tokens, n_heads * query_group, head_dim] or NULL                          */
+  void* q_out;         /* dev, the same shape; may be q itself                                             */
+  const int32_t* cu;   /* dev [batch + 1]: sequence b has tokens cu[b] .. cu[b + 1] - 1; NULL: token b alone */
+  const int64_t* positions; /* dev [axes][n_tokens] for the rotation, or NULL: the token's row, on every axis */
+  int64_t n_tokens;    /* tokens in k, v and q                                                             */
+  int64_t kv_stride, q_stride, q_out_stride; /* elements between tokens, 0: dense; multiples of 8          */
+  int64_t position_stride; /* entries from axis to axis, 0: n_tokens                                       */
+  int32_t query_group; /* query heads per K/V head, >= 1 (without q: unused)                               */
+  int32_t batch;       /* sequences, 0 .. 65535                                                            */
+} h2o_tokens_t;
+/*
+ * Appends the tokens to their sequences: v as it is, k rotated by `rotary` (NULL: as it is), q rotated into q_out.  A token
+ * whose row does not exist (a negative one, behind max_length or max_pages, or in no page) is left out of the cache; its query
+ * is rotated all the same.  Tokens that belong to no sequence are left alone.  Two tokens must not share a row.
+ */
+int h2o_pages_append(h2o_pages_t* pages, const h2o_tokens_t* tokens, const h2o_sequences_t* sequences, const h2o_rotary_t* rotary,
+                     void* stream);
+/*
+ * Attention of each sequence's new tokens to its rows, causal: query token i of n_b, at row p = length[b] - n_b + i, sees the
+ * rows x <= p, with `window` > 0 only those with x > p - window or x < sinks:
+ *   out = sum_x p_x v_x,  p = softmax over the rows it sees of c q.k_x,  lse = log sum_x exp(c q.k_x)
+ * queries->dtype is the pages' format; cu_q, max_q, strides, lse and the empty cases are those of h2o_cross_attend, as is the
+ * precision (bfloat16: probabilities keep 15 bits for up to 16 query rows of a K/V head, tokens times query_group, and are bfloat16
+ * beyond).  A query that sees no row gets out 0 and lse -infinity.  Rows that no query of a sequence sees are not read into
+ * any result (they may hold NaN, their pages may belong to others); a value that is not finite in a row that some see may
+ * reach all the query tokens of that sequence.  window, sinks >= 0; window 0: all rows up to the query's own.
+ */
+size_t h2o_pages_scratch_bytes(const h2o_pages_t* pages, const h2o_queries_t* queries, const h2o_sequences_t* sequences,
+                               int32_t window, int32_t sinks);
+int h2o_pages_attend(h2o_pages_t* pages, const h2o_queries_t* queries, const h2o_sequences_t* sequences, int32_t window,
+                     int32_t sinks, void* scratch, size_t scratch_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

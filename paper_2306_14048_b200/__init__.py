@@ -18,6 +18,8 @@ from .binding import (  # noqa: F401
     H2O_OK,
     H2OCache,
     H2OError,
+    H2OPages,
+    H2ORotary,
     H2OStore,
     h2o_cache_workspace_bytes,
     h2o_config_t,

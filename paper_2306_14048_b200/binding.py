@@ -60,6 +60,13 @@ EXPORTED = (
     "h2o_cross_attend",
     "h2o_prefix_scratch_bytes",
     "h2o_prefix_attend",
+    "h2o_rotate",
+    "h2o_pages_create",
+    "h2o_pages_destroy",
+    "h2o_debug_pages_set_polls",
+    "h2o_pages_append",
+    "h2o_pages_scratch_bytes",
+    "h2o_pages_attend",
     "h2o_strerror",
 )
 
@@ -113,6 +120,62 @@ class h2o_queries_t(ctypes.Structure):
 
 class h2o_ranges_t(ctypes.Structure):
     _fields_ = [("begin", ctypes.c_void_p), ("length", ctypes.c_void_p), ("max_length", ctypes.c_int32)]
+
+
+class h2o_rotary_t(ctypes.Structure):
+    _fields_ = [
+        ("frequency", ctypes.c_void_p),
+        ("axis", ctypes.c_void_p),
+        ("rotary_dim", ctypes.c_int32),
+        ("axes", ctypes.c_int32),
+        ("pairs", ctypes.c_int32),
+        ("device", ctypes.c_int32),
+    ]
+
+
+class h2o_pages_config_t(ctypes.Structure):
+    _fields_ = [
+        ("n_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("format", ctypes.c_int32),
+        ("device", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("page_stride", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("status", ctypes.c_void_p),
+    ]
+
+
+class h2o_sequences_t(ctypes.Structure):
+    _fields_ = [
+        ("table", ctypes.c_void_p),
+        ("length", ctypes.c_void_p),
+        ("table_stride", ctypes.c_int64),
+        ("max_pages", ctypes.c_int32),
+        ("max_length", ctypes.c_int32),
+    ]
+
+
+class h2o_tokens_t(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("q", ctypes.c_void_p),
+        ("q_out", ctypes.c_void_p),
+        ("cu", ctypes.c_void_p),
+        ("positions", ctypes.c_void_p),
+        ("n_tokens", ctypes.c_int64),
+        ("kv_stride", ctypes.c_int64),
+        ("q_stride", ctypes.c_int64),
+        ("q_out_stride", ctypes.c_int64),
+        ("position_stride", ctypes.c_int64),
+        ("query_group", ctypes.c_int32),
+        ("batch", ctypes.c_int32),
+    ]
 
 
 def _load() -> ctypes.CDLL:
@@ -201,6 +264,20 @@ def _load() -> ctypes.CDLL:
     lib.h2o_prefix_scratch_bytes.argtypes = [vp, qp, rp, c.c_int32, vp, c.c_int32, rp]
     lib.h2o_prefix_attend.restype = c.c_int
     lib.h2o_prefix_attend.argtypes = [vp, qp, rp, c.c_int32, vp, c.c_int32, rp, vp, c.c_size_t, vp]
+    lib.h2o_rotate.restype = c.c_int
+    lib.h2o_rotate.argtypes = [vp, vp, vp, c.c_int32, c.c_int64, c.c_int32, c.c_int32, c.c_int64, c.c_int64, vp, c.c_int64, c.c_int32, vp]
+    lib.h2o_pages_create.restype = c.c_int
+    lib.h2o_pages_create.argtypes = [c.POINTER(vp), c.POINTER(h2o_pages_config_t)]
+    lib.h2o_pages_destroy.restype = c.c_int
+    lib.h2o_pages_destroy.argtypes = [vp]
+    lib.h2o_debug_pages_set_polls.restype = c.c_int
+    lib.h2o_debug_pages_set_polls.argtypes = [vp, c.c_int32]
+    lib.h2o_pages_append.restype = c.c_int
+    lib.h2o_pages_append.argtypes = [vp, vp, vp, vp, vp]
+    lib.h2o_pages_scratch_bytes.restype = c.c_size_t
+    lib.h2o_pages_scratch_bytes.argtypes = [vp, qp, vp, c.c_int32, c.c_int32]
+    lib.h2o_pages_attend.restype = c.c_int
+    lib.h2o_pages_attend.argtypes = [vp, qp, vp, c.c_int32, c.c_int32, vp, c.c_size_t, vp]
     lib.h2o_strerror.restype = c.c_char_p
     lib.h2o_strerror.argtypes = [c.c_int]
     return lib
@@ -632,6 +709,248 @@ class H2OStore:
     def close(self):
         if getattr(self, "_h", None) is not None:
             lib.h2o_store_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _wrong(who: str, why: str):
+    raise ValueError(who + ": " + why)
+
+
+def _token_stride(who, what, shape, stride):
+    """The stride between the tokens of [tokens, heads, dim] with dense heads, 0 where there is one token at most."""
+    tokens, heads, dim = shape
+    if tokens and (stride[2] != 1 or (heads > 1 and stride[1] != dim)):
+        _wrong(who, "%s must have dense heads" % what)
+    if tokens <= 1:
+        return 0
+    if stride[0] == 0:  # (0 means dense to the library)
+        _wrong(who, "%s must not be broadcast over the tokens" % what)
+    return stride[0]
+
+
+class H2ORotary:
+    """Rotary positions of heads (h2o_rotate): pairs of channels turned by position * frequency.
+
+    ``frequencies``: radians per position of each of the rotary_dim / 2 pairs (None: base ** (-2 i / rotary_dim));
+    ``axes``: which axis of the positions each pair follows (None: one axis); ``pairs``: "halves" (channels i and
+    i + rotary_dim / 2) or "neighbours" (channels 2 i and 2 i + 1).  rotary_dim: the first channels of a head, all of them
+    by default; the others stay as they are.  The two small tables are kept on the device by this object.
+    """
+
+    def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, base: float = 10000.0, frequencies=None, axes=None,
+                 pairs: str = "halves", device=0):
+        self.head_dim = int(head_dim)
+        self.rotary_dim = self.head_dim if rotary_dim is None else int(rotary_dim)
+        if self.head_dim < 8 or self.head_dim > 512 or self.head_dim % 8:
+            _wrong("H2ORotary", "head_dim must be a multiple of 8, up to 512")
+        if not 2 <= self.rotary_dim <= self.head_dim or self.rotary_dim % 2:
+            _wrong("H2ORotary", "rotary_dim must be even, 2 .. head_dim")
+        half = self.rotary_dim // 2
+        if frequencies is None:
+            frequencies = [float(base) ** (-2.0 * i / self.rotary_dim) for i in range(half)]
+        frequencies = np.ascontiguousarray(np.asarray(frequencies, dtype=np.float64))
+        if frequencies.shape != (half,) or not np.isfinite(frequencies).all():
+            _wrong("H2ORotary", "frequencies must be %d finite numbers" % half)
+        self.axes = 1
+        if axes is not None:
+            axes = np.asarray(axes)
+            if axes.shape != (half,) or axes.dtype.kind not in "iu" or axes.min() < 0 or axes.max() > 7:
+                _wrong("H2ORotary", "axes must be %d whole numbers, 0 .. 7" % half)
+            self.axes = int(axes.max()) + 1
+        if pairs not in ("halves", "neighbours"):
+            _wrong("H2ORotary", "pairs must be 'halves' or 'neighbours'")
+        self.device = torch.device("cuda", device) if isinstance(device, int) else torch.device(device)
+        if self.device.type != "cuda":
+            _wrong("H2ORotary", "a CUDA device is needed; there is no fallback")
+        self._frequency = torch.from_numpy(frequencies).to(self.device)
+        self.device, self._index = self._frequency.device, self._frequency.device.index
+        self._axis = None if self.axes == 1 else torch.from_numpy(axes.astype(np.uint8)).to(self.device)
+        torch.cuda.current_stream(self.device).synchronize()  # the tables are there, whatever stream comes next
+        self._c = h2o_rotary_t(self._frequency.data_ptr(), None if self._axis is None else self._axis.data_ptr(), self.rotary_dim, self.axes,
+                               0 if pairs == "halves" else 1, self._index)
+        self._at = ctypes.addressof(self._c)
+
+    def _positions(self, positions, tokens):
+        """Address and axis stride of positions: int64 [axes, tokens], or [tokens] for one axis."""
+        shape = positions.shape
+        if positions.dtype is not torch.int64 or positions.get_device() != self._index:
+            _wrong("H2ORotary", "positions must be int64 on %s" % self.device)
+        if shape != (self.axes, tokens) and not (self.axes == 1 and shape == (tokens,)):
+            _wrong("H2ORotary", "positions must be [%d, %d]" % (self.axes, tokens))
+        stride = positions.stride()
+        if tokens > 1 and stride[-1] != 1:
+            _wrong("H2ORotary", "positions must lie token after token")
+        if self.axes > 1 and tokens and stride[0] < tokens:
+            _wrong("H2ORotary", "positions must not be broadcast over the axes")
+        return positions.data_ptr(), stride[0] if self.axes > 1 else 0
+
+    def apply(self, x, positions, out, inverse=False, stream=None):
+        """Rotates x [tokens, heads, head_dim] into out (which may be x).  inverse: takes the rotation back, which is also
+        the gradient of a rotation with respect to its input."""
+        shape = x.shape
+        if len(shape) != 3 or shape[2] != self.head_dim or out.shape != shape:
+            _wrong("H2ORotary", "x and out must be [tokens, heads, %d]" % self.head_dim)
+        dtype = _DTYPES.get(x.dtype)
+        if dtype is None or out.dtype is not x.dtype or x.get_device() != self._index or out.get_device() != self._index:
+            _wrong("H2ORotary", "x and out must both be float32 or bfloat16 on %s" % self.device)
+        at, stride = self._positions(positions, shape[0])
+        code = lib.h2o_rotate(self._at, x.data_ptr(), out.data_ptr(), dtype, shape[0], shape[1], shape[2],
+                              _token_stride("H2ORotary", "x", shape, x.stride()), _token_stride("H2ORotary", "out", shape, out.stride()),
+                              at, stride, 1 if inverse else 0, _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "h2o_rotate")
+
+
+# h2o_tokens_t and h2o_sequences_t as bytes
+_pack_tokens = struct.Struct("@PPPPPPqqqqqii").pack
+_pack_sequences = struct.Struct("@PPqii").pack
+
+
+class H2OPages:
+    """A paged K/V cache (h2o_pages_*): rows in pages of a pool, a table of pages for each sequence.
+
+    ``k``, ``v``: float32 or bfloat16 [pages, page_size, heads, head_dim] of the same strides, channels dense (any order of the
+    other three: a pool [pages, heads, page_size, head_dim] is given as its transpose(1, 2), one of K and V together as its
+    parts).  page_size: a multiple of 8.  The tensors stay the caller's (this object keeps a reference).  ``table``: int32 [batch,
+    most pages of a sequence], an entry outside the pool is no page; ``length``: int32 [batch], rows of each sequence, those
+    of the call's tokens included, which are its last ones.  Methods mirror the C calls: ``append`` ->
+    h2o_pages_append, ``attend`` -> h2o_pages_attend, ``close`` -> h2o_pages_destroy.  Results go to tensors that the caller
+    passes; scratch comes from torch's allocator on the call's stream, one piece per call.
+    """
+
+    def __init__(self, k, v):
+        if not k.is_cuda or k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device:
+            _wrong("H2OPages", "k and v must be CUDA tensors of one 4-d shape, dtype and device")
+        if k.dtype not in _DTYPES:
+            _wrong("H2OPages", "k and v must be float32 or bfloat16")
+        self.n_pages, self.page_size, self.n_heads, self.head_dim = k.shape
+        used = [i for i in range(4) if k.shape[i] > 1]
+        strides = list(k.stride())
+        if any(strides[i] != v.stride(i) for i in used) or (3 in used and strides[3] != 1):
+            _wrong("H2OPages", "k and v must have the same strides and dense channels")
+        if self.n_heads == 1:  # strides that are never used
+            strides[2] = self.head_dim
+        if self.n_pages == 1:
+            strides[0] = max(strides[1] * self.page_size, strides[2] * self.n_heads)
+        self.format = _DTYPES[k.dtype]
+        self.device, self._index = k.device, k.device.index
+        self._need = {}  # scratch bytes by the sizes of a call
+        self.k, self.v = k, v
+        self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        torch.cuda.current_stream(self.device).synchronize()  # the zero is there, whatever stream comes next
+        cfg = h2o_pages_config_t(self.n_heads, self.head_dim, self.format, self._index, self.n_pages, self.page_size, strides[0], strides[1],
+                                 strides[2], k.data_ptr(), v.data_ptr(), self._status.data_ptr())
+        self._h = None
+        handle = ctypes.c_void_p()
+        _check(lib.h2o_pages_create(ctypes.byref(handle), ctypes.byref(cfg)), "h2o_pages_create")
+        self._h = handle
+
+    # ---- argument checks ----
+    def _sequences(self, table, length, max_len):
+        batch = length.shape[0] if length.dim() == 1 else -1
+        if length.dtype is not torch.int32 or batch < 0 or length.get_device() != self._index or not length.is_contiguous():
+            _wrong("H2OPages", "length must be a contiguous int32 [batch] on %s" % self.device)
+        if table.dtype is not torch.int32 or table.dim() != 2 or table.shape[0] != batch or table.get_device() != self._index:
+            _wrong("H2OPages", "table must be int32 [batch, pages] on %s" % self.device)
+        stride, pages = table.stride(), table.shape[1]
+        if (pages > 1 and stride[1] != 1) or (batch > 1 and pages and stride[0] < pages):
+            _wrong("H2OPages", "a sequence's entries of the table must be dense, and its own")
+        return _pack_sequences(table.data_ptr(), length.data_ptr(), stride[0] if batch > 1 else 0, pages, max_len), batch, pages
+
+    def _cu(self, cu, batch, tokens):
+        if cu is None:
+            if tokens < batch:
+                _wrong("H2OPages", "without cu there is one token per sequence")
+            return 0
+        if cu.dtype is not torch.int32 or cu.shape != (batch + 1,) or cu.get_device() != self._index or not cu.is_contiguous():
+            _wrong("H2OPages", "cu must be a contiguous int32 [batch + 1] on %s" % self.device)
+        return cu.data_ptr()
+
+    def _heads(self, q, out, what):
+        """Query heads per K/V head and the token strides of q and out."""
+        shape = q.shape
+        if len(shape) != 3 or shape[2] != self.head_dim or shape[1] < self.n_heads or shape[1] % self.n_heads:
+            _wrong("H2OPages", "q must be [tokens, multiple of %d, %d]" % (self.n_heads, self.head_dim))
+        if _DTYPES.get(q.dtype) != self.format or out.dtype is not q.dtype or out.shape != shape:
+            _wrong("H2OPages", "q and %s must have the pages' dtype and one shape" % what)
+        if q.get_device() != self._index or out.get_device() != self._index:
+            _wrong("H2OPages", "q and %s must be on %s" % (what, self.device))
+        return (shape[1] // self.n_heads, _token_stride("H2OPages", "q", shape, q.stride()),
+                _token_stride("H2OPages", what, shape, out.stride()))
+
+    # ---- calls ----
+    def append(self, k, v, table, length, cu=None, rotary=None, positions=None, q=None, q_out=None, stream=None):
+        """Appends k, v [tokens, heads, head_dim] to their sequences' pages; with ``rotary`` k is rotated on the way, and q
+        [tokens, query heads, head_dim] into q_out (which may be q).  cu: int32 [batch + 1] first token of each sequence (None:
+        token b is sequence b); positions: as for H2ORotary.apply (None: each token's row, on every axis)."""
+        shape = k.shape
+        if len(shape) != 3 or v.shape != shape or shape[1] != self.n_heads or shape[2] != self.head_dim:
+            _wrong("H2OPages", "k and v must be [tokens, %d, %d]" % (self.n_heads, self.head_dim))
+        if _DTYPES.get(k.dtype) != self.format or v.dtype is not k.dtype or k.get_device() != self._index or v.get_device() != self._index:
+            _wrong("H2OPages", "k and v must have the pages' dtype and be on %s" % self.device)
+        tokens = shape[0]
+        stride = _token_stride("H2OPages", "k", shape, k.stride())
+        if _token_stride("H2OPages", "v", shape, v.stride()) != stride:
+            _wrong("H2OPages", "k and v must have one token stride")
+        seqs, batch, _ = self._sequences(table, length, 2147483647)
+        at, position_stride = 0, 0
+        if rotary is not None:
+            if rotary._index != self._index or rotary.head_dim != self.head_dim:
+                _wrong("H2OPages", "rotary must be for head_dim %d on %s" % (self.head_dim, self.device))
+            if positions is not None:
+                at, position_stride = rotary._positions(positions, tokens)
+        elif positions is not None:
+            _wrong("H2OPages", "positions belong to a rotary")
+        group, qs, os_ = 1, 0, 0
+        if (q is None) != (q_out is None):
+            _wrong("H2OPages", "q and q_out go together")
+        if q is not None:
+            group, qs, os_ = self._heads(q, q_out, "q_out")
+            if q.shape[0] != tokens:
+                _wrong("H2OPages", "q must have as many tokens as k")
+        packed = _pack_tokens(k.data_ptr(), v.data_ptr(), 0 if q is None else q.data_ptr(), 0 if q is None else q_out.data_ptr(),
+                              self._cu(cu, batch, tokens), at, tokens, stride, qs, os_, position_stride, group, batch)
+        code = lib.h2o_pages_append(self._h, packed, seqs, None if rotary is None else rotary._at,
+                                    _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "h2o_pages_append")
+
+    def attend(self, q, table, length, out, max_len, window=0, sinks=0, cu=None, max_q=1, lse=None, softmax_scale=0.0, stream=None):
+        """Each sequence's query tokens attend its rows up to their own, with ``window`` > 0 the last ``window`` of them (their own
+        included) and the sequence's first ``sinks``.  q, out: [tokens, query heads, head_dim]; cu: int32 [batch + 1] first
+        token of each sequence (None: token b is sequence b); max_q, max_len: upper bounds of a sequence's tokens and rows;
+        lse: float32 [tokens, query heads] or None."""
+        group, qs, os_ = self._heads(q, out, "out")
+        tokens, heads = q.shape[0], q.shape[1]
+        seqs, batch, pages = self._sequences(table, length, max_len)
+        if cu is None and max_q != 1:
+            _wrong("H2OPages", "without cu there is one token per sequence")
+        if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (tokens, heads) or lse.get_device() != self._index or not lse.is_contiguous()):
+            _wrong("H2OPages", "lse must be a contiguous float32 [tokens, query heads] on %s" % self.device)
+        queries = _pack_queries(q.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(), self._cu(cu, batch, tokens), tokens, qs, os_,
+                                softmax_scale, self.format, group, batch, max_q)
+        sizes = (tokens, group, batch, max_q, max_len, pages, window, sinks)
+        need = self._need.get(sizes)
+        if need is None:
+            need = lib.h2o_pages_scratch_bytes(self._h, queries, seqs, window, sinks)
+        scratch = self._scratch(need, stream) if need else None
+        code = lib.h2o_pages_attend(self._h, queries, seqs, window, sinks, scratch.data_ptr() if need else None, need,
+                                    _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "h2o_pages_attend")
+        self._needs(sizes, need)
+
+    _scratch, _needs, status = H2OStore._scratch, H2OStore._needs, H2OStore.status
+
+    def close(self):
+        if getattr(self, "_h", None) is not None:
+            lib.h2o_pages_destroy(self._h)
             self._h = None
 
     def __del__(self):
