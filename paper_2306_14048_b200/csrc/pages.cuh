@@ -6,6 +6,9 @@
 struct h2o_pages {
   h2o_pages_config_t cfg;  // strides filled in
   uint32_t polls;          // of a wait before it gives up
+  // bfloat16: tensor maps (opaque here) for few query rows, and for many in blocks of one and of two groups, and rows of their boxes
+  alignas(64) unsigned char few_k[128], few_v[128], one_k[128], one_v[128], two_k[128], two_v[128];
+  int few_box, one_box, two_box;
 };
 
 namespace h2o {
@@ -35,13 +38,5 @@ struct MoveArgs {
   int32_t* status;
 };
 cudaError_t launch_move(const MoveArgs& a, int dtype, cudaStream_t stream);
-
-struct PagesAttend {
-  AttendView a;
-  const int32_t* table;
-  int64_t table_stride, page_stride, row_stride, head_stride;
-  int n_pages, page_size, max_pages, window, sinks;
-};
-cudaError_t launch_pages_attend_simple(const PagesAttend& a, int dtype, cudaStream_t stream);
 
 }  // namespace h2o

@@ -4,28 +4,18 @@
 #include <cmath>
 #include <cstring>
 #include <new>
+#include <numeric>
 
 #include "pages.cuh"
+#include "store_plan.cuh"
 
 namespace {
 
-constexpr int kMaxGroup = 32, kMaxAxes = 8, kMaxHeadDim = 512, kMaxPageSize = 65536;
+using namespace h2o;
+
+constexpr int kMaxAxes = 8, kMaxHeadDim = 512, kMaxPageSize = 65536;
 constexpr int64_t kMaxStride = 1ll << 36;
-
-bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
-
-struct DeviceGuard {
-  int prev = -1;
-  bool ok = false, changed = false;
-  explicit DeviceGuard(int dev) {
-    if (cudaGetDevice(&prev) != cudaSuccess) return;
-    ok = prev == dev || cudaSetDevice(dev) == cudaSuccess;
-    changed = ok && prev != dev;
-  }
-  ~DeviceGuard() {
-    if (changed) cudaSetDevice(prev);
-  }
-};
+constexpr int kMaxRows = INT32_MAX - 4096;  // of a sequence (tiles of them are counted in 32 bits)
 
 int check_pages(const h2o_pages_config_t* c) {
   if (!c || !c->k || !c->v) return H2O_ERR_INVALID_ARG;
@@ -56,8 +46,8 @@ bool bad_stride(int64_t& s, int64_t dense) {
   return s < dense || s % 8 != 0;
 }
 
-h2o::Turn turn_of(const h2o_rotary_t* r, const int64_t* positions, int64_t stride, int64_t n_tokens, int inverse) {
-  h2o::Turn t = {};
+Turn turn_of(const h2o_rotary_t* r, const int64_t* positions, int64_t stride, int64_t n_tokens, int inverse) {
+  Turn t = {};
   if (!r) return t;
   t.frequency = r->frequency;
   t.axis = r->axis;
@@ -77,9 +67,6 @@ int check_sequences(const h2o_sequences_t* s) {
   return s->table_stride > kMaxStride ? H2O_ERR_UNSUPPORTED : H2O_OK;
 }
 
-// The softmax scale for logits in base 2.
-float base2(float scale) { return (float)((double)scale * 1.4426950408889634074); }
-
 int check_queries(const h2o_pages_t* pages, const h2o_queries_t* q) {
   if (!pages || !q) return H2O_ERR_INVALID_ARG;
   if (q->batch < 0 || q->q_rows < 0 || q->max_q < 0 || q->q_stride < 0 || q->out_stride < 0) return H2O_ERR_INVALID_ARG;
@@ -95,16 +82,103 @@ int check_queries(const h2o_pages_t* pages, const h2o_queries_t* q) {
     if (s != 0 && (s < dense || s % 8 != 0)) return H2O_ERR_INVALID_ARG;
   return misaligned(q->cu_q, 4) ? H2O_ERR_INVALID_ARG : H2O_OK;
 }
-bool nothing_to_do(const h2o_queries_t* q) { return q->batch == 0 || q->q_rows == 0 || q->max_q == 0; }
-int check_pointers(const h2o_queries_t* q) {
-  if (!q->q || !q->out || misaligned(q->q, 16) || misaligned(q->out, 16) || misaligned(q->lse, 4)) return H2O_ERR_INVALID_ARG;
-  return q->q == q->out ? H2O_ERR_INVALID_ARG : H2O_OK;
-}
 int check_attend(const h2o_pages_t* pages, const h2o_queries_t* q, const h2o_sequences_t* s, int window, int sinks) {
   int rc = check_queries(pages, q);
   if (rc != H2O_OK) return rc;
   if (window < 0 || sinks < 0) return H2O_ERR_INVALID_ARG;
   return nothing_to_do(q) ? H2O_OK : check_sequences(s);
+}
+
+// What a call launches and how much scratch it needs.
+struct Plan {
+  AttendView a;
+  Kernel kernel;
+  int tile;           // query rows of a block
+  size_t scratch;     // bytes of scratch
+  size_t lse_offset;  // of the partial log-sums in it
+  int rc;
+};
+
+// More query rows than this (of one K/V head) run on the tcgen05 kernel: as for the K/V store.
+constexpr int kFewRows = 16;
+
+Plan make_plan(const h2o_pages_t* pages, const h2o_queries_t* q, const h2o_sequences_t* s, int window, int sinks) {
+  Plan pl;
+  std::memset(&pl, 0, sizeof(pl));
+  const h2o_pages_config_t& c = pages->cfg;
+  AttendView& a = pl.a;
+  a.q = q->q;
+  a.out = q->out;
+  a.lse = q->lse;
+  a.heads = c.n_heads;
+  a.group = q->query_group;
+  a.dim = c.head_dim;
+  const int64_t dense = (int64_t)a.heads * a.group * a.dim;
+  a.q_stride = q->q_stride ? q->q_stride : dense;
+  a.out_stride = q->out_stride ? q->out_stride : dense;
+  a.q_rows = q->q_rows;
+  a.cu_q = q->cu_q;
+  a.batch = q->batch;
+  a.n_groups = a.max_group = 1;
+  a.max_q = (int)std::min<int64_t>(q->max_q, q->q_rows);
+  a.scale2 = base2(q->softmax_scale > 0.f ? q->softmax_scale : 1.0f / std::sqrt((float)a.dim));
+  a.k = c.k;
+  a.v = c.v;
+  a.rows = kMaxRows;
+  a.row_stride = c.row_stride;
+  a.status = c.status;
+  a.polls = pages->polls;
+  a.n_parts = 1;
+  AttendPart& p = a.part[0];
+  p.length = s->length;
+  p.max_length = (int)std::min({(int64_t)s->max_length, (int64_t)s->max_pages * c.page_size, (int64_t)kMaxRows});
+  p.causal = 1;
+  p.problems = a.batch;
+  Paging& g = a.pages;
+  g.table = s->max_pages > 0 ? s->table : s->length;  // (without a single page no entry is read)
+  g.stride = s->table_stride ? s->table_stride : s->max_pages;
+  g.page_stride = c.page_stride;
+  g.head_stride = c.head_stride;
+  g.n_pages = c.n_pages;
+  g.page_size = c.page_size;
+  g.window = window;
+  g.sinks = sinks;
+  const int64_t rows = (int64_t)a.max_q * a.group;
+  int step = 128, keys_of_tile;  // a chunk's keys are a multiple of a tile's
+  auto cut = [&](Kernel kernel, int tile) {
+    pl.kernel = kernel;
+    pl.tile = tile;
+    keys_of_tile = is_tc(kernel) ? attend_tc_box_rows(H2O_BF16, a.dim, kernel == Kernel::Tc1 ? 1 : 2) : 64;
+    g.box = kernel == Kernel::Fma ? 8 : kernel == Kernel::Mma ? pages->few_box : kernel == Kernel::Tc1 ? pages->one_box : pages->two_box;
+    if (is_tc(kernel)) step = 2 * keys_of_tile;
+    // the most keys a tile of query rows walks over: sinks in whole tiles, the window, as far as the tile's tokens lie apart, and
+    // down to the box the window starts in
+    p.most_keys = p.max_length;
+    if (window > 0) {
+      const int64_t span = std::min<int64_t>(a.max_q - 1, (tile + a.group - 2) / a.group);
+      const int64_t head = ((int64_t)std::min(sinks, p.max_length) + keys_of_tile - 1) / keys_of_tile * keys_of_tile;
+      p.most_keys = (int)std::min<int64_t>(p.max_length, head + window + span + g.box);
+    }
+  };
+  if (c.format == H2O_F32) {
+    cut(Kernel::Fma, attend_fma_row_tile(rows));
+  } else if (rows <= kFewRows) {
+    cut(Kernel::Mma, attend_mma_row_tile(rows));
+  } else {
+    cut(Kernel::Tc1, 128);
+    if (p.most_keys > kShortKeys) cut(Kernel::Tc2, 256);
+  }
+  p.row_tiles = (int)((rows + pl.tile - 1) / pl.tile);
+  const int64_t units = (int64_t)p.row_tiles * a.heads * p.problems;
+  split_part(p, p.most_keys, units, sm_count(c.device), pl.kernel, pl.tile, c.format, a.dim, step, true);
+  if (units * p.splits > INT32_MAX) pl.rc = H2O_ERR_UNSUPPORTED;
+  if (p.splits > 1) {
+    a.slots = p.splits;
+    const size_t n = (size_t)p.splits * a.q_rows * a.heads * a.group;
+    pl.lse_offset = align_up(n * a.dim * sizeof(float));
+    pl.scratch = pl.lse_offset + align_up(n * sizeof(float));
+  }
+  return pl;
 }
 
 int launched(cudaError_t e) {
@@ -132,7 +206,7 @@ int h2o_rotate(const h2o_rotary_t* rotary, const void* x, void* out, int32_t dty
   if (bad_stride(x_stride, dense) || bad_stride(out_stride, dense)) return H2O_ERR_INVALID_ARG;
   if (position_stride != 0 && position_stride < n_tokens) return H2O_ERR_INVALID_ARG;
   if (x == out && x_stride != out_stride && n_tokens > 1) return H2O_ERR_INVALID_ARG;
-  h2o::MoveArgs a = {};
+  MoveArgs a = {};
   a.q = x;
   a.q_out = out;
   a.q_stride = x_stride;
@@ -144,7 +218,7 @@ int h2o_rotate(const h2o_rotary_t* rotary, const void* x, void* out, int32_t dty
   a.turn = turn_of(rotary, positions, position_stride, n_tokens, inverse != 0);
   DeviceGuard guard(rotary->device);
   if (!guard.ok) return H2O_ERR_CUDA;
-  return launched(h2o::launch_move(a, dtype, static_cast<cudaStream_t>(stream)));
+  return launched(launch_move(a, dtype, static_cast<cudaStream_t>(stream)));
 }
 
 int h2o_pages_create(h2o_pages_t** out, const h2o_pages_config_t* cfg) {
@@ -162,11 +236,30 @@ int h2o_pages_create(h2o_pages_t** out, const h2o_pages_config_t* cfg) {
   h2o_pages* p = new (std::nothrow) h2o_pages();
   if (!p) return H2O_ERR_INVALID_ARG;
   p->cfg = *cfg;
-  p->polls = h2o::kStorePolls;
+  p->polls = kStorePolls;
   if (cfg->page_stride == 0) {
     p->cfg.head_stride = cfg->head_dim;
     p->cfg.row_stride = (int64_t)cfg->n_heads * cfg->head_dim;
     p->cfg.page_stride = p->cfg.row_stride * cfg->page_size;
+  }
+  if (cfg->format == H2O_BF16) {  // the kernels for bfloat16 read the pages by TMA
+    const int one = attend_tc_box_rows(H2O_BF16, cfg->head_dim, 1), two = attend_tc_box_rows(H2O_BF16, cfg->head_dim, 2);
+    p->few_box = std::gcd(cfg->page_size, kFewBoxRows);
+    p->one_box = std::gcd(cfg->page_size, one);
+    p->two_box = std::gcd(cfg->page_size, two);
+    struct {
+      unsigned char* map;
+      const void* base;
+      int box;
+      bool whole;
+    } const maps[6] = {{p->few_k, cfg->k, p->few_box, p->few_box == kFewBoxRows}, {p->few_v, cfg->v, p->few_box, p->few_box == kFewBoxRows},
+                       {p->one_k, cfg->k, p->one_box, false},                     {p->one_v, cfg->v, p->one_box, false},
+                       {p->two_k, cfg->k, p->two_box, false},                     {p->two_v, cfg->v, p->two_box, false}};
+    for (const auto& m : maps)
+      if (!make_page_map(reinterpret_cast<CUtensorMap_st*>(m.map), p->cfg, m.base, m.box, m.whole)) {
+        delete p;
+        return H2O_ERR_CUDA;
+      }
   }
   *out = p;
   return H2O_OK;
@@ -179,7 +272,7 @@ int h2o_pages_destroy(h2o_pages_t* pages) {
 
 int h2o_debug_pages_set_polls(h2o_pages_t* pages, int32_t polls) {
   if (!pages) return H2O_ERR_INVALID_ARG;
-  pages->polls = polls < 0 ? h2o::kStorePolls : std::min((uint32_t)polls, h2o::kStorePolls);
+  pages->polls = polls < 0 ? kStorePolls : std::min((uint32_t)polls, kStorePolls);
   return H2O_OK;
 }
 
@@ -204,7 +297,7 @@ int h2o_pages_append(h2o_pages_t* pages, const h2o_tokens_t* tokens, const h2o_s
   if (!t.cu && t.n_tokens < t.batch) return H2O_ERR_INVALID_ARG;
   if (bad_stride(t.kv_stride, (int64_t)c.n_heads * c.head_dim)) return H2O_ERR_INVALID_ARG;
   if (t.position_stride != 0 && t.position_stride < t.n_tokens) return H2O_ERR_INVALID_ARG;
-  h2o::MoveArgs a = {};
+  MoveArgs a = {};
   if (t.q) {
     if (!t.q_out || misaligned(t.q, 16) || misaligned(t.q_out, 16)) return H2O_ERR_INVALID_ARG;
     const int64_t dense = (int64_t)c.n_heads * t.query_group * c.head_dim;
@@ -241,13 +334,13 @@ int h2o_pages_append(h2o_pages_t* pages, const h2o_tokens_t* tokens, const h2o_s
   a.status = c.status;
   DeviceGuard guard(c.device);
   if (!guard.ok) return H2O_ERR_CUDA;
-  return launched(h2o::launch_move(a, c.format, static_cast<cudaStream_t>(stream)));
+  return launched(launch_move(a, c.format, static_cast<cudaStream_t>(stream)));
 }
 
 size_t h2o_pages_scratch_bytes(const h2o_pages_t* pages, const h2o_queries_t* queries, const h2o_sequences_t* sequences,
                                int32_t window, int32_t sinks) {
   if (check_attend(pages, queries, sequences, window, sinks) != H2O_OK || nothing_to_do(queries)) return 0;
-  return 0;
+  return make_plan(pages, queries, sequences, window, sinks).scratch;
 }
 
 int h2o_pages_attend(h2o_pages_t* pages, const h2o_queries_t* queries, const h2o_sequences_t* sequences, int32_t window,
@@ -256,42 +349,23 @@ int h2o_pages_attend(h2o_pages_t* pages, const h2o_queries_t* queries, const h2o
   if (rc != H2O_OK || nothing_to_do(queries)) return rc;
   rc = check_pointers(queries);
   if (rc != H2O_OK) return rc;
-  const h2o_pages_config_t& c = pages->cfg;
-  const h2o_queries_t* q = queries;
-  h2o::PagesAttend p = {};
-  h2o::AttendView& a = p.a;
-  a.q = q->q;
-  a.out = q->out;
-  a.lse = q->lse;
-  a.heads = c.n_heads;
-  a.group = q->query_group;
-  a.dim = c.head_dim;
-  const int64_t dense = (int64_t)a.heads * a.group * a.dim;
-  a.q_stride = q->q_stride ? q->q_stride : dense;
-  a.out_stride = q->out_stride ? q->out_stride : dense;
-  a.q_rows = q->q_rows;
-  a.cu_q = q->cu_q;
-  a.batch = q->batch;
-  a.max_q = std::min<int64_t>(q->max_q, q->q_rows);
-  a.scale2 = base2(q->softmax_scale > 0.f ? q->softmax_scale : 1.0f / std::sqrt((float)a.dim));
-  a.k = c.k;
-  a.v = c.v;
-  a.status = c.status;
-  a.part[0].length = sequences->length;
-  a.part[0].max_length = (int)std::min<int64_t>(sequences->max_length, (int64_t)sequences->max_pages * c.page_size);
-  p.table = sequences->table;
-  p.table_stride = sequences->table_stride ? sequences->table_stride : sequences->max_pages;
-  p.page_stride = c.page_stride;
-  p.row_stride = c.row_stride;
-  p.head_stride = c.head_stride;
-  p.n_pages = c.n_pages;
-  p.page_size = c.page_size;
-  p.max_pages = sequences->max_pages;
-  p.window = window;
-  p.sinks = sinks;
-  DeviceGuard guard(c.device);
+  Plan pl = make_plan(pages, queries, sequences, window, sinks);
+  if (pl.rc != H2O_OK) return pl.rc;
+  if (pl.scratch > 0) {
+    if (!scratch || scratch_bytes < pl.scratch || misaligned(scratch, kAlign)) return H2O_ERR_WORKSPACE;
+    pl.a.part_out = static_cast<float*>(scratch);
+    pl.a.part_lse = reinterpret_cast<float*>(static_cast<char*>(scratch) + pl.lse_offset);
+  }
+  DeviceGuard guard(pages->cfg.device);
   if (!guard.ok) return H2O_ERR_CUDA;
-  return launched(h2o::launch_pages_attend_simple(p, c.format, static_cast<cudaStream_t>(stream)));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (pl.kernel == Kernel::Fma) e = launch_attend_fma(pl.a, 0, pl.tile, H2O_F32, st);
+  else if (pl.kernel == Kernel::Mma) e = launch_attend_mma_paged(pl.a, pl.tile, pages->few_k, pages->few_v, st);
+  else if (pl.kernel == Kernel::Tc1) e = launch_attend_tc_paged(pl.a, 1, pages->one_k, pages->one_v, st);
+  else e = launch_attend_tc_paged(pl.a, 2, pages->two_k, pages->two_v, st);
+  if (e == cudaSuccess && pl.scratch > 0) e = launch_attend_join(pl.a, pages->cfg.format, st);
+  return launched(e);
 }
 
 }  // extern "C"

@@ -35,6 +35,17 @@ struct AttendPart {
   int chunk, splits;       // keys per split, splits per problem (of the longest)
   int row_tiles;           // tiles of query rows per problem (of the longest)
   int slot0;               // first partial slot of this part
+  int most_keys;           // paged rows: upper bound of the keys that a tile of query rows walks over
+};
+
+// Rows of a paged cache, and which of them a query sees (kernels with PAGED only; the parts' `begin` is unused there).
+struct Paging {
+  const int32_t* table;  // dev [sequences][stride]: page of each page_size rows of a sequence
+  int64_t stride;
+  int64_t page_stride, head_stride;  // elements (float32 rows; AttendView::row_stride within a page)
+  int n_pages, page_size;
+  int window, sinks;     // a query at row p sees the rows x <= p with x > p - window or x < sinks; window 0: all x <= p
+  int box;               // rows of a box of the tensor maps: divides page_size and the tile; float32: 8
 };
 
 struct AttendView {
@@ -61,6 +72,7 @@ struct AttendView {
   uint32_t polls;  // of a wait before it gives up
   int n_parts;
   AttendPart part[2];
+  Paging pages;
 };
 
 // A problem's query tokens and store rows, cut to what the caller allowed for, so that no index leaves its array
@@ -73,6 +85,7 @@ __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { 
 __device__ __forceinline__ int64_t first_token(const AttendView& a, int seq) {
   return clamp64(a.cu_q ? (int64_t)a.cu_q[seq] : (int64_t)seq, 0, a.q_rows);
 }
+template <bool PAGED = false>
 __device__ __forceinline__ Problem locate(const AttendView& a, const AttendPart& p, int i) {
   int s0 = i, s1 = i + 1;
   int64_t most = a.max_q;
@@ -85,6 +98,11 @@ __device__ __forceinline__ Problem locate(const AttendView& a, const AttendPart&
   Problem r;
   r.t0 = first_token(a, s0);
   r.nt = (int)clamp64(first_token(a, s1) - r.t0, 0, most);
+  if constexpr (PAGED) {
+    r.row0 = 0;
+    r.len = (int)clamp64(p.length[i], 0, p.max_length);
+    return r;
+  }
   r.row0 = clamp64(p.begin[i], 0, a.rows);
   r.len = (int)clamp64(p.length[i], 0, min((int64_t)p.max_length, a.rows - r.row0));
   return r;
@@ -102,6 +120,48 @@ __device__ __forceinline__ bool partial_ok(const AttendView& a, int64_t at) {
 // Rows of a problem that its query token `i` sees.
 __device__ __forceinline__ int seen_rows(const AttendPart& p, const Problem& r, int i) {
   return p.causal ? max(0, r.len - (r.nt - 1 - i)) : r.len;
+}
+
+// The keys that a block's query rows see, numbered as the block walks over them: the first `head` (the sinks, in whole tiles; 0 where
+// the window reaches down to them), then those from `start` on.  Without a window, and for ranges of a store: 0, 1, 2, ...
+struct Keys {
+  int head, start;  // start is a multiple of a box of rows
+  int end;          // behind the last one that the last row sees
+  int from;         // the first one behind the sinks that the first row sees (none between the sinks and it is seen by any row)
+  __device__ __forceinline__ int count() const { return head + end - start; }
+  __device__ __forceinline__ int at(int i) const { return i < head ? i : start + (i - head); }
+};
+// The first key behind the sinks that a row which sees `seen` keys in all (but for the window) sees.
+__device__ __forceinline__ int window_from(const AttendView& a, int seen) {
+  return a.pages.window > 0 ? max(0, max(0, seen) - a.pages.window) : 0;
+}
+// Keys of rows that see first_seen .. last_seen keys (but for the window), in tiles of `tile`.
+template <bool PAGED>
+__device__ __forceinline__ Keys keys_of(const AttendView& a, int first_seen, int last_seen, int tile) {
+  Keys k{0, 0, last_seen, 0};
+  if constexpr (PAGED) {
+    k.from = window_from(a, first_seen);
+    const int head = (min(a.pages.sinks, last_seen) + tile - 1) / tile * tile, start = k.from - k.from % a.pages.box;
+    if (start > head) {
+      k.head = head;
+      k.start = start;
+    }
+  }
+  return k;
+}
+// Is there no row that sees key x .. x + n - 1 of a tile?
+__device__ __forceinline__ bool unseen(const AttendView& a, const Keys& k, int x, int n) {
+  return x >= k.end || (x >= a.pages.sinks && x + n <= k.from);
+}
+// The keys that the chunks of a problem share out: of a paged one with a window, no more than the tile of rows that walks over most.
+template <bool PAGED>
+__device__ __forceinline__ int shared_keys(const AttendPart& p, const Problem& r) {
+  return PAGED ? min(r.len, p.most_keys) : r.len;
+}
+// The page of a sequence's row x, n_pages (which no tensor map holds: read as zeros) where it has none.
+__device__ __forceinline__ int page_of(const AttendView& a, int seq, int x) {
+  const int page = a.pages.table[seq * a.pages.stride + x / a.pages.page_size];
+  return page >= 0 && page < a.pages.n_pages ? page : a.pages.n_pages;
 }
 
 // The group of a sequence: the last one that starts at or before it.
@@ -202,10 +262,13 @@ int attend_mma_blocks_per_sm(int format, int tile);
 // part `first`, or (both) parts 0 and 1 in one launch, or (a.walk) part 1 with the prefix
 cudaError_t launch_attend_mma(const AttendView& a, int first, bool both, const int* tile, int format, const void* map_k,
                               const void* map_v, cudaStream_t stream);
+bool make_page_map(CUtensorMap_st* map, const h2o_pages_config_t& c, const void* base, int box_rows, bool whole);
+cudaError_t launch_attend_mma_paged(const AttendView& a, int tile, const void* map_k, const void* map_v, cudaStream_t stream);
 int attend_tc_box_rows(int format, int dim, int groups);
 // `groups` of 128 query rows to a block
 cudaError_t launch_attend_tc(const AttendView& a, int part, int groups, int format, const void* map_k, const void* map_v,
                              cudaStream_t stream);
+cudaError_t launch_attend_tc_paged(const AttendView& a, int groups, const void* map_k, const void* map_v, cudaStream_t stream);
 cudaError_t launch_attend_join(const AttendView& a, int q_dtype, cudaStream_t stream);
 
 }  // namespace h2o

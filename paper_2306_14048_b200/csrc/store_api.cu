@@ -5,29 +5,11 @@
 #include <cstring>
 #include <new>
 
-#include "store.cuh"
+#include "store_plan.cuh"
 
 namespace {
 
-constexpr size_t kAlign = 256;
-constexpr int kMaxGroup = 32;
-
-size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
-
-struct DeviceGuard {
-  int prev = -1;
-  bool ok = false;
-  explicit DeviceGuard(int dev) {
-    if (cudaGetDevice(&prev) != cudaSuccess) return;
-    ok = prev == dev || cudaSetDevice(dev) == cudaSuccess;
-    changed = ok && prev != dev;
-  }
-  ~DeviceGuard() {
-    if (changed) cudaSetDevice(prev);
-  }
-  bool changed = false;
-};
+using namespace h2o;
 
 int check_store(const h2o_store_config_t* c) {
   if (!c || !c->k || !c->v) return H2O_ERR_INVALID_ARG;
@@ -65,9 +47,6 @@ int check_rows(const h2o_store_t* store, const void* k, const void* v, int dtype
   return H2O_OK;
 }
 
-// The softmax scale for logits in base 2.
-float base2(float scale) { return (float)((double)scale * 1.4426950408889634074); }
-
 int check_queries(const h2o_store_t* store, const h2o_queries_t* q) {
   if (!store || !q) return H2O_ERR_INVALID_ARG;
   if (q->batch < 0 || q->q_rows < 0 || q->max_q < 0 || q->q_stride < 0 || q->out_stride < 0) return H2O_ERR_INVALID_ARG;
@@ -85,20 +64,11 @@ int check_queries(const h2o_store_t* store, const h2o_queries_t* q) {
   if (misaligned(q->cu_q, 4)) return H2O_ERR_INVALID_ARG;
   return H2O_OK;
 }
-bool nothing_to_do(const h2o_queries_t* q) { return q->batch == 0 || q->q_rows == 0 || q->max_q == 0; }
-int check_pointers(const h2o_queries_t* q) {
-  if (!q->q || !q->out || misaligned(q->q, 16) || misaligned(q->out, 16) || misaligned(q->lse, 4)) return H2O_ERR_INVALID_ARG;
-  if (q->q == q->out) return H2O_ERR_INVALID_ARG;
-  return H2O_OK;
-}
 int check_ranges(const h2o_ranges_t* r) {
   if (!r || r->max_length < 0) return H2O_ERR_INVALID_ARG;
   if (!r->begin || !r->length || misaligned(r->begin, 8) || misaligned(r->length, 4)) return H2O_ERR_INVALID_ARG;
   return H2O_OK;
 }
-
-enum class Kernel { Fma, Mma, Tc1, Tc2 };  // (tcgen05: one or two groups of 128 rows to a block)
-bool is_tc(Kernel k) { return k == Kernel::Tc1 || k == Kernel::Tc2; }
 
 // What a call launches and how much scratch it needs.
 struct Plan {
@@ -116,40 +86,11 @@ struct Plan {
 // and 37 / 37.  8-bit, 8 heads of 128, 32 query rows 26 / 28; 32 heads 61 / 73.
 int few_rows(int format) { return format == H2O_KV8 ? 32 : 16; }
 
-// Up to this many keys in a range the tcgen05 kernel takes 128 rows to a block, two blocks to an SM, so that one's start
-// and end run beside the other's tiles (bfloat16; the 8-bit kernel's shared memory holds one).  Own rows of 64 prompts of up
-// to 200 tokens behind a shared prefix: 117 -> 89 us; beside it, 515 keys for 32 heads of 131 tokens: 100 -> 108.
-constexpr int kShortKeys = 512;
-
 // Prefix and own rows together up to this many keys: each sequence's blocks read the prefix again (from the second-level
 // cache) rather than leave chunks for a joining kernel.  Device time of a call, joined / walked, prefix 300, up to 60 own
 // rows, 4 sequences, 8 heads of 128: 7.8 / 6.2 us, 8-bit 8.5 / 8.2; 660 keys: 6.6 / 7.4; and a launch less, 15 / 12 us a call.
 // Up to two blocks to an SM: prefix 400, 16 heads, 16 sequences: 11.7 / 8.4; 32 sequences, 8-bit: 16.4 / 17.7.
 constexpr int kWalkKeys = 512;
-
-// Splits the keys of a part: `units` blocks per split, `room` blocks that run at once.  Costs in keys of one block: a block
-// costs its keys and `fixed` more (start, merge, its result's trip through memory), the joining kernel twice as much;
-// a block that has its SM to itself is taken to run twice as fast, and the last blocks to finish to leave a quarter of a
-// block's time unused.  Only the longest length is known here: the lengths of a batch's sequences (`ragged`) are taken
-// to average two thirds of it.  Chunks are multiples of `step` keys, what a block takes at a time.
-void split_part(h2o::AttendPart& p, int64_t units, int64_t room, int64_t fixed, int64_t step, bool ragged) {
-  const int64_t len = std::max(1, p.max_length), num = ragged ? 2 : 3;
-  int64_t best = -1;
-  for (int64_t n = 1; n <= h2o::kMaxSplits && (n == 1 || units * n <= 16 * room); ++n) {
-    const int64_t chunk = ((len + n - 1) / n + step - 1) / step * step;
-    const int64_t splits = (len + chunk - 1) / chunk;
-    const int64_t one = std::min(chunk, len) + fixed;
-    const int64_t blocks = std::max(units, units * splits * num / 3);
-    int64_t cost = std::max(one / 2, (units * len * num / 3 + blocks * fixed) / room) + one / 4;
-    if (splits > 1) cost += 2 * fixed;
-    if (best < 0 || cost < best) {
-      best = cost;
-      p.chunk = (int)chunk;
-      p.splits = (int)splits;
-    }
-    if (chunk == step) break;
-  }
-}
 
 Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_ranges_t* prefix, int n_groups,
                const int32_t* cu_group, int max_group, const h2o_ranges_t* own) {
@@ -208,14 +149,7 @@ Plan make_plan(const h2o_store_t* store, const h2o_queries_t* q, const h2o_range
     }
     p.row_tiles = (int)((rows + pl.tile[n] - 1) / pl.tile[n]);
     const int64_t units = (int64_t)p.row_tiles * a.heads * p.problems;
-    // Fixed costs: about 3 us at a block's share of the memory's 6.4 TB/s; of the tcgen05 kernel 8 us at 80 keys in 1 us, of
-    // the FMA kernel 2 us at 64 keys in 3.5.
-    const int key_bytes = 2 * a.dim * (c.format == H2O_KV8 ? 1 : c.format == H2O_BF16 ? 2 : 4);
-    const bool tiles = pl.kernel[n] == Kernel::Fma && pl.tile[n] >= 16;
-    const int per_sm = pl.kernel[n] == Kernel::Tc2 ? 1 : pl.kernel[n] == Kernel::Tc1 || tiles ? 2 : pl.kernel[n] == Kernel::Fma ? 4 : h2o::attend_mma_blocks_per_sm(c.format, pl.tile[n]);
-    const int64_t room = (int64_t)sms * per_sm;
-    split_part(p, units, room, is_tc(pl.kernel[n]) ? 640 : tiles ? 36 : 19200000 / (room * key_bytes),
-               tiles ? 64 : 128, !p.grouped);
+    split_part(p, p.max_length, units, sms, pl.kernel[n], pl.tile[n], c.format, a.dim, 128, !p.grouped);
     if (units * p.splits > INT32_MAX) pl.rc = H2O_ERR_UNSUPPORTED;
     p.slot0 = n == 0 ? 0 : a.part[0].splits;
     ++n;

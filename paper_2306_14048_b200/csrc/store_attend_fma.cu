@@ -1,4 +1,4 @@
-// Attention over a K/V store for float32 queries, on the fp32 FMA pipe (float32 or 8-bit rows, head_dim 64 and 128): a kernel
+// Attention over a K/V store or a paged cache for float32 queries, on the fp32 FMA pipe (float32 or 8-bit rows, head_dim 64 and 128): a kernel
 // for up to four query rows (a decoding step) and one for more.
 //
 // More: a block takes BM query rows (query tokens times the query heads of one K/V head) and walks over its keys 64 at a
@@ -39,6 +39,27 @@ struct Smem {
   float p[BM][kBN + 4];
 };
 
+// Element 0 of row x of a sequence in a paged cache; null where it has no page (zeros).  Eight rows from a multiple of 8 on lie in one
+// page.
+__device__ __forceinline__ const float* paged_row(const void* base, const AttendView& a, int seq, int head, int x) {
+  const int page = page_of(a, seq, x);
+  if (page >= a.pages.n_pages) return nullptr;
+  return static_cast<const float*>(base) + page * a.pages.page_stride + x % a.pages.page_size * a.row_stride + head * a.pages.head_stride;
+}
+
+// One tile of K or V of a paged cache, rows x .. x + 63 (x a multiple of 8), those that nobody sees zero.
+template <int D, int PITCH>
+__device__ __forceinline__ void load_paged_tile(float* dst, const void* base, const AttendView& a, const Keys& keys, int seq, int head, int x) {
+  constexpr int kV = D / 4;
+  for (int i = threadIdx.x; i < kBN * kV; i += kThreads) {
+    const int r = i / kV, c = (i % kV) * 4;
+    const float* from = unseen(a, keys, x + r, 1) ? nullptr : paged_row(base, a, seq, head, x + r);
+    if (from) cp_async16(dst + r * PITCH + c, from + c);
+    else *reinterpret_cast<float4*>(dst + r * PITCH + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  cp_commit();
+}
+
 // One tile of K or V (rows row0 .. row0 + n - 1 of one head; the rest of the tile zero: a key that no row sees may
 // hold anything, and 0 * NaN must not reach the sums).
 template <int FMT, int D, int PITCH>
@@ -73,14 +94,14 @@ __device__ __forceinline__ void load_tile(float* dst, const void* base, const ui
   cp_commit();
 }
 
-template <int FMT, int D, int BM>
+template <int FMT, int D, int BM, bool PAGED>
 __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_constant__ AttendView a, int part_index) {
   constexpr int RM = BM / 16, NC = D / 64;
   extern __shared__ __align__(16) unsigned char dyn[];
   Smem<D, BM>& sh = *reinterpret_cast<Smem<D, BM>*>(dyn);
   const AttendPart& part = a.part[part_index];
   const BlockWork w = block_work(a, part, blockIdx.x);
-  const Problem pr = locate(a, part, w.problem);
+  const Problem pr = locate<PAGED>(a, part, w.problem);
   const int rows = pr.nt * a.group;
   const int r0 = w.row_tile * BM;
   if (r0 >= rows) return;
@@ -88,9 +109,10 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
   const int key0 = w.split * part.chunk;
   // keys beyond what the tile's last row sees are never needed
   const int last_seen = seen_rows(part, pr, (r0 + n_rows - 1) / a.group);
-  const int key1 = min(last_seen, key0 + part.chunk);
+  const Keys keys = keys_of<PAGED>(a, PAGED ? seen_rows(part, pr, r0 / a.group) : last_seen, last_seen, kBN);
+  const int key1 = min(keys.count(), key0 + part.chunk);
   const bool direct = a.part_out == nullptr;
-  if (!direct && key0 >= pr.len) return;  // (the join kernel does not read it)
+  if (!direct && key0 >= shared_keys<PAGED>(part, pr)) return;  // (the join kernel does not read it)
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
 
   // the query rows, zero behind the last one
@@ -119,8 +141,14 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
 #pragma unroll
     for (int j = 0; j < NC; ++j) o[i][j] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
-  auto load_k = [&](int key) { load_tile<FMT, D, D + 4>(&sh.k[0][0], a.k, a.k_scale, a, w.head, pr.row0 + key, max(0, min(kBN, key1 - key))); };
-  auto load_v = [&](int key) { load_tile<FMT, D, D>(&sh.v[0][0], a.v, a.v_scale, a, w.head, pr.row0 + key, max(0, min(kBN, key1 - key))); };
+  auto load_k = [&](int key) {
+    if constexpr (PAGED) load_paged_tile<D, D + 4>(&sh.k[0][0], a.k, a, keys, w.problem, w.head, keys.at(key));
+    else load_tile<FMT, D, D + 4>(&sh.k[0][0], a.k, a.k_scale, a, w.head, pr.row0 + key, max(0, min(kBN, key1 - key)));
+  };
+  auto load_v = [&](int key) {
+    if constexpr (PAGED) load_paged_tile<D, D>(&sh.v[0][0], a.v, a, keys, w.problem, w.head, keys.at(key));
+    else load_tile<FMT, D, D>(&sh.v[0][0], a.v, a.v_scale, a, w.head, pr.row0 + key, max(0, min(kBN, key1 - key)));
+  };
   if (key0 < key1) {
     load_k(key0);
     load_v(key0);
@@ -158,8 +186,9 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
         float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < kJ; ++j) {
-          const int kx = key + x + 16 * j;
-          s[i][j] = kx < seen[i] && kx < key1 ? s[i][j] * a.scale2 : -INFINITY;
+          const int kx = (PAGED ? keys.at(key) : key) + x + 16 * j;
+          const bool there = PAGED ? kx < seen[i] && (kx < a.pages.sinks || kx >= window_from(a, seen[i])) : kx < seen[i] && kx < key1;
+          s[i][j] = there ? s[i][j] * a.scale2 : -INFINITY;
           top = fmaxf(top, s[i][j]);
         }
 #pragma unroll
@@ -265,21 +294,23 @@ __device__ __forceinline__ float4 load_row4(const void* base, const uint8_t* sca
   }
 }
 
-template <int FMT, int D, int R>
+template <int FMT, int D, int R, bool PAGED>
 __global__ void __launch_bounds__(kFewThreads) attend_few_kernel(const __grid_constant__ AttendView a, int part_index) {
   constexpr int kLanes = D / 4, kPer = 32 / kLanes, kKeys = kLoads * kPer;  // lanes of a key, keys of a load, of a step
   __shared__ float sh_m[kFewWarps][R], sh_l[kFewWarps][R];
   __shared__ __align__(16) float sh_o[kFewWarps][R][D];
   const AttendPart& part = a.part[part_index];
   const BlockWork w = block_work(a, part, blockIdx.x);
-  const Problem pr = locate(a, part, w.problem);
+  const Problem pr = locate<PAGED>(a, part, w.problem);
   const int rows = pr.nt * a.group, r0 = w.row_tile * R;
   if (r0 >= rows) return;
   const int n_rows = min(R, rows - r0);
   const int key0 = w.split * part.chunk;
   const bool direct = a.part_out == nullptr;
-  if (!direct && key0 >= pr.len) return;  // (the join kernel does not read it)
-  const int key1 = min(seen_rows(part, pr, (r0 + n_rows - 1) / a.group), key0 + part.chunk);
+  if (!direct && key0 >= shared_keys<PAGED>(part, pr)) return;  // (the join kernel does not read it)
+  const int last_seen = seen_rows(part, pr, (r0 + n_rows - 1) / a.group);
+  const Keys keys = keys_of<PAGED>(a, PAGED ? seen_rows(part, pr, r0 / a.group) : last_seen, last_seen, kKeys);
+  const int key1 = min(keys.count(), key0 + part.chunk);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int c = lane % kLanes * 4, sub = lane / kLanes;  // the lane's channels, its key of a load
 
@@ -295,7 +326,7 @@ __global__ void __launch_bounds__(kFewThreads) attend_few_kernel(const __grid_co
     q[r] = make_float4(0.f, 0.f, 0.f, 0.f);
     if (token_ok(a, pr.t0 + tok, (int)hq))
       q[r] = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (pr.t0 + tok) * a.q_stride + hq * D + c);
-    seen[r] = there ? min(key1, seen_rows(part, pr, tok)) : 0;
+    seen[r] = !there ? 0 : PAGED ? seen_rows(part, pr, tok) : min(key1, seen_rows(part, pr, tok));
     m[r] = -INFINITY;
     l[r] = 0.f;
     o[r] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -304,8 +335,28 @@ __global__ void __launch_bounds__(kFewThreads) attend_few_kernel(const __grid_co
   const int mine = kPer == 1 ? lane >> 2 : 2 * ((lane >> 1) & 7) + (lane >> 4);
   for (int key = key0 + warp * kKeys; key < key1; key += kFewWarps * kKeys) {
     float4 kk[kLoads], vv[kLoads];
+    const int key_at = PAGED ? keys.at(key) : key;
+    if constexpr (PAGED) {
+      // eight rows to a page, whose place is looked up once (the same for the whole warp)
+#pragma unroll
+      for (int h = 0; h < kKeys / 8; ++h) {
+        const int x0 = key_at + 8 * h;
+        const bool none = unseen(a, keys, x0, 8);
+        const float* from_k = none ? nullptr : paged_row(a.k, a, w.problem, w.head, x0);
+        const float* from_v = none ? nullptr : static_cast<const float*>(a.v) + (from_k - static_cast<const float*>(a.k));
+#pragma unroll
+        for (int i = h * kLoads / kPer; i < (h + 1) * kLoads / kPer; ++i) {
+          const int x = i * kPer + sub;
+          const bool there = from_k && !unseen(a, keys, key_at + x, 1);
+          const int64_t at = (int64_t)(x - 8 * h) * a.row_stride + c;
+          kk[i] = there ? __ldcs(reinterpret_cast<const float4*>(from_k + at)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          vv[i] = there ? __ldcs(reinterpret_cast<const float4*>(from_v + at)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      }
+    }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
+      if constexpr (PAGED) break;
       const int x = key + i * kPer + sub;
       const bool there = x < key1;  // (what lies behind the range may be anything)
       kk[i] = there ? load_row4<FMT, D>(a.k, a.k_scale, a, w.head, pr.row0 + x, c) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -330,7 +381,9 @@ __global__ void __launch_bounds__(kFewThreads) attend_few_kernel(const __grid_co
       }
 #pragma unroll
       for (; bit > 0; bit >>= 1) d[0] += __shfl_xor_sync(0xffffffffu, d[0], bit);
-      s[r] = key + mine < seen[r] ? d[0] * a.scale2 : -INFINITY;
+      const int x = key_at + mine;
+      const bool sees = x < seen[r] && (!PAGED || x < a.pages.sinks || x >= window_from(a, seen[r]));
+      s[r] = sees ? d[0] * a.scale2 : -INFINITY;
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -410,28 +463,28 @@ __global__ void __launch_bounds__(kFewThreads) attend_few_kernel(const __grid_co
   }
 }
 
-template <int FMT, int D, int R>
+template <int FMT, int D, int R, bool PAGED>
 cudaError_t launch_few(const AttendView& a, int part, cudaStream_t stream) {
-  attend_few_kernel<FMT, D, R><<<(unsigned)part_blocks(a, a.part[part]), kFewThreads, 0, stream>>>(a, part);
+  attend_few_kernel<FMT, D, R, PAGED><<<(unsigned)part_blocks(a, a.part[part]), kFewThreads, 0, stream>>>(a, part);
   return cudaGetLastError();
 }
-template <int FMT, int D, int BM>
+template <int FMT, int D, int BM, bool PAGED>
 cudaError_t launch(const AttendView& a, int part, cudaStream_t stream) {
   constexpr int smem = (int)sizeof(Smem<D, BM>);
   static unsigned long long flags = 0;
-  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(attend_fma_kernel<FMT, D, BM>), smem, &flags);
+  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(attend_fma_kernel<FMT, D, BM, PAGED>), smem, &flags);
   if (e != cudaSuccess) return e;
-  attend_fma_kernel<FMT, D, BM><<<(unsigned)part_blocks(a, a.part[part]), kThreads, smem, stream>>>(a, part);
+  attend_fma_kernel<FMT, D, BM, PAGED><<<(unsigned)part_blocks(a, a.part[part]), kThreads, smem, stream>>>(a, part);
   return cudaGetLastError();
 }
-template <int FMT, int D>
+template <int FMT, int D, bool PAGED = false>
 cudaError_t launch_shape(const AttendView& a, int part, int tile, cudaStream_t stream) {
   switch (tile) {
-    case 1: return launch_few<FMT, D, 1>(a, part, stream);
-    case 2: return launch_few<FMT, D, 2>(a, part, stream);
-    case 4: return launch_few<FMT, D, 4>(a, part, stream);
-    case 16: return launch<FMT, D, 16>(a, part, stream);
-    default: return launch<FMT, D, 64>(a, part, stream);
+    case 1: return launch_few<FMT, D, 1, PAGED>(a, part, stream);
+    case 2: return launch_few<FMT, D, 2, PAGED>(a, part, stream);
+    case 4: return launch_few<FMT, D, 4, PAGED>(a, part, stream);
+    case 16: return launch<FMT, D, 16, PAGED>(a, part, stream);
+    default: return launch<FMT, D, 64, PAGED>(a, part, stream);
   }
 }
 
@@ -442,6 +495,7 @@ cudaError_t launch_shape(const AttendView& a, int part, int tile, cudaStream_t s
 int attend_fma_row_tile(int64_t rows) { return rows <= 2 ? (int)rows : rows <= 4 ? 4 : rows <= 16 ? 16 : 64; }
 
 cudaError_t launch_attend_fma(const AttendView& a, int part, int tile, int format, cudaStream_t stream) {
+  if (a.pages.table) return a.dim == 128 ? launch_shape<H2O_F32, 128, true>(a, part, tile, stream) : launch_shape<H2O_F32, 64, true>(a, part, tile, stream);
   if (format == H2O_F32) return a.dim == 128 ? launch_shape<H2O_F32, 128>(a, part, tile, stream) : launch_shape<H2O_F32, 64>(a, part, tile, stream);
   return a.dim == 128 ? launch_shape<H2O_KV8, 128>(a, part, tile, stream) : launch_shape<H2O_KV8, 64>(a, part, tile, stream);
 }

@@ -1,5 +1,5 @@
-// Attention over a K/V store for few query rows (a decoding step): bfloat16 queries, bfloat16 or 8-bit rows,
-// head_dim 64 or 128.  Bound by reading K and V once.
+// Attention over a K/V store or a paged cache for few query rows (a decoding step): bfloat16 queries, bfloat16 or 8-bit
+// rows, head_dim 64 or 128.  Bound by reading K and V once.
 //
 // Rows here are query tokens times the query heads of one K/V head: one for a plain decoding step, the group for
 // grouped heads, all sequences of a group for a shared prefix.  A block takes 8 NT of them and a chunk of the keys;
@@ -71,6 +71,15 @@ __device__ __forceinline__ void tma_4d(void* dst, const CUtensorMap* map, int c1
       : "memory");
 }
 
+// One box of a page: dimensions {64 channels, row in the page, half of the head dimension, head, page}.
+__device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, int row, int half, int head, int page, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::
+          "r"(dst),
+      "l"(map), "r"(0), "r"(row), "r"(half), "r"(head), "r"(page), "r"(smem_u32(bar))
+      : "memory");
+}
+
 template <bool F16>
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if constexpr (F16)
@@ -135,8 +144,10 @@ __device__ __forceinline__ uint32_t chunk_addr(uint32_t tile, int r, int c) {
 }
 
 // NTB: the kernel's larger number of n-tiles, which the ring is made for.  WALK: the block takes its sequence's prefix
-// (part 0's range) and then its own rows, and writes the result: no chunks, no joining kernel.
-template <int FMT, int D, int NT, int NTB, bool WALK>
+// (part 0's range) and then its own rows, and writes the result: no chunks, no joining kernel.  PAGED: the rows lie in
+// pages; a tile is one copy where its 32 rows lie in one page, else a copy for each box of 16 or 8 rows and half of the
+// head dimension, each issued by a lane of its own, which has looked its page up a tile ahead.
+template <int FMT, int D, int NT, int NTB, bool WALK, bool PAGED>
 __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* map_k, const CUtensorMap* map_v,
                                        const AttendPart& part, unsigned block, unsigned char* ring, Shared<NTB>& sh) {
   constexpr bool kF16 = FMT == H2O_KV8;
@@ -146,16 +157,18 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   static_assert(kRows * kPitch * 4 <= kSlots * kTile, "a warp's partial output fits its ring");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gl = lane >> 2, c4 = lane & 3;
   const BlockWork w = block_work(a, part, block);
-  const Problem pr = locate(a, part, w.problem);
+  const Problem pr = locate<PAGED>(a, part, w.problem);
   const int rows = pr.nt * a.group, r0 = w.row_tile * kRows;
   if (r0 >= rows) return;
   const int n_rows = min(kRows, rows - r0);
   const int key0 = w.split * part.chunk;
   const bool direct = a.part_out == nullptr;
-  if (!direct && key0 >= pr.len) return;  // (the join kernel does not read it)
+  if (!direct && key0 >= shared_keys<PAGED>(part, pr)) return;  // (the join kernel does not read it)
   const int last_seen = seen_rows(part, pr, (r0 + n_rows - 1) / a.group);  // the tile's last row sees the most
-  const int key1 = min(last_seen, key0 + part.chunk);
   const int first_seen = part.causal ? seen_rows(part, pr, r0 / a.group) : last_seen;
+  const Keys keys = keys_of<PAGED>(a, first_seen, last_seen, kKeys);
+  const int key1 = min(keys.count(), key0 + part.chunk);
+  [[maybe_unused]] const int last_from = PAGED ? window_from(a, last_seen) : 0;
 
   [[maybe_unused]] Problem prefix{0, 0, 0, 0};
   if constexpr (WALK) prefix = locate(a, a.part[0], group_of(a, w.problem));
@@ -166,6 +179,23 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   const int mine = n_tiles > warp ? (n_tiles - warp + kWarps - 1) / kWarps : 0;
   unsigned char* my_ring = ring + warp * (kSlots * kTile);
   uint64_t* full = sh.full[warp];
+  // PAGED: this lane's copy of a tile (one of `copies`): box `my_box`, half `my_half` of the channels (all, where it is one copy)
+  const int boxes = PAGED ? kKeys / a.pages.box : 1, copies = boxes == 1 ? 1 : boxes * (D / 64);
+  const int my_box = lane / (D / 64), my_half = lane % (D / 64);
+  int page_a = 0, page_b = 0;  // the pages of the tiles whose next K and V this lane asks for
+  auto row_of = [&](int j) { return keys.at(key0 + (warp + kWarps * j) * kKeys) + (boxes == 1 ? 0 : my_box * a.pages.box); };
+  auto lookup = [&](int j) {  // of tile j; what no row sees need not be read
+    if (j >= mine || lane >= copies) return 0;
+    const int x = row_of(j);
+    return unseen(a, keys, x, a.pages.box) ? a.pages.n_pages : page_of(a, w.problem, x);
+  };
+  auto issue_paged = [&](int i, int page) {  // item i, all lanes
+    if (lane == 0) mbar_expect_tx(&full[i % kSlots], kTile);
+    __syncwarp();
+    if (lane < copies)
+      tma_page(smem_u32(my_ring + (i % kSlots) * kTile) + (boxes == 1 ? 0 : my_half * (kKeys * 128) + my_box * a.pages.box * 128), (i & 1) ? map_v : map_k,
+               row_of(i >> 1) % a.pages.page_size, boxes == 1 ? 0 : my_half, w.head, page, &full[i % kSlots]);
+  };
   auto issue = [&](int i) {  // item i: K of tile i / 2, then its V; lane 0 only
     const int t = warp + kWarps * (i >> 1);
     int row = WALK && t < pre_tiles ? (int)prefix.row0 + t * kKeys : (int)pr.row0 + key0 + (t - pre_tiles) * kKeys;
@@ -177,9 +207,21 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   if (lane == 0) {
     for (int s = 0; s < kSlots; ++s) mbar_init(&full[s], 1);
     fence_barrier_init();
-    for (int i = 0; i < min(kSlots, 2 * mine); ++i) issue(i);
+    if constexpr (!PAGED) {
+      for (int i = 0; i < min(kSlots, 2 * mine); ++i) issue(i);
+    }
   }
   __syncwarp();
+  if constexpr (PAGED) {
+    int pages[(kSlots + 1) / 2];
+#pragma unroll
+    for (int j = 0; j < (kSlots + 1) / 2; ++j) pages[j] = lookup(j);
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i)
+      if (i < 2 * mine) issue_paged(i, pages[i >> 1]);
+    page_b = lookup((kSlots + 1) / 2);
+    page_a = kSlots % 2 ? pages[(kSlots - 1) / 2] : page_b;
+  }
 
   // ---- the query operand: lane (gl, c4) of n-tile nt holds row 8 nt + gl (the warps share the n-tiles) ----
   for (int nt = warp; nt < NT; nt += kWarps) {
@@ -277,7 +319,8 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   for (; j < mine; ++j) {
     const int tile_no = warp + kWarps * j;
     const bool in_prefix = WALK && tile_no < pre_tiles;
-    const int tile_key = in_prefix ? tile_no * kKeys : key0 + (tile_no - pre_tiles) * kKeys, end = in_prefix ? pre : key1;
+    const int tile_key = PAGED ? keys.at(key0 + tile_no * kKeys) : in_prefix ? tile_no * kKeys : key0 + (tile_no - pre_tiles) * kKeys;
+    const int end = PAGED ? keys.end : in_prefix ? pre : key1;
     const int there = min(kKeys, end - tile_key);
     if constexpr (kF16) {
       sh.k_factor[warp][lane] = kv8_scale(scale_k);
@@ -347,10 +390,15 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
         }
       }
       __syncwarp();
-      if (lane == 0 && i + kSlots < limit) issue(i + kSlots);
+      if constexpr (PAGED) {
+        if (__shfl_sync(0xffffffffu, limit, 0) > i + kSlots) issue_paged(i + kSlots, page_a);
+      } else {
+        if (lane == 0 && i + kSlots < limit) issue(i + kSlots);
+      }
     }
     // ---- logits (base 2); lane: keys gl, gl + 8 (+ 16 mt), rows 2 c4, 2 c4 + 1 (+ 8 nt) ----
-    const bool masked = tile_key + kKeys > (in_prefix ? pre : min(first_seen, key1));
+    const bool masked = PAGED ? tile_key + kKeys > first_seen || (tile_key < last_from && tile_key + kKeys > a.pages.sinks)
+                              : tile_key + kKeys > (in_prefix ? pre : min(first_seen, key1));
     bool grows = false;
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
@@ -368,7 +416,11 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
           x *= factor[nt][e & 1];
           if (masked) {
             const int key = tile_key + mt * 16 + gl + 8 * (e >> 1);
-            if (key >= (in_prefix ? pre : min(seen[nt][e & 1], key1))) x = -INFINITY;
+            if constexpr (PAGED) {
+              if (key >= seen[nt][e & 1] || (key >= a.pages.sinks && key < window_from(a, seen[nt][e & 1]))) x = -INFINITY;
+            } else {
+              if (key >= (in_prefix ? pre : min(seen[nt][e & 1], key1))) x = -INFINITY;
+            }
           }
           s[mt][nt][e] = x;
           grows |= x > m[nt][e & 1] + (kRescale + kHead);
@@ -422,7 +474,15 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
       const int i = 2 * j + 1, slot = i % kSlots;
       if (!wait(&full[slot], (uint32_t)(i / kSlots) & 1u, a.polls) && limit >= 0) limit = -1 - i;
       const uint32_t tile = smem_u32(my_ring + slot * kTile);
-      if (there < kKeys) {
+      if (PAGED && (there < kKeys || (tile_key < keys.from && tile_key + kKeys > a.pages.sinks))) {
+        // rows that nobody sees may hold anything
+        for (int x = lane; x < kKeys * (row_bytes(FMT, D) / 16); x += 32) {
+          const int r = x / (row_bytes(FMT, D) / 16);
+          const uint32_t at = chunk_addr<FMT, D>(tile, r, x % (row_bytes(FMT, D) / 16));
+          if (unseen(a, keys, tile_key + r, 1)) asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(at), "r"(0) : "memory");
+        }
+        __syncwarp();
+      } else if (!PAGED && there < kKeys) {
         // rows behind the range may hold anything, and 0 * NaN must not reach the sums
         for (int x = lane; x < (kKeys - there) * (row_bytes(FMT, D) / 16); x += 32) {
           const uint32_t at = chunk_addr<FMT, D>(tile, there + x / (row_bytes(FMT, D) / 16), x % (row_bytes(FMT, D) / 16));
@@ -470,9 +530,17 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
           }
         }
       }
-      if (WALK && there < kKeys) fence_proxy_async();  // (the zeros come before the copy that may go over them)
+      // (the zeros come before the copy that may go over them)
+      if (PAGED ? there < kKeys || tile_key < keys.from : WALK && there < kKeys) fence_proxy_async();
       __syncwarp();
-      if (lane == 0 && i + kSlots < limit) issue(i + kSlots);
+      if constexpr (PAGED) {
+        if (__shfl_sync(0xffffffffu, limit, 0) > i + kSlots) issue_paged(i + kSlots, page_b);
+        const int next = lookup(j + 1 + (kSlots + 1) / 2);
+        page_a = kSlots % 2 ? page_b : next;  // (an odd ring: the V of a tile is asked for when its K's successor is not yet)
+        page_b = next;
+      } else {
+        if (lane == 0 && i + kSlots < limit) issue(i + kSlots);
+      }
     }
   }
   if (__any_sync(0xffffffffu, limit < 0)) {
@@ -552,7 +620,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
 
 // One launch for part `first` alone, with 8 NT0 rows to a block, or for parts 0 and 1 (a shared prefix: many rows and
 // few), with 8 NT0 and 8 NT1.
-template <int FMT, int D, int NT0, int NT1, bool WALK>
+template <int FMT, int D, int NT0, int NT1, bool WALK, bool PAGED>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(FMT, NT0))
 attend_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                   const __grid_constant__ AttendView a, int first, unsigned blocks0) {
@@ -562,23 +630,23 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   let_next_start();  // (the joining kernel waits for this one's end; others are launched to start after it)
   if (NT0 == NT1 || blockIdx.x < blocks0) {
     const bool second = blockIdx.x >= blocks0;
-    attend<FMT, D, NT0, NT0, WALK>(a, &map_k, &map_v, a.part[second ? 1 : first], blockIdx.x - (second ? blocks0 : 0), ring, sh);
+    attend<FMT, D, NT0, NT0, WALK, PAGED>(a, &map_k, &map_v, a.part[second ? 1 : first], blockIdx.x - (second ? blocks0 : 0), ring, sh);
   } else {
-    attend<FMT, D, NT1, NT0, false>(a, &map_k, &map_v, a.part[1], blockIdx.x - blocks0, ring, sh);
+    attend<FMT, D, NT1, NT0, false, PAGED>(a, &map_k, &map_v, a.part[1], blockIdx.x - blocks0, ring, sh);
   }
   // a launch that started early does not end before the one in front of it, whatever its blocks have to do
   if (a.early && blockIdx.x == 0) wait_for_earlier();
 }
 
-template <int FMT, int D, int NT0, int NT1, bool WALK = false>
+template <int FMT, int D, int NT0, int NT1, bool WALK = false, bool PAGED = false>
 cudaError_t launch(const AttendView& a, int first, bool both, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t stream) {
   constexpr int smem = kWarps * ring_slots(FMT, D, NT0) * tile_bytes(FMT, D) + 1024;
   static unsigned long long flags = 0;
-  const void* f = reinterpret_cast<const void*>(attend_mma_kernel<FMT, D, NT0, NT1, WALK>);
+  const void* f = reinterpret_cast<const void*>(attend_mma_kernel<FMT, D, NT0, NT1, WALK, PAGED>);
   const cudaError_t e = ensure_dynamic_smem(f, smem, &flags);
   if (e != cudaSuccess) return e;
   const int64_t b0 = part_blocks(a, a.part[first]), b1 = both ? part_blocks(a, a.part[1]) : 0;
-  return launch_kernel(attend_mma_kernel<FMT, D, NT0, NT1, WALK>, dim3((unsigned)(b0 + b1)), kThreads, smem, stream, a.early != 0, map_k, map_v, a,
+  return launch_kernel(attend_mma_kernel<FMT, D, NT0, NT1, WALK, PAGED>, dim3((unsigned)(b0 + b1)), kThreads, smem, stream, a.early != 0, map_k, map_v, a,
                        first, (unsigned)b0);
 }
 
@@ -596,9 +664,27 @@ cudaError_t launch_rows(const AttendView& a, int first, bool both, const int* ti
   return cudaErrorInvalidValue;
 }
 
+template <int D>
+cudaError_t launch_paged(const AttendView& a, int tile, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t st) {
+  return tile == 8 ? launch<H2O_BF16, D, 1, 1, false, true>(a, 0, false, k, v, st) : launch<H2O_BF16, D, 2, 2, false, true>(a, 0, false, k, v, st);
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_tiled() {
+  static EncodeTiledFn fn = nullptr;
+  if (!fn) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      return nullptr;
+    fn = reinterpret_cast<EncodeTiledFn>(p);
+  }
+  return fn;
+}
 
 }  // namespace
 
@@ -608,15 +694,8 @@ int attend_mma_blocks_per_sm(int format, int tile) { return blocks_per_sm(format
 // Rows of a store: {bytes or elements of up to 128 bytes, rows, pieces of a row, heads}; a box is `box_rows` rows of one
 // head, swizzled over as many bytes as its inner extent.
 bool make_store_map(CUtensorMap_st* map, const h2o_store_config_t& c, const void* base, int box_rows) {
-  static EncodeTiledFn fn = nullptr;
-  if (!fn) {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess ||
-        found != cudaDriverEntryPointSuccess)
-      return false;
-    fn = reinterpret_cast<EncodeTiledFn>(p);
-  }
+  const EncodeTiledFn fn = encode_tiled();
+  if (!fn) return false;
   const bool eight = c.format == H2O_KV8;
   const cuuint64_t inner = eight ? c.head_dim : 64, pieces = eight ? 1 : c.head_dim / 64;
   const cuuint64_t row = eight ? c.head_dim : c.row_stride * 2, head = eight ? c.rows * c.head_dim : c.head_dim * 2;
@@ -628,6 +707,26 @@ bool make_store_map(CUtensorMap_st* map, const h2o_store_config_t& c, const void
             strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             eight && c.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Pages of bfloat16 rows: {64 channels, rows of a page, halves of the head dimension, heads, pages}; a box is `box_rows` rows of one
+// head and one page, all channels of them (`whole`) or 64.
+bool make_page_map(CUtensorMap_st* map, const h2o_pages_config_t& c, const void* base, int box_rows, bool whole) {
+  const EncodeTiledFn fn = encode_tiled();
+  if (!fn) return false;
+  const cuuint64_t halves = c.head_dim / 64;
+  const cuuint64_t dims[5] = {64, (cuuint64_t)c.page_size, halves, (cuuint64_t)c.n_heads, (cuuint64_t)c.n_pages};
+  const cuuint64_t strides[4] = {(cuuint64_t)c.row_stride * 2, 128, (cuuint64_t)c.head_stride * 2, (cuuint64_t)c.page_stride * 2};
+  const cuuint32_t box[5] = {64, (cuuint32_t)box_rows, whole ? (cuuint32_t)halves : 1, 1, 1};
+  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t launch_attend_mma_paged(const AttendView& a, int tile, const void* map_k, const void* map_v, cudaStream_t st) {
+  const CUtensorMap& k = *static_cast<const CUtensorMap*>(map_k);
+  const CUtensorMap& v = *static_cast<const CUtensorMap*>(map_v);
+  return a.dim == 128 ? launch_paged<128>(a, tile, k, v, st) : launch_paged<64>(a, tile, k, v, st);
 }
 
 cudaError_t launch_attend_mma(const AttendView& a, int first, bool both, const int* tile, int format, const void* map_k,

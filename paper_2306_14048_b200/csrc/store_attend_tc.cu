@@ -1,4 +1,4 @@
-// Attention over a K/V store for many query rows (prompts, a prefix shared by many sequences): tcgen05 with the
+// Attention over a K/V store or a paged cache for many query rows (prompts, a prefix shared by many sequences): tcgen05 with the
 // accumulators in tensor memory; bfloat16 queries, bfloat16 or 8-bit rows, head_dim 64 or 128.
 //
 // A block takes up to 256 query rows (query tokens times the query heads of one K/V head) as two groups of 128, A and
@@ -207,8 +207,18 @@ __device__ __forceinline__ void codes_to_f16(uint32_t word, __half2 scale, uint3
   hi = *reinterpret_cast<const uint32_t*>(&y);
 }
 
+// One box of a page, 64 channels wide: dimensions {64 channels, row in the page, half of the head dimension, head, page}.
+__device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, int row, int half, int head, int page, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::
+          "r"(dst),
+      "l"(map), "r"(0), "r"(row), "r"(half), "r"(head), "r"(page), "r"(smem_u32(bar))
+      : "memory");
+}
+
 // FINISH: part 1 of a shared prefix, which joins what part 0 left (an instance of its own: the rest is 5 % faster without).
-template <int FMT, int D, int G, bool FINISH>
+// PAGED: the rows lie in pages; the lanes of warp 0 issue a copy each for every box of rows and half of the head dimension.
+template <int FMT, int D, int G, bool FINISH, bool PAGED>
 __global__ void __launch_bounds__(threads(FMT, G), 3 - G)
 attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                  const __grid_constant__ AttendView a, int part_index) {
@@ -257,7 +267,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   }
   const AttendPart& part = a.part[part_index];
   const BlockWork w = block_work(a, part, blockIdx.x);
-  const Problem pr = locate(a, part, w.problem);
+  const Problem pr = locate<PAGED>(a, part, w.problem);
   const int rows = pr.nt * a.group, r0 = w.row_tile * (G * kM);
   // (a launch that started early does not end before the one in front of it, whatever its blocks have to do)
   if (a.early && part_index == 1 && blockIdx.x == 0) wait_for_earlier();
@@ -265,9 +275,15 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   const int n_rows = min(G * kM, rows - r0);
   const int key0 = w.split * part.chunk;
   const bool direct = a.part_out == nullptr || FINISH;
-  if (!direct && key0 >= pr.len) return;  // (the join kernel does not read it)
+  if (!direct && key0 >= shared_keys<PAGED>(part, pr)) return;  // (the join kernel does not read it)
   const int last_seen = seen_rows(part, pr, (r0 + n_rows - 1) / a.group);
-  const int key1 = min(last_seen, key0 + part.chunk);
+  const Keys keys = keys_of<PAGED>(a, PAGED ? seen_rows(part, pr, r0 / a.group) : last_seen, last_seen, kN);
+  const int key1 = min(keys.count(), key0 + part.chunk);
+  // PAGED: does tile j hold keys that no row sees (other than behind the chunk's end)?
+  auto has_hole = [&](int j) {
+    const int x = keys.at(key0 + j * kN);
+    return PAGED && x < keys.from && x + kN > a.pages.sinks;
+  };
   // (the shuffle tells the compiler that the value is the same in all lanes: the issuing loops then stay in uniform registers)
   const int nt = __shfl_sync(0xffffffffu, max(0, (key1 - key0 + kN - 1) / kN), 0);
   const bool alt = G == 2 && __shfl_sync(0xffffffffu, n_rows, 0) <= kM;  // both groups on the same rows, tiles in turn
@@ -324,7 +340,42 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 
   if (!softmax_warp) {
     setmaxnreg_dec<regs_other(FMT, G)>();
-    if (warp == 0) {
+    if (PAGED && warp == 0) {
+      // ---- TMA, a box to a lane: lane x has boxes x, x + 32, .. of K's and then V's ----
+      constexpr int kMost = (2 * kN / 8 * (D / 64) + 31) / 32;
+      const int per = kN / a.pages.box * (D / 64), box_bytes = a.pages.box * 128;  // boxes of a tile of K or V
+      int page[kMost], row[kMost];
+      auto lookup = [&](int j) {  // a tile ahead of its copies
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+          const int b = (lane + 32 * i) % per / (D / 64), x = keys.at(key0 + j * kN) + b * a.pages.box;
+          page[i] = a.pages.n_pages;
+          row[i] = x % a.pages.page_size;
+          if (j < nt && lane + 32 * i < 2 * per && !unseen(a, keys, x, a.pages.box)) page[i] = page_of(a, w.problem, x);
+        }
+      };
+      lookup(0);
+      int slot = 0, j = 0;
+      uint32_t phase = 1;
+      for (; j < nt; ++j) {
+        if (!__all_sync(0xffffffffu, wait_or_abort(&sh.kv_empty[slot], phase, abort_flag, a.polls))) break;
+        if (lane == 0) mbar_expect_tx(&sh.kv_full[slot], 2 * kTile);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+          const int x = lane + 32 * i, kv = x >= per, y = x - kv * per, half = y % (D / 64);
+          if (x < 2 * per)
+            tma_page(smem_u32(ring + (2 * slot + kv) * kTile) + half * (kN * 128) + y / (D / 64) * box_bytes, kv ? &map_v : &map_k, row[i], half, w.head,
+                     page[i], &sh.kv_full[slot]);
+        }
+        lookup(j + 1);
+        if (++slot == n_load) {
+          slot = 0;
+          phase ^= 1;
+        }
+      }
+      if (lane == 0) sh.loads = j;
+    } else if (warp == 0) {
       // ---- TMA ----
       if (lane == 0) {
         int slot = 0, j = 0;
@@ -349,6 +400,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       bool ok = first >= nt || wait_or_abort(&sh.q_full[alt ? 0 : g], 0, abort_flag, a.polls);
       int slot = first;
       uint32_t phase = 0;
+      int cleared = 0;
       for (int j = first, n = 0; j < nt; j += step, ++n) {
         if (slot >= n_stages) {
           slot -= n_stages;
@@ -359,20 +411,30 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         ok = __all_sync(0xffffffffu, ok) != 0;
         if (!ok) break;
         tc_fence_after();
-        if (!kF16 && j == nt - 1) {
-          // the range's last V tile: zeros behind it, by group A's warp or the one that uses it
+        if (!kF16 && (j == nt - 1 || has_hole(j))) {
+          // the range's last V tile: zeros behind it (PAGED: in every row that nobody sees, also of up to two tiles that reach into
+          // what lies between the sinks and the window), by group A's warp or the one that uses it.  Group A may be tiles ahead:
+          // each cleared tile has a barrier of its own (bfloat16 rows use no ring of codes).
+          uint64_t* const tail = cleared == 0 ? &sh.tail : &sh.raw_full[cleared == 1 ? 0 : 1];
           if (alt || g == 0) {
-            const int there = key1 - key0 - j * kN;
             const uint32_t tile = smem_u32(ring + (2 * slot + 1) * kTile);
-            for (int x = lane; x < (kN - there) * (D / 8); x += 32)
-              st_shared16(operand_addr(tile, kN, there + x / (D / 8), x % (D / 8)), make_uint4(0, 0, 0, 0));
+            if constexpr (PAGED) {
+              const int key = keys.at(key0 + j * kN);
+              for (int x = lane; x < kN * (D / 8); x += 32)
+                if (unseen(a, keys, key + x / (D / 8), 1)) st_shared16(operand_addr(tile, kN, x / (D / 8), x % (D / 8)), make_uint4(0, 0, 0, 0));
+            } else {
+              const int there = key1 - key0 - j * kN;
+              for (int x = lane; x < (kN - there) * (D / 8); x += 32)
+                st_shared16(operand_addr(tile, kN, there + x / (D / 8), x % (D / 8)), make_uint4(0, 0, 0, 0));
+            }
             fence_proxy_async();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.tail);
+            if (lane == 0) mbar_arrive(tail);
           } else {
-            ok = __all_sync(0xffffffffu, wait_or_abort(&sh.tail, 0, abort_flag, a.polls)) != 0;
+            ok = __all_sync(0xffffffffu, wait_or_abort(tail, 0, abort_flag, a.polls)) != 0;
             if (!ok) break;
           }
+          ++cleared;
         }
         const uint64_t dk = smem_desc_sw128(smem_u32(ring + 2 * slot * kTile), 16, 1024);
         if (elect_one()) {
@@ -529,8 +591,11 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const int rt = quarter * 32 + lane, r = base + rt;
       int tok, hq;
       split_row(r, tok, hq);
-      const int seen = min(key1, r < n_rows ? seen_rows(part, pr, tok) : key1);
-      const int all_seen = part.causal ? min(key1, seen_rows(part, pr, (r0 + base) / a.group)) : key1;
+      // the first key that the row does not see; of the group's first row
+      const int seen = PAGED ? (r < n_rows ? seen_rows(part, pr, tok) : last_seen) : min(key1, r < n_rows ? seen_rows(part, pr, tok) : key1);
+      const int all_seen = PAGED ? seen_rows(part, pr, (r0 + base) / a.group) : part.causal ? min(key1, seen_rows(part, pr, (r0 + base) / a.group)) : key1;
+      // PAGED: the first key behind the sinks that the row sees; of the block's last row
+      [[maybe_unused]] const int from = PAGED ? window_from(a, seen) : 0, last_from = PAGED ? window_from(a, last_seen) : 0;
       const float factor = kF16 ? sh.row_factor[r] : a.scale2;
       const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
       const uint32_t t_s = tmem + kColS + kStepS * g + lane_addr, t_o = tmem + kColO + kStepO * g + lane_addr;
@@ -556,7 +621,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           continue;
         }
         tc_fence_after();
-        const int key = key0 + j * kN;
+        const int key = PAGED ? keys.at(key0 + j * kN) : key0 + j * kN;
         uint32_t s[kN], p[kN / 2];
         tmem_load(t_s, s);
         tmem_wait_ld_of(s);
@@ -567,6 +632,11 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll
           for (int e = 0; e < kN; ++e)
             if (key + e >= seen) s[e] = 0xff800000u;
+        }
+        if (PAGED && key < last_from && key + kN > a.pages.sinks) {
+#pragma unroll
+          for (int e = 0; e < kN; ++e)
+            if (key + e < from && key + e >= a.pages.sinks) s[e] = 0xff800000u;
         }
         // two 16-bit probabilities to a word of p, words FROM .. TO - 1; returns their sum
         auto exponentials = [&](auto from, auto to) {
@@ -798,13 +868,13 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   }
 }
 
-template <int FMT, int D, int G, bool FINISH>
+template <int FMT, int D, int G, bool FINISH, bool PAGED = false>
 cudaError_t launch_finish(const AttendView& a, int part, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t stream) {
   constexpr int smem = smem_bytes(FMT, D, G);
   static unsigned long long flags = 0;
-  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(attend_tc_kernel<FMT, D, G, FINISH>), smem, &flags);
+  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(attend_tc_kernel<FMT, D, G, FINISH, PAGED>), smem, &flags);
   if (e != cudaSuccess) return e;
-  return launch_kernel(attend_tc_kernel<FMT, D, G, FINISH>, dim3((unsigned)part_blocks(a, a.part[part])), threads(FMT, G), smem, stream,
+  return launch_kernel(attend_tc_kernel<FMT, D, G, FINISH, PAGED>, dim3((unsigned)part_blocks(a, a.part[part])), threads(FMT, G), smem, stream,
                        a.early != 0 && part == 1, k, v, a, part);
 }
 template <int FMT, int D, int G>
@@ -815,6 +885,14 @@ cudaError_t launch(const AttendView& a, int part, const CUtensorMap& k, const CU
 }  // namespace
 
 int attend_tc_box_rows(int format, int dim, int groups) { return tile_keys(format, dim, groups); }
+
+cudaError_t launch_attend_tc_paged(const AttendView& a, int groups, const void* map_k, const void* map_v, cudaStream_t st) {
+  const CUtensorMap& k = *static_cast<const CUtensorMap*>(map_k);
+  const CUtensorMap& v = *static_cast<const CUtensorMap*>(map_v);
+  if (groups == 1)
+    return a.dim == 128 ? launch_finish<H2O_BF16, 128, 1, false, true>(a, 0, k, v, st) : launch_finish<H2O_BF16, 64, 1, false, true>(a, 0, k, v, st);
+  return a.dim == 128 ? launch_finish<H2O_BF16, 128, 2, false, true>(a, 0, k, v, st) : launch_finish<H2O_BF16, 64, 2, false, true>(a, 0, k, v, st);
+}
 
 cudaError_t launch_attend_tc(const AttendView& a, int part, int groups, int format, const void* map_k, const void* map_v, cudaStream_t st) {
   const CUtensorMap& k = *static_cast<const CUtensorMap*>(map_k);

@@ -1,4 +1,4 @@
-// Joins the chunks of split attention over a K/V store.
+// Joins the chunks of split attention over a K/V store or a paged cache.
 //
 // A chunk i of a query row has left its normalised output o_i and the base-2 logarithm L_i of its sum of exponentials;
 // the row's output is sum w_i o_i / sum w_i with w_i = 2^(L_i - max L), in the fixed order of the chunks.  One warp per
@@ -11,7 +11,7 @@ namespace {
 
 constexpr int kMaxSlots = 2 * kMaxSplits;  // two parts
 
-template <typename T, int D>
+template <typename T, int D, bool PAGED>
 __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant__ AttendView a) {
   constexpr int kPer = D / 32;
   const int seq = blockIdx.y;
@@ -30,10 +30,10 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
     if (k >= a.n_parts || !live) break;
     const AttendPart& p = a.part[k];
     const int which = p.grouped ? group_of(a, seq) : seq;
-    const Problem pr = locate(a, p, which);
+    const Problem pr = locate<PAGED>(a, p, which);
     if (token < pr.t0 || token >= pr.t0 + pr.nt) live = false;  // beyond what the caller allowed for: left as it was
     slot[k] = p.slot0;
-    used[k] = (pr.len + p.chunk - 1) / p.chunk;
+    used[k] = (shared_keys<PAGED>(p, pr) + p.chunk - 1) / p.chunk;
   }
   // (Launched while the kernels that leave the chunks may still run: what does not depend on them is looked up before.  All
   // wait, so that this kernel never ends before them.)
@@ -100,7 +100,9 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
 template <typename T, int D>
 cudaError_t launch(const AttendView& a, cudaStream_t stream) {
   const int64_t rows = (int64_t)a.max_q * a.heads * a.group;
-  return launch_kernel(attend_join_kernel<T, D>, dim3((unsigned)((rows + 7) / 8), (unsigned)a.batch), 256, 0, stream, true, a);
+  const dim3 grid((unsigned)((rows + 7) / 8), (unsigned)a.batch);
+  return a.pages.table ? launch_kernel(attend_join_kernel<T, D, true>, grid, 256, 0, stream, true, a)
+                       : launch_kernel(attend_join_kernel<T, D, false>, grid, 256, 0, stream, true, a);
 }
 
 }  // namespace
