@@ -6,9 +6,9 @@
 struct h2o_pages {
   h2o_pages_config_t cfg;  // strides filled in
   uint32_t polls;          // of a wait before it gives up
-  // bfloat16: tensor maps (opaque here) for few query rows, and for many in blocks of one and of two groups, and rows of their boxes
-  alignas(64) unsigned char few_k[128], few_v[128], one_k[128], one_v[128], two_k[128], two_v[128];
-  int few_box, one_box, two_box;
+  // bfloat16: tensor maps (opaque here) for few query rows and for many, and the rows of their boxes
+  alignas(64) unsigned char few_k[128], few_v[128], many_k[128], many_v[128];
+  int few_box, many_box;
 };
 
 namespace h2o {
@@ -37,6 +37,8 @@ struct MoveArgs {
   int n_pages, page_size, max_pages, max_length, batch;
   int32_t* status;
 };
+int pages_tc_tile_keys();
+cudaError_t launch_pages_tc(const AttendView& a, const void* map_k, const void* map_v, cudaStream_t stream);
 cudaError_t launch_move(const MoveArgs& a, int dtype, cudaStream_t stream);
 
 }  // namespace h2o

@@ -144,33 +144,25 @@ Plan make_plan(const h2o_pages_t* pages, const h2o_queries_t* q, const h2o_seque
   g.window = window;
   g.sinks = sinks;
   const int64_t rows = (int64_t)a.max_q * a.group;
-  int step = 128, keys_of_tile;  // a chunk's keys are a multiple of a tile's
-  auto cut = [&](Kernel kernel, int tile) {
-    pl.kernel = kernel;
-    pl.tile = tile;
-    keys_of_tile = is_tc(kernel) ? attend_tc_box_rows(H2O_BF16, a.dim, kernel == Kernel::Tc1 ? 1 : 2) : 64;
-    g.box = kernel == Kernel::Fma ? 8 : kernel == Kernel::Mma ? pages->few_box : kernel == Kernel::Tc1 ? pages->one_box : pages->two_box;
-    if (is_tc(kernel)) step = 2 * keys_of_tile;
-    // the most keys a tile of query rows walks over: sinks in whole tiles, the window, as far as the tile's tokens lie apart, and
-    // down to the box the window starts in
-    p.most_keys = p.max_length;
-    if (window > 0) {
-      const int64_t span = std::min<int64_t>(a.max_q - 1, (tile + a.group - 2) / a.group);
-      const int64_t head = ((int64_t)std::min(sinks, p.max_length) + keys_of_tile - 1) / keys_of_tile * keys_of_tile;
-      p.most_keys = (int)std::min<int64_t>(p.max_length, head + window + span + g.box);
-    }
-  };
   if (c.format == H2O_F32) {
-    cut(Kernel::Fma, attend_fma_row_tile(rows));
-  } else if (rows <= kFewRows) {
-    cut(Kernel::Mma, attend_mma_row_tile(rows));
+    pl.kernel = Kernel::Fma;
+    pl.tile = attend_fma_row_tile(rows);
   } else {
-    cut(Kernel::Tc1, 128);
-    if (p.most_keys > kShortKeys) cut(Kernel::Tc2, 256);
+    pl.kernel = rows <= kFewRows ? Kernel::Mma : Kernel::Tc1;
+    pl.tile = rows <= kFewRows ? attend_mma_row_tile(rows) : 128;
+  }
+  g.box = pl.kernel == Kernel::Fma ? 8 : pl.kernel == Kernel::Mma ? pages->few_box : pages->many_box;
+  // the most keys a tile of query rows walks over: sinks in whole tiles (of 64 keys at most), the window, as far as the tile's tokens
+  // lie apart, and down to the box the window starts in
+  p.most_keys = p.max_length;
+  if (window > 0) {
+    const int64_t span = std::min<int64_t>(a.max_q - 1, (pl.tile + a.group - 2) / a.group);
+    const int64_t head = ((int64_t)std::min(sinks, p.max_length) + 63) / 64 * 64;
+    p.most_keys = (int)std::min<int64_t>(p.max_length, head + window + span + g.box);
   }
   p.row_tiles = (int)((rows + pl.tile - 1) / pl.tile);
   const int64_t units = (int64_t)p.row_tiles * a.heads * p.problems;
-  split_part(p, p.most_keys, units, sm_count(c.device), pl.kernel, pl.tile, c.format, a.dim, step, true);
+  split_part(p, p.most_keys, units, sm_count(c.device), pl.kernel, pl.tile, c.format, a.dim, 128, true);
   if (units * p.splits > INT32_MAX) pl.rc = H2O_ERR_UNSUPPORTED;
   if (p.splits > 1) {
     a.slots = p.splits;
@@ -243,18 +235,17 @@ int h2o_pages_create(h2o_pages_t** out, const h2o_pages_config_t* cfg) {
     p->cfg.page_stride = p->cfg.row_stride * cfg->page_size;
   }
   if (cfg->format == H2O_BF16) {  // the kernels for bfloat16 read the pages by TMA
-    const int one = attend_tc_box_rows(H2O_BF16, cfg->head_dim, 1), two = attend_tc_box_rows(H2O_BF16, cfg->head_dim, 2);
     p->few_box = std::gcd(cfg->page_size, kFewBoxRows);
-    p->one_box = std::gcd(cfg->page_size, one);
-    p->two_box = std::gcd(cfg->page_size, two);
+    p->many_box = std::gcd(cfg->page_size, pages_tc_tile_keys());
     struct {
       unsigned char* map;
       const void* base;
       int box;
       bool whole;
-    } const maps[6] = {{p->few_k, cfg->k, p->few_box, p->few_box == kFewBoxRows}, {p->few_v, cfg->v, p->few_box, p->few_box == kFewBoxRows},
-                       {p->one_k, cfg->k, p->one_box, false},                     {p->one_v, cfg->v, p->one_box, false},
-                       {p->two_k, cfg->k, p->two_box, false},                     {p->two_v, cfg->v, p->two_box, false}};
+    } const maps[4] = {{p->few_k, cfg->k, p->few_box, p->few_box == kFewBoxRows},
+                       {p->few_v, cfg->v, p->few_box, p->few_box == kFewBoxRows},
+                       {p->many_k, cfg->k, p->many_box, p->many_box == pages_tc_tile_keys()},
+                       {p->many_v, cfg->v, p->many_box, true}};
     for (const auto& m : maps)
       if (!make_page_map(reinterpret_cast<CUtensorMap_st*>(m.map), p->cfg, m.base, m.box, m.whole)) {
         delete p;
@@ -362,8 +353,7 @@ int h2o_pages_attend(h2o_pages_t* pages, const h2o_queries_t* queries, const h2o
   cudaError_t e;
   if (pl.kernel == Kernel::Fma) e = launch_attend_fma(pl.a, 0, pl.tile, H2O_F32, st);
   else if (pl.kernel == Kernel::Mma) e = launch_attend_mma_paged(pl.a, pl.tile, pages->few_k, pages->few_v, st);
-  else if (pl.kernel == Kernel::Tc1) e = launch_attend_tc_paged(pl.a, 1, pages->one_k, pages->one_v, st);
-  else e = launch_attend_tc_paged(pl.a, 2, pages->two_k, pages->two_v, st);
+  else e = launch_pages_tc(pl.a, pages->many_k, pages->many_v, st);
   if (e == cudaSuccess && pl.scratch > 0) e = launch_attend_join(pl.a, pages->cfg.format, st);
   return launched(e);
 }

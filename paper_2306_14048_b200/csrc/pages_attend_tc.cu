@@ -1,0 +1,599 @@
+// Attention over a paged cache for many query rows (prompts, pieces of prompts, windows): tcgen05 with the accumulators in
+// tensor memory; bfloat16, head_dim 64 or 128.
+//
+// An item of work is up to 128 query rows (query tokens times the query heads of one K/V head) against the keys that they see,
+// 64 at a time:
+//   S(j) = Q K_j^T         into tensor memory, from there into the softmax threads' registers, which frees S at once
+//   P(j) = exp2(S - m)     bf16, into tensor memory of its own
+//   O   += P(j) V_j        P is the tensor-memory operand, V the MN-major shared-memory operand
+// Two blocks share an SM, so that one's exponentials run beside the other's products.  A block goes on to further items until
+// there are none: it takes over the place of a block of the grid that has not started (clusterlaunchcontrol), so that the
+// hardware hands the work out in the grid's order and nobody counts.  The next item's keys and queries are on their way while
+// the last tiles of an item are computed, and its first S while the item's result is written.
+// Measured (us; blocks of one item each before): see the table of the document that describes the design.
+// Roles: warp 0 takes items and issues the copies of K and V, a box of a page to a lane; warp 1 issues S, warp 3 issues P V,
+// clears what nobody sees in a V tile (0 * NaN must not reach the sums) and owns tensor memory; warp 2 copies query rows;
+// warps 4..7 are the softmax, one thread per row.
+// The reference m of a row is the maximum of its first tile.  Later tiles compute their exponentials against it without
+// looking for a maximum: only when a tile's sum comes out large (kLargeSum) the tile is done again with the new maximum and O
+// is rescaled.  A value far above the reference costs no precision in floating point, only range.
+// Rounding: P is one bf16.  Its error, up to 2^-8 relative per key and of either sign, averages over the keys to about that of
+// the output's own rounding, which is up to 2^-8 as well.  Row sums are fp32 sums of the unrounded values.
+#include "attend_tc.cuh"
+#include "pages.cuh"
+
+namespace h2o {
+
+namespace {
+
+using namespace tc;
+
+constexpr int kM = 128, kN = 64;  // rows and keys of a tile
+constexpr int kThreads = 256;
+constexpr int kItems = 2;  // ring of items, the one under way and the next
+// Rings of tiles of K and of V, what fits half an SM's shared memory beside the queries.  (K is done with a tile earlier than V: a
+// ring of pairs would hold it as long.)
+__host__ __device__ constexpr int tile_bytes(int d) { return kN * d * 2; }
+__host__ __device__ constexpr int slots_k(int d) { return d == 128 ? 2 : 4; }
+__host__ __device__ constexpr int slots_v(int d) { return d == 128 ? 3 : 5; }
+constexpr int kMaxSlots = 5;
+// Registers of a thread: 256 start with 128 each = 128 x 176 + 128 x 80.
+constexpr int kRegsSoftmax = 176, kRegsOther = 80;
+constexpr int kPolyEvery = 8;  // every so many pairs of exponentials one runs on the FMA pipe
+constexpr float kRescale = 8.f;
+constexpr float kLargeSum = 1048576.f;  // O, which is divided by its sum at the end, then holds values up to 2^100
+
+// What a block works on; nt < 0: nothing any more.
+struct Item {
+  int nt;              // tiles of keys
+  int head, split;
+  int r0, n_rows;      // rows of the problem
+  int problem, key0;   // first key of the chunk, as the block numbers them
+  int tokens, len;     // of the problem
+  int64_t t0;          // its first token
+  Keys keys;
+};
+
+struct Shared {
+  uint4 answer;  // to the request for another block's place
+  uint64_t full[2][kMaxSlots], empty[2][kMaxSlots];  // K, V
+  uint64_t item_full[kItems], item_empty[kItems];
+  uint64_t answered;
+  uint64_t q_full, q_empty;
+  uint64_t s_full, s_read;   // S is complete / in the softmax threads' registers
+  uint64_t p_full, p_empty;  // P is complete / used, and O includes it
+  uint64_t o_final;
+  uint64_t ended;  // of a block that gives up: the products of warps 1 and 3 have ended
+  Item item[kItems];
+  uint32_t tmem_base;
+  int abort_flag;
+};
+__host__ __device__ constexpr int smem_bytes(int d) { return kM * d * 2 + (slots_k(d) + slots_v(d)) * tile_bytes(d) + (int)sizeof(Shared); }
+
+// One box of a page: dimensions {64 channels, row in the page, half of the head dimension, head, page}.
+__device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, int row, int half, int head, int page, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::
+          "r"(dst),
+      "l"(map), "r"(0), "r"(row), "r"(half), "r"(head), "r"(page), "r"(smem_u32(bar))
+      : "memory");
+}
+// Asks for the place of a block that has not started.
+__device__ __forceinline__ void request_place(uint4* answer, uint64_t* bar) {
+  mbar_expect_tx(bar, 16);
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(answer)), "r"(smem_u32(bar))
+               : "memory");
+}
+// The place (its block index), or -1: there is none any more.
+__device__ __forceinline__ int place_of(const uint4* answer) {
+  uint32_t there, x;
+  asm volatile(
+      "{\n\t.reg .b128 a;\n\t.reg .pred p;\n\t.reg .b32 y, z, w;\n\t"
+      "ld.shared.b128 a, [%2];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "mov.b32 %1, 0;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, y, z, w}, a;\n\t}"
+      : "=r"(there), "=r"(x)
+      : "r"(smem_u32(answer))
+      : "memory");
+  return there ? (int)x : -1;
+}
+// The lowest n bits, for any n.
+__device__ __forceinline__ uint64_t bits_below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 2)
+pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttendView a) {
+  constexpr int kTile = tile_bytes(D), kQTile = kM * D * 2, kSlotsK = slots_k(D), kSlotsV = slots_v(D), kHalves = D / 64;
+  constexpr uint32_t kColO = 0, kColS = D, kColP = D + kN, kCols = 256;
+  static_assert(kColP + kN / 2 <= kCols, "tensor memory");
+  static_assert(smem_bytes(D) + 1024 <= 114 * 1024, "two blocks on an SM");
+  extern __shared__ unsigned char dyn[];
+  unsigned char* const q_tile = dyn;
+  unsigned char* const ring_k = dyn + kQTile;
+  unsigned char* const ring_v = ring_k + kSlotsK * kTile;
+  Shared& sh = *reinterpret_cast<Shared*>(ring_v + kSlotsV * kTile);
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    prefetch_tensormap(&map_k);
+    prefetch_tensormap(&map_v);
+    for (int i = 0; i < 2 * kMaxSlots; ++i) {
+      mbar_init(&sh.full[0][i], 1);
+      mbar_init(&sh.empty[0][i], 1);
+    }
+    for (int i = 0; i < kItems; ++i) {
+      mbar_init(&sh.item_full[i], 1);
+      mbar_init(&sh.item_empty[i], 7);  // all warps but warp 0
+    }
+    mbar_init(&sh.answered, 1);
+    mbar_init(&sh.q_full, 1);
+    mbar_init(&sh.q_empty, 1);
+    mbar_init(&sh.s_full, 1);
+    mbar_init(&sh.s_read, 4);
+    mbar_init(&sh.p_full, 4);
+    mbar_init(&sh.p_empty, 1);
+    mbar_init(&sh.o_final, 1);
+    mbar_init(&sh.ended, 2);
+    // the operands' swizzle counts from multiples of 1024 bytes
+    sh.abort_flag = (smem_u32(dyn) & 1023u) != 0;
+    fence_barrier_init();
+  }
+  if (warp == 3) tmem_alloc(&sh.tmem_base, kCols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem_base, 0);
+  volatile int* const abort_flag = &sh.abort_flag;
+  const AttendPart& part = a.part[0];
+  const int box = a.pages.box, shift = 31 - __clz(box);  // 8, 16, 32 or 64
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return wait_or_abort(bar, parity & 1u, abort_flag, a.polls); };
+  // all lanes of a warp
+  auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+  // Item number n, by a whole warp; its fields are copied, so that its place is free again.
+  auto next_item = [&](uint32_t n, Item& it) {
+    if (!wait_all(&sh.item_full[n % kItems], n / kItems)) return false;
+    it = sh.item[n % kItems];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sh.item_empty[n % kItems]);
+    return it.nt >= 0;
+  };
+  // token and query head of row r of an item: (first + r) / group by a multiplication (exact: first + r < 2^8, group <= 32)
+  const uint32_t magic = (65536u + a.group - 1) / a.group;
+  auto split_row = [&](const Item& it, int r, int& tok, int& hq) {
+    const int tok0 = it.r0 / a.group, first = it.r0 - tok0 * a.group;
+    const int d = (int)((uint32_t)(first + r) * magic >> 16);
+    tok = tok0 + d;
+    hq = it.head * a.group + first + r - d * a.group;
+  };
+
+  if (warp < 4) {
+    setmaxnreg_dec<kRegsOther>();
+    if (warp == 0) {
+      // ---- items, and the copies of their K and V ----
+      // A lane's copies of a tile: of K a box of rows and half of the channels (all, if the tile is one box), of V a box.
+      const int boxes = kN / box;
+      const int copies_k = boxes == 1 ? 1 : boxes * kHalves, my_k = boxes == 1 ? 0 : lane / kHalves, my_half = boxes == 1 ? 0 : lane % kHalves;
+      uint32_t n = 0, tiles_k = 0, tiles_v = 0, requests = 0;  // items published, tiles and places asked for
+      bool ok = true, pending = false;
+      Item it, next;
+      // What a place stands for: row tiles last to first (the longest of a causal prompt first), then head, split, sequence.
+      // False: no work.
+      auto describe = [&](unsigned i) {
+        const int row_tile = part.row_tiles - 1 - (int)(i % part.row_tiles);
+        i /= part.row_tiles;
+        next.head = (int)(i % a.heads);
+        i /= a.heads;
+        next.split = (int)(i % part.splits);
+        next.problem = (int)(i / part.splits);
+        const Problem pr = locate<true>(a, part, next.problem);
+        next.r0 = row_tile * kM;
+        next.n_rows = min(kM, pr.nt * a.group - next.r0);
+        next.key0 = next.split * part.chunk;
+        next.tokens = pr.nt;
+        next.len = pr.len;
+        next.t0 = pr.t0;
+        if (next.n_rows <= 0 || (a.part_out != nullptr && next.key0 >= shared_keys<true>(part, pr))) return false;
+        next.keys = keys_of<true>(a, seen_rows(part, pr, next.r0 / a.group), seen_rows(part, pr, (next.r0 + next.n_rows - 1) / a.group), kN);
+        next.nt = max(0, (min(next.keys.count(), next.key0 + part.chunk) - next.key0 + kN - 1) / kN);
+        return true;
+      };
+      auto publish = [&] {
+        ok = ok && wait_all(&sh.item_empty[n % kItems], n / kItems + 1);
+        if (ok && lane == 0) {
+          sh.item[n % kItems] = next;
+          mbar_arrive(&sh.item_full[n % kItems]);
+        }
+        __syncwarp();
+        ++n;
+      };
+      auto request = [&] {
+        if (lane == 0) request_place(&sh.answer, &sh.answered);
+        __syncwarp();
+        pending = true;
+      };
+      // The next item, or the end (nt < 0), found and published.
+      auto advance = [&](bool first) {
+        next.nt = -1;
+        for (bool found = first && describe(blockIdx.x); !found;) {
+          if (!pending) request();
+          ok = wait_all(&sh.answered, requests);
+          if (!ok) return;
+          pending = false;
+          ++requests;
+          const int place = place_of(&sh.answer);
+          fence_proxy_async();  // (read before the next answer is written over it)
+          __syncwarp();
+          if (place < 0) {
+            next.nt = -1;
+            break;
+          }
+          found = describe((unsigned)place);
+        }
+        publish();
+      };
+      advance(true);
+      while (ok && next.nt >= 0) {
+        it = next;
+        // The next place is asked for a few tiles before this item's last copies and taken two tiles before (not earlier: what a
+        // block holds back nobody else can take).
+        const int ask = max(0, it.nt - 4), take = max(0, it.nt - 2);
+        int page_k = 0, row_k = 0, page_v = 0, row_v = 0;  // of this lane's boxes, looked up a tile ahead of their copies
+        auto lookup = [&](int j, int b, int& page, int& row) {
+          const int x = it.keys.at(it.key0 + j * kN) + b * box;
+          page = j < it.nt && b < boxes && !unseen(a, it.keys, x, box) ? page_of(a, it.problem, x) : a.pages.n_pages;
+          row = x % a.pages.page_size;
+        };
+        lookup(0, my_k, page_k, row_k);
+        lookup(0, lane, page_v, row_v);
+        if (it.nt == 0) advance(false);
+        for (int j = 0; j < it.nt && ok; ++j) {
+          if (j == ask) request();
+          const uint32_t at_k = tiles_k % kSlotsK, at_v = tiles_v % kSlotsV;
+          ok = wait_all(&sh.empty[0][at_k], tiles_k / kSlotsK + 1);
+          if (!ok) break;
+          if (lane == 0) mbar_expect_tx(&sh.full[0][at_k], kTile);
+          __syncwarp();
+          if (lane < copies_k)
+            tma_page(smem_u32(ring_k + at_k * kTile) + my_half * (kN * 128) + my_k * box * 128, &map_k, row_k, my_half, it.head, page_k, &sh.full[0][at_k]);
+          lookup(j + 1, my_k, page_k, row_k);
+          ++tiles_k;
+          ok = wait_all(&sh.empty[1][at_v], tiles_v / kSlotsV + 1);
+          if (!ok) break;
+          if (lane == 0) mbar_expect_tx(&sh.full[1][at_v], kTile);
+          __syncwarp();
+          if (lane < boxes)
+            tma_page(smem_u32(ring_v + at_v * kTile) + lane * box * (128 * kHalves), &map_v, row_v, 0, it.head, page_v, &sh.full[1][at_v]);
+          lookup(j + 1, lane, page_v, row_v);
+          ++tiles_v;
+          if (j == take) advance(false);
+        }
+      }
+      // of a block that gives up: nothing of its own is under way when it ends
+      if (*abort_flag) {
+        auto settle = [&](uint64_t* bar, uint32_t parity) {
+          for (uint32_t x = 0; x < kStorePolls && !mbar_try_wait(bar, parity & 1u); ++x) {}
+        };
+        if (pending) settle(&sh.answered, requests);
+        for (uint32_t t = tiles_k > kSlotsK ? tiles_k - kSlotsK : 0u; t < tiles_k; ++t) settle(&sh.full[0][t % kSlotsK], t / kSlotsK);
+        for (uint32_t t = tiles_v > kSlotsV ? tiles_v - kSlotsV : 0u; t < tiles_v; ++t) settle(&sh.full[1][t % kSlotsV], t / kSlotsV);
+      }
+    } else if (warp == 1) {
+      // ---- S (the whole warp walks, one elected lane issues) ----
+      constexpr uint32_t idesc = instr_desc_f16(kM, kN, kFmtBF16, kFmtBF16, false, false);
+      const uint64_t dq = smem_desc_sw128(smem_u32(q_tile), 16, 1024);
+      const uint32_t d_s = tmem + kColS;
+      uint32_t count = 0, queries = 0;  // tiles, items with tiles
+      bool ok = true;
+      Item it;
+      for (uint32_t n = 0; ok && next_item(n, it); ++n) {
+        const int nt = __shfl_sync(0xffffffffu, it.nt, 0);
+        if (nt == 0) continue;
+        ok = wait_all(&sh.q_full, queries++);
+        for (int j = 0; j < nt && ok; ++j, ++count) {
+          const uint32_t slot = count % kSlotsK;
+          ok = wait_all(&sh.full[0][slot], count / kSlotsK);
+          if (ok && count > 0) ok = wait_all(&sh.s_read, count - 1);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t dk = smem_desc_sw128(smem_u32(ring_k + slot * kTile), 16, 1024);
+          if (elect_one()) {
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+              const uint32_t qoff = ((uint32_t)(ks >> 2) * (kM * 128) + (uint32_t)(ks & 3) * 32u) >> 4;
+              const uint32_t koff = ((uint32_t)(ks >> 2) * (kN * 128) + (uint32_t)(ks & 3) * 32u) >> 4;
+              if (ks == 0) mma_ss_lohi<false>(d_s, desc_lo(dq), desc_hi(dq), desc_lo(dk), desc_hi(dk), idesc);
+              else mma_ss_lohi<true>(d_s, desc_lo(dq) + qoff, desc_hi(dq), desc_lo(dk) + koff, desc_hi(dk), idesc);
+            }
+            mma_commit(&sh.s_full);
+            mma_commit(&sh.empty[0][slot]);
+            if (j == nt - 1) mma_commit(&sh.q_empty);
+          }
+          __syncwarp();
+        }
+      }
+    } else if (warp == 2) {
+      // ---- the items' query rows, as soon as the last S of the item before has been computed ----
+      uint32_t queries = 0;
+      bool ok = true;
+      Item it;
+      const uint32_t tile = smem_u32(q_tile);
+      for (uint32_t n = 0; ok && next_item(n, it); ++n) {
+        if (it.nt == 0) continue;
+        if (queries > 0) ok = wait_all(&sh.q_empty, queries - 1);
+        if (!ok) break;
+        ++queries;
+        constexpr int kLanes = D / 8, kPer = 32 / kLanes;  // lanes to a row, rows to a copy
+        const int tok0 = it.r0 / a.group, first = it.r0 - tok0 * a.group, c = lane % kLanes;
+        const __nv_bfloat16* const from = static_cast<const __nv_bfloat16*>(a.q) + (it.t0 + tok0) * a.q_stride + (int64_t)it.head * a.group * D + c * 8;
+#pragma unroll 8
+        for (int r = lane / kLanes; r < kM; r += kPer) {
+          const uint32_t x = (uint32_t)(first + min(r, it.n_rows - 1)), tok = x * magic >> 16, g = x - tok * a.group;
+          const bool there = r < it.n_rows && token_ok(a, it.t0 + tok0 + tok, it.head * a.group + (int)g);
+          cp_async16(tile + (c >> 3) * (kM * 128) + r * 128 + (((c ^ r) & 7) << 4), from + (int64_t)tok * a.q_stride + g * D, there);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.q_full);
+      }
+    } else {
+      // ---- O += P V ----
+      constexpr uint32_t idesc = instr_desc_f16(kM, D, kFmtBF16, kFmtBF16, false, true);
+      const uint32_t d_o = tmem + kColO, d_p = tmem + kColP;
+      // V lies box after box, a box as halves of 64 channels; groups of 8 rows, 16 rows to a step
+      const uint32_t group = box == 8 ? 1024u * kHalves : 1024u;
+      uint32_t step[kN / 16];
+#pragma unroll
+      for (int ks = 0; ks < kN / 16; ++ks) step[ks] = (uint32_t)(ks * 16 / box * (box * 128 * kHalves) + ks * 16 % box * 128) >> 4;
+      uint32_t count = 0;
+      bool ok = true;
+      Item it;
+      for (uint32_t n = 0; ok && next_item(n, it); ++n) {
+        const int nt = __shfl_sync(0xffffffffu, it.nt, 0);
+        for (int j = 0; j < nt && ok; ++j, ++count) {
+          const uint32_t slot = count % kSlotsV;
+          ok = wait_all(&sh.full[1][slot], count / kSlotsV);
+          if (!ok) break;
+          const uint32_t tile = smem_u32(ring_v + slot * kTile);
+          const int key = it.keys.at(it.key0 + j * kN);
+          if (key + kN > it.keys.end || (key < it.keys.from && key + kN > a.pages.sinks)) {
+            constexpr int kLanes = D / 8;  // lanes to a row
+            const int c = lane % kLanes;
+#pragma unroll 4
+            for (int r = lane / kLanes; r < kN; r += 32 / kLanes)
+              if (unseen(a, it.keys, key + r, 1))
+                st_shared16(tile + (r >> shift) * (box * 128 * kHalves) + (c >> 3) * (box * 128) + (r & (box - 1)) * 128 + (((c ^ r) & 7) << 4),
+                            make_uint4(0, 0, 0, 0));
+            fence_proxy_async();
+            __syncwarp();
+          }
+          ok = wait_all(&sh.p_full, count);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t dv = smem_desc_sw128(tile, (uint32_t)box * 128u, group);
+          if (elect_one()) {
+            if (j == 0) mma_ts_lohi<false>(d_o, d_p, desc_lo(dv), desc_hi(dv), idesc);
+            else mma_ts_lohi<true>(d_o, d_p, desc_lo(dv), desc_hi(dv), idesc);
+#pragma unroll
+            for (int ks = 1; ks < kN / 16; ++ks) mma_ts_lohi<true>(d_o, d_p + 8u * ks, desc_lo(dv) + step[ks], desc_hi(dv), idesc);
+            mma_commit(&sh.p_empty);
+            mma_commit(&sh.empty[1][slot]);
+            if (j == nt - 1) mma_commit(&sh.o_final);
+          }
+          __syncwarp();
+        }
+      }
+    }
+  } else {
+    setmaxnreg_inc<kRegsSoftmax>();
+    const int quarter = warp & 3, r = quarter * 32 + lane;
+    const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
+    const uint32_t t_s = tmem + kColS + lane_addr, t_o = tmem + kColO + lane_addr, t_p = tmem + kColP + lane_addr;
+    const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.out_stride * 2)) & 31u) == 0;
+    uint32_t count = 0, done = 0;  // tiles, items with tiles
+    bool ok = true;
+    Item it;
+    for (uint32_t n = 0; ok && next_item(n, it); ++n) {
+      const int nt = __shfl_sync(0xffffffffu, it.nt, 0);
+      int tok, hq;
+      split_row(it, r, tok, hq);
+      const Problem pr{it.t0, 0, it.tokens, it.len};
+      // the first key that the row does not see; of the item's first row; the first key behind the sinks that the row sees; of the
+      // item's last row
+      const int seen = r < it.n_rows ? seen_rows(part, pr, tok) : it.keys.end, all_seen = seen_rows(part, pr, it.r0 / a.group);
+      const int from = window_from(a, seen), last_from = window_from(a, it.keys.end);
+      const bool idle = quarter * 32 >= it.n_rows;
+      float m = -INFINITY;
+      float2 l2 = make_float2(0.f, 0.f);
+      for (int j = 0; j < nt; ++j, ++count) {
+        ok = wait_all(&sh.s_full, count);
+        if (!ok) break;
+        if (idle) {  // none of the warp's rows exists: whatever P holds there goes into rows of O that nobody reads
+          if (count > 0) ok = wait_all(&sh.p_empty, count - 1);
+          if (!ok) break;
+          if (lane == 0) {
+            mbar_arrive(&sh.s_read);
+            mbar_arrive(&sh.p_full);
+          }
+          continue;
+        }
+        tc_fence_after();
+        const int key = it.keys.at(it.key0 + j * kN);
+        uint32_t s[kN], p[kN / 2];
+        tmem_load(t_s, s);
+        tmem_wait_ld_of(s);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.s_read);
+        if (key + kN > all_seen || (key < last_from && key + kN > a.pages.sinks)) {
+          const uint64_t visible = bits_below(seen - key) & ~(bits_below(from - key) & ~bits_below(a.pages.sinks - key));
+          const uint32_t lo = (uint32_t)visible, hi = (uint32_t)(visible >> 32);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            if (!(lo & (1u << e))) s[e] = 0xff800000u;
+            if (!(hi & (1u << e))) s[32 + e] = 0xff800000u;
+          }
+        }
+        // two 16-bit probabilities to a word of p, words FROM .. TO - 1; returns their sum
+        auto exponentials = [&](int first, int last) {
+          const float neg = m == -INFINITY ? 0.f : -m;
+          float2 sum = make_float2(0.f, 0.f);
+          float top = -INFINITY;  // of the exponents ex2_fma2 gets
+#pragma unroll
+          for (int e = 0; e < kN / 2; ++e) {
+            if (e < first || e >= last) continue;
+            const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), make_float2(a.scale2, a.scale2),
+                                        make_float2(neg, neg));
+            const bool poly = e % kPolyEvery == kPolyEvery - 1;
+            if (poly) top = max3(top, x.x, x.y);
+            const float2 y = poly ? ex2_fma2(x) : make_float2(ex2(x.x), ex2(x.y));
+            sum = __fadd2_rn(sum, y);
+            p[e] = Vec16<__nv_bfloat16>::pack2(y.x, y.y);
+          }
+          if (top > kPolyMax) sum.x = INFINITY;
+          return sum;
+        };
+        float2 sum = make_float2(0.f, 0.f);
+        bool again = true;  // (the first tile: its maximum first)
+        // Has the P before been used (and does O include it)?  Asked ahead: the last exponentials hide the answer's way.
+        bool used = count == 0;
+        if (j > 0) {
+          sum = exponentials(0, kN * 3 / 8);
+          used = mbar_test_wait(&sh.p_empty, (count - 1) & 1u);
+          sum = __fadd2_rn(sum, exponentials(kN * 3 / 8, kN / 2));
+          again = m == -INFINITY || sum.x + sum.y > kLargeSum;
+        }
+        if (!used) ok = wait(&sh.p_empty, count - 1);
+        if (__any_sync(0xffffffffu, again || !ok)) {
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          float top = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < kN; e += 2) top = max3(top, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+          top *= a.scale2;  // (positive: the maximum commutes with it)
+          const float mn = top > m + kRescale ? top : m;
+          const float alpha = mn == -INFINITY ? 1.f : ex2(m - mn);
+          l2 = __fmul2_rn(l2, make_float2(alpha, alpha));
+          m = mn;
+          if (j > 0) {
+            tc_fence_after();
+#pragma unroll
+            for (int cc = 0; cc < D / 16; ++cc) {
+              uint32_t o[16];
+              tmem_ld16(t_o + 16u * cc, o);
+              tmem_wait_ld_of(o);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+              tmem_st16(t_o + 16u * cc, o);
+            }
+          }
+          sum = exponentials(0, kN / 2);
+        }
+        l2 = __fadd2_rn(l2, sum);
+        tc_fence_after();
+        tmem_store(t_p, p);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.p_full);
+      }
+      if (!ok) break;
+      // ---- the item's result ----
+      if (nt > 0) ok = wait_all(&sh.o_final, done++);
+      if (!ok) break;
+      tc_fence_after();
+      const float total = l2.x + l2.y;
+      const bool none = nt == 0 || total == 0.f;  // no key seen (NaN is a result)
+      const float inv = none ? 0.f : 1.f / total;
+      const float lse2 = none ? -INFINITY : m + log2f(total);
+      const int64_t token = it.t0 + tok;
+      const int64_t at = ((int64_t)(part.slot0 + it.split) * a.q_rows + token) * a.heads * a.group + hq;
+      const bool direct = a.part_out == nullptr;
+      const bool write = r < it.n_rows && token_ok(a, token, hq) && (direct || partial_ok(a, at));
+      __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out) + token * a.out_stride + (int64_t)hq * D;
+#pragma unroll
+      for (int cc = 0; cc < D / 32; ++cc) {
+        uint32_t o[32];
+        if (nt > 0) {
+          tmem_ld32(t_o + 32u * cc, o);
+          tmem_wait_ld_of(o);
+        }
+        if (!write) continue;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) o[e] = none ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv);
+        if (direct) {
+          uint32_t x[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] = Vec16<__nv_bfloat16>::pack2(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1]));
+          if (wide) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              uint32_t v[8];
+#pragma unroll
+              for (int b = 0; b < 8; ++b) v[b] = x[8 * e + b];
+              st_global_256(to + cc * 32 + e * 16, v);
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              *reinterpret_cast<uint4*>(to + cc * 32 + e * 8) = make_uint4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint32_t v[8];
+#pragma unroll
+            for (int b = 0; b < 8; ++b) v[b] = o[8 * e + b];
+            st_global_256(a.part_out + at * D + cc * 32 + e * 8, v);
+          }
+        }
+      }
+      // (the next item's first P, which lets O be written again, comes after these loads)
+      tc_fence_before();
+      if (write) {
+        if (!direct) a.part_lse[at] = lse2;
+        else if (a.lse) a.lse[token * a.heads * a.group + hq] = lse2 * 0.6931471805599453f;
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (sh.abort_flag) {  // the block ends after its copies (warp 0, above) and products under way, waited for with a limit
+    if (warp == 0 && lane == 0 && a.status) atomicCAS(a.status, 0, H2O_ERR_TIMEOUT);
+    if (warp == 1 || warp == 3) {
+      if (elect_one()) mma_commit(&sh.ended);
+      __syncwarp();
+      for (uint32_t x = 0; x < kStorePolls && !mbar_try_wait(&sh.ended, 0); ++x) {}
+    }
+    __syncthreads();
+  }
+  if (warp == 3) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kCols);
+  }
+}
+
+template <int D>
+cudaError_t launch(const AttendView& a, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t stream) {
+  constexpr int smem = smem_bytes(D);
+  static unsigned long long flags = 0;
+  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(pages_tc_kernel<D>), smem, &flags);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(pages_tc_kernel<D>, dim3((unsigned)part_blocks(a, a.part[0])), kThreads, smem, stream, false, k, v, a);
+}
+
+}  // namespace
+
+int pages_tc_tile_keys() { return kN; }
+
+cudaError_t launch_pages_tc(const AttendView& a, const void* map_k, const void* map_v, cudaStream_t stream) {
+  const CUtensorMap& k = *static_cast<const CUtensorMap*>(map_k);
+  const CUtensorMap& v = *static_cast<const CUtensorMap*>(map_v);
+  return a.dim == 128 ? launch<128>(a, k, v, stream) : launch<64>(a, k, v, stream);
+}
+
+}  // namespace h2o

@@ -268,7 +268,6 @@ int attend_tc_box_rows(int format, int dim, int groups);
 // `groups` of 128 query rows to a block
 cudaError_t launch_attend_tc(const AttendView& a, int part, int groups, int format, const void* map_k, const void* map_v,
                              cudaStream_t stream);
-cudaError_t launch_attend_tc_paged(const AttendView& a, int groups, const void* map_k, const void* map_v, cudaStream_t stream);
 cudaError_t launch_attend_join(const AttendView& a, int q_dtype, cudaStream_t stream);
 
 }  // namespace h2o

@@ -1,4 +1,4 @@
-// Attention over a K/V store or a paged cache for many query rows (prompts, a prefix shared by many sequences): tcgen05 with the
+// Attention over a K/V store for many query rows (prompts, a prefix shared by many sequences): tcgen05 with the
 // accumulators in tensor memory; bfloat16 queries, bfloat16 or 8-bit rows, head_dim 64 or 128.
 //
 // A block takes up to 256 query rows (query tokens times the query heads of one K/V head) as two groups of 128, A and
@@ -32,7 +32,7 @@
 
 #include <type_traits>
 
-#include "sm100_ptx.cuh"
+#include "attend_tc.cuh"
 #include "store.cuh"
 
 namespace h2o {
@@ -40,6 +40,7 @@ namespace h2o {
 namespace {
 
 using namespace ptx;
+using namespace tc;
 
 constexpr int kM = 128;  // rows of a group
 // G: groups of a block, 2, or 1 (bfloat16 rows only: half the block, two of them on an SM).
@@ -80,51 +81,6 @@ struct Shared {
   __half scale[2][2][96];    // 8-bit rows: the powers of two of K and V of the tile being converted
 };
 
-// Up to `polls` polls, or until another wait of the block has given up.
-__device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint32_t polls) {
-  for (uint32_t it = 0; it < polls; ++it) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if ((it & 1023u) == 1023u && *abort_flag) return false;
-  }
-  *abort_flag = 1;
-  return false;
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-// exp2 of two values on the FMA pipe: nearest integer by the 1.5 * 2^23 trick, degree-5 polynomial of 2^f on
-// [-0.5, 0.5] (1.8e-7 relative, as good as ex2.approx), times 2^n put together with integer arithmetic.  Below -126.5,
-// -infinity (a key that is not seen) included: 0, as the exponent field of 2^-127 is; NaN stays NaN; above kPolyMax the
-// result means nothing.
-constexpr float kPolyMax = 100.f;
-__device__ __forceinline__ float max_or_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float2 ex2_fma2(float2 x) {
-  x.x = max_or_nan(x.x, -127.f);
-  x.y = max_or_nan(x.y, -127.f);
-  const float2 t = __fadd2_rn(x, make_float2(12582912.f, 12582912.f));
-  const float2 n = __fadd2_rn(t, make_float2(-12582912.f, -12582912.f));
-  const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
-  float2 p = make_float2(0.0013280353741720319f, 0.0013280353741720319f);
-  p = __ffma2_rn(p, f, make_float2(0.009675574488937855f, 0.009675574488937855f));
-  p = __ffma2_rn(p, f, make_float2(0.05550701171159744f, 0.05550701171159744f));
-  p = __ffma2_rn(p, f, make_float2(0.24022118747234344f, 0.24022118747234344f));
-  p = __ffma2_rn(p, f, make_float2(0.6931470036506653f, 0.6931470036506653f));
-  p = __ffma2_rn(p, f, make_float2(1.0000001192092896f, 1.0000001192092896f));
-  return __fmul2_rn(p, make_float2(__uint_as_float((__float_as_uint(t.x) << 23) + 0x3f800000u),
-                                   __uint_as_float((__float_as_uint(t.y) << 23) + 0x3f800000u)));
-}
-
 constexpr float kRescale = 8.f;
 // A tile whose sum against the old reference exceeds this is done again against its own maximum: inside f16's range (largest
 // 65504) for the 8-bit rows; for bfloat16 rows so that O, which is divided by its sum at the end, holds values up to 2^100.
@@ -136,44 +92,8 @@ constexpr float kLargeSumOf = FMT == H2O_KV8 ? 32768.f : 1048576.f;
 template <int FMT>
 constexpr float kHeadOf = FMT == H2O_KV8 ? 7.f : 0.f;
 
-// 32-byte global load: a whole sector, where neighbouring threads read rows far apart (the address is 32-byte aligned)
-__device__ __forceinline__ void ld_global_256(const float* p, float4& a, float4& b) {
-  asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=f"(a.x), "=f"(a.y), "=f"(a.z), "=f"(a.w), "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w)
-               : "l"(p)
-               : "memory");
-}
 // Barrier of the eight softmax warps.
 __device__ __forceinline__ void softmax_sync() { asm volatile("barrier.cta.sync 3, 256;" ::: "memory"); }
-// N consecutive columns of the warp's 32 lanes from / to registers
-__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t* r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr), "r"(r[0]), "r"(r[1]),
-               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-               : "memory");
-}
-template <int N>
-__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[N]) {
-#pragma unroll
-  for (int i = 0; i + 32 <= N; i += 32) tmem_ld32(addr + i, *reinterpret_cast<uint32_t(*)[32]>(&r[i]));
-  if constexpr (N % 32 != 0) tmem_ld16(addr + N / 32 * 32, *reinterpret_cast<uint32_t(*)[16]>(&r[N / 32 * 32]));
-}
-// Waits for loads under way into r; no use of r moves ahead of it.
-template <int N>
-__device__ __forceinline__ void tmem_wait_ld_of(uint32_t (&r)[N]) {
-  tmem_wait_ld();
-#pragma unroll
-  for (int i = 0; i < N; i += 8)
-    asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
-}
-template <int N>
-__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[N]) {
-  static_assert(N % 32 == 0 || N % 32 == 8 || N % 32 == 16, "");
-  if constexpr (N % 32 == 8) tmem_st8(addr + N / 32 * 32, &r[N / 32 * 32]);
-#pragma unroll
-  for (int i = 0; i + 32 <= N; i += 32) tmem_st32(addr + i, *reinterpret_cast<const uint32_t(*)[32]>(&r[i]));
-  if constexpr (N % 32 == 16) tmem_st16(addr + N / 32 * 32, *reinterpret_cast<const uint32_t(*)[16]>(&r[N / 32 * 32]));
-}
-
 // Barrier of the four warps that convert K (kv = 0) or V (1), that tells each of them whether all are well.
 __device__ __forceinline__ bool together(bool ok, int kv) {
   uint32_t all;
@@ -188,13 +108,6 @@ __device__ __forceinline__ bool together(bool ok, int kv) {
   return all != 0;
 }
 
-// 16-byte chunk `c` of row `r` of a 16-bit operand tile: halves of 64 channels, each [rows][128 bytes] swizzled.
-__device__ __forceinline__ uint32_t operand_addr(uint32_t tile, int rows, int r, int c) {
-  return tile + (c >> 3) * (rows * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
-}
-__device__ __forceinline__ void st_shared16(uint32_t addr, uint4 v) {
-  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -207,18 +120,8 @@ __device__ __forceinline__ void codes_to_f16(uint32_t word, __half2 scale, uint3
   hi = *reinterpret_cast<const uint32_t*>(&y);
 }
 
-// One box of a page, 64 channels wide: dimensions {64 channels, row in the page, half of the head dimension, head, page}.
-__device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, int row, int half, int head, int page, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::
-          "r"(dst),
-      "l"(map), "r"(0), "r"(row), "r"(half), "r"(head), "r"(page), "r"(smem_u32(bar))
-      : "memory");
-}
-
 // FINISH: part 1 of a shared prefix, which joins what part 0 left (an instance of its own: the rest is 5 % faster without).
-// PAGED: the rows lie in pages; the lanes of warp 0 issue a copy each for every box of rows and half of the head dimension.
-template <int FMT, int D, int G, bool FINISH, bool PAGED>
+template <int FMT, int D, int G, bool FINISH>
 __global__ void __launch_bounds__(threads(FMT, G), 3 - G)
 attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                  const __grid_constant__ AttendView a, int part_index) {
@@ -267,7 +170,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   }
   const AttendPart& part = a.part[part_index];
   const BlockWork w = block_work(a, part, blockIdx.x);
-  const Problem pr = locate<PAGED>(a, part, w.problem);
+  const Problem pr = locate(a, part, w.problem);
   const int rows = pr.nt * a.group, r0 = w.row_tile * (G * kM);
   // (a launch that started early does not end before the one in front of it, whatever its blocks have to do)
   if (a.early && part_index == 1 && blockIdx.x == 0) wait_for_earlier();
@@ -275,15 +178,9 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   const int n_rows = min(G * kM, rows - r0);
   const int key0 = w.split * part.chunk;
   const bool direct = a.part_out == nullptr || FINISH;
-  if (!direct && key0 >= shared_keys<PAGED>(part, pr)) return;  // (the join kernel does not read it)
+  if (!direct && key0 >= pr.len) return;  // (the join kernel does not read it)
   const int last_seen = seen_rows(part, pr, (r0 + n_rows - 1) / a.group);
-  const Keys keys = keys_of<PAGED>(a, PAGED ? seen_rows(part, pr, r0 / a.group) : last_seen, last_seen, kN);
-  const int key1 = min(keys.count(), key0 + part.chunk);
-  // PAGED: does tile j hold keys that no row sees (other than behind the chunk's end)?
-  auto has_hole = [&](int j) {
-    const int x = keys.at(key0 + j * kN);
-    return PAGED && x < keys.from && x + kN > a.pages.sinks;
-  };
+  const int key1 = min(last_seen, key0 + part.chunk);
   // (the shuffle tells the compiler that the value is the same in all lanes: the issuing loops then stay in uniform registers)
   const int nt = __shfl_sync(0xffffffffu, max(0, (key1 - key0 + kN - 1) / kN), 0);
   const bool alt = G == 2 && __shfl_sync(0xffffffffu, n_rows, 0) <= kM;  // both groups on the same rows, tiles in turn
@@ -340,42 +237,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 
   if (!softmax_warp) {
     setmaxnreg_dec<regs_other(FMT, G)>();
-    if (PAGED && warp == 0) {
-      // ---- TMA, a box to a lane: lane x has boxes x, x + 32, .. of K's and then V's ----
-      constexpr int kMost = (2 * kN / 8 * (D / 64) + 31) / 32;
-      const int per = kN / a.pages.box * (D / 64), box_bytes = a.pages.box * 128;  // boxes of a tile of K or V
-      int page[kMost], row[kMost];
-      auto lookup = [&](int j) {  // a tile ahead of its copies
-#pragma unroll
-        for (int i = 0; i < kMost; ++i) {
-          const int b = (lane + 32 * i) % per / (D / 64), x = keys.at(key0 + j * kN) + b * a.pages.box;
-          page[i] = a.pages.n_pages;
-          row[i] = x % a.pages.page_size;
-          if (j < nt && lane + 32 * i < 2 * per && !unseen(a, keys, x, a.pages.box)) page[i] = page_of(a, w.problem, x);
-        }
-      };
-      lookup(0);
-      int slot = 0, j = 0;
-      uint32_t phase = 1;
-      for (; j < nt; ++j) {
-        if (!__all_sync(0xffffffffu, wait_or_abort(&sh.kv_empty[slot], phase, abort_flag, a.polls))) break;
-        if (lane == 0) mbar_expect_tx(&sh.kv_full[slot], 2 * kTile);
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < kMost; ++i) {
-          const int x = lane + 32 * i, kv = x >= per, y = x - kv * per, half = y % (D / 64);
-          if (x < 2 * per)
-            tma_page(smem_u32(ring + (2 * slot + kv) * kTile) + half * (kN * 128) + y / (D / 64) * box_bytes, kv ? &map_v : &map_k, row[i], half, w.head,
-                     page[i], &sh.kv_full[slot]);
-        }
-        lookup(j + 1);
-        if (++slot == n_load) {
-          slot = 0;
-          phase ^= 1;
-        }
-      }
-      if (lane == 0) sh.loads = j;
-    } else if (warp == 0) {
+    if (warp == 0) {
       // ---- TMA ----
       if (lane == 0) {
         int slot = 0, j = 0;
@@ -400,7 +262,6 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       bool ok = first >= nt || wait_or_abort(&sh.q_full[alt ? 0 : g], 0, abort_flag, a.polls);
       int slot = first;
       uint32_t phase = 0;
-      int cleared = 0;
       for (int j = first, n = 0; j < nt; j += step, ++n) {
         if (slot >= n_stages) {
           slot -= n_stages;
@@ -411,30 +272,20 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         ok = __all_sync(0xffffffffu, ok) != 0;
         if (!ok) break;
         tc_fence_after();
-        if (!kF16 && (j == nt - 1 || has_hole(j))) {
-          // the range's last V tile: zeros behind it (PAGED: in every row that nobody sees, also of up to two tiles that reach into
-          // what lies between the sinks and the window), by group A's warp or the one that uses it.  Group A may be tiles ahead:
-          // each cleared tile has a barrier of its own (bfloat16 rows use no ring of codes).
-          uint64_t* const tail = cleared == 0 ? &sh.tail : &sh.raw_full[cleared == 1 ? 0 : 1];
+        if (!kF16 && j == nt - 1) {
+          // the range's last V tile: zeros behind it, by group A's warp or the one that uses it
           if (alt || g == 0) {
+            const int there = key1 - key0 - j * kN;
             const uint32_t tile = smem_u32(ring + (2 * slot + 1) * kTile);
-            if constexpr (PAGED) {
-              const int key = keys.at(key0 + j * kN);
-              for (int x = lane; x < kN * (D / 8); x += 32)
-                if (unseen(a, keys, key + x / (D / 8), 1)) st_shared16(operand_addr(tile, kN, x / (D / 8), x % (D / 8)), make_uint4(0, 0, 0, 0));
-            } else {
-              const int there = key1 - key0 - j * kN;
-              for (int x = lane; x < (kN - there) * (D / 8); x += 32)
-                st_shared16(operand_addr(tile, kN, there + x / (D / 8), x % (D / 8)), make_uint4(0, 0, 0, 0));
-            }
+            for (int x = lane; x < (kN - there) * (D / 8); x += 32)
+              st_shared16(operand_addr(tile, kN, there + x / (D / 8), x % (D / 8)), make_uint4(0, 0, 0, 0));
             fence_proxy_async();
             __syncwarp();
-            if (lane == 0) mbar_arrive(tail);
+            if (lane == 0) mbar_arrive(&sh.tail);
           } else {
-            ok = __all_sync(0xffffffffu, wait_or_abort(tail, 0, abort_flag, a.polls)) != 0;
+            ok = __all_sync(0xffffffffu, wait_or_abort(&sh.tail, 0, abort_flag, a.polls)) != 0;
             if (!ok) break;
           }
-          ++cleared;
         }
         const uint64_t dk = smem_desc_sw128(smem_u32(ring + 2 * slot * kTile), 16, 1024);
         if (elect_one()) {
@@ -591,11 +442,8 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       const int rt = quarter * 32 + lane, r = base + rt;
       int tok, hq;
       split_row(r, tok, hq);
-      // the first key that the row does not see; of the group's first row
-      const int seen = PAGED ? (r < n_rows ? seen_rows(part, pr, tok) : last_seen) : min(key1, r < n_rows ? seen_rows(part, pr, tok) : key1);
-      const int all_seen = PAGED ? seen_rows(part, pr, (r0 + base) / a.group) : part.causal ? min(key1, seen_rows(part, pr, (r0 + base) / a.group)) : key1;
-      // PAGED: the first key behind the sinks that the row sees; of the block's last row
-      [[maybe_unused]] const int from = PAGED ? window_from(a, seen) : 0, last_from = PAGED ? window_from(a, last_seen) : 0;
+      const int seen = min(key1, r < n_rows ? seen_rows(part, pr, tok) : key1);
+      const int all_seen = part.causal ? min(key1, seen_rows(part, pr, (r0 + base) / a.group)) : key1;
       const float factor = kF16 ? sh.row_factor[r] : a.scale2;
       const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
       const uint32_t t_s = tmem + kColS + kStepS * g + lane_addr, t_o = tmem + kColO + kStepO * g + lane_addr;
@@ -621,7 +469,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           continue;
         }
         tc_fence_after();
-        const int key = PAGED ? keys.at(key0 + j * kN) : key0 + j * kN;
+        const int key = key0 + j * kN;
         uint32_t s[kN], p[kN / 2];
         tmem_load(t_s, s);
         tmem_wait_ld_of(s);
@@ -632,11 +480,6 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll
           for (int e = 0; e < kN; ++e)
             if (key + e >= seen) s[e] = 0xff800000u;
-        }
-        if (PAGED && key < last_from && key + kN > a.pages.sinks) {
-#pragma unroll
-          for (int e = 0; e < kN; ++e)
-            if (key + e < from && key + e >= a.pages.sinks) s[e] = 0xff800000u;
         }
         // two 16-bit probabilities to a word of p, words FROM .. TO - 1; returns their sum
         auto exponentials = [&](auto from, auto to) {
@@ -868,13 +711,13 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   }
 }
 
-template <int FMT, int D, int G, bool FINISH, bool PAGED = false>
+template <int FMT, int D, int G, bool FINISH>
 cudaError_t launch_finish(const AttendView& a, int part, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t stream) {
   constexpr int smem = smem_bytes(FMT, D, G);
   static unsigned long long flags = 0;
-  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(attend_tc_kernel<FMT, D, G, FINISH, PAGED>), smem, &flags);
+  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(attend_tc_kernel<FMT, D, G, FINISH>), smem, &flags);
   if (e != cudaSuccess) return e;
-  return launch_kernel(attend_tc_kernel<FMT, D, G, FINISH, PAGED>, dim3((unsigned)part_blocks(a, a.part[part])), threads(FMT, G), smem, stream,
+  return launch_kernel(attend_tc_kernel<FMT, D, G, FINISH>, dim3((unsigned)part_blocks(a, a.part[part])), threads(FMT, G), smem, stream,
                        a.early != 0 && part == 1, k, v, a, part);
 }
 template <int FMT, int D, int G>
@@ -885,14 +728,6 @@ cudaError_t launch(const AttendView& a, int part, const CUtensorMap& k, const CU
 }  // namespace
 
 int attend_tc_box_rows(int format, int dim, int groups) { return tile_keys(format, dim, groups); }
-
-cudaError_t launch_attend_tc_paged(const AttendView& a, int groups, const void* map_k, const void* map_v, cudaStream_t st) {
-  const CUtensorMap& k = *static_cast<const CUtensorMap*>(map_k);
-  const CUtensorMap& v = *static_cast<const CUtensorMap*>(map_v);
-  if (groups == 1)
-    return a.dim == 128 ? launch_finish<H2O_BF16, 128, 1, false, true>(a, 0, k, v, st) : launch_finish<H2O_BF16, 64, 1, false, true>(a, 0, k, v, st);
-  return a.dim == 128 ? launch_finish<H2O_BF16, 128, 2, false, true>(a, 0, k, v, st) : launch_finish<H2O_BF16, 64, 2, false, true>(a, 0, k, v, st);
-}
 
 cudaError_t launch_attend_tc(const AttendView& a, int part, int groups, int format, const void* map_k, const void* map_v, cudaStream_t st) {
   const CUtensorMap& k = *static_cast<const CUtensorMap*>(map_k);
