@@ -35,7 +35,7 @@ constexpr int kItems = 2;  // ring of items, the one under way and the next
 // ring of pairs would hold it as long.)
 __host__ __device__ constexpr int tile_bytes(int d) { return kN * d * 2; }
 __host__ __device__ constexpr int slots_k(int d) { return d == 128 ? 2 : 4; }
-__host__ __device__ constexpr int slots_v(int d) { return d == 128 ? 3 : 5; }
+__host__ __device__ constexpr int slots_v(int d) { return d == 128 ? (kN == 64 ? 3 : 2) : 4; }
 constexpr int kMaxSlots = 5;
 // Registers of a thread: 256 start with 128 each = 128 x 176 + 128 x 80.
 constexpr int kRegsSoftmax = 176, kRegsOther = 80;
@@ -100,10 +100,23 @@ __device__ __forceinline__ int place_of(const uint4* answer) {
   return there ? (int)x : -1;
 }
 // The lowest n bits, for any n.
-__device__ __forceinline__ uint64_t bits_below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
+
+// A lane's box of the tile that comes next, looked up a tile ahead of its copy.  (The entry is looked at only when the copy is
+// issued: a use of it where it is read would wait for it, 400 cycles of the 1000 that a tile takes.)
+struct Box {
+  int entry, row;
+  __device__ __forceinline__ void find(const AttendView& a, const Item& it, int j, int b) {
+    const int x = it.keys.at(it.key0 + j * kN) + b * a.pages.box, in = x / a.pages.page_size;
+    row = x - in * a.pages.page_size;
+    entry = a.pages.n_pages;
+    if (j < it.nt && b * a.pages.box < kN && !unseen(a, it.keys, x, a.pages.box)) entry = a.pages.table[it.problem * a.pages.stride + in];
+  }
+  __device__ __forceinline__ int page(const AttendView& a) const { return entry >= 0 && entry < a.pages.n_pages ? entry : a.pages.n_pages; }
+};
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 2)
@@ -153,6 +166,10 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
   auto wait = [&](uint64_t* bar, uint32_t parity) { return wait_or_abort(bar, parity & 1u, abort_flag, a.polls); };
   // all lanes of a warp
   auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+  // what a block that gives up has under way ends before it does
+  auto settle = [&](uint64_t* bar, uint32_t parity) {
+    for (uint32_t x = 0; x < kStorePolls && !mbar_try_wait(bar, parity & 1u); ++x) {}
+  };
   // Item number n, by a whole warp; its fields are copied, so that its place is free again.
   auto next_item = [&](uint32_t n, Item& it) {
     if (!wait_all(&sh.item_full[n % kItems], n / kItems)) return false;
@@ -173,11 +190,11 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
   if (warp < 4) {
     setmaxnreg_dec<kRegsOther>();
     if (warp == 0) {
-      // ---- items, and the copies of their K and V ----
-      // A lane's copies of a tile: of K a box of rows and half of the channels (all, if the tile is one box), of V a box.
-      const int boxes = kN / box;
-      const int copies_k = boxes == 1 ? 1 : boxes * kHalves, my_k = boxes == 1 ? 0 : lane / kHalves, my_half = boxes == 1 ? 0 : lane % kHalves;
-      uint32_t n = 0, tiles_k = 0, tiles_v = 0, requests = 0;  // items published, tiles and places asked for
+      // ---- items, and the copies of their K ----
+      // A lane has a box of rows of a tile and half of its channels (one lane all of the tile, if that is one box).
+      const int boxes = kN / box, copies = boxes == 1 ? 1 : boxes * kHalves;
+      const int my_box = boxes == 1 ? lane : lane / kHalves, my_half = boxes == 1 ? 0 : lane % kHalves;
+      uint32_t n = 0, tiles = 0, requests = 0;  // items published, tiles and places asked for
       bool ok = true, pending = false;
       Item it, next;
       // What a place stands for: row tiles last to first (the longest of a causal prompt first), then head, split, sequence.
@@ -241,45 +258,28 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
         // The next place is asked for a few tiles before this item's last copies and taken two tiles before (not earlier: what a
         // block holds back nobody else can take).
         const int ask = max(0, it.nt - 4), take = max(0, it.nt - 2);
-        int page_k = 0, row_k = 0, page_v = 0, row_v = 0;  // of this lane's boxes, looked up a tile ahead of their copies
-        auto lookup = [&](int j, int b, int& page, int& row) {
-          const int x = it.keys.at(it.key0 + j * kN) + b * box;
-          page = j < it.nt && b < boxes && !unseen(a, it.keys, x, box) ? page_of(a, it.problem, x) : a.pages.n_pages;
-          row = x % a.pages.page_size;
-        };
-        lookup(0, my_k, page_k, row_k);
-        lookup(0, lane, page_v, row_v);
+        Box next_box;
+        next_box.find(a, it, 0, my_box);
         if (it.nt == 0) advance(false);
         for (int j = 0; j < it.nt && ok; ++j) {
           if (j == ask) request();
-          const uint32_t at_k = tiles_k % kSlotsK, at_v = tiles_v % kSlotsV;
-          ok = wait_all(&sh.empty[0][at_k], tiles_k / kSlotsK + 1);
+          const uint32_t at = tiles % kSlotsK;
+          ok = wait_all(&sh.empty[0][at], tiles / kSlotsK + 1);
           if (!ok) break;
-          if (lane == 0) mbar_expect_tx(&sh.full[0][at_k], kTile);
+          if (lane == 0) mbar_expect_tx(&sh.full[0][at], kTile);
           __syncwarp();
-          if (lane < copies_k)
-            tma_page(smem_u32(ring_k + at_k * kTile) + my_half * (kN * 128) + my_k * box * 128, &map_k, row_k, my_half, it.head, page_k, &sh.full[0][at_k]);
-          lookup(j + 1, my_k, page_k, row_k);
-          ++tiles_k;
-          ok = wait_all(&sh.empty[1][at_v], tiles_v / kSlotsV + 1);
-          if (!ok) break;
-          if (lane == 0) mbar_expect_tx(&sh.full[1][at_v], kTile);
-          __syncwarp();
-          if (lane < boxes)
-            tma_page(smem_u32(ring_v + at_v * kTile) + lane * box * (128 * kHalves), &map_v, row_v, 0, it.head, page_v, &sh.full[1][at_v]);
-          lookup(j + 1, lane, page_v, row_v);
-          ++tiles_v;
+          if (lane < copies)
+            tma_page(smem_u32(ring_k + at * kTile) + my_half * (kN * 128) + my_box * box * 128, &map_k, next_box.row, my_half, it.head, next_box.page(a),
+                     &sh.full[0][at]);
+          ++tiles;
+          next_box.find(a, it, j + 1, my_box);
           if (j == take) advance(false);
         }
       }
       // of a block that gives up: nothing of its own is under way when it ends
       if (*abort_flag) {
-        auto settle = [&](uint64_t* bar, uint32_t parity) {
-          for (uint32_t x = 0; x < kStorePolls && !mbar_try_wait(bar, parity & 1u); ++x) {}
-        };
         if (pending) settle(&sh.answered, requests);
-        for (uint32_t t = tiles_k > kSlotsK ? tiles_k - kSlotsK : 0u; t < tiles_k; ++t) settle(&sh.full[0][t % kSlotsK], t / kSlotsK);
-        for (uint32_t t = tiles_v > kSlotsV ? tiles_v - kSlotsV : 0u; t < tiles_v; ++t) settle(&sh.full[1][t % kSlotsV], t / kSlotsV);
+        for (uint32_t t = tiles > kSlotsK ? tiles - kSlotsK : 0u; t < tiles; ++t) settle(&sh.full[0][t % kSlotsK], t / kSlotsK);
       }
     } else if (warp == 1) {
       // ---- S (the whole warp walks, one elected lane issues) ----
@@ -316,13 +316,16 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
         }
       }
     } else if (warp == 2) {
-      // ---- the items' query rows, as soon as the last S of the item before has been computed ----
-      uint32_t queries = 0;
+      // ---- the items' query rows, as soon as the last S of the item before has been computed, and the copies of their V ----
+      const int boxes = kN / box;
+      uint32_t queries = 0, tiles = 0;  // items with keys, tiles
       bool ok = true;
       Item it;
       const uint32_t tile = smem_u32(q_tile);
       for (uint32_t n = 0; ok && next_item(n, it); ++n) {
         if (it.nt == 0) continue;
+        Box next_box;
+        next_box.find(a, it, 0, lane);
         if (queries > 0) ok = wait_all(&sh.q_empty, queries - 1);
         if (!ok) break;
         ++queries;
@@ -335,11 +338,27 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
           const bool there = r < it.n_rows && token_ok(a, it.t0 + tok0 + tok, it.head * a.group + (int)g);
           cp_async16(tile + (c >> 3) * (kM * 128) + r * 128 + (((c ^ r) & 7) << 4), from + (int64_t)tok * a.q_stride + g * D, there);
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.q_full);
+        for (int j = 0; j < it.nt && ok; ++j) {
+          const uint32_t at = tiles % kSlotsV;
+          ok = wait_all(&sh.empty[1][at], tiles / kSlotsV + 1);
+          if (ok) {
+            if (lane == 0) mbar_expect_tx(&sh.full[1][at], kTile);
+            __syncwarp();
+            if (lane < boxes)
+              tma_page(smem_u32(ring_v + at * kTile) + lane * box * (128 * kHalves), &map_v, next_box.row, 0, it.head, next_box.page(a), &sh.full[1][at]);
+            ++tiles;
+            next_box.find(a, it, j + 1, lane);
+          }
+          if (j == 0) {  // (the first tile's V is asked for while the query rows are on their way)
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.q_full);
+          }
+        }
       }
+      if (*abort_flag)
+        for (uint32_t t = tiles > kSlotsV ? tiles - kSlotsV : 0u; t < tiles; ++t) settle(&sh.full[1][t % kSlotsV], t / kSlotsV);
     } else {
       // ---- O += P V ----
       constexpr uint32_t idesc = instr_desc_f16(kM, D, kFmtBF16, kFmtBF16, false, true);
@@ -430,12 +449,13 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.s_read);
         if (key + kN > all_seen || (key < last_from && key + kN > a.pages.sinks)) {
-          const uint64_t visible = bits_below(seen - key) & ~(bits_below(from - key) & ~bits_below(a.pages.sinks - key));
-          const uint32_t lo = (uint32_t)visible, hi = (uint32_t)(visible >> 32);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            if (!(lo & (1u << e))) s[e] = 0xff800000u;
-            if (!(hi & (1u << e))) s[32 + e] = 0xff800000u;
+          for (int w = 0; w < kN; w += 32) {
+            const int x = key + w;
+            const uint32_t visible = bits_below(seen - x) & ~(bits_below(from - x) & ~bits_below(a.pages.sinks - x));
+#pragma unroll
+            for (int e = 0; e < 32 && w + e < kN; ++e)
+              if (!(visible & (1u << e))) s[w + e] = 0xff800000u;
           }
         }
         // two 16-bit probabilities to a word of p, words FROM .. TO - 1; returns their sum
@@ -462,9 +482,9 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
         // Has the P before been used (and does O include it)?  Asked ahead: the last exponentials hide the answer's way.
         bool used = count == 0;
         if (j > 0) {
-          sum = exponentials(0, kN * 3 / 8);
+          sum = exponentials(0, kN / 2 - 8);
           used = mbar_test_wait(&sh.p_empty, (count - 1) & 1u);
-          sum = __fadd2_rn(sum, exponentials(kN * 3 / 8, kN / 2));
+          sum = __fadd2_rn(sum, exponentials(kN / 2 - 8, kN / 2));
           again = m == -INFINITY || sum.x + sum.y > kLargeSum;
         }
         if (!used) ok = wait(&sh.p_empty, count - 1);
