@@ -115,7 +115,6 @@ struct Box {
     entry = a.pages.n_pages;
     if (j < it.nt && b * a.pages.box < kN && !unseen(a, it.keys, x, a.pages.box)) entry = a.pages.table[it.problem * a.pages.stride + in];
   }
-  __device__ __forceinline__ int page(const AttendView& a) const { return entry >= 0 && entry < a.pages.n_pages ? entry : a.pages.n_pages; }
 };
 
 template <int D>
@@ -269,7 +268,7 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
           if (lane == 0) mbar_expect_tx(&sh.full[0][at], kTile);
           __syncwarp();
           if (lane < copies)
-            tma_page(smem_u32(ring_k + at * kTile) + my_half * (kN * 128) + my_box * box * 128, &map_k, next_box.row, my_half, it.head, next_box.page(a),
+            tma_page(smem_u32(ring_k + at * kTile) + my_half * (kN * 128) + my_box * box * 128, &map_k, next_box.row, my_half, it.head, page_in(a, next_box.entry),
                      &sh.full[0][at]);
           ++tiles;
           next_box.find(a, it, j + 1, my_box);
@@ -345,7 +344,7 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
             if (lane == 0) mbar_expect_tx(&sh.full[1][at], kTile);
             __syncwarp();
             if (lane < boxes)
-              tma_page(smem_u32(ring_v + at * kTile) + lane * box * (128 * kHalves), &map_v, next_box.row, 0, it.head, next_box.page(a), &sh.full[1][at]);
+              tma_page(smem_u32(ring_v + at * kTile) + lane * box * (128 * kHalves), &map_v, next_box.row, 0, it.head, page_in(a, next_box.entry), &sh.full[1][at]);
             ++tiles;
             next_box.find(a, it, j + 1, lane);
           }

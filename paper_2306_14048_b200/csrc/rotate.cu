@@ -5,6 +5,8 @@
 // goes to sincospif.  (In fp32 the angle of position 1e6 would be off by 0.06.)  A block computes the sines and cosines of
 // its token once, into shared memory, and all heads use them; so the kernel is bound by memory: every value read once,
 // written once.  Products are fp32, rounded to the type once.
+#include <algorithm>
+
 #include "pages.cuh"
 
 namespace h2o {
@@ -12,7 +14,9 @@ namespace h2o {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kMaxHalf = 256;  // pairs of a head (head_dim up to 512)
+constexpr int kMaxHalf = 256;  // pairs of a head (head_dim up to 512), or of a block's tokens together
+constexpr int kMaxTokens = 8;  // of a block
+constexpr int kAhead = 2;      // items a thread has under way
 
 // 16 bytes of a head's channels, as they lie in memory and as numbers.
 template <typename T>
@@ -64,34 +68,109 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu, int batch, int64_t
 //   Single      one pair of channels, or two of those that are not rotated
 enum class Kind { Halves, Neighbours, Single };
 
+// An item: where it comes from, where it goes (null: nowhere), which of its channels, and whether it is rotated.
+template <typename T>
+struct Piece {
+  const T* from;
+  T* to;
+  int x0, x1, pair, turns;  // first pair's angle, pairs from it on that are rotated (Neighbours)
+  bool turn;
+};
+
+// How a launch is cut: `tokens` to a block, which share its threads and their sines; quotients of small numbers by
+// multiplication, x / d = the upper half of x * (2^32 / d + 1) (exact as long as x * d < 2^32).
+struct Cut {
+  int tokens, per, items;  // items of a head, of a token
+  uint32_t by_per, by_items;
+};
+constexpr int64_t kNoPage = -1, kNoSequence = -2;
+
 template <typename T, Kind KIND>
-__global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ MoveArgs a) {
+__global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ MoveArgs a, const __grid_constant__ Cut cut) {
   constexpr int N = Chunk<T>::N;
   __shared__ float2 cs[kMaxHalf];
-  const int64_t t = blockIdx.x;
-  const int half = a.turn.half;
-  // ---- the token's sequence and row ----
-  int64_t row = 0;
-  T *to_k = nullptr, *to_v = nullptr;
+  __shared__ int64_t place[kMaxTokens], rows[kMaxTokens];  // of K and V of each token in the pages; its row
+  const int64_t t0 = (int64_t)blockIdx.x * cut.tokens;
+  const int here = (int)min((int64_t)cut.tokens, a.n_tokens - t0), half = a.turn.half;
+  const int turned = half / N;  // items of a head with a rotation (Halves)
+  const int items = cut.items * here;
+  auto piece = [&](int i, bool to) {  // (to: where it goes is known by now)
+    Piece<T> p;
+    const int k = cut.tokens == 1 ? 0 : (int)__umulhi((uint32_t)i, cut.by_items);
+    const int64_t t = t0 + k;
+    i -= k * cut.items;
+    int head = cut.per == 1 ? i : (int)__umulhi((uint32_t)i, cut.by_per);
+    const int c = i - head * cut.per;
+    const int64_t at = a.kv_heads > 0 && to ? place[k] : kNoPage;
+    if (head < a.q_heads) {
+      p.from = static_cast<const T*>(a.q) + t * a.q_stride + (int64_t)head * a.dim;
+      p.to = at == kNoSequence ? nullptr : static_cast<T*>(a.q_out) + t * a.q_out_stride + (int64_t)head * a.dim;
+      p.turn = a.q_turn;
+    } else {
+      head -= a.q_heads;
+      const bool is_v = head >= a.kv_heads;
+      if (is_v) head -= a.kv_heads;
+      p.from = static_cast<const T*>(is_v ? a.v : a.k) + t * a.kv_stride + (int64_t)head * a.dim;
+      p.to = at < 0 ? nullptr : static_cast<T*>(is_v ? a.pv : a.pk) + at + head * a.head_stride;
+      p.turn = !is_v && a.k_turn;
+    }
+    if constexpr (KIND == Kind::Single) {
+      const bool apart = a.turn.halves && c < half;
+      p.x0 = apart ? c : 2 * c;
+      p.x1 = apart ? c + half : 2 * c + 1;
+      p.pair = k * half + c;
+      p.turn = p.turn && c < half;
+    } else {
+      const bool apart = KIND == Kind::Halves && c < turned;
+      p.x0 = apart ? c * N : 2 * c * N;
+      p.x1 = apart ? c * N + half : p.x0 + N;
+      p.pair = k * half + (apart ? c * N : p.x0 / 2);
+      p.turns = half - (apart ? c * N : p.x0 / 2);
+      p.turn = p.turn && (KIND == Kind::Halves ? apart : p.turns > 0);
+    }
+    return p;
+  };
+  // ---- the first items' values are asked for before anything is known about the token ----
+  const int first = blockIdx.y * kThreads + threadIdx.x, stride = gridDim.y * kThreads;
+  Chunk<T> u[kAhead], w[kAhead];
+  if constexpr (KIND != Kind::Single) {
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n)
+      if (first + n * stride < items) {
+        const Piece<T> p = piece(first + n * stride, false);
+        u[n].load(p.from + p.x0);
+        w[n].load(p.from + p.x1);
+      }
+  }
+  // ---- the tokens' sequences and rows ----
   if (a.kv_heads > 0) {
-    int s = a.cu ? sequence_of(a.cu, a.batch, t) : t < a.batch ? (int)t : -1;
-    if (s < 0) return;  // (the whole block: the token belongs to no sequence)
-    row = (int64_t)a.length[s] - (a.cu ? (int64_t)a.cu[s + 1] - t : 1);
-    if (row >= 0 && row < a.max_length && row / a.page_size < a.max_pages) {
-      const int x = (int)row;
-      const int page = a.table[s * a.table_stride + x / a.page_size];
-      if (page >= 0 && page < a.n_pages && H2O_IN_RANGE(page, a.n_pages, a.status)) {
-        const int64_t at = page * a.page_stride + x % a.page_size * a.row_stride;
-        to_k = static_cast<T*>(a.pk) + at;
-        to_v = static_cast<T*>(a.pv) + at;
+    for (int k = threadIdx.x >> 5; k < here; k += kThreads / 32) {
+      const int64_t t = t0 + k;
+      const int s = a.cu ? sequence_of(a.cu, a.batch, t) : t < a.batch ? (int)t : -1;
+      int64_t row = 0, at = kNoSequence;
+      if (s >= 0) {
+        row = (int64_t)a.length[s] - (a.cu ? (int64_t)a.cu[s + 1] - t : 1);
+        at = kNoPage;
+        if (row >= 0 && row < a.max_length && row / a.page_size < a.max_pages) {
+          const int x = (int)row;
+          const int page = a.table[s * a.table_stride + x / a.page_size];
+          if (page >= 0 && page < a.n_pages && H2O_IN_RANGE(page, a.n_pages, a.status)) at = page * a.page_stride + x % a.page_size * a.row_stride;
+        }
+      }
+      if ((threadIdx.x & 31) == 0) {
+        place[k] = at;
+        rows[k] = row;
       }
     }
+    __syncthreads();
   }
   // ---- sines and cosines ----
-  for (int i = threadIdx.x; i < half; i += kThreads) {
-    int64_t p = row;
-    if (a.turn.positions) p = a.turn.positions[(a.turn.axis ? min((int)a.turn.axis[i], a.turn.axes - 1) : 0) * a.turn.position_stride + t];
-    double turns = (double)p * a.turn.frequency[i] * 0.15915494309189533577;  // 1 / 2 pi
+  for (int i = threadIdx.x; i < half * here; i += kThreads) {
+    const int k = here == 1 ? 0 : i / half, pair = i - k * half;
+    int64_t p;
+    if (a.turn.positions) p = a.turn.positions[(a.turn.axis ? min((int)a.turn.axis[pair], a.turn.axes - 1) : 0) * a.turn.position_stride + t0 + k];
+    else p = rows[k];
+    double turns = (double)p * a.turn.frequency[pair] * 0.15915494309189533577;  // 1 / 2 pi
     turns -= rint(turns);
     float s, c;
     sincospif(2.f * (float)turns, &s, &c);
@@ -99,75 +178,61 @@ __global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ 
   }
   __syncthreads();
   // ---- the heads ----
-  const int per = KIND == Kind::Single ? a.dim / 2 : a.dim / (2 * N);  // items of a head
-  const int turned = half / N;                                         // of them with a rotation (Halves)
-  const int items = (a.q_heads + 2 * a.kv_heads) * per;
-  for (int i = blockIdx.y * kThreads + threadIdx.x; i < items; i += gridDim.y * kThreads) {
-    int head = i / per;
-    const int c = i - head * per;
-    const T* from;
-    T* to;
-    bool turn;
-    if (head < a.q_heads) {
-      from = static_cast<const T*>(a.q) + t * a.q_stride + (int64_t)head * a.dim;
-      to = static_cast<T*>(a.q_out) + t * a.q_out_stride + (int64_t)head * a.dim;
-      turn = a.q_turn;
-    } else {
-      head -= a.q_heads;
-      const bool is_v = head >= a.kv_heads;
-      if (is_v) head -= a.kv_heads;
-      from = static_cast<const T*>(is_v ? a.v : a.k) + t * a.kv_stride + (int64_t)head * a.dim;
-      to = is_v ? to_v : to_k;
-      if (!to) continue;
-      to += head * a.head_stride;
-      turn = !is_v && a.k_turn;
+  if constexpr (KIND == Kind::Single) {
+    for (int i = first; i < items; i += stride) {
+      const Piece<T> p = piece(i, true);
+      if (!p.to) continue;
+      float2 x = make_float2((float)p.from[p.x0], (float)p.from[p.x1]);
+      if (p.turn) x = turn_of(x, cs[p.pair]);
+      p.to[p.x0] = (T)x.x;
+      p.to[p.x1] = (T)x.y;
     }
-    if constexpr (KIND == Kind::Single) {
-      const bool apart = a.turn.halves && c < half;
-      const int x0 = apart ? c : 2 * c, x1 = apart ? c + half : 2 * c + 1;
-      turn = turn && c < half;
-      float2 x = make_float2((float)from[x0], (float)from[x1]);
-      if (turn) x = turn_of(x, cs[c]);
-      to[x0] = (T)x.x;
-      to[x1] = (T)x.y;
-    } else {
-      const int x0 = KIND == Kind::Halves && c < turned ? c * N : 2 * c * N;
-      const int x1 = KIND == Kind::Halves && c < turned ? c * N + half : x0 + N;
-      Chunk<T> u, w;
-      u.load(from + x0);
-      w.load(from + x1);
-      if (turn && (KIND == Kind::Halves ? c < turned : x0 < 2 * half)) {
-        float f[N], g[N];
-        u.numbers(f);
-        w.numbers(g);
-        if constexpr (KIND == Kind::Halves) {
+  } else {
+    for (int at = first; at < items; at += kAhead * stride) {
 #pragma unroll
-          for (int e = 0; e < N; ++e) {
-            const float2 y = turn_of(make_float2(f[e], g[e]), cs[c * N + e]);
-            f[e] = y.x;
-            g[e] = y.y;
-          }
-        } else {
+      for (int n = 0; n < kAhead; ++n) {
+        const int i = at + n * stride;
+        if (i >= items) break;
+        const Piece<T> p = piece(i, true);
+        if (p.turn) {
+          float f[N], g[N];
+          u[n].numbers(f);
+          w[n].numbers(g);
+          if constexpr (KIND == Kind::Halves) {
 #pragma unroll
-          for (int e = 0; e < N; e += 2) {
-            const int i0 = (x0 + e) / 2, i1 = (x1 + e) / 2;
-            if (i0 < half) {
-              const float2 y = turn_of(make_float2(f[e], f[e + 1]), cs[i0]);
+            for (int e = 0; e < N; ++e) {
+              const float2 y = turn_of(make_float2(f[e], g[e]), cs[p.pair + e]);
               f[e] = y.x;
-              f[e + 1] = y.y;
+              g[e] = y.y;
             }
-            if (i1 < half) {
-              const float2 y = turn_of(make_float2(g[e], g[e + 1]), cs[i1]);
-              g[e] = y.x;
-              g[e + 1] = y.y;
+          } else {
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+              if (e / 2 < p.turns) {
+                const float2 y = turn_of(make_float2(f[e], f[e + 1]), cs[p.pair + e / 2]);
+                f[e] = y.x;
+                f[e + 1] = y.y;
+              }
+              if (N / 2 + e / 2 < p.turns) {
+                const float2 y = turn_of(make_float2(g[e], g[e + 1]), cs[p.pair + N / 2 + e / 2]);
+                g[e] = y.x;
+                g[e + 1] = y.y;
+              }
             }
           }
+          u[n].set(f);
+          w[n].set(g);
         }
-        u.set(f);
-        w.set(g);
+        if (p.to) {
+          u[n].store(p.to + p.x0);
+          w[n].store(p.to + p.x1);
+        }
+        if (i + kAhead * stride < items) {
+          const Piece<T> next = piece(i + kAhead * stride, false);
+          u[n].load(next.from + next.x0);
+          w[n].load(next.from + next.x1);
+        }
       }
-      u.store(to + x0);
-      w.store(to + x1);
     }
   }
 }
@@ -178,11 +243,24 @@ cudaError_t launch(const MoveArgs& a, cudaStream_t stream) {
   // pairs of chunks need a head of whole pairs of chunks and, for halves, rotated channels of whole pairs
   const bool chunks = a.dim % (2 * N) == 0;
   const Kind kind = !chunks || (a.turn.halves && a.turn.half % N != 0) ? Kind::Single : a.turn.halves ? Kind::Halves : Kind::Neighbours;
-  const int64_t items = (int64_t)(a.q_heads + 2 * a.kv_heads) * (kind == Kind::Single ? a.dim / 2 : a.dim / (2 * N));
-  const dim3 grid((unsigned)a.n_tokens, (unsigned)((items + 4 * kThreads - 1) / (4 * kThreads)));
-  if (kind == Kind::Halves) move_kernel<T, Kind::Halves><<<grid, kThreads, 0, stream>>>(a);
-  else if (kind == Kind::Neighbours) move_kernel<T, Kind::Neighbours><<<grid, kThreads, 0, stream>>>(a);
-  else move_kernel<T, Kind::Single><<<grid, kThreads, 0, stream>>>(a);
+  Cut cut;
+  cut.per = kind == Kind::Single ? a.dim / 2 : a.dim / (2 * N);
+  cut.items = (a.q_heads + 2 * a.kv_heads) * cut.per;
+  cut.by_per = cut.per > 1 ? (uint32_t)((1ull << 32) / cut.per) + 1 : 0;
+  cut.by_items = cut.items > 1 ? (uint32_t)((1ull << 32) / cut.items) + 1 : 0;
+  // Few tokens: blocks enough that a thread has one item.  Many: each token's sines computed once, several tokens to a block as long
+  // as that leaves a thread up to four items.
+  const int64_t most = (cut.items + kThreads - 1) / kThreads;
+  cut.tokens = 1;
+  int64_t parts = most;
+  if (a.n_tokens * most > 8 * sm_count()) {
+    parts = (cut.items + 8 * kThreads - 1) / (8 * kThreads);
+    cut.tokens = std::max(1, std::min({kMaxTokens, 4 * kThreads / cut.items, kMaxHalf / std::max(1, a.turn.half)}));
+  }
+  const dim3 grid((unsigned)((a.n_tokens + cut.tokens - 1) / cut.tokens), (unsigned)std::min<int64_t>(65535, parts));
+  if (kind == Kind::Halves) move_kernel<T, Kind::Halves><<<grid, kThreads, 0, stream>>>(a, cut);
+  else if (kind == Kind::Neighbours) move_kernel<T, Kind::Neighbours><<<grid, kThreads, 0, stream>>>(a, cut);
+  else move_kernel<T, Kind::Single><<<grid, kThreads, 0, stream>>>(a, cut);
   return cudaGetLastError();
 }
 

@@ -158,11 +158,8 @@ template <bool PAGED>
 __device__ __forceinline__ int shared_keys(const AttendPart& p, const Problem& r) {
   return PAGED ? min(r.len, p.most_keys) : r.len;
 }
-// The page of a sequence's row x, n_pages (which no tensor map holds: read as zeros) where it has none.
-__device__ __forceinline__ int page_of(const AttendView& a, int seq, int x) {
-  const int page = a.pages.table[seq * a.pages.stride + x / a.pages.page_size];
-  return page >= 0 && page < a.pages.n_pages ? page : a.pages.n_pages;
-}
+// The page that an entry of a sequence's table names; n_pages (which no tensor map holds: read as zeros) for none.
+__device__ __forceinline__ int page_in(const AttendView& a, int entry) { return entry >= 0 && entry < a.pages.n_pages ? entry : a.pages.n_pages; }
 
 // The group of a sequence: the last one that starts at or before it.
 __device__ __forceinline__ int group_of(const AttendView& a, int seq) {

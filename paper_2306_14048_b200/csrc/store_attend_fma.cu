@@ -39,22 +39,28 @@ struct Smem {
   float p[BM][kBN + 4];
 };
 
-// Element 0 of row x of a sequence in a paged cache; null where it has no page (zeros).  Eight rows from a multiple of 8 on lie in one
-// page.
-__device__ __forceinline__ const float* paged_row(const void* base, const AttendView& a, int seq, int head, int x) {
-  const int page = page_of(a, seq, x);
-  if (page >= a.pages.n_pages) return nullptr;
-  return static_cast<const float*>(base) + page * a.pages.page_stride + x % a.pages.page_size * a.row_stride + head * a.pages.head_stride;
+// Rows of a paged cache.  Eight rows from a multiple of 8 on lie in one page: the table's entry for them (n_pages where no row sees
+// any of them), and the place of the first relative to K's and V's base, negative where it has none (zeros).
+__device__ __forceinline__ int paged_entry(const AttendView& a, const Keys& keys, int seq, int x) {
+  return unseen(a, keys, x, 8) ? a.pages.n_pages : a.pages.table[seq * a.pages.stride + x / a.pages.page_size];
+}
+__device__ __forceinline__ int64_t paged_rows(const AttendView& a, int entry, int head, int x) {
+  const int page = page_in(a, entry);
+  return page >= a.pages.n_pages ? -1 : page * a.pages.page_stride + x % a.pages.page_size * a.row_stride + head * a.pages.head_stride;
 }
 
-// One tile of K or V of a paged cache, rows x .. x + 63 (x a multiple of 8), those that nobody sees zero.
+// One tile of K or V of a paged cache, rows x .. x + 63 (x a multiple of 8), those that nobody sees zero.  Lane l of a warp looks up
+// where rows x + 8 l .. + 7 lie; the rows of a step belong to one such group for the whole warp.
 template <int D, int PITCH>
 __device__ __forceinline__ void load_paged_tile(float* dst, const void* base, const AttendView& a, const Keys& keys, int seq, int head, int x) {
   constexpr int kV = D / 4;
+  const int mine = x + 8 * (threadIdx.x & 7);
+  const int64_t rows8 = paged_rows(a, paged_entry(a, keys, seq, mine), head, mine);
+  const bool whole = x + kBN <= keys.end && (x >= keys.from || x + kBN <= a.pages.sinks);
   for (int i = threadIdx.x; i < kBN * kV; i += kThreads) {
     const int r = i / kV, c = (i % kV) * 4;
-    const float* from = unseen(a, keys, x + r, 1) ? nullptr : paged_row(base, a, seq, head, x + r);
-    if (from) cp_async16(dst + r * PITCH + c, from + c);
+    const int64_t at = __shfl_sync(0xffffffffu, rows8, r >> 3);
+    if (at >= 0 && (whole || !unseen(a, keys, x + r, 1))) cp_async16(dst + r * PITCH + c, static_cast<const float*>(base) + at + (r & 7) * a.row_stride + c);
     else *reinterpret_cast<float4*>(dst + r * PITCH + c) = make_float4(0.f, 0.f, 0.f, 0.f);
   }
   cp_commit();
@@ -333,26 +339,31 @@ __global__ void __launch_bounds__(kFewThreads) attend_few_kernel(const __grid_co
   }
   // the key of a step whose logit this lane ends up with (a few lanes the same one)
   const int mine = kPer == 1 ? lane >> 2 : 2 * ((lane >> 1) & 7) + (lane >> 4);
+  // PAGED: the entries of a step's rows, read a step ahead
+  constexpr int kEntries = kKeys / 8;
+  [[maybe_unused]] int entry[kEntries];
+  auto lookup = [&](int key) {
+#pragma unroll
+    for (int h = 0; h < kEntries; ++h) entry[h] = key < key1 ? paged_entry(a, keys, w.problem, keys.at(key) + 8 * h) : 0;
+  };
+  if constexpr (PAGED) lookup(key0 + warp * kKeys);
   for (int key = key0 + warp * kKeys; key < key1; key += kFewWarps * kKeys) {
     float4 kk[kLoads], vv[kLoads];
     const int key_at = PAGED ? keys.at(key) : key;
     if constexpr (PAGED) {
-      // eight rows to a page, whose place is looked up once (the same for the whole warp)
 #pragma unroll
-      for (int h = 0; h < kKeys / 8; ++h) {
-        const int x0 = key_at + 8 * h;
-        const bool none = unseen(a, keys, x0, 8);
-        const float* from_k = none ? nullptr : paged_row(a.k, a, w.problem, w.head, x0);
-        const float* from_v = none ? nullptr : static_cast<const float*>(a.v) + (from_k - static_cast<const float*>(a.k));
+      for (int h = 0; h < kEntries; ++h) {
+        const int64_t rows8 = paged_rows(a, entry[h], w.head, key_at + 8 * h);
 #pragma unroll
         for (int i = h * kLoads / kPer; i < (h + 1) * kLoads / kPer; ++i) {
           const int x = i * kPer + sub;
-          const bool there = from_k && !unseen(a, keys, key_at + x, 1);
-          const int64_t at = (int64_t)(x - 8 * h) * a.row_stride + c;
-          kk[i] = there ? __ldcs(reinterpret_cast<const float4*>(from_k + at)) : make_float4(0.f, 0.f, 0.f, 0.f);
-          vv[i] = there ? __ldcs(reinterpret_cast<const float4*>(from_v + at)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          const bool there = rows8 >= 0 && !unseen(a, keys, key_at + x, 1);
+          const int64_t at = rows8 + (int64_t)(x - 8 * h) * a.row_stride + c;
+          kk[i] = there ? __ldcs(reinterpret_cast<const float4*>(static_cast<const float*>(a.k) + at)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          vv[i] = there ? __ldcs(reinterpret_cast<const float4*>(static_cast<const float*>(a.v) + at)) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
       }
+      lookup(key + kFewWarps * kKeys);
     }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {

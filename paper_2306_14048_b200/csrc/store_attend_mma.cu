@@ -182,19 +182,27 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   // PAGED: this lane's copy of a tile (one of `copies`): box `my_box`, half `my_half` of the channels (all, where it is one copy)
   const int boxes = PAGED ? kKeys / a.pages.box : 1, copies = boxes == 1 ? 1 : boxes * (D / 64);
   const int my_box = lane / (D / 64), my_half = lane % (D / 64);
-  int page_a = 0, page_b = 0;  // the pages of the tiles whose next K and V this lane asks for
-  auto row_of = [&](int j) { return keys.at(key0 + (warp + kWarps * j) * kKeys) + (boxes == 1 ? 0 : my_box * a.pages.box); };
-  auto lookup = [&](int j) {  // of tile j; what no row sees need not be read
-    if (j >= mine || lane >= copies) return 0;
-    const int x = row_of(j);
-    return unseen(a, keys, x, a.pages.box) ? a.pages.n_pages : page_of(a, w.problem, x);
+  // This lane's box of a tile: the table's entry (looked at when the copy is issued: a use where it is read would wait for it) and
+  // the row in the page.
+  struct Box {
+    int entry, row;
   };
-  auto issue_paged = [&](int i, int page) {  // item i, all lanes
+  Box box_a{0, 0}, box_b{0, 0};  // of the tiles whose next K and V this lane asks for
+  auto lookup = [&](int j) {  // of tile j; what no row sees need not be read
+    Box b{a.pages.n_pages, 0};
+    if (j < mine && lane < copies) {
+      const int x = keys.at(key0 + (warp + kWarps * j) * kKeys) + (boxes == 1 ? 0 : my_box * a.pages.box), page = x / a.pages.page_size;
+      b.row = x - page * a.pages.page_size;
+      if (!unseen(a, keys, x, a.pages.box)) b.entry = a.pages.table[w.problem * a.pages.stride + page];
+    }
+    return b;
+  };
+  auto issue_paged = [&](int i, const Box& b) {  // item i, all lanes
     if (lane == 0) mbar_expect_tx(&full[i % kSlots], kTile);
     __syncwarp();
     if (lane < copies)
       tma_page(smem_u32(my_ring + (i % kSlots) * kTile) + (boxes == 1 ? 0 : my_half * (kKeys * 128) + my_box * a.pages.box * 128), (i & 1) ? map_v : map_k,
-               row_of(i >> 1) % a.pages.page_size, boxes == 1 ? 0 : my_half, w.head, page, &full[i % kSlots]);
+               b.row, boxes == 1 ? 0 : my_half, w.head, page_in(a, b.entry), &full[i % kSlots]);
   };
   auto issue = [&](int i) {  // item i: K of tile i / 2, then its V; lane 0 only
     const int t = warp + kWarps * (i >> 1);
@@ -213,14 +221,14 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   }
   __syncwarp();
   if constexpr (PAGED) {
-    int pages[(kSlots + 1) / 2];
+    Box first[(kSlots + 1) / 2];
 #pragma unroll
-    for (int j = 0; j < (kSlots + 1) / 2; ++j) pages[j] = lookup(j);
+    for (int j = 0; j < (kSlots + 1) / 2; ++j) first[j] = lookup(j);
 #pragma unroll
     for (int i = 0; i < kSlots; ++i)
-      if (i < 2 * mine) issue_paged(i, pages[i >> 1]);
-    page_b = lookup((kSlots + 1) / 2);
-    page_a = kSlots % 2 ? pages[(kSlots - 1) / 2] : page_b;
+      if (i < 2 * mine) issue_paged(i, first[i >> 1]);
+    box_b = lookup((kSlots + 1) / 2);
+    box_a = kSlots % 2 ? first[(kSlots - 1) / 2] : box_b;
   }
 
   // ---- the query operand: lane (gl, c4) of n-tile nt holds row 8 nt + gl (the warps share the n-tiles) ----
@@ -391,7 +399,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
       }
       __syncwarp();
       if constexpr (PAGED) {
-        if (__shfl_sync(0xffffffffu, limit, 0) > i + kSlots) issue_paged(i + kSlots, page_a);
+        if (__shfl_sync(0xffffffffu, limit, 0) > i + kSlots) issue_paged(i + kSlots, box_a);
       } else {
         if (lane == 0 && i + kSlots < limit) issue(i + kSlots);
       }
@@ -534,10 +542,10 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
       if (PAGED ? there < kKeys || tile_key < keys.from : WALK && there < kKeys) fence_proxy_async();
       __syncwarp();
       if constexpr (PAGED) {
-        if (__shfl_sync(0xffffffffu, limit, 0) > i + kSlots) issue_paged(i + kSlots, page_b);
-        const int next = lookup(j + 1 + (kSlots + 1) / 2);
-        page_a = kSlots % 2 ? page_b : next;  // (an odd ring: the V of a tile is asked for when its K's successor is not yet)
-        page_b = next;
+        if (__shfl_sync(0xffffffffu, limit, 0) > i + kSlots) issue_paged(i + kSlots, box_b);
+        const Box next = lookup(j + 1 + (kSlots + 1) / 2);
+        box_a = kSlots % 2 ? box_b : next;  // (an odd ring: the V of a tile is asked for when its K's successor is not yet)
+        box_b = next;
       } else {
         if (lane == 0 && i + kSlots < limit) issue(i + kSlots);
       }
