@@ -718,20 +718,22 @@ class H2OStore:
             pass
 
 
+def _load_pages():
+    try:
+        from . import _pages
+    except ImportError as e:
+        raise ImportError("_pages.so is not built (run `python paper_2306_14048_b200/build.py`); there is no fallback path") from e
+    _pages.bind(*[ctypes.cast(f, ctypes.c_void_p).value
+                  for f in (lib.h2o_rotate, lib.h2o_pages_append, lib.h2o_pages_scratch_bytes, lib.h2o_pages_attend)])
+    return _pages
+
+
+# checks of arguments of the calls below, packing and the call itself, in C++ (csrc/pages_binding.cpp): a step's host time counts
+_pages = _load_pages()
+
+
 def _wrong(who: str, why: str):
     raise ValueError(who + ": " + why)
-
-
-def _token_stride(who, what, shape, stride):
-    """The stride between the tokens of [tokens, heads, dim] with dense heads, 0 where there is one token at most."""
-    tokens, heads, dim = shape
-    if tokens and (stride[2] != 1 or (heads > 1 and stride[1] != dim)):
-        _wrong(who, "%s must have dense heads" % what)
-    if tokens <= 1:
-        return 0
-    if stride[0] == 0:  # (0 means dense to the library)
-        _wrong(who, "%s must not be broadcast over the tokens" % what)
-    return stride[0]
 
 
 class H2ORotary:
@@ -776,40 +778,13 @@ class H2ORotary:
                                0 if pairs == "halves" else 1, self._index)
         self._at = ctypes.addressof(self._c)
 
-    def _positions(self, positions, tokens):
-        """Address and axis stride of positions: int64 [axes, tokens], or [tokens] for one axis."""
-        shape = positions.shape
-        if positions.dtype is not torch.int64 or positions.get_device() != self._index:
-            _wrong("H2ORotary", "positions must be int64 on %s" % self.device)
-        if shape != (self.axes, tokens) and not (self.axes == 1 and shape == (tokens,)):
-            _wrong("H2ORotary", "positions must be [%d, %d]" % (self.axes, tokens))
-        stride = positions.stride()
-        if tokens > 1 and stride[-1] != 1:
-            _wrong("H2ORotary", "positions must lie token after token")
-        if self.axes > 1 and tokens and stride[0] < tokens:
-            _wrong("H2ORotary", "positions must not be broadcast over the axes")
-        return positions.data_ptr(), stride[0] if self.axes > 1 else 0
-
     def apply(self, x, positions, out, inverse=False, stream=None):
         """Rotates x [tokens, heads, head_dim] into out (which may be x).  inverse: takes the rotation back, which is also
         the gradient of a rotation with respect to its input."""
-        shape = x.shape
-        if len(shape) != 3 or shape[2] != self.head_dim or out.shape != shape:
-            _wrong("H2ORotary", "x and out must be [tokens, heads, %d]" % self.head_dim)
-        dtype = _DTYPES.get(x.dtype)
-        if dtype is None or out.dtype is not x.dtype or x.get_device() != self._index or out.get_device() != self._index:
-            _wrong("H2ORotary", "x and out must both be float32 or bfloat16 on %s" % self.device)
-        at, stride = self._positions(positions, shape[0])
-        code = lib.h2o_rotate(self._at, x.data_ptr(), out.data_ptr(), dtype, shape[0], shape[1], shape[2],
-                              _token_stride("H2ORotary", "x", shape, x.stride()), _token_stride("H2ORotary", "out", shape, out.stride()),
-                              at, stride, 1 if inverse else 0, _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        code = _pages.rotate(self._at, self._index, self.head_dim, self.axes, x, positions, out, inverse,
+                             _raw_stream(self._index) if stream is None else stream.cuda_stream)
         if code:
             _check(code, "h2o_rotate")
-
-
-# h2o_tokens_t and h2o_sequences_t as bytes
-_pack_tokens = struct.Struct("@PPPPPPqqqqqii").pack
-_pack_sequences = struct.Struct("@PPqii").pack
 
 
 class H2OPages:
@@ -840,7 +815,6 @@ class H2OPages:
             strides[0] = max(strides[1] * self.page_size, strides[2] * self.n_heads)
         self.format = _DTYPES[k.dtype]
         self.device, self._index = k.device, k.device.index
-        self._need = {}  # scratch bytes by the sizes of a call
         self.k, self.v = k, v
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
         torch.cuda.current_stream(self.device).synchronize()  # the zero is there, whatever stream comes next
@@ -850,74 +824,15 @@ class H2OPages:
         handle = ctypes.c_void_p()
         _check(lib.h2o_pages_create(ctypes.byref(handle), ctypes.byref(cfg)), "h2o_pages_create")
         self._h = handle
+        self._at = handle.value
 
-    # ---- argument checks ----
-    def _sequences(self, table, length, max_len):
-        batch = length.shape[0] if length.dim() == 1 else -1
-        if length.dtype is not torch.int32 or batch < 0 or length.get_device() != self._index or not length.is_contiguous():
-            _wrong("H2OPages", "length must be a contiguous int32 [batch] on %s" % self.device)
-        if table.dtype is not torch.int32 or table.dim() != 2 or table.shape[0] != batch or table.get_device() != self._index:
-            _wrong("H2OPages", "table must be int32 [batch, pages] on %s" % self.device)
-        stride, pages = table.stride(), table.shape[1]
-        if (pages > 1 and stride[1] != 1) or (batch > 1 and pages and stride[0] < pages):
-            _wrong("H2OPages", "a sequence's entries of the table must be dense, and its own")
-        return _pack_sequences(table.data_ptr(), length.data_ptr(), stride[0] if batch > 1 else 0, pages, max_len), batch, pages
-
-    def _cu(self, cu, batch, tokens):
-        if cu is None:
-            if tokens < batch:
-                _wrong("H2OPages", "without cu there is one token per sequence")
-            return 0
-        if cu.dtype is not torch.int32 or cu.shape != (batch + 1,) or cu.get_device() != self._index or not cu.is_contiguous():
-            _wrong("H2OPages", "cu must be a contiguous int32 [batch + 1] on %s" % self.device)
-        return cu.data_ptr()
-
-    def _heads(self, q, out, what):
-        """Query heads per K/V head and the token strides of q and out."""
-        shape = q.shape
-        if len(shape) != 3 or shape[2] != self.head_dim or shape[1] < self.n_heads or shape[1] % self.n_heads:
-            _wrong("H2OPages", "q must be [tokens, multiple of %d, %d]" % (self.n_heads, self.head_dim))
-        if _DTYPES.get(q.dtype) != self.format or out.dtype is not q.dtype or out.shape != shape:
-            _wrong("H2OPages", "q and %s must have the pages' dtype and one shape" % what)
-        if q.get_device() != self._index or out.get_device() != self._index:
-            _wrong("H2OPages", "q and %s must be on %s" % (what, self.device))
-        return (shape[1] // self.n_heads, _token_stride("H2OPages", "q", shape, q.stride()),
-                _token_stride("H2OPages", what, shape, out.stride()))
-
-    # ---- calls ----
     def append(self, k, v, table, length, cu=None, rotary=None, positions=None, q=None, q_out=None, stream=None):
         """Appends k, v [tokens, heads, head_dim] to their sequences' pages; with ``rotary`` k is rotated on the way, and q
         [tokens, query heads, head_dim] into q_out (which may be q).  cu: int32 [batch + 1] first token of each sequence (None:
         token b is sequence b); positions: as for H2ORotary.apply (None: each token's row, on every axis)."""
-        shape = k.shape
-        if len(shape) != 3 or v.shape != shape or shape[1] != self.n_heads or shape[2] != self.head_dim:
-            _wrong("H2OPages", "k and v must be [tokens, %d, %d]" % (self.n_heads, self.head_dim))
-        if _DTYPES.get(k.dtype) != self.format or v.dtype is not k.dtype or k.get_device() != self._index or v.get_device() != self._index:
-            _wrong("H2OPages", "k and v must have the pages' dtype and be on %s" % self.device)
-        tokens = shape[0]
-        stride = _token_stride("H2OPages", "k", shape, k.stride())
-        if _token_stride("H2OPages", "v", shape, v.stride()) != stride:
-            _wrong("H2OPages", "k and v must have one token stride")
-        seqs, batch, _ = self._sequences(table, length, 2147483647)
-        at, position_stride = 0, 0
-        if rotary is not None:
-            if rotary._index != self._index or rotary.head_dim != self.head_dim:
-                _wrong("H2OPages", "rotary must be for head_dim %d on %s" % (self.head_dim, self.device))
-            if positions is not None:
-                at, position_stride = rotary._positions(positions, tokens)
-        elif positions is not None:
-            _wrong("H2OPages", "positions belong to a rotary")
-        group, qs, os_ = 1, 0, 0
-        if (q is None) != (q_out is None):
-            _wrong("H2OPages", "q and q_out go together")
-        if q is not None:
-            group, qs, os_ = self._heads(q, q_out, "q_out")
-            if q.shape[0] != tokens:
-                _wrong("H2OPages", "q must have as many tokens as k")
-        packed = _pack_tokens(k.data_ptr(), v.data_ptr(), 0 if q is None else q.data_ptr(), 0 if q is None else q_out.data_ptr(),
-                              self._cu(cu, batch, tokens), at, tokens, stride, qs, os_, position_stride, group, batch)
-        code = lib.h2o_pages_append(self._h, packed, seqs, None if rotary is None else rotary._at,
-                                    _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        turn = (0, 0, 0, 0) if rotary is None else (rotary._at, rotary._index, rotary.head_dim, rotary.axes)
+        code = _pages.append(self._at, self._index, self.n_heads, self.head_dim, self.format, k, v, table, length, cu, *turn, positions, q, q_out,
+                             _raw_stream(self._index) if stream is None else stream.cuda_stream)
         if code:
             _check(code, "h2o_pages_append")
 
@@ -926,32 +841,20 @@ class H2OPages:
         included) and the sequence's first ``sinks``.  q, out: [tokens, query heads, head_dim]; cu: int32 [batch + 1] first
         token of each sequence (None: token b is sequence b); max_q, max_len: upper bounds of a sequence's tokens and rows;
         lse: float32 [tokens, query heads] or None."""
-        group, qs, os_ = self._heads(q, out, "out")
-        tokens, heads = q.shape[0], q.shape[1]
-        seqs, batch, pages = self._sequences(table, length, max_len)
-        if cu is None and max_q != 1:
-            _wrong("H2OPages", "without cu there is one token per sequence")
-        if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (tokens, heads) or lse.get_device() != self._index or not lse.is_contiguous()):
-            _wrong("H2OPages", "lse must be a contiguous float32 [tokens, query heads] on %s" % self.device)
-        queries = _pack_queries(q.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(), self._cu(cu, batch, tokens), tokens, qs, os_,
-                                softmax_scale, self.format, group, batch, max_q)
-        sizes = (tokens, group, batch, max_q, max_len, pages, window, sinks)
-        need = self._need.get(sizes)
-        if need is None:
-            need = lib.h2o_pages_scratch_bytes(self._h, queries, seqs, window, sinks)
-        scratch = self._scratch(need, stream) if need else None
-        code = lib.h2o_pages_attend(self._h, queries, seqs, window, sinks, scratch.data_ptr() if need else None, need,
-                                    _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        if stream is not None:  # its scratch, too, comes from that stream
+            with torch.cuda.stream(stream):
+                return self.attend(q, table, length, out, max_len, window, sinks, cu, max_q, lse, softmax_scale)
+        code = _pages.attend(self._at, self._index, self.n_heads, self.head_dim, self.format, q, table, length, out, max_len, window, sinks, cu, max_q,
+                             lse, softmax_scale, _raw_stream(self._index))
         if code:
             _check(code, "h2o_pages_attend")
-        self._needs(sizes, need)
 
-    _scratch, _needs, status = H2OStore._scratch, H2OStore._needs, H2OStore.status
+    status = H2OStore.status
 
     def close(self):
         if getattr(self, "_h", None) is not None:
             lib.h2o_pages_destroy(self._h)
-            self._h = None
+            self._h, self._at = None, 0
 
     def __del__(self):
         try:

@@ -1,4 +1,5 @@
-"""Build libh2o_b200.so (the C-ABI library) in-tree with nvcc for sm_100a.
+"""Build libh2o_b200.so (the C-ABI library) in-tree with nvcc for sm_100a, and _pages.so (argument checks of the paged
+cache's calls, host code) with the C++ compiler.
 
 ``python paper_2306_14048_b200/build.py`` (run as a script, so that the package — which refuses to
 import without the library — is not imported first) or ``build()``; the library is rebuilt
@@ -12,6 +13,7 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -19,6 +21,9 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "build")
 LIB = os.path.join(PKG, "libh2o_b200.so")
 LIB_BOUNDS = os.path.join(PKG, "libh2o_b200_bounds.so")  # the same sources with -DH2O_BOUNDS (every index checked)
+
+PAGES = os.path.join(PKG, "_pages.so")
+PAGES_SOURCE = os.path.join(CSRC, "pages_binding.cpp")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -41,9 +46,31 @@ def needs_build(lib: str = LIB) -> bool:
     return any(os.path.getmtime(p) > t for p in _deps())
 
 
+def build_pages(force: bool = False) -> str:
+    """_pages.so: host code that reads torch tensors, rebuilt only when its sources are newer."""
+    newest = max(os.path.getmtime(p) for p in [PAGES_SOURCE] + glob.glob(os.path.join(ROOT, "include", "*.h")))
+    if not force and os.path.exists(PAGES) and os.path.getmtime(PAGES) >= newest:
+        return PAGES
+    import torch
+
+    at = os.path.dirname(torch.__file__)
+    tmp = PAGES + ".tmp.%d" % os.getpid()
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+    for d in (os.path.join(ROOT, "include"), os.path.join(at, "include"), os.path.join(at, "include", "torch", "csrc", "api", "include"),
+              sysconfig.get_paths()["include"]):
+        cmd += ["-I", d]
+    cmd += [PAGES_SOURCE, "-o", tmp, "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("%s failed for %s:\n%s\n%s" % (cmd[0], PAGES_SOURCE, res.stdout, res.stderr))
+    os.replace(tmp, PAGES)
+    return PAGES
+
+
 def build(force: bool = False, verbose: bool = False, bounds: bool = False) -> str:
     """``bounds``: build libh2o_b200_bounds.so instead, the checked variant (-DH2O_BOUNDS)."""
     lib = LIB_BOUNDS if bounds else LIB
+    build_pages(force)
     if not force and not needs_build(lib):
         return lib
     nvcc = os.environ.get("NVCC", "nvcc")

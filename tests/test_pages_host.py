@@ -1,7 +1,6 @@
 """Refusals of the paged cache and of rotary positions, which need no GPU: every argument error is found on the host, before any
 CUDA call.  A handle is laid out here as the library does it (its configuration comes first).  Addresses are never read."""
 import ctypes
-from types import SimpleNamespace
 
 import numpy as np
 import pytest
@@ -185,20 +184,27 @@ def test_empty_calls_do_nothing(b):
     assert b.lib.h2o_rotate(ctypes.byref(_rotary(b)), None, None, 1, 0, 4, 128, 0, 0, None, 0, 0, None) == 0
 
 
-def test_packed_arguments_match_the_structures(b):
-    for pack, kind, values in ((b._pack_tokens, b.h2o_tokens_t, range(1, 14)), (b._pack_sequences, b.h2o_sequences_t, range(1, 6))):
-        got = kind.from_buffer_copy(pack(*values))
-        assert ctypes.sizeof(kind) == len(pack(*values))
-        assert [getattr(got, n) for n, _ in kind._fields_] == list(values)
+# ---- what the Python side refuses, with CPU tensors (whose device index is -1): a refusal comes before the library is called ----
+def _call(b, name, **kw):
+    z = torch.zeros
+    if name == "rotate":
+        f = dict(at=0, device=-1, dim=64, axes=1, x=z(5, 4, 64), positions=z(5, dtype=torch.int64), out=z(5, 4, 64), inverse=False, stream=0)
+    else:
+        f = dict(at=0, device=-1, heads=2, dim=64, format=b.H2O_F32)
+        if name == "append":
+            f.update(k=z(3, 2, 64), v=z(3, 2, 64), table=z(3, 4, dtype=torch.int32), length=z(3, dtype=torch.int32), cu=None, rotary=0, r_device=0, r_dim=0,
+                     r_axes=0, positions=None, q=None, q_out=None, stream=0)
+        else:
+            f.update(q=z(5, 4, 64), table=z(3, 4, dtype=torch.int32), length=z(3, dtype=torch.int32), out=z(5, 4, 64), max_len=9, window=0, sinks=0, cu=None,
+                     max_q=1, lse=None, scale=0.0, stream=0)
+    assert set(kw) <= set(f)
+    f.update(kw)
+    return getattr(b._pages, name)(*f.values())
 
 
-# ---- what the Python side refuses, with CPU tensors (whose device index is -1) ----
-def _pages(b, heads=2, dim=64, page=16, pages=5, fmt=None):
-    me = SimpleNamespace(_index=-1, device="cpu", n_heads=heads, head_dim=dim, format=b.H2O_F32 if fmt is None else fmt, page_size=page,
-                         n_pages=pages, _h=None, _need={})
-    for name in ("_sequences", "_cu", "_heads"):
-        setattr(me, name, getattr(b.H2OPages, name).__get__(me))
-    return me
+def _refused(b, name, **kw):
+    with pytest.raises(ValueError):
+        _call(b, name, **kw)
 
 
 def test_python_argument_checks(b):
@@ -210,49 +216,64 @@ def test_python_argument_checks(b):
                dict(head_dim=8, axes=[0.0, 1.0, 1.0, 0.0]), dict(head_dim=64, pairs="both"), dict(head_dim=1024), dict(head_dim=64, device="cpu")):
         with pytest.raises(ValueError):
             b.H2ORotary(**kw)
-    me = _pages(b)
-    table, length = z(3, 4, dtype=torch.int32), z(3, dtype=torch.int32)
-    me._sequences(table, length, 9), me._sequences(z(3, 9, dtype=torch.int32)[:, 2:6], length, 9)
-    for bad in ((table.long(), length), (table, length.long()), (table[:2], length), (table.t().contiguous().t(), length), (table[0].expand(3, 4), length),
-                (table[:, ::2], length), (table, length.expand(2, 3)), (table, z(6, dtype=torch.int32)[::2])):
-        with pytest.raises(ValueError):
-            me._sequences(*bad, 9)
-    for cu, batch, tokens in ((None, 3, 2), (z(3, dtype=torch.int32), 3, 9), (z(4), 3, 9), (z(8, dtype=torch.int32)[::2], 3, 9)):
-        with pytest.raises(ValueError):
-            me._cu(cu, batch, tokens)
+
+
+@pytest.mark.parametrize("name", ["append", "attend"])
+def test_sequences_and_cu_are_checked(b, name):
+    z = torch.zeros
+    i32 = lambda *n: z(*n, dtype=torch.int32)
+    assert _call(b, name) == -1  # (past these checks: no handle)
+    for kw in (dict(table=i32(3, 9)[:, 2:6]), dict(table=i32(3, 0)), dict(cu=i32(4))):
+        assert _call(b, name, **kw) == -1
+    table, length = i32(3, 4), i32(3)
+    for kw in (dict(table=table.long()), dict(length=length.long()), dict(table=table[:2]), dict(table=table.t().contiguous().t()),
+               dict(table=table[0].expand(3, 4)), dict(table=table[:, ::2]), dict(length=length.expand(2, 3)), dict(length=i32(6)[::2]),
+               dict(table=None), dict(length=[1, 2, 3]), dict(cu=i32(3)), dict(cu=z(4)), dict(cu=i32(8)[::2]), dict(cu=i32(4, 1)),
+               dict(table=i32(9, 4), length=i32(9))):  # (without cu: a token for each sequence)
+        _refused(b, name, **kw)
+
+
+def test_append_tensors_are_checked(b):
+    z = torch.zeros
+    k, q = z(3, 2, 64), z(3, 4, 64)
+    assert _call(b, "append", q=q, q_out=q) == -1
+    assert _call(b, "append", rotary=HERE, r_device=-1, r_dim=64, r_axes=3, positions=z((3, 3), dtype=torch.int64)) == -1
+    for kw in (dict(v=z(3, 2, 128)), dict(k=z(3, 3, 64), v=z(3, 3, 64)), dict(v=k.bfloat16()), dict(k=k.bfloat16(), v=k.bfloat16()), dict(v=z(3, 4, 64)[:, :2]),
+               dict(k=z(1, 2, 64).expand(3, 2, 64)), dict(k=k[0], v=k[0]), dict(q=q), dict(q_out=q), dict(q=z(4, 4, 64), q_out=z(4, 4, 64)),
+               dict(q=q, q_out=q.bfloat16()), dict(q=z(3, 3, 64), q_out=z(3, 3, 64)), dict(positions=z(3, dtype=torch.int64)), dict(k=k[:2], v=k[:2]),
+               dict(rotary=HERE, r_device=0, r_dim=64, r_axes=1), dict(rotary=HERE, r_device=-1, r_dim=128, r_axes=1),
+               dict(rotary=HERE, r_device=-1, r_dim=64, r_axes=3, positions=z(3, dtype=torch.int64))):
+        _refused(b, "append", **kw)
+
+
+def test_query_tensors_are_checked(b):
+    z = torch.zeros
     q = z(5, 4, 64)
-    assert me._heads(q, q, "out") == (2, 256, 256) and me._heads(z(1, 2, 64), z(1, 2, 64), "out") == (1, 0, 0)
-    for a, o in ((z(5, 3, 64), z(5, 3, 64)), (z(5, 4, 128), z(5, 4, 128)), (q, z(5, 2, 64)), (q.bfloat16(), q.bfloat16()), (q, q.bfloat16()),
-                 (z(1, 4, 64).expand(5, 4, 64), q), (q, z(4, 5, 64).transpose(0, 1)), (z(5, 4, 128)[..., ::2], q)):
-        with pytest.raises(ValueError):
-            me._heads(a, o, "out")
-    append = b.H2OPages.append
-    k = z(3, 2, 64)
-    for kw in (dict(v=z(3, 2, 128)), dict(k=z(3, 3, 64), v=z(3, 3, 64)), dict(v=k.bfloat16()), dict(v=z(3, 4, 64)[:, :2]), dict(q=z(3, 4, 64)),
-               dict(q_out=z(3, 4, 64)), dict(q=z(4, 4, 64), q_out=z(4, 4, 64)), dict(positions=z(3, dtype=torch.int64)), dict(k=k[:2], v=k[:2]),
-               dict(rotary=SimpleNamespace(_index=0, head_dim=64)), dict(rotary=SimpleNamespace(_index=-1, head_dim=128))):
-        f = dict(k=k, v=k, table=table, length=length)
-        f.update(kw)
-        with pytest.raises(ValueError):
-            append(me, **f)
-    attend = b.H2OPages.attend
-    for kw in (dict(max_q=2), dict(lse=z(5, 3)), dict(lse=z(5, 4).double()), dict(lse=z(4, 5).t())):
-        f = dict(q=q, table=table, length=length, out=q, max_len=9)
-        f.update(kw)
-        with pytest.raises(ValueError):
-            attend(me, **f)
+    assert _call(b, "attend", lse=z(5, 4)) == -1
+    one = z(1, 5, 64).transpose(0, 1)  # one head: its stride says nothing
+    assert _call(b, "attend", heads=1, q=one, out=z(5, 1, 64)) == -1
+    for kw in (dict(q=z(5, 3, 64), out=z(5, 3, 64)), dict(q=z(5, 4, 128), out=z(5, 4, 128)), dict(out=z(5, 2, 64)), dict(q=q.bfloat16(), out=q.bfloat16()),
+               dict(out=q.bfloat16()), dict(q=z(1, 4, 64).expand(5, 4, 64)), dict(out=z(4, 5, 64).transpose(0, 1)), dict(q=z(5, 4, 128)[..., ::2]),
+               dict(max_q=2), dict(lse=z(5, 3)), dict(lse=z(5, 4).double()), dict(lse=z(4, 5).t()), dict(max_len=2 ** 40), dict(window=2 ** 31),
+               dict(sinks=-2 ** 40), dict(device=0)):
+        _refused(b, "attend", **kw)
+    with pytest.raises(TypeError):
+        b._pages.attend(1, 2)
+    with pytest.raises(TypeError):
+        _call(b, "attend", max_len="9")
 
 
-def test_python_position_checks(b):
-    me = SimpleNamespace(_index=-1, device="cpu", axes=3)
-    check = b.H2ORotary._positions
-    p = torch.zeros((3, 7), dtype=torch.int64)
-    assert check(me, p, 7)[1] == 7 and check(me, torch.zeros((3, 20), dtype=torch.int64)[:, 5:12], 7)[1] == 20
-    for bad in (p.int(), p[:2], p[0], p.t().contiguous().t(), torch.zeros((3, 14), dtype=torch.int64)[:, ::2], p[:1].expand(3, 7)):
-        with pytest.raises(ValueError):
-            check(me, bad, 7)
-    me.axes = 1
-    assert check(me, p[0], 7)[1] == 0 and check(me, p[1:2], 7)[1] == 0
+def test_rotate_tensors_are_checked(b):
+    z = torch.zeros
+    p = z((3, 5), dtype=torch.int64)
+    assert _call(b, "rotate") == -1 and _call(b, "rotate", axes=3, positions=p) == -1
+    assert _call(b, "rotate", axes=3, positions=z((3, 20), dtype=torch.int64)[:, 5:10]) == -1 and _call(b, "rotate", positions=p[1:2]) == -1
+    for bad in (p.int(), p[:2], p[0], p.t().contiguous().t(), z((3, 10), dtype=torch.int64)[:, ::2], p[:1].expand(3, 5)):
+        _refused(b, "rotate", axes=3, positions=bad)
+    x = z(5, 4, 64)
+    for kw in (dict(x=z(5, 4, 128)), dict(out=z(5, 4, 32)), dict(x=x.double(), out=x.double()), dict(out=x.bfloat16()), dict(x=x[0], out=x[0]),
+               dict(x=z(1, 4, 64).expand(5, 4, 64)), dict(out=z(4, 5, 64).transpose(0, 1)), dict(device=3), dict(positions=p[0].expand(2, 5)), dict(x=None)):
+        _refused(b, "rotate", **kw)
 
 
 def test_references_agree_with_torch():
