@@ -102,6 +102,26 @@ struct Plan {
 // More query rows than this (of one K/V head) run on the tcgen05 kernel: as for the K/V store.
 constexpr int kFewRows = 16;
 
+// Splits the keys of a prompt between the items of the tcgen05 kernel, `rows` query rows in each.  Costs in keys of one block, of
+// which two share an SM and take 64 in a microsecond: an item costs its keys and 4 us more, the last ones to finish leave a
+// quarter of an item's time unused; chunks cost the joining kernel's start and their rows' trip through memory and back.
+void split_prompt(AttendPart& p, int64_t units, int64_t rows, int dim, int sms) {
+  const int64_t len = std::max(1, p.most_keys), num = p.problems > 1 ? 2 : 3, room = 2 * sms, fixed = 256, step = 128;
+  int64_t best = -1;
+  for (int64_t n = 1; n <= kMaxSplits && (n == 1 || units * n <= 16 * room); ++n) {
+    const int64_t chunk = ((len + n - 1) / n + step - 1) / step * step;
+    const int64_t splits = (len + chunk - 1) / chunk, one = std::min(chunk, len) + fixed;
+    int64_t cost = std::max(one, (units * len * num / 3 + units * splits * num / 3 * fixed) / room) + one / 4;
+    if (splits > 1) cost += 200 + units * splits * num / 3 * rows * dim * 8 * 64 / 6400000;
+    if (best < 0 || cost < best) {
+      best = cost;
+      p.chunk = (int)chunk;
+      p.splits = (int)splits;
+    }
+    if (chunk == step) break;
+  }
+}
+
 Plan make_plan(const h2o_pages_t* pages, const h2o_queries_t* q, const h2o_sequences_t* s, int window, int sinks) {
   Plan pl;
   std::memset(&pl, 0, sizeof(pl));
@@ -162,7 +182,8 @@ Plan make_plan(const h2o_pages_t* pages, const h2o_queries_t* q, const h2o_seque
   }
   p.row_tiles = (int)((rows + pl.tile - 1) / pl.tile);
   const int64_t units = (int64_t)p.row_tiles * a.heads * p.problems;
-  split_part(p, p.most_keys, units, sm_count(c.device), pl.kernel, pl.tile, c.format, a.dim, 128, true);
+  if (pl.kernel == Kernel::Tc1) split_prompt(p, units, std::min<int64_t>(rows, pl.tile), a.dim, sm_count(c.device));
+  else split_part(p, p.most_keys, units, sm_count(c.device), pl.kernel, pl.tile, c.format, a.dim, 128, true);
   if (units * p.splits > INT32_MAX) pl.rc = H2O_ERR_UNSUPPORTED;
   if (p.splits > 1) {
     a.slots = p.splits;
