@@ -44,8 +44,9 @@ struct Paging {
   int64_t stride;
   int64_t page_stride, head_stride;  // elements (float32 rows; AttendView::row_stride within a page)
   int n_pages, page_size;
+  int shift;             // page_size is 2^shift, or -1: not a power of two
   int window, sinks;     // a query at row p sees the rows x <= p with x > p - window or x < sinks; window 0: all x <= p
-  int box;               // rows of a box of the tensor maps: divides page_size and the tile; float32: 8
+  int box;               // rows of a box of the tensor maps: a power of two that divides page_size and the tile; float32: 8
 };
 
 struct AttendView {
@@ -86,7 +87,7 @@ __device__ __forceinline__ int64_t first_token(const AttendView& a, int seq) {
   return clamp64(a.cu_q ? (int64_t)a.cu_q[seq] : (int64_t)seq, 0, a.q_rows);
 }
 template <bool PAGED = false>
-__device__ __forceinline__ Problem locate(const AttendView& a, const AttendPart& p, int i) {
+__device__ __forceinline__ Problem locate(const AttendView& a, const AttendPart& p, int i, const int32_t* length = nullptr) {
   int s0 = i, s1 = i + 1;
   int64_t most = a.max_q;
   if (p.grouped) {
@@ -100,7 +101,7 @@ __device__ __forceinline__ Problem locate(const AttendView& a, const AttendPart&
   r.nt = (int)clamp64(first_token(a, s1) - r.t0, 0, most);
   if constexpr (PAGED) {
     r.row0 = 0;
-    r.len = (int)clamp64(p.length[i], 0, p.max_length);
+    r.len = (int)clamp64(length ? *length : p.length[i], 0, p.max_length);  // (one that is on its way already)
     return r;
   }
   r.row0 = clamp64(p.begin[i], 0, a.rows);
@@ -140,11 +141,13 @@ template <bool PAGED>
 __device__ __forceinline__ Keys keys_of(const AttendView& a, int first_seen, int last_seen, int tile) {
   Keys k{0, 0, last_seen, 0};
   if constexpr (PAGED) {
-    k.from = window_from(a, first_seen);
-    const int head = (min(a.pages.sinks, last_seen) + tile - 1) / tile * tile, start = k.from - k.from % a.pages.box;
-    if (start > head) {
-      k.head = head;
-      k.start = start;
+    if (a.pages.window > 0) {
+      k.from = window_from(a, first_seen);
+      const int head = (min(a.pages.sinks, last_seen) + tile - 1) / tile * tile, start = k.from & ~(a.pages.box - 1);
+      if (start > head) {
+        k.head = head;
+        k.start = start;
+      }
     }
   }
   return k;
@@ -158,6 +161,8 @@ template <bool PAGED>
 __device__ __forceinline__ int shared_keys(const AttendPart& p, const Problem& r) {
   return PAGED ? min(r.len, p.most_keys) : r.len;
 }
+// The place in a sequence's table of row x.
+__device__ __forceinline__ int page_index(const AttendView& a, int x) { return a.pages.shift >= 0 ? x >> a.pages.shift : x / a.pages.page_size; }
 // The page that an entry of a sequence's table names; n_pages (which no tensor map holds: read as zeros) for none.
 __device__ __forceinline__ int page_in(const AttendView& a, int entry) { return entry >= 0 && entry < a.pages.n_pages ? entry : a.pages.n_pages; }
 

@@ -156,16 +156,50 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   constexpr int kPitch = D + 4;  // floats per row of a warp's partial output
   static_assert(kRows * kPitch * 4 <= kSlots * kTile, "a warp's partial output fits its ring");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gl = lane >> 2, c4 = lane & 3;
-  const BlockWork w = block_work(a, part, block);
-  const Problem pr = locate<PAGED>(a, part, w.problem);
+  BlockWork w;
+  if constexpr (PAGED) {  // (the grid's dimensions: no divisions before the first loads)
+    w.head = part.row_tiles == 1 ? blockIdx.x : blockIdx.x / part.row_tiles;
+    w.row_tile = blockIdx.x - w.head * part.row_tiles;
+    w.split = blockIdx.y;
+    w.problem = blockIdx.z;
+  } else {
+    w = block_work(a, part, block);
+  }
+  [[maybe_unused]] const int32_t length = PAGED ? part.length[w.problem] : 0;
+  // PAGED: this lane's copy of a tile (one of `copies`): box `my_box`, half `my_half` of the channels (all, where it is one copy)
+  const int boxes = PAGED ? kKeys / a.pages.box : 1, copies = boxes == 1 ? 1 : boxes * (D / 64);
+  const int my_box = lane / (D / 64), my_half = lane % (D / 64);
+  // Without a window the first tiles' places in the table do not depend on the length, which is still on its way: their entries
+  // are asked for at once (within the table, whatever the length will be).
+  constexpr int kFirst = (kSlots + 1) / 2 + 1;  // tiles looked up before the loop
+  [[maybe_unused]] int early[kFirst];
+  if constexpr (PAGED) {
+    if (threadIdx.x == 0) {
+      prefetch_tensormap(map_k);
+      prefetch_tensormap(map_v);
+    }
+#pragma unroll
+    for (int j = 0; j < kFirst; ++j) {
+      const int64_t x = (int64_t)w.split * part.chunk + (warp + kWarps * j) * kKeys + (boxes == 1 ? 0 : my_box * a.pages.box);
+      early[j] = a.pages.n_pages;
+      if (a.pages.window == 0 && lane < copies && x < part.max_length) early[j] = a.pages.table[w.problem * a.pages.stride + page_index(a, (int)x)];
+    }
+    if (threadIdx.x == 0) sh.gave_up = 0;
+    if (lane == 0) {
+      for (int s = 0; s < kSlots; ++s) mbar_init(&sh.full[warp][s], 1);
+      fence_barrier_init();
+    }
+  }
+  const Problem pr = locate<PAGED>(a, part, w.problem, PAGED ? &length : nullptr);
   const int rows = pr.nt * a.group, r0 = w.row_tile * kRows;
   if (r0 >= rows) return;
   const int n_rows = min(kRows, rows - r0);
   const int key0 = w.split * part.chunk;
   const bool direct = a.part_out == nullptr;
   if (!direct && key0 >= shared_keys<PAGED>(part, pr)) return;  // (the join kernel does not read it)
-  const int last_seen = seen_rows(part, pr, (r0 + n_rows - 1) / a.group);  // the tile's last row sees the most
-  const int first_seen = part.causal ? seen_rows(part, pr, r0 / a.group) : last_seen;
+  auto token_of_row = [&](int r) { return PAGED && a.group == 1 ? r : r / a.group; };
+  const int last_seen = seen_rows(part, pr, token_of_row(r0 + n_rows - 1));  // the tile's last row sees the most
+  const int first_seen = part.causal ? seen_rows(part, pr, token_of_row(r0)) : last_seen;
   const Keys keys = keys_of<PAGED>(a, first_seen, last_seen, kKeys);
   const int key1 = min(keys.count(), key0 + part.chunk);
   [[maybe_unused]] const int last_from = PAGED ? window_from(a, last_seen) : 0;
@@ -179,21 +213,18 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   const int mine = n_tiles > warp ? (n_tiles - warp + kWarps - 1) / kWarps : 0;
   unsigned char* my_ring = ring + warp * (kSlots * kTile);
   uint64_t* full = sh.full[warp];
-  // PAGED: this lane's copy of a tile (one of `copies`): box `my_box`, half `my_half` of the channels (all, where it is one copy)
-  const int boxes = PAGED ? kKeys / a.pages.box : 1, copies = boxes == 1 ? 1 : boxes * (D / 64);
-  const int my_box = lane / (D / 64), my_half = lane % (D / 64);
   // This lane's box of a tile: the table's entry (looked at when the copy is issued: a use where it is read would wait for it) and
   // the row in the page.
   struct Box {
     int entry, row;
   };
   Box box_a{0, 0}, box_b{0, 0};  // of the tiles whose next K and V this lane asks for
-  auto lookup = [&](int j) {  // of tile j; what no row sees need not be read
+  auto lookup = [&](int j, const int* entry) {  // of tile j, whose entry may be there; what no row sees need not be read
     Box b{a.pages.n_pages, 0};
     if (j < mine && lane < copies) {
-      const int x = keys.at(key0 + (warp + kWarps * j) * kKeys) + (boxes == 1 ? 0 : my_box * a.pages.box), page = x / a.pages.page_size;
+      const int x = keys.at(key0 + (warp + kWarps * j) * kKeys) + (boxes == 1 ? 0 : my_box * a.pages.box), page = page_index(a, x);
       b.row = x - page * a.pages.page_size;
-      if (!unseen(a, keys, x, a.pages.box)) b.entry = a.pages.table[w.problem * a.pages.stride + page];
+      if (!unseen(a, keys, x, a.pages.box)) b.entry = entry && a.pages.window == 0 ? *entry : a.pages.table[w.problem * a.pages.stride + page];
     }
     return b;
   };
@@ -211,28 +242,47 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
     mbar_expect_tx(&full[i % kSlots], kTile);
     tma_4d(my_ring + (i % kSlots) * kTile, (i & 1) ? map_v : map_k, row, w.head, &full[i % kSlots]);
   };
-  if (threadIdx.x == 0) sh.gave_up = 0;
-  if (lane == 0) {
-    for (int s = 0; s < kSlots; ++s) mbar_init(&full[s], 1);
-    fence_barrier_init();
-    if constexpr (!PAGED) {
+  if constexpr (!PAGED) {
+    if (threadIdx.x == 0) sh.gave_up = 0;
+    if (lane == 0) {
+      for (int s = 0; s < kSlots; ++s) mbar_init(&full[s], 1);
+      fence_barrier_init();
       for (int i = 0; i < min(kSlots, 2 * mine); ++i) issue(i);
     }
   }
   __syncwarp();
+  // PAGED: the query rows are asked for before the first copies wait for their table entries
+  [[maybe_unused]] uint2 q_early[kSteps];
   if constexpr (PAGED) {
-    Box first[(kSlots + 1) / 2];
+    const int r = r0 + warp * 8 + gl, r_tok = token_of_row(r);
+    const bool there = warp < NT && warp * 8 + gl < n_rows && token_ok(a, pr.t0 + r_tok, w.head * a.group + r - r_tok * a.group);
+    const int tok = there ? r_tok : 0;
+    const __nv_bfloat16* qr = static_cast<const __nv_bfloat16*>(a.q) + (pr.t0 + tok) * a.q_stride + ((int64_t)w.head * a.group + (there ? r - tok * a.group : 0)) * D;
 #pragma unroll
-    for (int j = 0; j < (kSlots + 1) / 2; ++j) first[j] = lookup(j);
+    for (int ks = 0; ks < kSteps; ++ks) {
+      q_early[ks] = make_uint2(0, 0);
+      if (there) {
+        q_early[ks].x = *reinterpret_cast<const uint32_t*>(qr + 16 * ks + 2 * c4);
+        q_early[ks].y = *reinterpret_cast<const uint32_t*>(qr + 16 * ks + 2 * c4 + 8);
+      }
+    }
+    Box first[kFirst];
+#pragma unroll
+    for (int j = 0; j < kFirst; ++j) first[j] = lookup(j, &early[j]);
 #pragma unroll
     for (int i = 0; i < kSlots; ++i)
       if (i < 2 * mine) issue_paged(i, first[i >> 1]);
-    box_b = lookup((kSlots + 1) / 2);
+    box_b = first[kFirst - 1];
     box_a = kSlots % 2 ? first[(kSlots - 1) / 2] : box_b;
+    if (warp < NT) {
+#pragma unroll
+      for (int ks = 0; ks < kSteps; ++ks) sh.q[warp][ks][lane] = q_early[ks];
+      if (c4 == 0) sh.row_factor[warp * 8 + gl] = a.scale2;
+    }
   }
 
   // ---- the query operand: lane (gl, c4) of n-tile nt holds row 8 nt + gl (the warps share the n-tiles) ----
-  for (int nt = warp; nt < NT; nt += kWarps) {
+  for (int nt = PAGED ? NT : warp; nt < NT; nt += kWarps) {
     const int r = nt * 8 + gl;
     const bool there = r < n_rows && token_ok(a, pr.t0 + (r0 + r) / a.group, w.head * a.group + (r0 + r) % a.group);
     const int tok = there ? (r0 + r) / a.group : 0;
@@ -286,7 +336,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
     for (int e = 0; e < 2; ++e) {
       const int r = nt * 8 + 2 * c4 + e;
       factor[nt][e] = sh.row_factor[r];
-      seen[nt][e] = r < n_rows ? (part.causal ? seen_rows(part, pr, (r0 + r) / a.group) : last_seen) : last_seen;
+      seen[nt][e] = r < n_rows ? (part.causal ? seen_rows(part, pr, token_of_row(r0 + r)) : last_seen) : last_seen;
     }
   uint2 qf[NT == 1 ? kSteps : 1];
   if constexpr (NT == 1) {
@@ -543,7 +593,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
       __syncwarp();
       if constexpr (PAGED) {
         if (__shfl_sync(0xffffffffu, limit, 0) > i + kSlots) issue_paged(i + kSlots, box_b);
-        const Box next = lookup(j + 1 + (kSlots + 1) / 2);
+        const Box next = lookup(j + 1 + (kSlots + 1) / 2, nullptr);
         box_a = kSlots % 2 ? box_b : next;  // (an odd ring: the V of a tile is asked for when its K's successor is not yet)
         box_b = next;
       } else {
@@ -587,7 +637,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   constexpr int kLanes = D / 4;  // threads of a row, four channels each
   for (int r = threadIdx.x / kLanes; r < n_rows; r += kThreads / kLanes) {
     const int c = (threadIdx.x % kLanes) * 4;
-    const int tok = (r0 + r) / a.group;
+    const int tok = token_of_row(r0 + r);
     const int64_t token = pr.t0 + tok;
     const int hq = w.head * a.group + (r0 + r) - tok * a.group;
     if (WALK && (token < prefix.t0 || token >= prefix.t0 + prefix.nt)) continue;  // beyond what the caller allowed for
@@ -637,7 +687,7 @@ attend_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   unsigned char* ring = dyn + ((1024u - (smem_u32(dyn) & 1023u)) & 1023u);
   let_next_start();  // (the joining kernel waits for this one's end; others are launched to start after it)
   if (NT0 == NT1 || blockIdx.x < blocks0) {
-    const bool second = blockIdx.x >= blocks0;
+    const bool second = !PAGED && blockIdx.x >= blocks0;
     attend<FMT, D, NT0, NT0, WALK, PAGED>(a, &map_k, &map_v, a.part[second ? 1 : first], blockIdx.x - (second ? blocks0 : 0), ring, sh);
   } else {
     attend<FMT, D, NT1, NT0, false, PAGED>(a, &map_k, &map_v, a.part[1], blockIdx.x - blocks0, ring, sh);
@@ -654,6 +704,11 @@ cudaError_t launch(const AttendView& a, int first, bool both, const CUtensorMap&
   const cudaError_t e = ensure_dynamic_smem(f, smem, &flags);
   if (e != cudaSuccess) return e;
   const int64_t b0 = part_blocks(a, a.part[first]), b1 = both ? part_blocks(a, a.part[1]) : 0;
+  if constexpr (PAGED) {
+    const AttendPart& p = a.part[0];
+    return launch_kernel(attend_mma_kernel<FMT, D, NT0, NT1, WALK, PAGED>, dim3((unsigned)(p.row_tiles * a.heads), (unsigned)p.splits, (unsigned)p.problems),
+                         kThreads, smem, stream, false, map_k, map_v, a, 0, 0u);
+  }
   return launch_kernel(attend_mma_kernel<FMT, D, NT0, NT1, WALK, PAGED>, dim3((unsigned)(b0 + b1)), kThreads, smem, stream, a.early != 0, map_k, map_v, a,
                        first, (unsigned)b0);
 }
