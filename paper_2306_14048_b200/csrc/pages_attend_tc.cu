@@ -10,10 +10,19 @@
 // there are none: it takes over the place of a block of the grid that has not started (clusterlaunchcontrol), so that the
 // hardware hands the work out in the grid's order and nobody counts.  The next item's keys and queries are on their way while
 // the last tiles of an item are computed, and its first S while the item's result is written.
-// Measured (us; blocks of one item each before): see the table of the document that describes the design.
-// Roles: warp 0 takes items and issues the copies of K and V, a box of a page to a lane; warp 1 issues S, warp 3 issues P V,
-// clears what nobody sees in a V tile (0 * NaN must not reach the sums) and owns tensor memory; warp 2 copies query rows;
-// warps 4..7 are the softmax, one thread per row.
+// Roles: warp 0 takes items and issues the copies of K, a box of a page to a lane; warp 2 copies query rows and V; warp 1 issues
+// S, warp 3 issues P V, clears what nobody sees in a V tile (0 * NaN must not reach the sums) and owns tensor memory; warps
+// 4..7 are the softmax, one thread per row.
+// Bound by the softmax warps and the power limit.  A tile takes 1640 cycles with two blocks on the SM (1350 alone): 900 for the
+// exponentials (450 of them the special function unit's), 330 to learn that S is there, 320 for loading, masking and storing;
+// its products take 640 (S reads the queries from shared memory again for every 16 channels, 48 cycles of 32; the keys of a tile
+// are as many as tensor memory holds beside O and P).  An item costs 4 to 5 us more: the last product, the result, the first
+// tile's maximum.  Four prompts of up to 4096 tokens, 32 heads of 128, window 1020 and 4 sinks, pages of 64: 245 us, 750 TFLOP/s of
+// what the mask leaves (282 at 1600 MHz, once the power limit has lowered the clock); 360 with blocks of one item, two groups of
+// rows and pairs of K and V in one ring, 310 with further items, 247 once no warp waited for a table entry where it read it; with
+// steps of 16 keys that nobody sees left out of the products 245.
+// Tried: tiles of 80 keys (long ranges 3 % faster, windows 5 % slower); S of 128 keys at once with P over it (304 against 285 us
+// under the power limit); more or fewer exponentials on the FMA pipe (one pair in 4: 266, in 16: 248).
 // The reference m of a row is the maximum of its first tile.  Later tiles compute their exponentials against it without
 // looking for a maximum: only when a tile's sum comes out large (kLargeSum) the tile is done again with the new maximum and O
 // is rescaled.  A value far above the reference costs no precision in floating point, only range.
@@ -35,7 +44,7 @@ constexpr int kItems = 2;  // ring of items, the one under way and the next
 // ring of pairs would hold it as long.)
 __host__ __device__ constexpr int tile_bytes(int d) { return kN * d * 2; }
 __host__ __device__ constexpr int slots_k(int d) { return d == 128 ? 2 : 4; }
-__host__ __device__ constexpr int slots_v(int d) { return d == 128 ? (kN == 64 ? 3 : 2) : 4; }
+__host__ __device__ constexpr int slots_v(int d) { return d == 128 ? 3 : 4; }
 constexpr int kMaxSlots = 5;
 // Registers of a thread: 256 start with 128 each = 128 x 176 + 128 x 80.
 constexpr int kRegsSoftmax = 176, kRegsOther = 80;
@@ -98,6 +107,12 @@ __device__ __forceinline__ int place_of(const uint4* answer) {
       : "r"(smem_u32(answer))
       : "memory");
   return there ? (int)x : -1;
+}
+// Steps of 16 keys of the tile that starts at `key`, up to the last one with a key that some row of the item sees.
+__device__ __forceinline__ int steps_of(const AttendView& a, const Keys& k, int key) {
+  int end = min(k.end - key, kN);
+  if (key + kN <= k.from) end = min(end, a.pages.sinks - key);
+  return max(1, (end + 15) >> 4);
 }
 // The lowest n bits, for any n.
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
@@ -282,7 +297,7 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
       }
     } else if (warp == 1) {
       // ---- S (the whole warp walks, one elected lane issues) ----
-      constexpr uint32_t idesc = instr_desc_f16(kM, kN, kFmtBF16, kFmtBF16, false, false);
+      constexpr uint32_t idesc_16 = instr_desc_f16(kM, 16, kFmtBF16, kFmtBF16, false, false);
       const uint64_t dq = smem_desc_sw128(smem_u32(q_tile), 16, 1024);
       const uint32_t d_s = tmem + kColS;
       uint32_t count = 0, queries = 0;  // tiles, items with tiles
@@ -299,6 +314,8 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
           if (!ok) break;
           tc_fence_after();
           const uint64_t dk = smem_desc_sw128(smem_u32(ring_k + slot * kTile), 16, 1024);
+          // (as many columns as hold a key that somebody sees; the others keep what was there, and are masked)
+          const uint32_t idesc = idesc_16 + ((uint32_t)(__shfl_sync(0xffffffffu, steps_of(a, it.keys, it.keys.at(it.key0 + j * kN)), 0) - 1) << 18);
           if (elect_one()) {
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks) {
@@ -377,12 +394,12 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
           ok = wait_all(&sh.full[1][slot], count / kSlotsV);
           if (!ok) break;
           const uint32_t tile = smem_u32(ring_v + slot * kTile);
-          const int key = it.keys.at(it.key0 + j * kN);
+          const int key = it.keys.at(it.key0 + j * kN), steps = __shfl_sync(0xffffffffu, steps_of(a, it.keys, key), 0);
           if (key + kN > it.keys.end || (key < it.keys.from && key + kN > a.pages.sinks)) {
             constexpr int kLanes = D / 8;  // lanes to a row
             const int c = lane % kLanes;
 #pragma unroll 4
-            for (int r = lane / kLanes; r < kN; r += 32 / kLanes)
+            for (int r = lane / kLanes; r < 16 * steps; r += 32 / kLanes)
               if (unseen(a, it.keys, key + r, 1))
                 st_shared16(tile + (r >> shift) * (box * 128 * kHalves) + (c >> 3) * (box * 128) + (r & (box - 1)) * 128 + (((c ^ r) & 7) << 4),
                             make_uint4(0, 0, 0, 0));
@@ -397,7 +414,8 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
             if (j == 0) mma_ts_lohi<false>(d_o, d_p, desc_lo(dv), desc_hi(dv), idesc);
             else mma_ts_lohi<true>(d_o, d_p, desc_lo(dv), desc_hi(dv), idesc);
 #pragma unroll
-            for (int ks = 1; ks < kN / 16; ++ks) mma_ts_lohi<true>(d_o, d_p + 8u * ks, desc_lo(dv) + step[ks], desc_hi(dv), idesc);
+            for (int ks = 1; ks < kN / 16; ++ks)
+              if (ks < steps) mma_ts_lohi<true>(d_o, d_p + 8u * ks, desc_lo(dv) + step[ks], desc_hi(dv), idesc);
             mma_commit(&sh.p_empty);
             mma_commit(&sh.empty[1][slot]);
             if (j == nt - 1) mma_commit(&sh.o_final);

@@ -3,8 +3,11 @@
 // A pair of channels (a, b) at position p with frequency f turns by t = p f:  a' = a cos t - b sin t,  b' = b cos t + a sin t.
 // p f is a product in 64 bits, reduced to turns: t / 2 pi minus the nearest integer, at most half a turn, becomes fp32 and
 // goes to sincospif.  (In fp32 the angle of position 1e6 would be off by 0.06.)  A block computes the sines and cosines of
-// its token once, into shared memory, and all heads use them; so the kernel is bound by memory: every value read once,
+// its tokens once, into shared memory, and all heads use them; so the kernel is bound by memory: every value read once,
 // written once.  Products are fp32, rounded to the type once.
+// Appending 15700 tokens, 32 query and 32 K/V heads of 128, bfloat16: 122 us, 6.1 TB/s (a plain copy of as many bytes 6.3); rotating
+// 9001 tokens of 32 heads 31 us, 4.7 TB/s (a copy 27: its launches are as short, and half the instruction slots are taken
+// here).  64 tokens of a step: 2.9 us on the device.
 #include <algorithm>
 
 #include "pages.cuh"

@@ -146,7 +146,9 @@ __device__ __forceinline__ uint32_t chunk_addr(uint32_t tile, int r, int c) {
 // NTB: the kernel's larger number of n-tiles, which the ring is made for.  WALK: the block takes its sequence's prefix
 // (part 0's range) and then its own rows, and writes the result: no chunks, no joining kernel.  PAGED: the rows lie in
 // pages; a tile is one copy where its 32 rows lie in one page, else a copy for each box of 16 or 8 rows and half of the
-// head dimension, each issued by a lane of its own, which has looked its page up a tile ahead.
+// head dimension, each issued by a lane of its own, which has looked its page up a tile ahead (64 sequences of up to 4096
+// rows, 32 heads: pages of 64 382 us, of 16 381, of 8 393; 6.9 to 7.0 TB/s).  Nothing between the start and the first copy
+// waits for more than one trip to memory: three sequences of up to 300 rows take 6.7 us, 3 of them the launch.
 template <int FMT, int D, int NT, int NTB, bool WALK, bool PAGED>
 __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* map_k, const CUtensorMap* map_v,
                                        const AttendPart& part, unsigned block, unsigned char* ring, Shared<NTB>& sh) {
