@@ -40,6 +40,7 @@ using namespace tc;
 constexpr int kM = 128, kN = 64;  // rows and keys of a tile
 constexpr int kThreads = 256;
 constexpr int kItems = 2;  // ring of items, the one under way and the next
+constexpr int kMostSkipped = 256;  // places in a row without work (1.5 us each)
 // Rings of tiles of K and of V, what fits half an SM's shared memory beside the queries.  (K is done with a tile earlier than V: a
 // ring of pairs would hold it as long.)
 __host__ __device__ constexpr int tile_bytes(int d) { return kN * d * 2; }
@@ -246,9 +247,11 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
         __syncwarp();
         pending = true;
       };
-      // The next item, or the end (nt < 0), found and published.
+      // The next item, or the end (nt < 0), found and published; after many places without work an item of no rows, so that nobody
+      // waits for long.
       auto advance = [&](bool first) {
         next.nt = -1;
+        int skipped = 0;
         for (bool found = first && describe(blockIdx.x); !found;) {
           if (!pending) request();
           ok = wait_all(&sh.answered, requests);
@@ -263,6 +266,10 @@ pages_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
             break;
           }
           found = describe((unsigned)place);
+          if (!found && ++skipped == kMostSkipped) {
+            next.nt = next.n_rows = 0;
+            found = true;
+          }
         }
         publish();
       };

@@ -560,3 +560,58 @@ def test_two_graphs_and_two_streams_share_a_cache(pkg):
     torch.cuda.synchronize()
     for a, b in zip(alone, outs):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("new,rows", [([300, 40], [700, 40]), ([20, 0], [900, 5])])
+def test_captured_prompts_follow_the_arrays(pkg, new, rows):
+    """A captured prompt, replayed with other lengths, token counts and tables: the results of calls of their own."""
+    heads, dim, page = 2, 128, 16
+    pool = Pool(pkg, "bf16", heads, dim, page, [1000, 1000])
+    for b in range(2):
+        pool.fill(b, _randn(b, 1000, heads, dim), _randn(b + 7, 1000, heads, dim))
+    q = _randn(3, 400, heads, dim).to(torch.bfloat16).cuda()
+    table, length, cu = _i32(pool.table), _i32(rows), _i32(_sums(new))
+    out, want = torch.full_like(q, 5.0), torch.full_like(q, 5.0)
+    args = dict(max_len=1000, window=333, sinks=3, max_q=300)
+    pool.pages.attend(q, table, length, out, cu=cu, **args)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        pool.pages.attend(q, table, length, out, cu=cu, **args)
+    for new2, rows2, swap in ((new, rows, False), (new[::-1], rows[::-1], True), ([1, 1], [1000, 999], False), ([0, 300], [0, 300], True), ([0, 0], [9, 9], False)):
+        table.copy_(_i32(pool.table[::-1] if swap else pool.table)), length.copy_(_i32(rows2)), cu.copy_(_i32(_sums(new2)))
+        out.fill_(5.0), want.fill_(5.0)
+        pool.pages.attend(q, table, length, want, cu=cu, **args)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        assert (out[sum(new2):] == 5.0).all()
+    assert pool.pages.status() == 0
+
+
+def test_many_places_without_work(pkg):
+    """Thousands of sequences with one token beside one with 2000: almost no tile of query rows exists."""
+    batch, heads, dim, page, n = 3000, 2, 64, 16, 2000
+    g = torch.Generator(device="cuda").manual_seed(3)
+    pages = batch - 1 + n // page
+    k, v = (torch.randn((pages, page, heads, dim), generator=g, device="cuda").bfloat16() for _ in range(2))
+    table = torch.full((batch, n // page), -1, dtype=torch.int32, device="cuda")
+    table[:, 0] = torch.arange(batch, dtype=torch.int32, device="cuda")
+    table[1234] = torch.cat([table[1234, :1], torch.arange(batch, pages + 0, dtype=torch.int32, device="cuda"), torch.full((n // page,), 7, dtype=torch.int32, device="cuda")])[:n // page]
+    new = torch.ones(batch, dtype=torch.int64)
+    new[1234] = n
+    length = new.int().cuda()
+    length[:1234] = 9
+    cu = torch.cat([torch.zeros(1, dtype=torch.int64), new.cumsum(0)]).int().cuda()
+    tokens = int(new.sum())
+    q = torch.randn((tokens, heads, dim), generator=g, device="cuda").bfloat16()
+    out = torch.full_like(q, 5.0)
+    h = pkg.H2OPages(k, v)
+    h.attend(q, table, length, out, max_len=n, cu=cu, max_q=n)
+    torch.cuda.synchronize()
+    assert h.status() == 0
+    at = int(cu[1234])
+    for b, first, count, m in ((5, 5, 1, 9), (1234, at, n, n), (2500, 2500 + n - 1, 1, 1)):
+        rows = [x[table[b].clamp(min=0).long()].flatten(0, 1)[:m].double().cpu().numpy() for x in (k, v)]
+        want = ref.attend(q[first:first + count].double().cpu().numpy(), *rows, ref.visible(count, m, 0, 0), ref.scale_of(dim), "bf16", True)
+        ref.compare(out[first:first + count], want[0], want[2], "sequence %d" % b)
