@@ -122,7 +122,7 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool t
 }
 
 // A lane's box of the tile that comes next, looked up a tile ahead of its copy.  (The entry is looked at only when the copy is
-// issued: a use of it where it is read would wait for it, 400 cycles of the 1000 that a tile takes.)
+// issued: a use of it where it is read would wait for it, 400 cycles for each of K and V.)
 struct Box {
   int entry, row;
   __device__ __forceinline__ void find(const AttendView& a, const Item& it, int j, int b) {
