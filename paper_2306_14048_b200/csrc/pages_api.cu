@@ -185,6 +185,19 @@ Plan make_plan(const h2o_pages_t* pages, const h2o_queries_t* q, const h2o_seque
   const int64_t units = (int64_t)p.row_tiles * a.heads * p.problems;
   if (pl.kernel == Kernel::Tc1) split_prompt(p, units, std::min<int64_t>(rows, pl.tile), a.dim, sm_count(c.device));
   else split_part(p, p.most_keys, units, sm_count(c.device), pl.kernel, pl.tile, c.format, a.dim, 128, true);
+  // Few units of few query rows: split_part's costs lead to more blocks here than are fastest (as measured; what costs the time was
+  // not profiled).  Three blocks to two SMs are enough, of several sequences half as many again, as their lengths are taken to average
+  // two thirds of the longest.  Without / with this, in us (bf16, head_dim 128, replayed from a graph): one sequence of 8 heads, 5000
+  // keys 18.7 / 12.6, 20000 28.7 / 21.8, 70000 68.2 / 53.1; with 16 query heads each 24.7 / 16.2, 36.6 / 27.0; of 32 heads 20000
+  // 66.1 / 53.5; 2 and 3 sequences of up to 20000 36.7 / 29.9, 47.4 / 39.6; up to 1000 keys the same.  Of 87 calls measured two lose
+  // more than 3 %, both of head_dim 64: one sequence of 8 heads, 33000 keys, 23.4 / 24.3; four of up to 20000, 25.5 / 30.9.
+  if (pl.kernel == Kernel::Mma && 4 * units <= sm_count(c.device)) {
+    const int64_t blocks = (int64_t)sm_count(c.device) * 3 / 2 * (p.problems > 1 ? 3 : 2) / 2, most = (blocks + units - 1) / units;
+    if (p.splits > most) {
+      p.chunk = (int)(((p.most_keys + most - 1) / most + 127) / 128 * 128);
+      p.splits = (p.most_keys + p.chunk - 1) / p.chunk;
+    }
+  }
   if (units * p.splits > INT32_MAX) pl.rc = H2O_ERR_UNSUPPORTED;
   if (p.splits > 1) {
     a.slots = p.splits;

@@ -362,6 +362,13 @@ def test_long_sequences_are_cut_and_joined(pkg, dtype, heads, group, dim, page, 
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,group,dim,page", [(8, 1, 128, 16), (8, 2, 64, 32), (8, 16, 128, 64), (12, 1, 64, 16), (37, 1, 128, 16), (38, 1, 128, 16)])
+@pytest.mark.parametrize("rows", [[5003], [4100, 1, 2500]])
+def test_few_heads_of_long_sequences(pkg, dtype, heads, group, dim, page, rows):
+    _check_attend(pkg, dtype, heads, group, dim, page, [1] * len(rows), rows)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("dim,page", [(64, 16), (128, 16), (128, 64), (64, 24), (128, 8)])
 @pytest.mark.parametrize("new,rows,group", [
     ([2, 1, 5], [2, 1, 90], 1), ([16, 0, 3], [300, 40, 3], 1), ([17, 1], [17, 260], 1), ([100, 128, 129], [100, 500, 129], 1),
