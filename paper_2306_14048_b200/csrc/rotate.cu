@@ -10,15 +10,14 @@
 // sees few of them in so short a launch).  64 tokens of a step: 2.9 us on the device.
 #include <algorithm>
 
+#include "move_cut.cuh"
 #include "pages.cuh"
 
 namespace h2o {
 
 namespace {
 
-constexpr int kThreads = 128;
-constexpr int kMaxHalf = 256;  // pairs of a head (head_dim up to 512), or of a block's tokens together
-constexpr int kMaxTokens = 8;  // of a block
+constexpr int kThreads = kMoveThreads;
 constexpr int kAhead = 2;      // items a thread has under way
 
 // 16 bytes of a head's channels, as they lie in memory and as numbers.
@@ -80,16 +79,10 @@ struct Piece {
   bool turn;
 };
 
-// How a launch is cut: `tokens` to a block, which share its threads and their sines; quotients of small numbers by
-// multiplication, x / d = the upper half of x * (2^32 / d + 1) (exact as long as x * d < 2^32).
-struct Cut {
-  int tokens, per, items;  // items of a head, of a token
-  uint32_t by_per, by_items;
-};
 constexpr int64_t kNoPage = -1, kNoSequence = -2;
 
 template <typename T, Kind KIND>
-__global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ MoveArgs a, const __grid_constant__ Cut cut) {
+__global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ MoveArgs a, const __grid_constant__ MoveCut cut) {
   constexpr int N = Chunk<T>::N;
   __shared__ float2 cs[kMaxHalf];
   __shared__ int64_t place[kMaxTokens], rows[kMaxTokens];  // of K and V of each token in the pages; its row
@@ -99,11 +92,9 @@ __global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ 
   const int items = cut.items * here;
   auto piece = [&](int i, bool to) {  // (to: where it goes is known by now)
     Piece<T> p;
-    const int k = cut.tokens == 1 ? 0 : (int)__umulhi((uint32_t)i, cut.by_items);
+    int k, head, c;
+    cut.split(i, k, head, c);
     const int64_t t = t0 + k;
-    i -= k * cut.items;
-    int head = cut.per == 1 ? i : (int)__umulhi((uint32_t)i, cut.by_per);
-    const int c = i - head * cut.per;
     const int64_t at = a.kv_heads > 0 && to ? place[k] : kNoPage;
     if (head < a.q_heads) {
       p.from = static_cast<const T*>(a.q) + t * a.q_stride + (int64_t)head * a.dim;
@@ -246,20 +237,9 @@ cudaError_t launch(const MoveArgs& a, cudaStream_t stream) {
   // pairs of chunks need a head of whole pairs of chunks and, for halves, rotated channels of whole pairs
   const bool chunks = a.dim % (2 * N) == 0;
   const Kind kind = !chunks || (a.turn.halves && a.turn.half % N != 0) ? Kind::Single : a.turn.halves ? Kind::Halves : Kind::Neighbours;
-  Cut cut;
-  cut.per = kind == Kind::Single ? a.dim / 2 : a.dim / (2 * N);
-  cut.items = (a.q_heads + 2 * a.kv_heads) * cut.per;
-  cut.by_per = cut.per > 1 ? (uint32_t)((1ull << 32) / cut.per) + 1 : 0;
-  cut.by_items = cut.items > 1 ? (uint32_t)((1ull << 32) / cut.items) + 1 : 0;
-  // Few tokens: blocks enough that a thread has one item.  Many: each token's sines computed once, several tokens to a block as long
-  // as that leaves a thread up to four items.
-  const int64_t most = (cut.items + kThreads - 1) / kThreads;
-  cut.tokens = 1;
-  int64_t parts = most;
-  if (a.n_tokens * most > 8 * sm_count()) {
-    parts = (cut.items + 8 * kThreads - 1) / (8 * kThreads);
-    cut.tokens = std::max(1, std::min({kMaxTokens, 4 * kThreads / cut.items, kMaxHalf / std::max(1, a.turn.half)}));
-  }
+  const int per = kind == Kind::Single ? a.dim / 2 : a.dim / (2 * N);
+  int64_t parts;
+  const MoveCut cut = move_cut(a.n_tokens, a.q_heads + 2 * a.kv_heads, per, a.turn.half, sm_count(), parts);
   const dim3 grid((unsigned)((a.n_tokens + cut.tokens - 1) / cut.tokens), (unsigned)std::min<int64_t>(65535, parts));
   if (kind == Kind::Halves) move_kernel<T, Kind::Halves><<<grid, kThreads, 0, stream>>>(a, cut);
   else if (kind == Kind::Neighbours) move_kernel<T, Kind::Neighbours><<<grid, kThreads, 0, stream>>>(a, cut);
