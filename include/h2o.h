@@ -504,6 +504,8 @@ typedef struct {
   int32_t axes;            /* 1 .. 8                                                                           */
   int32_t pairs;           /* 0: channels i and i + rotary_dim / 2 (halves); 1: channels 2 i and 2 i + 1       */
   int32_t device;          /* CUDA device ordinal                                                              */
+  int32_t* status;         /* dev, one int32 the caller has set to 0, or NULL: where h2o_rotate of the checked build leaves
+                              H2O_ERR_STATE (h2o_debug_bounds_checked; not used otherwise)                     */
 } h2o_rotary_t;
 /*
  * x: dev [n_tokens, n_heads, head_dim] of `dtype` (H2O_F32 or H2O_BF16) -> out, the same shape; out may be x itself, but must not

@@ -130,6 +130,7 @@ class h2o_rotary_t(ctypes.Structure):
         ("axes", ctypes.c_int32),
         ("pairs", ctypes.c_int32),
         ("device", ctypes.c_int32),
+        ("status", ctypes.c_void_p),
     ]
 
 
@@ -773,9 +774,10 @@ class H2ORotary:
         self._frequency = torch.from_numpy(frequencies).to(self.device)
         self.device, self._index = self._frequency.device, self._frequency.device.index
         self._axis = None if self.axes == 1 else torch.from_numpy(axes.astype(np.uint8)).to(self.device)
+        self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
         torch.cuda.current_stream(self.device).synchronize()  # the tables are there, whatever stream comes next
         self._c = h2o_rotary_t(self._frequency.data_ptr(), None if self._axis is None else self._axis.data_ptr(), self.rotary_dim, self.axes,
-                               0 if pairs == "halves" else 1, self._index)
+                               0 if pairs == "halves" else 1, self._index, self._status.data_ptr())
         self._at = ctypes.addressof(self._c)
 
     def apply(self, x, positions, out, inverse=False, stream=None):
@@ -785,6 +787,8 @@ class H2ORotary:
                              _raw_stream(self._index) if stream is None else stream.cuda_stream)
         if code:
             _check(code, "h2o_rotate")
+
+    status = H2OStore.status
 
 
 class H2OPages:

@@ -56,9 +56,10 @@ struct CacheView {
 };
 
 // Debug build (-DH2O_BOUNDS, the stand-in for a memory checker): every slot, unit and prompt-row index that
-// addresses the cache, the prompt tensors or the per-unit arrays, and every row, token and partial result of the K/V
-// store's operators, is checked right before it is used; a violation
-// records H2O_ERR_STATE in the cache's (store's) status word and the access is skipped.  In normal builds the checks
+// addresses the cache, the prompt tensors or the per-unit arrays, every row, token and partial result of the K/V
+// store's operators, every place of a paged cache's tables and the rows in its pages, and every item of a rotation, is checked right
+// before it is used; a violation records H2O_ERR_STATE in the status word of the cache (store, pages, rotary) and the access is
+// skipped.  In normal builds the checks
 // compile to nothing.
 #ifdef H2O_BOUNDS
 __device__ __forceinline__ bool index_in_range(long long idx, long long limit, int32_t* status) {

@@ -160,6 +160,7 @@ Plan make_plan(const h2o_pages_t* pages, const h2o_queries_t* q, const h2o_seque
   g.page_stride = c.page_stride;
   g.head_stride = c.head_stride;
   g.n_pages = c.n_pages;
+  g.max_pages = s->max_pages;
   g.page_size = c.page_size;
   g.shift = (c.page_size & (c.page_size - 1)) == 0 ? (int)std::log2((double)c.page_size) : -1;
   g.window = window;
@@ -243,6 +244,7 @@ int h2o_rotate(const h2o_rotary_t* rotary, const void* x, void* out, int32_t dty
   a.dim = head_dim;
   a.q_turn = 1;
   a.turn = turn_of(rotary, positions, position_stride, n_tokens, inverse != 0);
+  a.status = rotary->status;
   DeviceGuard guard(rotary->device);
   if (!guard.ok) return H2O_ERR_CUDA;
   return launched(launch_move(a, dtype, static_cast<cudaStream_t>(stream)));

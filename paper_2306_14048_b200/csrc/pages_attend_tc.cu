@@ -126,10 +126,11 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool t
 struct Box {
   int entry, row;
   __device__ __forceinline__ void find(const AttendView& a, const Item& it, int j, int b) {
-    const int x = it.keys.at(it.key0 + j * kN) + b * a.pages.box, in = page_index(a, x);
-    row = x - in * a.pages.page_size;
+    const int x = it.keys.at(it.key0 + j * kN) + b * a.pages.box;
+    row = x - page_index(a, x) * a.pages.page_size;
     entry = a.pages.n_pages;
-    if (j < it.nt && b * a.pages.box < kN && !unseen(a, it.keys, x, a.pages.box)) entry = a.pages.table[it.problem * a.pages.stride + in];
+    if (j < it.nt && b * a.pages.box < kN && !unseen(a, it.keys, x, a.pages.box) && page_rows_ok(a, it.head, row, a.pages.box))
+      entry = table_entry(a, it.problem, x);
   }
 };
 

@@ -49,19 +49,19 @@ __device__ __forceinline__ float2 turn_of(float2 x, float2 cs) {
 }
 
 // The last s with cu[s] <= t, found by a whole warp 32 entries at a time; -1 if t lies in no sequence.
-__device__ __forceinline__ int sequence_of(const int32_t* cu, int batch, int64_t t) {
+__device__ __forceinline__ int sequence_of(const int32_t* cu, int batch, int64_t t, int32_t* status) {
   const int lane = threadIdx.x & 31;
   int lo = 0, n = batch;
   while (n > 0) {
     const int step = (n + 31) / 32, at = lo + lane * step;
-    const unsigned below = __ballot_sync(0xffffffffu, lane * step < n && cu[at] <= t);
+    const unsigned below = __ballot_sync(0xffffffffu, lane * step < n && H2O_IN_RANGE(at, batch, status) && cu[at] <= t);
     const int c = __popc(below);
     if (c == 0) return -1;
     lo += (c - 1) * step;
     if (step == 1) break;
     n = min(step, n - (c - 1) * step);
   }
-  return cu[lo] <= t && t < cu[lo + 1] ? lo : -1;
+  return H2O_IN_RANGE(lo, batch, status) && cu[lo] <= t && t < cu[lo + 1] ? lo : -1;
 }
 
 // How the channels of a head are shared out to threads.  An item is what a thread moves at once:
@@ -70,13 +70,14 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu, int batch, int64_t
 //   Single      one pair of channels, or two of those that are not rotated
 enum class Kind { Halves, Neighbours, Single };
 
-// An item: where it comes from, where it goes (null: nowhere), which of its channels, and whether it is rotated.
+// An item: where it comes from, where it goes (null: nowhere), which of its channels, and whether it is rotated; whether there is
+// such an item (known only in the checked build, elsewhere always).
 template <typename T>
 struct Piece {
   const T* from;
   T* to;
   int x0, x1, pair, turns;  // first pair's angle, pairs from it on that are rotated (Neighbours)
-  bool turn;
+  bool turn, ok;
 };
 
 constexpr int64_t kNoPage = -1, kNoSequence = -2;
@@ -94,8 +95,9 @@ __global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ 
     Piece<T> p;
     int k, head, c;
     cut.split(i, k, head, c);
+    p.ok = H2O_IN_RANGE(k, here, a.status) && H2O_IN_RANGE(head, a.q_heads + 2 * a.kv_heads, a.status) && H2O_IN_RANGE(c, cut.per, a.status);
     const int64_t t = t0 + k;
-    const int64_t at = a.kv_heads > 0 && to ? place[k] : kNoPage;
+    const int64_t at = a.kv_heads > 0 && to && p.ok ? place[k] : kNoPage;
     if (head < a.q_heads) {
       p.from = static_cast<const T*>(a.q) + t * a.q_stride + (int64_t)head * a.dim;
       p.to = at == kNoSequence ? nullptr : static_cast<T*>(a.q_out) + t * a.q_out_stride + (int64_t)head * a.dim;
@@ -114,6 +116,7 @@ __global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ 
       p.x1 = apart ? c + half : 2 * c + 1;
       p.pair = k * half + c;
       p.turn = p.turn && c < half;
+      p.ok = p.ok && H2O_IN_RANGE(max(p.x0, p.x1), a.dim, a.status) && (!p.turn || H2O_IN_RANGE(p.pair, half * here, a.status));
     } else {
       const bool apart = KIND == Kind::Halves && c < turned;
       p.x0 = apart ? c * N : 2 * c * N;
@@ -121,6 +124,12 @@ __global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ 
       p.pair = k * half + (apart ? c * N : p.x0 / 2);
       p.turns = half - (apart ? c * N : p.x0 / 2);
       p.turn = p.turn && (KIND == Kind::Halves ? apart : p.turns > 0);
+      p.ok = p.ok && H2O_IN_RANGE(p.x1 + N - 1, a.dim, a.status) &&
+             (!p.turn || H2O_IN_RANGE(p.pair + (KIND == Kind::Halves ? N : min(N, p.turns)) - 1, half * here, a.status));
+    }
+    if (!p.ok) {
+      p.to = nullptr;
+      p.turn = false;
     }
     return p;
   };
@@ -132,6 +141,7 @@ __global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ 
     for (int n = 0; n < kAhead; ++n)
       if (first + n * stride < items) {
         const Piece<T> p = piece(first + n * stride, false);
+        if (!p.ok) continue;
         u[n].load(p.from + p.x0);
         w[n].load(p.from + p.x1);
       }
@@ -140,15 +150,15 @@ __global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ 
   if (a.kv_heads > 0) {
     for (int k = threadIdx.x >> 5; k < here; k += kThreads / 32) {
       const int64_t t = t0 + k;
-      const int s = a.cu ? sequence_of(a.cu, a.batch, t) : t < a.batch ? (int)t : -1;
+      const int s = a.cu ? sequence_of(a.cu, a.batch, t, a.status) : t < a.batch ? (int)t : -1;
       int64_t row = 0, at = kNoSequence;
       if (s >= 0) {
         row = (int64_t)a.length[s] - (a.cu ? (int64_t)a.cu[s + 1] - t : 1);
         at = kNoPage;
         if (row >= 0 && row < a.max_length && row / a.page_size < a.max_pages) {
-          const int x = (int)row;
-          const int page = a.table[s * a.table_stride + x / a.page_size];
-          if (page >= 0 && page < a.n_pages && H2O_IN_RANGE(page, a.n_pages, a.status)) at = page * a.page_stride + x % a.page_size * a.row_stride;
+          const int x = (int)row, in = x / a.page_size;
+          const int page = H2O_IN_RANGE(s, a.batch, a.status) && H2O_IN_RANGE(in, a.max_pages, a.status) ? a.table[s * a.table_stride + in] : -1;
+          if (page >= 0 && page < a.n_pages) at = page * a.page_stride + x % a.page_size * a.row_stride;
         }
       }
       if ((threadIdx.x & 31) == 0) {
@@ -161,6 +171,7 @@ __global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ 
   // ---- sines and cosines ----
   for (int i = threadIdx.x; i < half * here; i += kThreads) {
     const int k = here == 1 ? 0 : i / half, pair = i - k * half;
+    if (!(H2O_IN_RANGE(k, here, a.status) && H2O_IN_RANGE(pair, half, a.status) && H2O_IN_RANGE(i, kMaxHalf, a.status))) continue;
     int64_t p;
     if (a.turn.positions) p = a.turn.positions[(a.turn.axis ? min((int)a.turn.axis[pair], a.turn.axes - 1) : 0) * a.turn.position_stride + t0 + k];
     else p = rows[k];
@@ -223,6 +234,7 @@ __global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ 
         }
         if (i + kAhead * stride < items) {
           const Piece<T> next = piece(i + kAhead * stride, false);
+          if (!next.ok) continue;
           u[n].load(next.from + next.x0);
           w[n].load(next.from + next.x1);
         }

@@ -42,11 +42,11 @@ struct Smem {
 // Rows of a paged cache.  Eight rows from a multiple of 8 on lie in one page: the table's entry for them (n_pages where no row sees
 // any of them), and the place of the first relative to K's and V's base, negative where it has none (zeros).
 __device__ __forceinline__ int paged_entry(const AttendView& a, const Keys& keys, int seq, int x) {
-  return unseen(a, keys, x, 8) ? a.pages.n_pages : a.pages.table[seq * a.pages.stride + page_index(a, x)];
+  return unseen(a, keys, x, 8) ? a.pages.n_pages : table_entry(a, seq, x);
 }
 __device__ __forceinline__ int64_t paged_rows(const AttendView& a, int entry, int head, int x) {
-  const int page = page_in(a, entry);
-  return page >= a.pages.n_pages ? -1 : page * a.pages.page_stride + (x - page_index(a, x) * a.pages.page_size) * a.row_stride + head * a.pages.head_stride;
+  const int page = page_in(a, entry), row = x - page_index(a, x) * a.pages.page_size;
+  return page >= a.pages.n_pages || !page_rows_ok(a, head, row, 8) ? -1 : page * a.pages.page_stride + row * a.row_stride + head * a.pages.head_stride;
 }
 
 // One tile of K or V of a paged cache, rows x .. x + 63 (x a multiple of 8), those that nobody sees zero.  Lane l of a warp looks up

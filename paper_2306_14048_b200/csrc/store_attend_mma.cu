@@ -184,7 +184,7 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
     for (int j = 0; j < kFirst; ++j) {
       const int64_t x = (int64_t)w.split * part.chunk + (warp + kWarps * j) * kKeys + (boxes == 1 ? 0 : my_box * a.pages.box);
       early[j] = a.pages.n_pages;
-      if (a.pages.window == 0 && lane < copies && x < part.max_length) early[j] = a.pages.table[w.problem * a.pages.stride + page_index(a, (int)x)];
+      if (a.pages.window == 0 && lane < copies && x < part.max_length) early[j] = table_entry(a, w.problem, (int)x);
     }
     if (threadIdx.x == 0) sh.gave_up = 0;
     if (lane == 0) {
@@ -224,9 +224,10 @@ __device__ __forceinline__ void attend(const AttendView& a, const CUtensorMap* m
   auto lookup = [&](int j, const int* entry) {  // of tile j, whose entry may be there; what no row sees need not be read
     Box b{a.pages.n_pages, 0};
     if (j < mine && lane < copies) {
-      const int x = keys.at(key0 + (warp + kWarps * j) * kKeys) + (boxes == 1 ? 0 : my_box * a.pages.box), page = page_index(a, x);
-      b.row = x - page * a.pages.page_size;
-      if (!unseen(a, keys, x, a.pages.box)) b.entry = entry && a.pages.window == 0 ? *entry : a.pages.table[w.problem * a.pages.stride + page];
+      const int x = keys.at(key0 + (warp + kWarps * j) * kKeys) + (boxes == 1 ? 0 : my_box * a.pages.box);
+      b.row = x - page_index(a, x) * a.pages.page_size;
+      if (!unseen(a, keys, x, a.pages.box) && page_rows_ok(a, w.head, b.row, a.pages.box))
+        b.entry = entry && a.pages.window == 0 ? *entry : table_entry(a, w.problem, x);
     }
     return b;
   };
