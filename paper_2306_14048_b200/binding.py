@@ -791,6 +791,21 @@ class H2ORotary:
     status = H2OStore.status
 
 
+def _pool_strides(k, v):
+    """Elements between pages, rows, heads and channels of a pool's k and v [pages, page_size, heads, head_dim]."""
+    shape, strides = k.shape, list(k.stride())
+    used = [i for i in range(4) if shape[i] > 1]
+    if any(strides[i] != v.stride(i) for i in used) or (3 in used and strides[3] != 1):
+        _wrong("H2OPages", "k and v must have the same strides and dense channels")
+    if any(strides[i] == 0 for i in used):  # (three zeros mean dense to the library)
+        _wrong("H2OPages", "k and v must not be broadcast over the pages, rows or heads")
+    if shape[2] == 1:  # strides that are never used
+        strides[2] = shape[3]
+    if shape[0] == 1:
+        strides[0] = max(strides[1] * shape[1], strides[2] * shape[2])
+    return strides
+
+
 class H2OPages:
     """A paged K/V cache (h2o_pages_*): rows in pages of a pool, a table of pages for each sequence.
 
@@ -809,14 +824,7 @@ class H2OPages:
         if k.dtype not in _DTYPES:
             _wrong("H2OPages", "k and v must be float32 or bfloat16")
         self.n_pages, self.page_size, self.n_heads, self.head_dim = k.shape
-        used = [i for i in range(4) if k.shape[i] > 1]
-        strides = list(k.stride())
-        if any(strides[i] != v.stride(i) for i in used) or (3 in used and strides[3] != 1):
-            _wrong("H2OPages", "k and v must have the same strides and dense channels")
-        if self.n_heads == 1:  # strides that are never used
-            strides[2] = self.head_dim
-        if self.n_pages == 1:
-            strides[0] = max(strides[1] * self.page_size, strides[2] * self.n_heads)
+        strides = _pool_strides(k, v)
         self.format = _DTYPES[k.dtype]
         self.device, self._index = k.device, k.device.index
         self.k, self.v = k, v
