@@ -2,17 +2,21 @@
 
 Every step of the path runs in the CUDA kernels behind the C ABI.  PyTorch is
 used here for device memory and streams, nothing else.  There is no fallback:
-if the shared library is missing the import of this module fails.
+if the shared library is missing the import of this module fails; if the
+_pages extension for this Python and torch is, H2ORotary and H2OPages do.
 """
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 import struct
 from typing import Optional, Sequence
 
 import numpy as np
 import torch
+
+from .build import pages_path
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 # H2O_B200_LIB names another build of the same library (the checked variant libh2o_b200_bounds.so of build.py)
@@ -719,11 +723,28 @@ class H2OStore:
             pass
 
 
+class _NoPages:
+    """Stands where the _pages extension should be: whatever is asked of it says why it is not there."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def __getattr__(self, name):
+        raise ImportError(self._why)
+
+
 def _load_pages():
+    at = pages_path()
+    if not os.path.exists(at):
+        return _NoPages(os.path.basename(at) + " is not built, which H2ORotary and H2OPages need with this Python and torch (run "
+                        "`python paper_2306_14048_b200/build.py`); there is no fallback path")
+    spec = importlib.util.spec_from_file_location(__package__ + "._pages", at)
     try:
-        from . import _pages
+        _pages = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(_pages)
     except ImportError as e:
-        raise ImportError("_pages.so is not built (run `python paper_2306_14048_b200/build.py`); there is no fallback path") from e
+        return _NoPages("%s does not load (%s): build it again (`python paper_2306_14048_b200/build.py --force`); there is no fallback path"
+                        % (os.path.basename(at), e))
     _pages.bind(*[ctypes.cast(f, ctypes.c_void_p).value
                   for f in (lib.h2o_rotate, lib.h2o_pages_append, lib.h2o_pages_scratch_bytes, lib.h2o_pages_attend)])
     return _pages
@@ -748,6 +769,7 @@ class H2ORotary:
 
     def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, base: float = 10000.0, frequencies=None, axes=None,
                  pairs: str = "halves", device=0):
+        _pages.rotate  # (says so where the extension is missing)
         self.head_dim = int(head_dim)
         self.rotary_dim = self.head_dim if rotary_dim is None else int(rotary_dim)
         if self.head_dim < 8 or self.head_dim > 512 or self.head_dim % 8:
@@ -819,6 +841,7 @@ class H2OPages:
     """
 
     def __init__(self, k, v):
+        _pages.attend  # (says so where the extension is missing)
         if not k.is_cuda or k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device:
             _wrong("H2OPages", "k and v must be CUDA tensors of one 4-d shape, dtype and device")
         if k.dtype not in _DTYPES:

@@ -1,5 +1,5 @@
-"""Build libh2o_b200.so (the C-ABI library) in-tree with nvcc for sm_100a, and _pages.so (argument checks of the paged
-cache's calls, host code) with the C++ compiler.
+"""Build libh2o_b200.so (the C-ABI library) in-tree with nvcc for sm_100a, and the _pages extension (argument checks of the
+paged cache's calls, host code) with the C++ compiler.
 
 ``python paper_2306_14048_b200/build.py`` (run as a script, so that the package — which refuses to
 import without the library — is not imported first) or ``build()``; the library is rebuilt
@@ -11,6 +11,7 @@ from __future__ import annotations
 import concurrent.futures
 import glob
 import os
+import re
 import subprocess
 import sys
 import sysconfig
@@ -22,7 +23,6 @@ OBJ = os.path.join(PKG, "build")
 LIB = os.path.join(PKG, "libh2o_b200.so")
 LIB_BOUNDS = os.path.join(PKG, "libh2o_b200_bounds.so")  # the same sources with -DH2O_BOUNDS (every index checked)
 
-PAGES = os.path.join(PKG, "_pages.so")
 PAGES_SOURCE = os.path.join(CSRC, "pages_binding.cpp")
 
 NVCC_FLAGS = [
@@ -46,15 +46,26 @@ def needs_build(lib: str = LIB) -> bool:
     return any(os.path.getmtime(p) > t for p in _deps())
 
 
+def pages_path() -> str:
+    """Where the _pages extension for the running Python and torch lies: it reads tensors by torch's C++ headers, so that one built for
+    another of either must not be loaded."""
+    import torch
+
+    version = "%s-%s" % (torch.__version__, (torch.version.git_version or "")[:8])
+    return os.path.join(PKG, "_pages-torch" + re.sub(r"[^0-9A-Za-z.-]", "_", version) + sysconfig.get_config_var("EXT_SUFFIX"))
+
+
 def build_pages(force: bool = False) -> str:
-    """_pages.so: host code that reads torch tensors, rebuilt only when its sources are newer."""
+    """The _pages extension: host code that reads torch tensors, built where there is none for this Python and torch, or where its
+    sources are newer."""
+    lib = pages_path()
     newest = max(os.path.getmtime(p) for p in [PAGES_SOURCE] + glob.glob(os.path.join(ROOT, "include", "*.h")))
-    if not force and os.path.exists(PAGES) and os.path.getmtime(PAGES) >= newest:
-        return PAGES
+    if not force and os.path.exists(lib) and os.path.getmtime(lib) >= newest:
+        return lib
     import torch
 
     at = os.path.dirname(torch.__file__)
-    tmp = PAGES + ".tmp.%d" % os.getpid()
+    tmp = lib + ".tmp.%d" % os.getpid()
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
     for d in (os.path.join(ROOT, "include"), os.path.join(at, "include"), os.path.join(at, "include", "torch", "csrc", "api", "include"),
               sysconfig.get_paths()["include"]):
@@ -63,8 +74,8 @@ def build_pages(force: bool = False) -> str:
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("%s failed for %s:\n%s\n%s" % (cmd[0], PAGES_SOURCE, res.stdout, res.stderr))
-    os.replace(tmp, PAGES)
-    return PAGES
+    os.replace(tmp, lib)
+    return lib
 
 
 def build(force: bool = False, verbose: bool = False, bounds: bool = False) -> str:

@@ -1,6 +1,13 @@
 """What H2OPages and H2ORotary refuse or accept, without a GPU."""
+import os
+import subprocess
+import sys
+import types
+
 import pytest
 import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
@@ -43,3 +50,63 @@ def test_strides_of_pools(b):
     for k, v in ((z(5, 16, 2, 64), heads), (z(5, 16, 2, 128)[..., ::2], z(5, 16, 2, 128)[..., ::2])):
         with pytest.raises(ValueError):
             b._pool_strides(k, v)
+
+
+# ---- the extension that checks tensors ----
+SCRIPT = """
+import sys, types
+sys.modules["paper_2306_14048_b200._pages"] = None  # nothing to import by that name
+fake = types.ModuleType("paper_2306_14048_b200.build")
+fake.pages_path = lambda: sys.argv[1]
+sys.modules["paper_2306_14048_b200.build"] = fake
+import paper_2306_14048_b200 as pkg
+import torch
+cfg, keep = pkg.make_config(2, 2, 64, pkg.H2O_F32, [4, 4], [4, 4])
+assert pkg.h2o_cache_workspace_bytes(cfg) > 0
+try:
+    pkg.H2OStore(torch.zeros(8, 2, 64), torch.zeros(8, 2, 64))
+except ValueError:  # (a CUDA tensor is needed)
+    pass
+for make in (lambda: pkg.H2ORotary(64), lambda: pkg.H2OPages(torch.zeros(1, 8, 1, 64), torch.zeros(1, 8, 1, 64))):
+    try:
+        make()
+    except ImportError as e:
+        assert "build.py" in str(e) and "_pages" in str(e), e
+    else:
+        raise AssertionError("made without the extension")
+print("ALL WELL")
+"""
+
+
+@pytest.mark.parametrize("there", [False, True])
+def test_the_other_classes_do_without_the_extension(b, tmp_path, there):
+    """Missing, or one that does not load."""
+    at = tmp_path / "_pages-torch9.so"
+    if there:
+        at.write_bytes(b"\x7fELF nothing")
+    res = subprocess.run([sys.executable, "-c", SCRIPT, str(at)], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0 and "ALL WELL" in res.stdout, res.stderr[-2000:]
+
+
+def test_the_extension_is_of_this_python_and_torch(b, monkeypatch):
+    from paper_2306_14048_b200 import build
+
+    here = build.pages_path()
+    assert os.path.exists(here) and b._pages.__file__ == here
+    monkeypatch.setattr(torch, "__version__", "9.9.9+cu999")
+    other = build.pages_path()
+    monkeypatch.undo()
+    monkeypatch.setattr(build.sysconfig, "get_config_var", lambda name: ".cpython-399-x86_64-linux-gnu.so")
+    assert len({here, other, build.pages_path()}) == 3 and "9.9.9" in other
+
+
+def test_an_extension_for_another_torch_is_built(b, monkeypatch, tmp_path):
+    """A tree whose extension belongs to another torch: build.py makes one for this torch, although no source is newer."""
+    from paper_2306_14048_b200 import build
+
+    at = tmp_path / os.path.basename(build.pages_path())
+    made = []
+    monkeypatch.setattr(build, "pages_path", lambda: str(at))
+    monkeypatch.setattr(build.subprocess, "run", lambda cmd, **kw: made.append(cmd) or open(cmd[cmd.index("-o") + 1], "w").close() or types.SimpleNamespace(returncode=0))
+    assert build.build_pages() == str(at) and at.exists() and len(made) == 1
+    assert build.build_pages() == str(at) and len(made) == 1  # there now
