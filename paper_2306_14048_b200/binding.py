@@ -758,13 +758,35 @@ def _wrong(who: str, why: str):
     raise ValueError(who + ": " + why)
 
 
-class H2ORotary:
+_NO_TURN = (0, 0, 0, 0)
+
+
+class _Lasting:
+    """Small tensors on the device that belong to an object and that its calls' kernels use: when the object goes, torch's allocator
+    gives their memory to others only after what has been enqueued on every stream that a call has used (once per stream, noted by the
+    first call).  Streams that torch does not own may be gone by then: a call on one needs the object until it has run."""
+
+    def _keep(self, *tensors):
+        self._kept, self._streams = tensors, {_raw_stream(self._index)}
+
+    def _note(self, raw, stream):
+        self._streams.add(raw)
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
+        if isinstance(stream, torch.cuda.Stream) and stream.device_index == self._index and (raw == 0 or stream.stream_id != raw):  # (another library's has its address as its id)
+            for t in self._kept:
+                t.record_stream(stream)
+
+
+class H2ORotary(_Lasting):
     """Rotary positions of heads (h2o_rotate): pairs of channels turned by position * frequency.
 
     ``frequencies``: radians per position of each of the rotary_dim / 2 pairs (None: base ** (-2 i / rotary_dim));
     ``axes``: which axis of the positions each pair follows (None: one axis); ``pairs``: "halves" (channels i and
     i + rotary_dim / 2) or "neighbours" (channels 2 i and 2 i + 1).  rotary_dim: the first channels of a head, all of them
-    by default; the others stay as they are.  The two small tables are kept on the device by this object.
+    by default; the others stay as they are.  The two small tables are kept on the device by this object:
+    making it copies them there and waits for the copy, so a program makes one for each kind of layer and keeps it.  It may go once
+    its last call has been made (on a stream that torch does not own: has run); a captured graph needs it for as long as it is replayed.
     """
 
     def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, base: float = 10000.0, frequencies=None, axes=None,
@@ -801,12 +823,16 @@ class H2ORotary:
         self._c = h2o_rotary_t(self._frequency.data_ptr(), None if self._axis is None else self._axis.data_ptr(), self.rotary_dim, self.axes,
                                0 if pairs == "halves" else 1, self._index, self._status.data_ptr())
         self._at = ctypes.addressof(self._c)
+        self._turn = (self._at, self._index, self.head_dim, self.axes)  # what an append passes on
+        self._keep(*[t for t in (self._frequency, self._axis, self._status) if t is not None])
 
     def apply(self, x, positions, out, inverse=False, stream=None):
         """Rotates x [tokens, heads, head_dim] into out (which may be x).  inverse: takes the rotation back, which is also
         the gradient of a rotation with respect to its input."""
-        code = _pages.rotate(self._at, self._index, self.head_dim, self.axes, x, positions, out, inverse,
-                             _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        raw = _raw_stream(self._index) if stream is None else stream.cuda_stream
+        if raw not in self._streams:
+            self._note(raw, stream)
+        code = _pages.rotate(self._at, self._index, self.head_dim, self.axes, x, positions, out, inverse, raw)
         if code:
             _check(code, "h2o_rotate")
 
@@ -828,7 +854,7 @@ def _pool_strides(k, v):
     return strides
 
 
-class H2OPages:
+class H2OPages(_Lasting):
     """A paged K/V cache (h2o_pages_*): rows in pages of a pool, a table of pages for each sequence.
 
     ``k``, ``v``: float32 or bfloat16 [pages, page_size, heads, head_dim] of the same strides, channels dense (any order of the
@@ -838,6 +864,7 @@ class H2OPages:
     of the call's tokens included, which are its last ones.  Methods mirror the C calls: ``append`` ->
     h2o_pages_append, ``attend`` -> h2o_pages_attend, ``close`` -> h2o_pages_destroy.  Results go to tensors that the caller
     passes; scratch comes from torch's allocator on the call's stream, one piece per call.
+    A captured graph needs the object, and the rotary it was captured with, for as long as it is replayed.
     """
 
     def __init__(self, k, v):
@@ -860,14 +887,21 @@ class H2OPages:
         _check(lib.h2o_pages_create(ctypes.byref(handle), ctypes.byref(cfg)), "h2o_pages_create")
         self._h = handle
         self._at = handle.value
+        self._keep(self._status)
 
     def append(self, k, v, table, length, cu=None, rotary=None, positions=None, q=None, q_out=None, stream=None):
         """Appends k, v [tokens, heads, head_dim] to their sequences' pages; with ``rotary`` k is rotated on the way, and q
         [tokens, query heads, head_dim] into q_out (which may be q).  cu: int32 [batch + 1] first token of each sequence (None:
         token b is sequence b); positions: as for H2ORotary.apply (None: each token's row, on every axis)."""
-        turn = (0, 0, 0, 0) if rotary is None else (rotary._at, rotary._index, rotary.head_dim, rotary.axes)
-        code = _pages.append(self._at, self._index, self.n_heads, self.head_dim, self.format, k, v, table, length, cu, *turn, positions, q, q_out,
-                             _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        raw = _raw_stream(self._index) if stream is None else stream.cuda_stream
+        if raw not in self._streams:
+            self._note(raw, stream)
+        turn = _NO_TURN
+        if rotary is not None:
+            turn = rotary._turn
+            if raw not in rotary._streams:
+                rotary._note(raw, stream)
+        code = _pages.append(self._at, self._index, self.n_heads, self.head_dim, self.format, k, v, table, length, cu, *turn, positions, q, q_out, raw)
         if code:
             _check(code, "h2o_pages_append")
 
@@ -879,8 +913,11 @@ class H2OPages:
         if stream is not None:  # its scratch, too, comes from that stream
             with torch.cuda.stream(stream):
                 return self.attend(q, table, length, out, max_len, window, sinks, cu, max_q, lse, softmax_scale)
+        raw = _raw_stream(self._index)
+        if raw not in self._streams:
+            self._note(raw, None)
         code = _pages.attend(self._at, self._index, self.n_heads, self.head_dim, self.format, q, table, length, out, max_len, window, sinks, cu, max_q,
-                             lse, softmax_scale, _raw_stream(self._index))
+                             lse, softmax_scale, raw)
         if code:
             _check(code, "h2o_pages_attend")
 
