@@ -758,6 +758,13 @@ def _wrong(who: str, why: str):
     raise ValueError(who + ": " + why)
 
 
+def _raw_of(stream, index, who):
+    """The handle of a stream that a caller passes, which has to be of the object's device."""
+    if getattr(stream, "device_index", index) != index:
+        _wrong(who, "stream must be of device %d" % index)
+    return stream.cuda_stream
+
+
 _NO_TURN = (0, 0, 0, 0)
 
 
@@ -773,7 +780,7 @@ class _Lasting:
         self._streams.add(raw)
         if stream is None:
             stream = torch.cuda.current_stream(self.device)
-        if isinstance(stream, torch.cuda.Stream) and stream.device_index == self._index and (raw == 0 or stream.stream_id != raw):  # (another library's has its address as its id)
+        if isinstance(stream, torch.cuda.Stream) and (raw == 0 or stream.stream_id != raw):  # (another library's has its address as its id)
             for t in self._kept:
                 t.record_stream(stream)
 
@@ -829,7 +836,7 @@ class H2ORotary(_Lasting):
     def apply(self, x, positions, out, inverse=False, stream=None):
         """Rotates x [tokens, heads, head_dim] into out (which may be x).  inverse: takes the rotation back, which is also
         the gradient of a rotation with respect to its input."""
-        raw = _raw_stream(self._index) if stream is None else stream.cuda_stream
+        raw = _raw_stream(self._index) if stream is None else _raw_of(stream, self._index, "H2ORotary")
         if raw not in self._streams:
             self._note(raw, stream)
         code = _pages.rotate(self._at, self._index, self.head_dim, self.axes, x, positions, out, inverse, raw)
@@ -893,7 +900,7 @@ class H2OPages(_Lasting):
         """Appends k, v [tokens, heads, head_dim] to their sequences' pages; with ``rotary`` k is rotated on the way, and q
         [tokens, query heads, head_dim] into q_out (which may be q).  cu: int32 [batch + 1] first token of each sequence (None:
         token b is sequence b); positions: as for H2ORotary.apply (None: each token's row, on every axis)."""
-        raw = _raw_stream(self._index) if stream is None else stream.cuda_stream
+        raw = _raw_stream(self._index) if stream is None else _raw_of(stream, self._index, "H2OPages")
         if raw not in self._streams:
             self._note(raw, stream)
         turn = _NO_TURN
@@ -911,6 +918,7 @@ class H2OPages(_Lasting):
         token of each sequence (None: token b is sequence b); max_q, max_len: upper bounds of a sequence's tokens and rows;
         lse: float32 [tokens, query heads] or None."""
         if stream is not None:  # its scratch, too, comes from that stream
+            _raw_of(stream, self._index, "H2OPages")
             with torch.cuda.stream(stream):
                 return self.attend(q, table, length, out, max_len, window, sinks, cu, max_q, lse, softmax_scale)
         raw = _raw_stream(self._index)

@@ -110,3 +110,16 @@ def test_an_extension_for_another_torch_is_built(b, monkeypatch, tmp_path):
     monkeypatch.setattr(build.subprocess, "run", lambda cmd, **kw: made.append(cmd) or open(cmd[cmd.index("-o") + 1], "w").close() or types.SimpleNamespace(returncode=0))
     assert build.build_pages() == str(at) and at.exists() and len(made) == 1
     assert build.build_pages() == str(at) and len(made) == 1  # there now
+
+
+# ---- streams ----
+@pytest.mark.parametrize("call", ["apply", "append", "attend"])
+def test_a_stream_of_another_device_is_refused(b, call):
+    """Before anything runs: the library is not reached, and no stream becomes the current one."""
+    other = types.SimpleNamespace(device_index=1, cuda_stream=0x1000)
+    it = types.SimpleNamespace(_index=0, _at=0, _turn=(0, 0, 0, 0), _streams=set(), _note=None, n_heads=2, head_dim=64, format=b.H2O_F32, axes=1)
+    kind = b.H2ORotary if call == "apply" else b.H2OPages
+    x, i32 = torch.zeros(3, 2, 64), torch.zeros(3, dtype=torch.int32)
+    args = {"apply": (x, torch.zeros(3, dtype=torch.int64), x), "append": (x, x, i32.view(3, 1), i32), "attend": (x, i32.view(3, 1), i32, x, 9)}[call]
+    with pytest.raises(ValueError, match="stream"):
+        getattr(kind, call)(it, *args, stream=other)
