@@ -122,6 +122,32 @@ void split_prompt(AttendPart& p, int64_t units, int64_t rows, int dim, int sms) 
   }
 }
 
+// Few units of few query rows: the blocks should all run at once.  split_part's costs lead to more chunks than that, and the blocks
+// that find no place at first then run alone at the end: with heads of 128, of which two blocks fit an SM, 20000 keys of 8 heads take
+// 24.1 us in 296 blocks and 32.1 in 384; of 32 heads 54.4 in 256 and 72.2 in 320.  With heads of 64 three fit (32 heads, 20000
+// keys: 34.3 us in 384 blocks, 43.2 in 512).  A few places stay free, as more chunks are more to join: 1.5 blocks to an SM where two
+// fit, 2 where three fit, there up to 32 chunks.  Of several sequences only the longest length is known; the lengths are taken to lie
+// evenly between a third of it and it (two thirds on average), and a window to cut what is longer: `share` is what such a sequence
+// has of the keys of the longest.  Without / with this, in us (bf16, K and V from memory, replayed from a graph): heads of 128: one
+// sequence of 8 heads, 5000 keys 20.7 / 13.5, 20000 31.4 / 23.7, 33000 40.1 / 31.7; 4 of up to 20000 51.5 / 43.9; 4 with a window of 4000
+// 23.9 / 19, of 10000 37.0 / 32.8; heads of 64: 8 heads, 5000 14.8 / 11.8, 32 heads, 20000 42.8 / 34.5; 4 of up to 20000 29.2 / 29.4, of
+// up to 33000 50.0 / 41; 16 query heads of each of 8, 20000 38.2 / 27.6.  Of 294 calls measured, seven lose 3 to 6 % (5000 keys of 32
+// heads of 64, 16 query heads each: 17.9 / 19.0; a window of 1020, 8 sequences of 4 heads: 10.6 / 11.1), the mean gains 9 %.
+void bound_chunks(AttendPart& p, int64_t units, int sms, int blocks_per_sm) {
+  double share = 1.0;
+  if (p.problems > 1) {
+    const double longest = std::max(1, p.max_length), shortest = longest / 3, keys = std::max(1, p.most_keys);
+    if (keys > shortest) share -= (keys - shortest) * (keys - shortest) / (2 * (longest - shortest) * keys);
+  }
+  const double per_sm = sms / (units * share), up = share == 1.0 ? 0.999 : 0.5;  // (lengths that are known: as many chunks as cover it)
+  int64_t most = (int64_t)(1.5 * per_sm + up);
+  if (blocks_per_sm > 2) most = std::max(most, std::min<int64_t>(32, (int64_t)(2 * per_sm + up)));
+  if (p.splits > most) {
+    p.chunk = (int)(((p.most_keys + most - 1) / most + 127) / 128 * 128);
+    p.splits = (p.most_keys + p.chunk - 1) / p.chunk;
+  }
+}
+
 Plan make_plan(const h2o_pages_t* pages, const h2o_queries_t* q, const h2o_sequences_t* s, int window, int sinks) {
   Plan pl;
   std::memset(&pl, 0, sizeof(pl));
@@ -186,19 +212,7 @@ Plan make_plan(const h2o_pages_t* pages, const h2o_queries_t* q, const h2o_seque
   const int64_t units = (int64_t)p.row_tiles * a.heads * p.problems;
   if (pl.kernel == Kernel::Tc1) split_prompt(p, units, std::min<int64_t>(rows, pl.tile), a.dim, sm_count(c.device));
   else split_part(p, p.most_keys, units, sm_count(c.device), pl.kernel, pl.tile, c.format, a.dim, 128, true);
-  // Few units of few query rows: split_part's costs lead to more blocks here than are fastest (as measured; what costs the time was
-  // not profiled).  Three blocks to two SMs are enough, of several sequences half as many again, as their lengths are taken to average
-  // two thirds of the longest.  Without / with this, in us (bf16, head_dim 128, replayed from a graph): one sequence of 8 heads, 5000
-  // keys 18.7 / 12.6, 20000 28.7 / 21.8, 70000 68.2 / 53.1; with 16 query heads each 24.7 / 16.2, 36.6 / 27.0; of 32 heads 20000
-  // 66.1 / 53.5; 2 and 3 sequences of up to 20000 36.7 / 29.9, 47.4 / 39.6; up to 1000 keys the same.  Of 87 calls measured two lose
-  // more than 3 %, both of head_dim 64: one sequence of 8 heads, 33000 keys, 23.4 / 24.3; four of up to 20000, 25.5 / 30.9.
-  if (pl.kernel == Kernel::Mma && 4 * units <= sm_count(c.device)) {
-    const int64_t blocks = (int64_t)sm_count(c.device) * 3 / 2 * (p.problems > 1 ? 3 : 2) / 2, most = (blocks + units - 1) / units;
-    if (p.splits > most) {
-      p.chunk = (int)(((p.most_keys + most - 1) / most + 127) / 128 * 128);
-      p.splits = (p.most_keys + p.chunk - 1) / p.chunk;
-    }
-  }
+  if (pl.kernel == Kernel::Mma && 4 * units <= sm_count(c.device)) bound_chunks(p, units, sm_count(c.device), attend_mma_paged_blocks_per_sm(a.dim, pl.tile));
   if (units * p.splits > INT32_MAX) pl.rc = H2O_ERR_UNSUPPORTED;
   if (p.splits > 1) {
     a.slots = p.splits;

@@ -272,6 +272,7 @@ constexpr int kFewBoxRows = 32;  // rows of a box of the store's tensor maps
 bool make_store_map(CUtensorMap_st* map, const h2o_store_config_t& c, const void* base, int box_rows);
 int attend_mma_row_tile(int64_t rows);
 int attend_mma_blocks_per_sm(int format, int tile);
+int attend_mma_paged_blocks_per_sm(int dim, int tile);
 // part `first`, or (both) parts 0 and 1 in one launch, or (a.walk) part 1 with the prefix
 cudaError_t launch_attend_mma(const AttendView& a, int first, bool both, const int* tile, int format, const void* map_k,
                               const void* map_v, cudaStream_t stream);

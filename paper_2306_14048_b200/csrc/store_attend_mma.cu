@@ -756,6 +756,9 @@ EncodeTiledFn encode_tiled() {
 
 int attend_mma_row_tile(int64_t rows) { return rows <= 8 ? 8 : rows <= 16 ? 16 : 32; }
 int attend_mma_blocks_per_sm(int format, int tile) { return blocks_per_sm(format, tile / 8); }
+// Blocks on paged rows that an SM holds.  8 query rows: a ring of 64 KB; heads of 128 take 170 registers a thread (two blocks), heads of
+// 64 128 (three, by the rings).  16 rows: a ring of 96 KB.
+int attend_mma_paged_blocks_per_sm(int dim, int tile) { return dim == 64 && tile == 8 ? 3 : 2; }
 
 // Rows of a store: {bytes or elements of up to 128 bytes, rows, pieces of a row, heads}; a box is `box_rows` rows of one
 // head, swizzled over as many bytes as its inner extent.
