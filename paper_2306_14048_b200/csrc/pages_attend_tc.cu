@@ -80,14 +80,6 @@ struct Shared {
 };
 __host__ __device__ constexpr int smem_bytes(int d) { return kM * d * 2 + (slots_k(d) + slots_v(d)) * tile_bytes(d) + (int)sizeof(Shared); }
 
-// One box of a page: dimensions {64 channels, row in the page, half of the head dimension, head, page}.
-__device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, int row, int half, int head, int page, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::
-          "r"(dst),
-      "l"(map), "r"(0), "r"(row), "r"(half), "r"(head), "r"(page), "r"(smem_u32(bar))
-      : "memory");
-}
 // Asks for the place of a block that has not started.
 __device__ __forceinline__ void request_place(uint4* answer, uint64_t* bar) {
   mbar_expect_tx(bar, 16);

@@ -71,15 +71,6 @@ __device__ __forceinline__ void tma_4d(void* dst, const CUtensorMap* map, int c1
       : "memory");
 }
 
-// One box of a page: dimensions {64 channels, row in the page, half of the head dimension, head, page}.
-__device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, int row, int half, int head, int page, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::
-          "r"(dst),
-      "l"(map), "r"(0), "r"(row), "r"(half), "r"(head), "r"(page), "r"(smem_u32(bar))
-      : "memory");
-}
-
 template <bool F16>
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if constexpr (F16)
