@@ -186,7 +186,6 @@ Plan make_plan(const h2o_pages_t* pages, const h2o_queries_t* q, const h2o_seque
   g.page_stride = c.page_stride;
   g.head_stride = c.head_stride;
   g.n_pages = c.n_pages;
-  g.max_pages = s->max_pages;
   g.page_size = c.page_size;
   g.shift = (c.page_size & (c.page_size - 1)) == 0 ? (int)std::log2((double)c.page_size) : -1;
   g.window = window;

@@ -44,7 +44,6 @@ struct Paging {
   int64_t stride;
   int64_t page_stride, head_stride;  // elements (float32 rows; AttendView::row_stride within a page)
   int n_pages, page_size;
-  int max_pages;         // entries of a sequence in the table
   int shift;             // page_size is 2^shift, or -1: not a power of two
   int window, sinks;     // a query at row p sees the rows x <= p with x > p - window or x < sinks; window 0: all x <= p
   int box;               // rows of a box of the tensor maps: a power of two that divides page_size and the tile; float32: 8
@@ -164,11 +163,11 @@ __device__ __forceinline__ int shared_keys(const AttendPart& p, const Problem& r
 }
 // The place in a sequence's table of row x.
 __device__ __forceinline__ int page_index(const AttendView& a, int x) { return a.pages.shift >= 0 ? x >> a.pages.shift : x / a.pages.page_size; }
-// The entry of a sequence's table for row x; in the checked build no page where the table has no such place.
+// The entry of a sequence's table for row x; in the checked build no page where the table has no such place (max_length is no more
+// than the rows of its places).
 __device__ __forceinline__ int table_entry(const AttendView& a, int seq, int x) {
-  const int place = page_index(a, x);
-  if (!(H2O_IN_RANGE(seq, a.part[0].problems, a.status) && H2O_IN_RANGE(place, a.pages.max_pages, a.status))) return a.pages.n_pages;
-  return a.pages.table[seq * a.pages.stride + place];
+  if (!(H2O_IN_RANGE(seq, a.part[0].problems, a.status) && H2O_IN_RANGE(x, a.part[0].max_length, a.status))) return a.pages.n_pages;
+  return a.pages.table[seq * a.pages.stride + page_index(a, x)];
 }
 // In the checked build: do rows row .. row + n - 1 of a page exist, and the head?  (Elsewhere always.)
 __device__ __forceinline__ bool page_rows_ok(const AttendView& a, int head, int row, int n) {

@@ -39,7 +39,7 @@ def _body(text, head):
 
 def test_attention_reads_the_table_in_one_checked_place():
     entry = _body(_source("store.cuh"), "int table_entry(")
-    assert entry.count("pages.table[") == 1 and entry.index("H2O_IN_RANGE(seq") < entry.index("H2O_IN_RANGE(place") < entry.index("pages.table[")
+    assert entry.count("pages.table[") == 1 and entry.index("H2O_IN_RANGE(seq") < entry.index("H2O_IN_RANGE(x") < entry.index("pages.table[")
     assert _source("store.cuh").count("pages.table[") == 1
     for name in ("pages_attend_tc.cu", "store_attend_mma.cu", "store_attend_fma.cu", "store_join.cu"):
         assert "pages.table[" not in _source(name), name
