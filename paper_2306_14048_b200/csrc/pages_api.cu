@@ -123,16 +123,17 @@ void split_prompt(AttendPart& p, int64_t units, int64_t rows, int dim, int sms) 
 }
 
 // Few units of few query rows: the blocks should all run at once.  split_part's costs lead to more chunks than that, and the blocks
-// that find no place at first then run alone at the end: with heads of 128, of which two blocks fit an SM, 20000 keys of 8 heads take
-// 24.1 us in 296 blocks and 32.1 in 384; of 32 heads 54.4 in 256 and 72.2 in 320.  With heads of 64 three fit (32 heads, 20000
-// keys: 34.3 us in 384 blocks, 43.2 in 512).  A few places stay free, as more chunks are more to join: 1.5 blocks to an SM where two
-// fit, 2 where three fit, there up to 32 chunks.  Of several sequences only the longest length is known; the lengths are taken to lie
-// evenly between a third of it and it (two thirds on average), and a window to cut what is longer: `share` is what such a sequence
-// has of the keys of the longest.  Without / with this, in us (bf16, K and V from memory, replayed from a graph): heads of 128: one
-// sequence of 8 heads, 5000 keys 20.7 / 13.5, 20000 31.4 / 23.7, 33000 40.1 / 31.7; 4 of up to 20000 51.5 / 43.9; 4 with a window of 4000
-// 23.9 / 19, of 10000 37.0 / 32.8; heads of 64: 8 heads, 5000 14.8 / 11.8, 32 heads, 20000 42.8 / 34.5; 4 of up to 20000 29.2 / 29.4, of
-// up to 33000 50.0 / 41; 16 query heads of each of 8, 20000 38.2 / 27.6.  Of 294 calls measured, seven lose 3 to 6 % (5000 keys of 32
-// heads of 64, 16 query heads each: 17.9 / 19.0; a window of 1020, 8 sequences of 4 heads: 10.6 / 11.1), the mean gains 9 %.
+// that find no place at first then run alone at the end: with heads of 128, of which two blocks fit an SM, 20000 keys of 8 heads
+// take 24.1 us in 296 blocks and 32.1 in 384; of 32 heads 54.4 in 256 and 72.2 in 320.  With heads of 64 three fit (32 heads, 20000
+// keys: 34.3 us in 384 blocks, 43.2 in 512).  A few places stay free, as each chunk costs the joining kernel about 0.1 us: 1.5
+// blocks to an SM where two fit, 2 where three fit, there up to 32 chunks.  Of several sequences only the longest length is known;
+// the lengths are taken to lie evenly between a third of it and it (two thirds on average), and a window to cut what is longer:
+// `share` is what such a sequence has of the keys of the longest.  Without / with this, in us (bf16, K and V from memory, replayed
+// from a graph): heads of 128: one sequence of 8 heads, 5000 keys 19.3 / 13.3, 20000 31.4 / 23.7, 33000 40.1 / 31.7; 4 of up to
+// 20000 51.5 / 43.2; 4 with a window of 4000 23.9 / 18.8, of 10000 37.0 / 32.8; with 16 query heads to each of 8, 20000 keys 38.2 / 27.8;
+// heads of 64: 8 heads, 5000 14.8 / 11.6; 32 heads, 20000 42.8 / 34.8; 4 of up to 20000 29.2 / 29.4, of up to 33000 50.0 / 41.  Of 294
+// calls measured, seven lose 3 to 6 % (32 heads of 64 with 16 query heads each, 5000 keys: 17.9 / 19.0; a window of 1020, 8 sequences
+// of 4 heads: 10.6 / 11.1); the mean gains 9 %.
 void bound_chunks(AttendPart& p, int64_t units, int sms, int blocks_per_sm) {
   double share = 1.0;
   if (p.problems > 1) {

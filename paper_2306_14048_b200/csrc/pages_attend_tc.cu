@@ -17,10 +17,10 @@
 // exponentials (450 of them the special function unit's), 330 to learn that S is there, 320 for loading, masking and storing;
 // its products take 640 (S reads the queries from shared memory again for every 16 channels, 48 cycles of 32; the keys of a tile
 // are as many as tensor memory holds beside O and P).  An item costs 4 to 5 us more: the last product, the result, the first
-// tile's maximum.  Four prompts of up to 4096 tokens, 32 heads of 128, window 1020 and 4 sinks, pages of 64: 245 us, 750 TFLOP/s of
-// what the mask leaves (282 at 1600 MHz, once the power limit has lowered the clock); 360 with blocks of one item, two groups of
-// rows and pairs of K and V in one ring, 310 with further items, 247 once no warp waited for a table entry where it read it; with
-// steps of 16 keys that nobody sees left out of the products 245.
+// tile's maximum.  Four prompts of up to 4096 tokens, 32 heads of 128, window 1020 and 4 sinks, pages of 64: 245-247 us, 745 TFLOP/s of
+// what the mask leaves, for a few calls; back to back 290 us, 635, at the 1600 MHz that the power limit leaves after a second.  Steps, for a
+// few calls: 360 with blocks of one item, two groups of rows and pairs of K and V in one ring; 310 with further items; 247 once no warp
+// waited for a table entry where it read it; 245 with steps of 16 keys that nobody sees left out of the products.
 // Tried: tiles of 80 keys (long ranges 3 % faster, windows 5 % slower); S of 128 keys at once with P over it (304 against 285 us
 // under the power limit); more or fewer exponentials on the FMA pipe (one pair in 4: 266, in 16: 248).
 // The reference m of a row is the maximum of its first tile.  Later tiles compute their exponentials against it without

@@ -5,9 +5,10 @@
 // goes to sincospif.  (In fp32 the angle of position 1e6 would be off by 0.06.)  A block computes the sines and cosines of
 // its tokens once, into shared memory, and all heads use them; so the kernel is bound by memory: every value read once,
 // written once.  Products are fp32, rounded to the type once.
-// Appending 15700 tokens, 32 query and 32 K/V heads of 128, bfloat16: 122 us, 6.1 TB/s (a plain copy of as many bytes 6.3); rotating
-// 9001 tokens of 32 heads 31 us, 4.7 TB/s (a copy 27; here each block has a chain of its own, positions, sines, products, and an SM
-// sees few of them in so short a launch).  64 tokens of a step: 2.9 us on the device.
+// Appending 15121 tokens, 32 query and 32 K/V heads of 128, bfloat16: 122-125 us, 5.9-6.1 TB/s (a plain copy of as many bytes 6.3);
+// 7785 tokens in float32 124 us, 6.2 TB/s.  Rotating 9001 tokens of 32 heads 31 us, 4.7 TB/s (a copy 27; here each block has a chain of its
+// own, positions, sines, products, and an SM sees few of them in so short a launch), neighbouring pairs 35; float32 50 us, 5.9 TB/s.
+// 64 tokens of a step: 2.9 us on the device.
 #include <algorithm>
 
 #include "move_cut.cuh"
@@ -67,7 +68,9 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu, int batch, int64_t
 // How the channels of a head are shared out to threads.  An item is what a thread moves at once:
 //   Halves      two chunks, one in each half of the rotated channels (or two of those that are not)
 //   Neighbours  two chunks in a row
-//   Single      one pair of channels, or two of those that are not rotated
+//   Single      one pair of channels, or two of those that are not rotated: heads, or halves, that are not whole chunks.  Loads of 2 or
+//               4 bytes, none of them ahead: 9001 tokens of 32 heads, bfloat16, 96 channels of which 24 rotate 59 us (1.9 TB/s), 80 of
+//               which 20 50 us.
 enum class Kind { Halves, Neighbours, Single };
 
 // An item: where it comes from, where it goes (null: nowhere), which of its channels, and whether it is rotated; whether there is
